@@ -332,6 +332,207 @@ mpfa_status mpfa_mixed_step(const mpfa_prefill_args* prefill, const mpfa_decode_
                             void* workspace, size_t workspace_bytes, mpfa_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* A cache held in 4 bits: its writer, attention with a window, eviction      */
+/* ------------------------------------------------------------------------ */
+/*
+ * Next to the QK4PV8 cache above, a cache whose K and V are both NVFP4 rows
+ * (144 bytes per token and KV head against 200 and 2 per query head), read by
+ * attention with BF16 queries, an optional sliding window with first tokens
+ * that stay visible, and an eviction that keeps the tokens which attention
+ * has looked at most.
+ *
+ * K is centered by its sequence's mean when it is written: q . (K - Kbar)
+ * differs from q . K by q . Kbar, the same for every key of a row, which the
+ * softmax does not see.  Queries stay BF16, so nothing has to be restored
+ * (the Delta_S of Eq. 9 belongs to quantized, centered queries).
+ *
+ * Layouts (page p, KV head h, slot o; head_dim 128, 64-token pages):
+ *   k_codes  u8  [P][H_kv][64][64]       NVFP4 code rows, as in the cache above
+ *   k_scales u8  [P][H_kv][64][8]        E4M3, one per 16 channels
+ *   v_codes  u8  [P][H_kv][16][16][4][4] quad of tokens o / 4, octet of channels
+ *                                        c / 8, token o % 4, the octet's 4 code
+ *                                        bytes (channel 8 u + 2 i in the low
+ *                                        nibble of byte i)
+ *   v_scales u8  [P][H_kv][8][64]        E4M3, [c / 16][o]
+ *   weights  f32 [P][H_kv][64]           accumulated attention weights; may be
+ *                                        NULL where nothing accumulates or evicts
+ * Value of channel c: t * e4m3(scale[c / 16]) * e2m1(code), t the power-of-two
+ * tensor scale of the (sequence, KV head).  Every plane is 16-byte aligned.
+ * Physical pages are found through page tables as above; entries past a
+ * sequence's last page are never read.
+ */
+#define MPFA_KV4_IN_PLACE 256u  /* evict: the destination pages are the sequence's own
+                                   first pages                                     */
+#define MPFA_KV4_WEIGHTS  512u  /* decode: add attention weights to cache.weights  */
+
+typedef struct {
+    uint8_t* k_codes;
+    uint8_t* k_scales;
+    uint8_t* v_codes;
+    uint8_t* v_scales;
+    float* weights;
+    int64_t num_pages;
+} mpfa_kv4_cache;
+
+/*
+ * mpfa_kv4_write: K and V of new tokens into the cache.
+ *  - With MPFA_COMPUTE_STATS, for each sequence with at least one token in the
+ *    call: Kbar = the per-(head, channel) mean over the call's tokens (FP64
+ *    sum and division, rounded to FP32, then to BF16; zero without
+ *    MPFA_SMOOTH) in k_mean, and k_tscale, v_tscale = the smallest 2^k (k in
+ *    [-63, 63]) with 2688 * 2^k >= max |K - Kbar|, max |V| (1 where that is
+ *    0).  Without the flag they are read: freeze them after a sequence's
+ *    first call.  A sequence without tokens keeps its statistics.
+ *  - Without MPFA_SMOOTH, K is not centered and k_mean is not read.
+ *  - K - Kbar in FP32, then per 16 channels scale = E4M3_RNE_sat(amax / (6 t)),
+ *    codes = E2M1_RNE_sat(x / (t * scale)); V the same without a mean.
+ *  - A token whose slot is negative or past the cache (padding) is not stored;
+ *    it does count in the statistics.  Two tokens of a call may not have the
+ *    same slot (the debug library returns MPFA_ERR_DATA).
+ *  - With cache.weights the weight of every stored slot becomes 0.
+ *  - k_out, v_out (or NULL): the values that the cache now stands for, K
+ *    without its mean (every value is exact in BF16).
+ * k_stride, v_stride: elements between tokens (heads * 128 for a contiguous
+ * tensor; a multiple of 8; the heads of a token are contiguous).  k, v,
+ * k_mean, k_out, v_out are 16-byte aligned.
+ * workspace: at least mpfa_kv4_write_workspace_size bytes with
+ * MPFA_COMPUTE_STATS (16-byte aligned), else unused; its contents on entry are
+ * ignored.  Deterministic: identical inputs give identical bytes.
+ */
+typedef struct {
+    int32_t batch;               /* 1 .. 65535                                     */
+    int32_t total_tokens;        /* cu_seqlens[batch] (host copy)                  */
+    int32_t max_seqlen;          /* most tokens of one sequence in this call       */
+    int32_t h_kv;                /* 1 .. 32                                        */
+    int32_t head_dim;            /* must be 128                                    */
+    uint32_t flags;              /* MPFA_SMOOTH | MPFA_COMPUTE_STATS               */
+    int64_t k_stride, v_stride;
+    const int32_t* cu_seqlens;   /* [batch+1]                                      */
+    const void* k;               /* bf16 [T][h_kv][128]                            */
+    const void* v;               /* bf16 [T][h_kv][128]                            */
+    const int64_t* slot_mapping; /* [T]: page * 64 + o                             */
+    void* k_mean;                /* bf16 [batch][h_kv][128]                        */
+    float* k_tscale;             /* [batch][h_kv]                                  */
+    float* v_tscale;             /* [batch][h_kv]                                  */
+    mpfa_kv4_cache cache;
+    void* k_out;                 /* bf16 [T][h_kv][128] or NULL                    */
+    void* v_out;
+} mpfa_kv4_write_args;
+
+mpfa_status mpfa_kv4_write_workspace_size(int32_t batch, int32_t total_tokens, int32_t h_kv,
+                                          size_t* bytes);
+mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, size_t workspace_bytes,
+                           mpfa_stream_t stream);
+
+/*
+ * Attention of BF16 queries over the 4-bit cache.  A query at absolute
+ * position i sees key j where j <= i and (window = 0, or i - j < window, or
+ * j < sinks):
+ *   S = q . Khat / sqrt(128);  out = BF16(sum_j softmax(S)_j Vhat_j)
+ * with FP32 scores, maxima and sums and P rounded to FP16 (2^-11 of each P, or
+ * 2^-40 of the row's largest where that is more).
+ * A row that sees no key is 0.  h_q / h_kv may be anything from 1 to 256.
+ * Keys at or past kv_len are never used, whatever their slots hold.
+ *
+ * mpfa_kv4_prefill: query i of sequence b (token cu_seqlens_q[b] + i) is at
+ * position q_start[b] + i; q_start[b] + its rows <= kv_len[b].  With
+ * partition_tokens = 0 every row is computed in one pass and no workspace is
+ * needed; with a multiple of 128 the tiles that a block of rows sees are cut
+ * into at most max_partitions parts of that many keys, whose states are
+ * merged (for few rows behind long contexts).  mpfa_kv4_prefill_plan chooses
+ * for lengths known on the host (rows and kv_len after the call's tokens).
+ *
+ * mpfa_kv4_decode: q_tokens rows per sequence (1, or a few drafted tokens),
+ * row t at position kv_len[b] - q_tokens + t; rows b * q_tokens + t.
+ * kv_len[b] = 0, or less than q_tokens, is allowed.  The visible 128-key tiles
+ * are cut into partitions of partition_tokens keys, of which max_partitions
+ * must cover every sequence's (mpfa_kv4_decode_plan chooses for lengths known
+ * on the host; a plan for the longest lengths that a captured graph will see
+ * holds for all shorter ones).
+ * With MPFA_KV4_WEIGHTS, cache.weights[slot] += sum over the rows of the call
+ * and the query heads of the KV head of softmax(S), for every visible key,
+ * summed in a fixed order (no atomics).  Sequences of such a call may not
+ * share pages.
+ *
+ * workspace: 16-byte aligned, at least the plan's workspace_bytes for the same
+ * arguments; its contents on entry are ignored.  Calls (and captured graphs)
+ * that may overlap need workspaces of their own.
+ */
+typedef struct {
+    int32_t batch;               /* 1 .. 65535                                     */
+    int32_t h_q, h_kv;           /* h_q <= 256, h_kv <= 32, h_q % h_kv == 0        */
+    int32_t head_dim;            /* must be 128                                    */
+    int32_t max_pages;           /* page_table row length                          */
+    int32_t total_tokens;        /* prefill: cu_seqlens_q[batch] (host copy)       */
+    int32_t max_seqlen_q;        /* prefill: most rows of one sequence             */
+    int32_t q_tokens;            /* decode: rows per sequence                      */
+    int32_t window;              /* 0: no window                                   */
+    int32_t sinks;               /* first keys that stay visible (with a window)   */
+    int32_t partition_tokens;    /* multiple of 128; prefill: 0 = one pass         */
+    int32_t max_partitions;
+    uint32_t flags;              /* decode: MPFA_KV4_WEIGHTS; prefill: 0           */
+    int64_t q_stride;            /* elements between tokens of q (multiple of 8)   */
+    const int32_t* cu_seqlens_q; /* prefill: [batch+1]                             */
+    const int32_t* q_start;      /* prefill: [batch]                               */
+    const int32_t* kv_len;       /* [batch]                                        */
+    const int32_t* page_table;   /* [batch][max_pages]                             */
+    const void* q;               /* bf16 [rows][h_q][128], 16-byte aligned         */
+    mpfa_kv4_cache cache;
+    const float* k_tscale;       /* [batch][h_kv]                                  */
+    const float* v_tscale;       /* [batch][h_kv]                                  */
+    void* out;                   /* bf16 [rows][h_q][128], 16-byte aligned         */
+} mpfa_kv4_attn_args;
+
+mpfa_status mpfa_kv4_prefill_plan(int32_t batch, const int32_t* rows_host,
+                                  const int32_t* kv_len_host, int32_t h_q, int32_t h_kv,
+                                  int32_t window, int32_t sinks, int32_t num_cus,
+                                  int32_t* partition_tokens, int32_t* max_partitions,
+                                  size_t* workspace_bytes);
+mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* args, void* workspace,
+                             size_t workspace_bytes, mpfa_stream_t stream);
+mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int32_t h_q,
+                                 int32_t h_kv, int32_t q_tokens, int32_t window, int32_t sinks,
+                                 uint32_t flags, int32_t num_cus, int32_t* partition_tokens,
+                                 int32_t* max_partitions, size_t* workspace_bytes);
+mpfa_status mpfa_kv4_decode(const mpfa_kv4_attn_args* args, void* workspace,
+                            size_t workspace_bytes, mpfa_stream_t stream);
+
+/*
+ * mpfa_kv4_evict: cuts every sequence to `budget` tokens.  Per (sequence, KV
+ * head) the first `sinks` and the last `recent` tokens stay (sinks + recent <=
+ * budget), and of the others those of the largest cache.weights, ties to the
+ * lower index (NaN counts as larger than every number).  kept[b][h] receives
+ * their indices in ascending order (-1 past the last), and codes, scales and
+ * weights of the i-th of them move to key i of the destination pages.  A
+ * sequence of at most `budget` tokens keeps all of them (and is copied).
+ * new_len[b] = min(kv_len[b], budget); destination slots from there on are left
+ * as they were.  dst_page_table needs ceil(new_len / 64) entries per sequence.
+ *  - Without MPFA_KV4_IN_PLACE no destination page may be a page that a
+ *    sequence of the call reads, or another sequence's destination (a prefix
+ *    shared by several sequences stays whole for the others).
+ *  - With it the destination pages are the sequence's own first pages, in
+ *    order, and no two sequences of the call share a page.
+ * Keys keep the positions they were rotated with; from then on positions,
+ * windows and sinks count what is left in the cache.
+ */
+typedef struct {
+    int32_t batch;                 /* 1 .. 65535                                   */
+    int32_t h_kv;                  /* 1 .. 32                                      */
+    int32_t max_pages;             /* page_table row length                        */
+    int32_t dst_max_pages;         /* dst_page_table row length                    */
+    int32_t budget, sinks, recent;
+    uint32_t flags;                /* MPFA_KV4_IN_PLACE                            */
+    const int32_t* kv_len;         /* [batch]; may be new_len                      */
+    const int32_t* page_table;
+    const int32_t* dst_page_table;
+    mpfa_kv4_cache cache;          /* with weights                                 */
+    int32_t* kept;                 /* [batch][h_kv][budget]                        */
+    int32_t* new_len;              /* [batch]                                      */
+} mpfa_kv4_evict_args;
+
+mpfa_status mpfa_kv4_evict(const mpfa_kv4_evict_args* args, mpfa_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Utilities                                                                  */
 /* ------------------------------------------------------------------------ */
 /* Element-wise device conversions, exposed so that their rounding can be

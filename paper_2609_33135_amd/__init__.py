@@ -19,13 +19,16 @@ LIB_PATH = DEBUG_LIB_PATH if os.environ.get("MPFA_DEBUG") == "1" else os.path.jo
  MPFA_ERR_DATA) = range(6)
 SMOOTH, COMPUTE_STATS, TSCALE_UNIT, SEED_MFMA, MXFP4, SEED_ELEMWISE = 1, 2, 4, 8, 16, 32
 PV_BF16, PV_NVFP4 = 64, 128
+KV4_IN_PLACE, KV4_WEIGHTS = 256, 512
 HEAD_DIM, PAGE, TILE = 128, 64, 128
 STATIC_SCRATCH_BYTES = 64 << 20   # MPFA_STATIC_SCRATCH_BYTES
 
 EXPORTED = ("mpfa_quantize_qk", "mpfa_prefill", "mpfa_decode_workspace_size",
             "mpfa_decode_choose_partition", "mpfa_decode_paged", "mpfa_decode_paged_static",
             "mpfa_mixed_workspace_size",
-            "mpfa_mixed_step", "mpfa_convert", "mpfa_status_string", "mpfa_version")
+            "mpfa_mixed_step", "mpfa_convert", "mpfa_status_string", "mpfa_version",
+            "mpfa_kv4_write_workspace_size", "mpfa_kv4_write", "mpfa_kv4_prefill_plan", "mpfa_kv4_prefill",
+            "mpfa_kv4_decode_plan", "mpfa_kv4_decode", "mpfa_kv4_evict")
 
 
 class MpfaError(RuntimeError):
@@ -66,6 +69,38 @@ class DecodeArgs(C.Structure):
                 ("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p),
                 ("ds", C.c_void_p), ("k_tscale", C.c_void_p), ("out", C.c_void_p),
                 ("num_pages", C.c_int64)]
+
+
+class Kv4Cache(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("k_scales", C.c_void_p), ("v_codes", C.c_void_p),
+                ("v_scales", C.c_void_p), ("weights", C.c_void_p), ("num_pages", C.c_int64)]
+
+
+class Kv4WriteArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("total_tokens", C.c_int32), ("max_seqlen", C.c_int32),
+                ("h_kv", C.c_int32), ("head_dim", C.c_int32), ("flags", C.c_uint32),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("cu_seqlens", C.c_void_p),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("slot_mapping", C.c_void_p), ("k_mean", C.c_void_p),
+                ("k_tscale", C.c_void_p), ("v_tscale", C.c_void_p), ("cache", Kv4Cache),
+                ("k_out", C.c_void_p), ("v_out", C.c_void_p)]
+
+
+class Kv4AttnArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("h_q", C.c_int32), ("h_kv", C.c_int32), ("head_dim", C.c_int32),
+                ("max_pages", C.c_int32), ("total_tokens", C.c_int32), ("max_seqlen_q", C.c_int32),
+                ("q_tokens", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
+                ("partition_tokens", C.c_int32), ("max_partitions", C.c_int32), ("flags", C.c_uint32),
+                ("q_stride", C.c_int64), ("cu_seqlens_q", C.c_void_p), ("q_start", C.c_void_p),
+                ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("q", C.c_void_p), ("cache", Kv4Cache),
+                ("k_tscale", C.c_void_p), ("v_tscale", C.c_void_p), ("out", C.c_void_p)]
+
+
+class Kv4EvictArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("h_kv", C.c_int32), ("max_pages", C.c_int32),
+                ("dst_max_pages", C.c_int32), ("budget", C.c_int32), ("sinks", C.c_int32),
+                ("recent", C.c_int32), ("flags", C.c_uint32), ("kv_len", C.c_void_p),
+                ("page_table", C.c_void_p), ("dst_page_table", C.c_void_p), ("cache", Kv4Cache),
+                ("kept", C.c_void_p), ("new_len", C.c_void_p)]
 
 
 _libs: dict = {}
@@ -109,6 +144,17 @@ def _load(path):
                                       C.c_size_t, C.c_void_p]
         L.mpfa_convert.restype = C.c_int
         L.mpfa_convert.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        i32, sized = C.c_int32, [C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_size_t)]
+        for name, args in (
+                ("mpfa_kv4_write_workspace_size", [i32, i32, i32, C.POINTER(C.c_size_t)]),
+                ("mpfa_kv4_write", [C.POINTER(Kv4WriteArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+                ("mpfa_kv4_prefill_plan", [i32, C.c_void_p, C.c_void_p, i32, i32, i32, i32, i32, *sized]),
+                ("mpfa_kv4_prefill", [C.POINTER(Kv4AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+                ("mpfa_kv4_decode_plan", [i32, C.c_void_p, i32, i32, i32, i32, i32, C.c_uint32, i32, *sized]),
+                ("mpfa_kv4_decode", [C.POINTER(Kv4AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+                ("mpfa_kv4_evict", [C.POINTER(Kv4EvictArgs), C.c_void_p])):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = args
         L.mpfa_status_string.restype = C.c_char_p
         L.mpfa_status_string.argtypes = [C.c_int]
         L.mpfa_version.restype = C.c_char_p
@@ -281,3 +327,220 @@ def convert(fmt: int, x, out, stream=None):
     0x300 + c / 0x400 + b: the same quotients from their definitions (IEEE
     division, exact scaling) through the fmt 1 encoder."""
     _check(lib().mpfa_convert(fmt, _ptr(x), x.numel(), _ptr(out), _stream(stream)), "mpfa_convert")
+
+
+# ---- the 4-bit cache: writer, windowed attention, eviction ------------------------------
+
+def _same(what, dtype, dev, *tensors):
+    """Contiguous tensors of one type on one device, or ValueError."""
+    for t in tensors:
+        if t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"{what}: a tensor is {t.dtype}, device {t.get_device()}, "
+                             f"{'' if t.is_contiguous() else 'not '}contiguous; "
+                             f"wanted contiguous {dtype} on device {dev}")
+
+
+def _rows(what, t, heads, dev):
+    """Token stride of a bf16 [T][heads][128] tensor whose tokens may lie apart (a slice of a
+    fused projection), or ValueError."""
+    import torch
+    if (t.dtype is not torch.bfloat16 or t.get_device() != dev or t.dim() != 3 or t.shape[1] != heads or
+            t.shape[2] != HEAD_DIM or t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM)):
+        raise ValueError(f"{what}: bf16 [T][{heads}][{HEAD_DIM}] on device {dev} with contiguous heads is wanted, got "
+                         f"{t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on device {t.get_device()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * HEAD_DIM)
+
+
+def _want(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _call(name, dev, stream, *args):
+    """The library call on the tensors' device (made current for it) and its current stream."""
+    import torch
+    if dev != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            return _check(getattr(lib(), name)(*args, _stream(stream)), name)
+    return _check(getattr(lib(), name)(*args, _stream(stream)), name)
+
+
+class PagedCache4:
+    """Planes of the paged 4-bit cache (NVFP4 K and V); weights: with the FP32 weight per
+    token that decode accumulates and eviction reads.  planes: existing tensors by plane
+    name instead of new zeroed ones."""
+
+    def __init__(self, num_pages: int, h_kv: int, device="cuda", weights=False, planes=None):
+        import torch
+        self.num_pages, self.h_kv = num_pages, h_kv
+        shapes = dict(k_codes=(PAGE, 64), k_scales=(PAGE, 8), v_codes=(PAGE, 64), v_scales=(8, PAGE), weights=(PAGE,))
+        if planes is None:
+            planes = {n: torch.zeros((num_pages, h_kv, *s), device=device,
+                                     dtype=torch.float32 if n == "weights" else torch.uint8)
+                      for n, s in shapes.items() if weights or n != "weights"}
+        self.device = planes["k_codes"].get_device()
+        for n, s in shapes.items():
+            t = planes.get(n)
+            if t is not None:
+                _same("PagedCache4", torch.float32 if n == "weights" else torch.uint8, self.device, t)
+                _want(tuple(t.shape) == (num_pages, h_kv, *s), f"PagedCache4: {n} has shape {tuple(t.shape)}")
+            else:
+                _want(n == "weights", f"PagedCache4: no plane {n}")
+            setattr(self, n, t)
+
+    def _c(self):
+        return Kv4Cache(_ptr(self.k_codes), _ptr(self.k_scales), _ptr(self.v_codes), _ptr(self.v_scales),
+                        _ptr(self.weights), self.num_pages)
+
+
+class SeqStats4:
+    """Per-sequence statistics of the 4-bit cache, frozen after a sequence's first write: K mean
+    and the tensor scales of K and V (existing tensors may be given)."""
+
+    def __init__(self, batch: int, h_kv: int, device="cuda", k_mean=None, k_tscale=None, v_tscale=None):
+        import torch
+        new = dict(dtype=torch.float32, device=device)
+        self.k_tscale = torch.ones((batch, h_kv), **new) if k_tscale is None else k_tscale
+        self.v_tscale = torch.ones((batch, h_kv), **new) if v_tscale is None else v_tscale
+        dev = self.k_tscale.device
+        self.k_mean = torch.zeros((batch, h_kv, HEAD_DIM), dtype=torch.bfloat16, device=dev) if k_mean is None else k_mean
+        self.batch, self.h_kv, self.device = batch, h_kv, self.k_tscale.get_device()
+        _same("SeqStats4", torch.float32, self.device, self.k_tscale, self.v_tscale)
+        _same("SeqStats4", torch.bfloat16, self.device, self.k_mean)
+        _want(tuple(self.k_tscale.shape) == tuple(self.v_tscale.shape) == (batch, h_kv) and
+              tuple(self.k_mean.shape) == (batch, h_kv, HEAD_DIM), "SeqStats4: shapes")
+
+
+class Kv4Plan:
+    """How a prefill or decode call is cut, and its workspace.  A plan serves one call at a time;
+    lengths up to those it was made for are fine."""
+
+    def __init__(self, what, partition_tokens, max_partitions, workspace):
+        self.what, self.partition_tokens, self.max_partitions = what, partition_tokens, max_partitions
+        self.workspace = workspace
+
+
+def _host_ints(x):
+    import numpy as np
+    return np.ascontiguousarray(x, dtype=np.int32)
+
+
+def _plan(name, what, device, call):
+    import torch
+    dev = torch.device(device)
+    part, maxp, size = C.c_int32(0), C.c_int32(0), C.c_size_t(0)
+    cus = torch.cuda.get_device_properties(dev).multi_processor_count
+    _check(call(cus, C.byref(part), C.byref(maxp), C.byref(size)), name)
+    ws = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
+    return Kv4Plan(what, part.value, maxp.value, ws)
+
+
+def kv4_prefill_plan(rows_host, kv_len_host, h_q: int, h_kv: int, window=0, sinks=0, device="cuda") -> Kv4Plan:
+    """mpfa_kv4_prefill_plan with its workspace: rows and keys (the call's tokens included) per sequence."""
+    rows, kv = _host_ints(rows_host), _host_ints(kv_len_host)
+    _want(rows.size == kv.size, "kv4_prefill_plan: as many row counts as lengths are wanted")
+    plan = _plan("mpfa_kv4_prefill_plan", ("prefill", rows.size, h_q, h_kv, window, sinks), device,
+                 lambda cus, *out: lib().mpfa_kv4_prefill_plan(rows.size, rows.ctypes.data, kv.ctypes.data, h_q, h_kv,
+                                                               window, sinks, cus, *out))
+    plan.max_rows = int(rows.max())
+    return plan
+
+
+def kv4_decode_plan(kv_len_host, h_q: int, h_kv: int, q_tokens=1, window=0, sinks=0, weights=False,
+                    device="cuda") -> Kv4Plan:
+    """mpfa_kv4_decode_plan with its workspace; weights: the calls accumulate attention weights."""
+    kv, flags = _host_ints(kv_len_host), KV4_WEIGHTS if weights else 0
+    plan = _plan("mpfa_kv4_decode_plan", ("decode", kv.size, h_q, h_kv, window, sinks), device,
+                 lambda cus, *out: lib().mpfa_kv4_decode_plan(kv.size, kv.ctypes.data, h_q, h_kv, q_tokens, window, sinks,
+                                                              flags, cus, *out))
+    plan.q_tokens, plan.flags = q_tokens, flags
+    return plan
+
+
+def kv4_write_workspace_size(batch: int, total_tokens: int, h_kv: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mpfa_kv4_write_workspace_size(batch, total_tokens, h_kv, C.byref(n)), "mpfa_kv4_write_workspace_size")
+    return n.value
+
+
+def kv4_write(k, v, cu_seqlens, slot_mapping, cache: PagedCache4, stats: SeqStats4, flags: int, max_seqlen: int,
+              workspace=None, k_out=None, v_out=None, stream=None):
+    """mpfa_kv4_write: k, v bf16 [T][Hkv][128] (tokens may lie apart) into the 4-bit cache; workspace:
+    kv4_write_workspace_size bytes, with COMPUTE_STATS."""
+    import torch
+    dev, T, batch = cache.device, k.shape[0], cu_seqlens.numel() - 1
+    ks, vs = _rows("kv4_write: k", k, cache.h_kv, dev), _rows("kv4_write: v", v, cache.h_kv, dev)
+    _same("kv4_write", torch.int32, dev, cu_seqlens)
+    _same("kv4_write", torch.int64, dev, slot_mapping)
+    _want(v.shape[0] == T and slot_mapping.numel() == T, "kv4_write: as many V rows and slots as K rows are wanted")
+    _want(stats.batch == batch and stats.h_kv == cache.h_kv and stats.device == dev, "kv4_write: stats of another batch")
+    for t in (k_out, v_out):
+        if t is not None:
+            _same("kv4_write", torch.bfloat16, dev, t)
+            _want(t.numel() == k.numel(), "kv4_write: k_out and v_out have the shape of k")
+    if workspace is not None:
+        _same("kv4_write: workspace", workspace.dtype, dev, workspace)
+    a = Kv4WriteArgs(batch, T, max_seqlen, cache.h_kv, HEAD_DIM, flags, ks, vs, _ptr(cu_seqlens), _ptr(k), _ptr(v),
+                     _ptr(slot_mapping), _ptr(stats.k_mean), _ptr(stats.k_tscale), _ptr(stats.v_tscale), cache._c(),
+                     _ptr(k_out), _ptr(v_out))
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _call("mpfa_kv4_write", dev, stream, C.byref(a), _ptr(workspace), size)
+
+
+def _kv4_attn(what, q, cache, stats, cu, q_start, kv_len, page_table, out, plan, max_seqlen_q, q_tokens, window, sinks,
+              flags, stream):
+    import torch
+    dev, batch, h_q = cache.device, kv_len.numel(), q.shape[1] if q.dim() == 3 else 0
+    stride = _rows(what, q, h_q, dev)
+    _same(what, torch.int32, dev, kv_len, page_table)
+    _same(what, torch.bfloat16, dev, out)
+    _want(out.numel() == q.numel() and page_table.dim() == 2 and page_table.shape[0] == batch, f"{what}: shapes")
+    _want(stats.batch == batch and stats.h_kv == cache.h_kv and stats.device == dev, f"{what}: stats of another batch")
+    kind = "decode" if q_tokens else "prefill"
+    _want(plan is None or plan.what == (kind, batch, h_q, cache.h_kv, window, sinks),
+          f"{what}: the plan was made for another call: {plan and plan.what}")
+    ws = plan.workspace if plan is not None else None
+    _want(ws is None or ws.get_device() == dev, f"{what}: the plan is of another device")
+    a = Kv4AttnArgs(batch, h_q, cache.h_kv, HEAD_DIM, page_table.shape[1], q.shape[0], max_seqlen_q, q_tokens, window, sinks,
+                    plan.partition_tokens if plan is not None else 0, plan.max_partitions if plan is not None else 0, flags,
+                    stride, _ptr(cu), _ptr(q_start), _ptr(kv_len), _ptr(page_table), _ptr(q), cache._c(), _ptr(stats.k_tscale),
+                    _ptr(stats.v_tscale), _ptr(out))
+    _call("mpfa_kv4_" + kind, dev, stream, C.byref(a), _ptr(ws), 0 if ws is None else ws.numel())
+
+
+def kv4_prefill(q, cache: PagedCache4, stats: SeqStats4, cu_seqlens_q, q_start, kv_len, page_table, out, plan=None,
+                window=0, sinks=0, max_seqlen_q=None, stream=None):
+    """mpfa_kv4_prefill: causal attention of bf16 queries [T][Hq][128] (tokens may lie apart) over the
+    4-bit cache; plan: kv4_prefill_plan of the same window and sinks (None: one pass).  max_seqlen_q: the
+    most rows of one sequence (by default the plan's, or T without one)."""
+    import torch
+    if max_seqlen_q is None:
+        max_seqlen_q = q.shape[0] if plan is None else plan.max_rows
+    _same("kv4_prefill", torch.int32, cache.device, cu_seqlens_q, q_start)
+    _want(cu_seqlens_q.numel() == kv_len.numel() + 1 and q_start.numel() == kv_len.numel(), "kv4_prefill: shapes")
+    _kv4_attn("kv4_prefill", q, cache, stats, cu_seqlens_q, q_start, kv_len, page_table, out, plan,
+              max_seqlen_q, 0, window, sinks, 0, stream)
+
+
+def kv4_decode(q, cache: PagedCache4, stats: SeqStats4, kv_len, page_table, out, plan: Kv4Plan, window=0, sinks=0,
+               stream=None):
+    """mpfa_kv4_decode: the plan's q_tokens rows per sequence, the last ones of its kv_len keys; with a
+    plan made for weights the attention weights are added to cache.weights."""
+    _want(q.shape[0] == kv_len.numel() * plan.q_tokens, "kv4_decode: q has q_tokens rows per sequence")
+    _kv4_attn("kv4_decode", q, cache, stats, None, None, kv_len, page_table, out, plan, 0, plan.q_tokens, window, sinks,
+              plan.flags, stream)
+
+
+def kv4_evict(cache: PagedCache4, kv_len, page_table, dst_page_table, budget: int, kept, new_len, sinks=0, recent=0,
+              in_place=False, stream=None):
+    """mpfa_kv4_evict: cuts every sequence to the `budget` tokens of the largest cache.weights (per KV head;
+    the first `sinks` and last `recent` always stay); kept int32 [B][Hkv][budget] and new_len [B] are written."""
+    import torch
+    dev, batch = cache.device, kv_len.numel()
+    _same("kv4_evict", torch.int32, dev, kv_len, page_table, dst_page_table, kept, new_len)
+    _want(page_table.dim() == dst_page_table.dim() == 2 and page_table.shape[0] == dst_page_table.shape[0] == batch and
+          tuple(kept.shape) == (batch, cache.h_kv, budget) and new_len.numel() == batch, "kv4_evict: shapes")
+    a = Kv4EvictArgs(batch, cache.h_kv, page_table.shape[1], dst_page_table.shape[1], budget, sinks, recent,
+                     KV4_IN_PLACE if in_place else 0, _ptr(kv_len), _ptr(page_table), _ptr(dst_page_table), cache._c(),
+                     _ptr(kept), _ptr(new_len))
+    _call("mpfa_kv4_evict", dev, stream, C.byref(a))

@@ -15,7 +15,10 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmpfa.so")
 
-SOURCES = ["api.cpp", "quantize.hip", "prefill.hip", "decode.hip", "mixed.hip", "debug_checks.hip"]
+HOST_SOURCES = ["api.cpp", "kv4_api.cpp"]   # compiled again with data checks for the debug library
+KERNEL_SOURCES = ["quantize.hip", "prefill.hip", "decode.hip", "mixed.hip", "debug_checks.hip",
+                  "kv4_write.hip", "kv4_prefill.hip", "kv4_decode.hip", "kv4_evict.hip"]
+SOURCES = HOST_SOURCES + KERNEL_SOURCES
 DEBUG_LIB = os.path.join(PKG, "libmpfa_debug.so")
 PROBE_LIB = os.path.join(PKG, "libmpfa_probe.so")
 # characterization library: the product kernels plus the softmax ablation
@@ -42,6 +45,7 @@ EXTRA = {"prefill.hip": ["-fno-honor-nans"], "mixed.hip": ["-fno-honor-nans"],
          # the same for the quantization pass: its max / min reductions need no
          # quieting instruction per loaded value
          "quantize.hip": ["-fno-honor-nans"],
+         "kv4_prefill.hip": ["-fno-honor-nans"], "kv4_decode.hip": ["-fno-honor-nans"],
          # the MFMA probe keeps its accumulators in VGPRs: with the AGPR form the
          # compiler copies them between the two register files inside the loop
          "probe.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
@@ -77,16 +81,17 @@ def build(verbose: bool = False) -> str:
     kernels; its entry points also check the data they are handed), the
     benchmark's probe library and its characterization library."""
     os.makedirs(BUILD, exist_ok=True)
-    jobs = [(s, False, False) for s in SOURCES] + [("api.cpp", True, False), ("probe.hip", False, False),
-                                                   ("prefill.hip", False, True)]
+    jobs = [(s, False, False) for s in SOURCES] + [(s, True, False) for s in HOST_SOURCES] + \
+        [("probe.hip", False, False), ("prefill.hip", False, True)]
     with ThreadPoolExecutor(max_workers=len(jobs)) as ex:
         objs = list(ex.map(lambda j: _compile(*j), jobs))
-    kernels = objs[1:len(SOURCES)]
-    _link(LIB, [objs[0], *kernels])
-    _link(DEBUG_LIB, [objs[len(SOURCES)], *kernels])
-    _link(PROBE_LIB, [objs[len(SOURCES) + 1]])
-    ablate_prefill = objs[len(SOURCES) + 2]
-    _link(ABLATE_LIB, [objs[0], *[ablate_prefill if k.endswith("/prefill.o") else k for k in kernels]])
+    n = len(HOST_SOURCES)
+    host, kernels = objs[:n], objs[n:len(SOURCES)]
+    probe, ablate_prefill = objs[-2:]
+    _link(LIB, [*host, *kernels])
+    _link(DEBUG_LIB, [*objs[len(SOURCES):len(SOURCES) + n], *kernels])
+    _link(PROBE_LIB, [probe])
+    _link(ABLATE_LIB, [*host, *[ablate_prefill if k.endswith("/prefill.o") else k for k in kernels]])
     if verbose:
         print("built", LIB, DEBUG_LIB, PROBE_LIB, ABLATE_LIB)
     return LIB

@@ -1,0 +1,294 @@
+// kv4_decode.hip -- split-KV attention of a few bf16 query rows per sequence over the
+// 4-bit cache for gfx950, the merge of its partitions, and the accumulation of the
+// attention weights.
+//
+// One wave takes one (sequence, KV head, 16 columns, partition of the visible tiles).  A
+// column is a query row: (token, query head of the KV head).  Keys are centered by their
+// sequence's mean when they are written; the term q . mean is the same for every key of a
+// row, so the softmax does not see it and bf16 queries need no compensation.
+//
+//   S^T = K Q^T      16x16x32 FP16 MFMA, K dequantized exactly (6 bits), Q exact (q_shift)
+//   P = 2^(S - m)    FP32 statistics, P rounded to FP16 (at most 2^-11 of each P, an
+//                    eighth of the bf16 output's own 2^-8; FP8 would be 2^-4)
+//   O^T += V^T P^T   16x16x32 FP16 MFMA
+//
+// K and V go from memory to registers, 16 bytes per lane and load, no LDS.  Inside a
+// 128-key tile MFMA row r of key block mb is key 32 (r/4) + 4 mb + r%4, so lane group g
+// (lanes 16g .. +15) ends up with the scores of keys 32g .. 32g+31 of its column, and
+// these are the keys it supplies to the PV product.  For V a lane holds the octet of
+// channels 8 lr .. +7 of those 32 keys: all its values share one scale group, and MFMA
+// row lr of channel block db is channel 8 lr + db.
+//
+// What bounds it: HBM reads, 144 bytes per (token, KV head).
+#include "kv4_device.h"
+
+#include <type_traits>
+
+namespace mpfa {
+
+namespace {
+
+constexpr int kDecodeWaves = 4;
+
+template <bool WEIGHTS>
+__global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4AttnParams p) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, lr = lane & 15;
+  const int grp = p.h_q / p.h_kv, cols = p.q_tokens * grp;
+  const int chunks = (cols + 15) >> 4;
+  const int b = blockIdx.z, hk = blockIdx.y / chunks, chunk = blockIdx.y - hk * chunks;
+  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
+  const int kvl = p.kv_len[b];
+  const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
+  const int v0 = part * p.partition_tiles, v1 = min(tiles.nt, v0 + p.partition_tiles);
+  if (v0 >= v1 || part >= p.max_partitions) return;
+
+  const int col = chunk * 16 + lr;
+  const bool valid = col < cols;
+  const int tok = valid ? col / grp : 0, h = hk * grp + (valid ? col - tok * grp : 0);
+  const int pos = kvl - p.q_tokens + tok;            // last visible key; negative: none
+  // keys below it are outside the window (unless they are sinks)
+  const int low = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
+  const int64_t row = (int64_t)b * p.q_tokens + tok;
+
+  // ---- Q: channels 32g .. +31 of the lane's column
+  f16x8 qop[4];
+  float lam;
+  {
+    const u32x4* src = reinterpret_cast<const u32x4*>(p.q + row * p.q_stride + h * kD + 32 * g);
+    u32x4 w[4];
+    float a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[i] = src[i];
+      a = fmaxf(a, q_amax(w[i]));
+    }
+    const int shift = q_shift(wave_max16(a));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) qop[i] = q_operand(w[i], shift);
+    lam = score_scale(p.lam, p.k_tscale[b * p.h_kv + hk], shift);
+  }
+
+  const int32_t* pt = p.page_table + (int64_t)b * p.max_pages;
+  const int npg = (kvl + 63) >> 6;
+  // the pages of 32 visible tiles, one per lane, read back with v_readlane: the loop has
+  // no page-table loads, whose results would drain the loads in flight
+  int win = 0, win_base = 0;
+  auto load_window = [&](int v) {
+    win_base = v;
+    const int x = v + (lane >> 1);
+    win = pt[min(2 * tiles.tile(min(x, tiles.nt - 1)) + (lane & 1), npg - 1)];
+  };
+  auto tile_pages = [&](int v, int& q0, int& q1) {
+    if (v - win_base >= 32) load_window(v);
+    q0 = __builtin_amdgcn_readlane(win, 2 * (v - win_base));
+    q1 = __builtin_amdgcn_readlane(win, 2 * (v - win_base) + 1);
+  };
+
+  const int krow = (32 * (lr >> 2) + (lr & 3)) & 63;   // + 4 mb: key of MFMA row lr in its page
+  u32x4 kc[8];
+  uint32_t ksc[8];
+  auto load_k = [&](int q0, int q1) {
+    const int64_t base = kv4_row((lr >> 3) ? q1 : q0, p.h_kv, hk) * kPage + krow;
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      ksc[mb] = *reinterpret_cast<const uint16_t*>(p.cache.k_scales + (base + 4 * mb) * 8 + 2 * g);
+      kc[mb] = *reinterpret_cast<const u32x4*>(p.cache.k_codes + (base + 4 * mb) * 64 + 16 * g);
+    }
+  };
+  u32x4 vc[8], vsc[2];
+  auto load_v = [&](int q0, int q1) {
+    const int64_t base = kv4_row((g >> 1) ? q1 : q0, p.h_kv, hk);
+    const uint8_t* src = p.cache.v_codes + (base * 16 + 8 * (g & 1)) * 256 + 16 * lr;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vc[i] = *reinterpret_cast<const u32x4*>(src + 256 * i);
+    const uint8_t* sc = p.cache.v_scales + (base * 8 + (lr >> 1)) * kPage + 32 * (g & 1);
+    vsc[0] = reinterpret_cast<const u32x4*>(sc)[0];
+    vsc[1] = reinterpret_cast<const u32x4*>(sc)[1];
+  };
+
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o[8];
+#pragma unroll
+  for (int db = 0; db < 8; ++db) o[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
+
+  int c0, c1;
+  load_window(v0);
+  tile_pages(v0, c0, c1);
+  load_k(c0, c1);
+  for (int v = v0; v < v1; ++v) {
+    const int key0 = tiles.tile(v) * kTile;
+    load_v(c0, c1);
+    __builtin_amdgcn_sched_barrier(0);   // the waits for K below leave V in flight
+    f32x4 s[8];
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      const f16x2 sc = e4m3_pair_f16(ksc[mb]);
+      f32x4 c = {0.f, 0.f, 0.f, 0.f};
+      c = mfma_f16(dequant8h(kc[mb][0], sc[0]), qop[0], c);
+      c = mfma_f16(dequant8h(kc[mb][1], sc[0]), qop[1], c);
+      c = mfma_f16(dequant8h(kc[mb][2], sc[1]), qop[2], c);
+      s[mb] = mfma_f16(dequant8h(kc[mb][3], sc[1]), qop[3], c);
+    }
+    tile_pages(min(v + 1, v1 - 1), c0, c1);
+    load_k(c0, c1);                      // past the last tile: it again
+    // ---- scores in log2 units; masked ones (which may come from stale bytes) by selection
+    const int k0 = key0 + 32 * g;
+    if (key0 + kTile - 1 > kvl - p.q_tokens || (p.window > 0 && key0 < kvl - p.window)) {   // uniform
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = k0 + 4 * mb + i;
+          const bool seen = key <= pos && (key >= low || key < p.sinks);
+          s[mb][i] = seen ? s[mb][i] * lam : -INFINITY;
+        }
+    } else {
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb) s[mb] *= lam;
+    }
+    if (WEIGHTS) {
+      if (valid) {
+        float* dst = p.scores + (((int64_t)b * p.h_kv + hk) * cols + col) * ((int64_t)p.max_partitions * p.partition_tiles * kTile) +
+                     (int64_t)v * kTile + 32 * g;
+#pragma unroll
+        for (int mb = 0; mb < 8; ++mb) *reinterpret_cast<f32x4*>(dst + 4 * mb) = s[mb];
+      }
+    }
+    float mxa = -INFINITY, mxb = -INFINITY;
+#pragma unroll
+    for (int mb = 0; mb < 8; mb += 2) {
+      mxa = fmaxf(fmaxf(mxa, s[mb][0]), s[mb][1]);
+      mxa = fmaxf(fmaxf(mxa, s[mb][2]), s[mb][3]);
+      mxb = fmaxf(fmaxf(mxb, s[mb + 1][0]), s[mb + 1][1]);
+      mxb = fmaxf(fmaxf(mxb, s[mb + 1][2]), s[mb + 1][3]);
+    }
+    const float mnew = fmaxf(m, wave_max16(fmaxf(mxa, mxb)));
+    const float muse = mnew == -INFINITY ? 0.0f : mnew;
+    const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - muse);
+    m = mnew;
+    const float bias = kLog2P - muse;
+    float ps = 0.0f;
+    f16x8 pb[4];
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) {
+      float e[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(s[mb][i] + bias);
+        pb[mb >> 1][4 * (mb & 1) + i] = (_Float16)e[i];
+      }
+      ps += (e[0] + e[1]) + (e[2] + e[3]);
+    }
+    l = alpha * l + ps;
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+      for (int db = 0; db < 8; ++db) o[db] *= alpha;
+    }
+    // ---- V: keys past the end hold stale bytes, P = 0 there: their scales are cleared so
+    // that 0 * NaN cannot occur
+    if (key0 + kTile > kvl) {
+      const int nv = kvl - k0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int keep = nv - 4 * i;
+        vsc[i >> 2][i & 3] &= keep >= 4 ? 0xFFFFFFFFu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {        // keys 32g + 8t .. +7
+      uint32_t ev[4], od[4];
+      f16x2 sc[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t a = vc[2 * t + (i >> 1)][2 * (i & 1)], c = vc[2 * t + (i >> 1)][2 * (i & 1) + 1];
+        ev[i] = keys_even(a, c);
+        od[i] = keys_odd(a, c);
+        const uint32_t w = vsc[t >> 1][2 * (t & 1) + (i >> 1)];
+        sc[i] = e4m3_pair_f16((i & 1) ? w >> 16 : w);
+      }
+      auto pv = [&](const uint32_t (&w)[4], auto sel, f32x4& acc) {
+        constexpr int S = decltype(sel)::value;
+        const f16x2 x0 = fp4_pair_f16<S>(w[0], sc[0]), x1 = fp4_pair_f16<S>(w[1], sc[1]);
+        const f16x2 x2 = fp4_pair_f16<S>(w[2], sc[2]), x3 = fp4_pair_f16<S>(w[3], sc[3]);
+        acc = mfma_f16((f16x8){x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]}, pb[t], acc);
+      };
+      pv(ev, std::integral_constant<int, 0>{}, o[0]);
+      pv(od, std::integral_constant<int, 0>{}, o[1]);
+      pv(ev, std::integral_constant<int, 1>{}, o[2]);
+      pv(od, std::integral_constant<int, 1>{}, o[3]);
+      pv(ev, std::integral_constant<int, 2>{}, o[4]);
+      pv(od, std::integral_constant<int, 2>{}, o[5]);
+      pv(ev, std::integral_constant<int, 3>{}, o[6]);
+      pv(od, std::integral_constant<int, 3>{}, o[7]);
+    }
+  }
+  // keep the products in full-wave control flow (the store below is under a branch)
+#pragma unroll
+  for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(o[db]));
+  const float lt = wave_sum16(l);
+  if (valid) {
+    float* st = p.states + ((row * p.h_q + h) * p.max_partitions + part) * kKv4State;
+    if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m, lt);
+    // accumulator row 4g + i of block db is channel 8 (4g + i) + db
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int db = 0; db < 8; db += 2)
+        *reinterpret_cast<float2*>(st + 2 + 32 * g + 8 * i + db) = make_float2(o[db][i], o[db + 1][i]);
+  }
+}
+
+// One wave per row (token, query head).
+__global__ __launch_bounds__(64) void kv4_decode_merge_kernel(Kv4AttnParams p) {
+  const int h = blockIdx.x, tok = blockIdx.y, b = blockIdx.z;
+  const int kvl = p.kv_len[b];
+  const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
+  const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
+  const int64_t r = ((int64_t)b * p.q_tokens + tok) * p.h_q + h;
+  kv4_merge_row(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD,
+                p.stats ? p.stats + 2 * r : nullptr);
+}
+
+// Adds every visible key's share of the attention, summed over the rows of its KV head in
+// order, to the cache's weights: four keys per thread.
+__global__ __launch_bounds__(256) void kv4_weights_kernel(Kv4AttnParams p) {
+  const int b = blockIdx.z, hk = blockIdx.y, kvl = p.kv_len[b];
+  const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
+  const int64_t per_col = (int64_t)p.max_partitions * p.partition_tiles * kTile;
+  const int vk = (blockIdx.x * 256 + threadIdx.x) * 4;
+  if (vk >= min((int64_t)tiles.nt * kTile, per_col)) return;
+  const int key = tiles.tile(vk / kTile) * kTile + (vk & (kTile - 1));
+  if (key >= kvl) return;
+  const int grp = p.h_q / p.h_kv, cols = p.q_tokens * grp;
+  const float* src = p.scores + ((int64_t)b * p.h_kv + hk) * cols * per_col + vk;
+  f32x4 w = {0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < cols; ++c) {
+    const float2 st = *reinterpret_cast<const float2*>(p.stats + 2 * (((int64_t)b * p.q_tokens + c / grp) * p.h_q + hk * grp + c % grp));
+    if (!(st.y > 0.0f)) continue;   // a row that sees nothing
+    const f32x4 s = *reinterpret_cast<const f32x4*>(src + c * per_col);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(s[i] - st.x + kLog2P), st.y, w[i]);
+  }
+  const int32_t pg = p.page_table[(int64_t)b * p.max_pages + (key >> 6)];
+  float* dst = p.cache.weights + kv4_row(pg, p.h_kv, hk) * kPage + (key & (kPage - 1));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (key + i < kvl) dst[i] += w[i];
+}
+
+}  // namespace
+
+hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream) {
+  const int chunks = (p.q_tokens * (p.h_q / p.h_kv) + 15) / 16;
+  const dim3 grid((p.max_partitions + kDecodeWaves - 1) / kDecodeWaves, p.h_kv * chunks, p.batch);
+  if (p.scores) kv4_decode_kernel<true><<<grid, 64 * kDecodeWaves, 0, stream>>>(p);
+  else kv4_decode_kernel<false><<<grid, 64 * kDecodeWaves, 0, stream>>>(p);
+  kv4_decode_merge_kernel<<<dim3(p.h_q, p.q_tokens, p.batch), 64, 0, stream>>>(p);
+  if (p.scores) {
+    const int64_t keys = (int64_t)p.max_partitions * p.partition_tiles * kTile;
+    kv4_weights_kernel<<<dim3((unsigned)((keys + 1023) / 1024), p.h_kv, p.batch), 256, 0, stream>>>(p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mpfa

@@ -1,0 +1,103 @@
+// kv4_device.h -- device helpers of the 4-bit cache's kernels: addresses of its planes
+// and the dequantization of V, whose codes pair channels where the matrix instructions
+// want pairs of keys.
+#pragma once
+#include "kv4_internal.h"
+#include "mpfa_device.h"
+
+namespace mpfa {
+
+namespace {
+
+// log2 of the factor P carries into its FP16 rounding.  P is at most 1: with 2^15 it
+// stays below the FP16 maximum and keeps its 11 bits down to 2^-29 (2^-14 without),
+// where a row of 128K equal keys still sums them exactly enough.
+constexpr float kLog2P = 15.0f;
+
+// (page, KV head) row of a plane
+__device__ __forceinline__ int64_t kv4_row(int64_t page, int h_kv, int hk) { return page * h_kv + hk; }
+
+// Bytes j of the results: channel 2j (even) / 2j + 1 (odd) of the octet, the first key in
+// the low nibble, the second in the high one.  a, b: an octet's codes of two keys.
+__device__ __forceinline__ uint32_t keys_even(uint32_t a, uint32_t b) { return (a & 0x0F0F0F0Fu) | ((b << 4) & 0xF0F0F0F0u); }
+__device__ __forceinline__ uint32_t keys_odd(uint32_t a, uint32_t b) { return ((a >> 4) & 0x0F0F0F0Fu) | (b & 0xF0F0F0F0u); }
+
+// Byte SEL of w: two E2M1 codes as FP16, times m.
+template <int SEL>
+__device__ __forceinline__ f16x2 fp4_pair_f16(uint32_t w, f16x2 m) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, SEL) * m;
+}
+
+// Exponent shift of a query row whose largest magnitude is a: the row times 2^shift is
+// below 2^15, so its bf16 values are exact in FP16 (11 bits) wherever they are above
+// 2^-28 of the largest, and off by at most 2^-39 of it elsewhere (a row below 2^-46
+// altogether, whose scores are below 2^-30 of a K unit, loses more).
+__device__ __forceinline__ int q_shift(float a) {
+  return a > 0.0f ? min(14 - ilog2f(a), 60) : 0;
+}
+// log2(e) / sqrt(128) for scores in units of the K tensor scale and the row's shift.  The
+// exponent stays where the factor is a normal number (2^-126 .. ): 0 times a masked
+// score's -inf would be NaN.
+__device__ __forceinline__ float score_scale(float lam, float k_tscale, int shift) {
+  return __builtin_ldexpf(lam, min(ilog2f(k_tscale) - shift, 120));
+}
+
+// Eight bf16 values times 2^shift as FP16.
+__device__ __forceinline__ f16x8 q_operand(u32x4 w, int shift) {
+  f16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = (_Float16)__builtin_ldexpf(__uint_as_float(w[i] << 16), shift);
+    r[2 * i + 1] = (_Float16)__builtin_ldexpf(__uint_as_float(w[i] & 0xFFFF0000u), shift);
+  }
+  return r;
+}
+__device__ __forceinline__ float q_amax(u32x4 w) {
+  float a = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    a = fmaxf(a, fmaxf(__builtin_fabsf(__uint_as_float(w[i] << 16)), __builtin_fabsf(__uint_as_float(w[i] & 0xFFFF0000u))));
+  return a;
+}
+
+// Merge of the partition states of one row (query token and head) by a wave: M is the
+// largest m, L = sum f l, O = sum f O with f = 2^(m - M), partitions in order; the row is
+// O / L * tv, or 0 where nothing was visible.  Lane l owns channels 2l and 2l + 1.
+// stats (or null) receives M and 1 / L.
+__device__ __forceinline__ void kv4_merge_row(const float* st, int np, float tv, uint16_t* out, float* stats) {
+  const int lane = threadIdx.x & 63;
+  float M = -INFINITY;
+  for (int q = lane; q < np; q += 64) M = fmaxf(M, st[(int64_t)q * kKv4State]);
+  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+  float L = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  if (M > -INFINITY) {
+    constexpr int kAhead = 8;
+    for (int q0 = 0; q0 < np; q0 += kAhead) {
+      float2 ml[kAhead], o[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const float* s = st + (int64_t)min(q0 + j, np - 1) * kKv4State;
+        ml[j] = *reinterpret_cast<const float2*>(s);
+        o[j] = *reinterpret_cast<const float2*>(s + 2 + 2 * lane);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const float f = q0 + j < np ? __builtin_amdgcn_exp2f(ml[j].x - M) : 0.0f;
+        L = __builtin_fmaf(f, ml[j].y, L);
+        o0 = __builtin_fmaf(f, o[j].x, o0);
+        o1 = __builtin_fmaf(f, o[j].y, o1);
+      }
+    }
+  }
+  const float inv = L > 0.0f ? __frcp_rn(L) : 0.0f;
+  const uint32_t lo = bf16_rne(o0 * inv * tv), hi = bf16_rne(o1 * inv * tv);
+  *reinterpret_cast<uint32_t*>(out + 2 * lane) = lo | (hi << 16);
+  if (stats && lane == 0) {
+    stats[0] = M;
+    stats[1] = inv;
+  }
+}
+
+}  // namespace
+
+}  // namespace mpfa

@@ -1,0 +1,270 @@
+// kv4_write.hip -- K and V into the 4-bit cache for gfx950: on a sequence's first call
+// its statistics (K means, tensor scales), then NVFP4 rows of both.
+//
+// Every rounding is fixed, so the codes are bit-reproducible: the means come from FP64
+// sums (bf16 tokens add exactly in 53 bits, in any order), centering is one FP32
+// subtraction, and x -> fl(x - mean) is monotone, so the largest |K - mean| is reached
+// at a channel's maximum or minimum and the tokens are read once for it.
+#include "kv4_device.h"
+
+#pragma clang fp contract(off)
+
+namespace mpfa {
+
+namespace {
+
+constexpr int kWriteTokens = 32;   // tokens per workgroup: eight per wave, eight lanes (groups of 16) each
+
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// Statistics partial of block blk of sequence b (the blocks of a batch are numbered so
+// that no two sequences share one: floor(t0 / 128) + b, since ceil(n / 128) more of them
+// end at or before the next sequence's first).
+__device__ __forceinline__ uint8_t* stat_block(const Kv4WriteParams& p, int64_t t0, int b, int blk, int hk) {
+  return p.ws + ((t0 / kKv4StatTokens + b + blk) * p.h_kv + hk) * kKv4StatBytes;
+}
+
+struct StatPtrs {
+  double* sum;
+  float *mx, *mn, *v;
+};
+__device__ __forceinline__ StatPtrs stat_ptrs(uint8_t* s) {
+  return {reinterpret_cast<double*>(s), reinterpret_cast<float*>(s + kD * 8), reinterpret_cast<float*>(s + kD * 12),
+          reinterpret_cast<float*>(s + kD * 16)};
+}
+
+// One workgroup per (128 tokens, KV head): 16 lanes per token row, 16 rows at a time.
+__global__ __launch_bounds__(256) void kv4_stats_kernel(Kv4WriteParams p) {
+  __shared__ double s_sum[4][kD];
+  __shared__ float s_mx[4][kD], s_mn[4][kD], s_v[4];
+  const int b = blockIdx.z, hk = blockIdx.y, blk = blockIdx.x;
+  const int64_t t0 = p.cu_seqlens[b];
+  const int n = p.cu_seqlens[b + 1] - (int)t0;
+  const int tb = blk * kKv4StatTokens, te = min(n, tb + kKv4StatTokens);
+  if (tb >= n) return;
+  const int c = threadIdx.x & 15, row = threadIdx.x >> 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double sum[8];
+  float mx[8], mn[8], va = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    sum[e] = 0.0;
+    mx[e] = -INFINITY;
+    mn[e] = INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < kKv4StatTokens / 16; ++i) {
+    const int t = tb + 16 * i + row;
+    if (t < te) {
+      const u32x4 kw = *reinterpret_cast<const u32x4*>(p.k + (t0 + t) * p.k_stride + hk * kD + 8 * c);
+      const u32x4 vw = *reinterpret_cast<const u32x4*>(p.v + (t0 + t) * p.v_stride + hk * kD + 8 * c);
+      va = fmaxf(va, q_amax(vw));
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = e & 1 ? bf_hi(kw[e >> 1]) : bf_lo(kw[e >> 1]);
+        sum[e] += (double)x;
+        mx[e] = fmaxf(mx[e], x);
+        mn[e] = fminf(mn[e], x);
+      }
+    }
+  }
+  // the four rows of a wave, then the four waves
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    for (int off = 16; off <= 32; off <<= 1) {
+      sum[e] += __shfl_xor(sum[e], off);
+      mx[e] = fmaxf(mx[e], __shfl_xor(mx[e], off));
+      mn[e] = fminf(mn[e], __shfl_xor(mn[e], off));
+    }
+  }
+  for (int off = 32; off >= 1; off >>= 1) va = fmaxf(va, __shfl_xor(va, off));
+  if (lane < 16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s_sum[wave][8 * c + e] = sum[e];
+      s_mx[wave][8 * c + e] = mx[e];
+      s_mn[wave][8 * c + e] = mn[e];
+    }
+  }
+  if (lane == 0) s_v[wave] = va;
+  __syncthreads();
+  const int t = threadIdx.x;
+  const StatPtrs o = stat_ptrs(stat_block(p, t0, b, blk, hk));
+  if (t < kD) {
+    o.sum[t] = (s_sum[0][t] + s_sum[1][t]) + (s_sum[2][t] + s_sum[3][t]);
+    o.mx[t] = fmaxf(fmaxf(s_mx[0][t], s_mx[1][t]), fmaxf(s_mx[2][t], s_mx[3][t]));
+    o.mn[t] = fminf(fminf(s_mn[0][t], s_mn[1][t]), fminf(s_mn[2][t], s_mn[3][t]));
+  }
+  if (t == 0) o.v[0] = fmaxf(fmaxf(s_v[0], s_v[1]), fmaxf(s_v[2], s_v[3]));
+}
+
+// The partials of one (sequence, KV head): means and tensor scales.  128 lanes hold the
+// channels, eight of them share the blocks.
+__global__ __launch_bounds__(1024) void kv4_stats_final_kernel(Kv4WriteParams p) {
+  __shared__ double s_sum[8][kD];
+  __shared__ float s_mx[8][kD], s_mn[8][kD], s_v[16], s_k[2];
+  const int b = blockIdx.y, hk = blockIdx.x, c = threadIdx.x & (kD - 1), part = threadIdx.x >> 7;
+  const int64_t t0 = p.cu_seqlens[b];
+  const int n = p.cu_seqlens[b + 1] - (int)t0;
+  if (n <= 0) return;   // no tokens: the statistics stay as they are
+  const int nblk = (n + kKv4StatTokens - 1) / kKv4StatTokens;
+  double sum = 0.0;
+  float mx = -INFINITY, mn = INFINITY, va = 0.0f;
+#pragma unroll 4
+  for (int blk = part; blk < nblk; blk += 8) {
+    const StatPtrs s = stat_ptrs(stat_block(p, t0, b, blk, hk));
+    sum += s.sum[c];
+    mx = fmaxf(mx, s.mx[c]);
+    mn = fminf(mn, s.mn[c]);
+  }
+  for (int blk = threadIdx.x; blk < nblk; blk += 1024) va = fmaxf(va, stat_ptrs(stat_block(p, t0, b, blk, hk)).v[0]);
+  for (int off = 32; off >= 1; off >>= 1) va = fmaxf(va, __shfl_xor(va, off));
+  s_sum[part][c] = sum;
+  s_mx[part][c] = mx;
+  s_mn[part][c] = mn;
+  if ((threadIdx.x & 63) == 0) s_v[threadIdx.x >> 6] = va;
+  __syncthreads();
+  if (threadIdx.x < kD) {
+    for (int i = 1; i < 8; ++i) {
+      sum += s_sum[i][c];
+      mx = fmaxf(mx, s_mx[i][c]);
+      mn = fminf(mn, s_mn[i][c]);
+    }
+    const uint16_t m = p.smooth ? bf16_rne((float)(sum / (double)n)) : 0;
+    p.k_mean[((int64_t)b * p.h_kv + hk) * kD + c] = m;
+    const float mean = bf16_to_f32(m);
+    float a = fmaxf(__builtin_fabsf(mx - mean), __builtin_fabsf(mn - mean));
+    for (int off = 32; off >= 1; off >>= 1) a = fmaxf(a, __shfl_xor(a, off));
+    if ((threadIdx.x & 63) == 0) s_k[threadIdx.x >> 6] = a;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 16; ++i) va = fmaxf(va, s_v[i]);
+    p.k_tscale[b * p.h_kv + hk] = tensor_scale(fmaxf(s_k[0], s_k[1]));
+    p.v_tscale[b * p.h_kv + hk] = tensor_scale(va);
+  }
+}
+
+// One group of 16 values: codes of channels 0..7 and 8..15, and the scale byte.
+struct Group {
+  uint32_t lo, hi, sc;
+  float step;   // t * scale
+};
+
+// x: the values divided by the tensor scale (exact, a power of two).  Values past the
+// format's largest (2688 of them; a frozen tensor scale and a later, larger token)
+// saturate, so they are cut at 8192 first and no quotient overflows.  div_by_scale is
+// the correctly rounded quotient; its rounding never moves a value onto or over a
+// boundary between codes, as a boundary times a scale has 7 bits.
+__device__ __forceinline__ Group quantize_group(const float* x, float t) {
+  float y[16], a = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    y[i] = fminf(fmaxf(x[i], -8192.0f), 8192.0f);
+    a = fmaxf(a, __builtin_fabsf(y[i]));
+  }
+  Group g;
+  g.sc = fp8_sat_pair(0u, div_by_scale(a, 6.0f, kRcp6), 0.0f, false) & 0xFFu;
+  const float sd = e4m3_value(g.sc);
+  g.step = t * sd;
+  g.lo = g.hi = 0u;
+  if (g.sc != 0u) {
+    const float r = __fdiv_rn(1.0f, sd);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      g.lo = fp4_pair(g.lo, div_by_scale(y[2 * j], sd, r), div_by_scale(y[2 * j + 1], sd, r), 1.0f, j);
+      g.hi = fp4_pair(g.hi, div_by_scale(y[8 + 2 * j], sd, r), div_by_scale(y[9 + 2 * j], sd, r), 1.0f, j);
+    }
+  } else {   // no scale, no value: sign-only codes
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      g.lo |= ((__float_as_uint(y[i]) >> 28) & 8u) << (4 * i);
+      g.hi |= ((__float_as_uint(y[8 + i]) >> 28) & 8u) << (4 * i);
+    }
+  }
+  return g;
+}
+
+// The values that a group's codes stand for, as bf16 (exact: six bits).
+__device__ __forceinline__ void store_values(uint16_t* out, const Group& g) {
+  u32x4 w[2];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const uint32_t c = half ? g.hi : g.lo;
+    const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      w[half][j] = (__float_as_uint(v[j][0] * g.step) >> 16) | (__float_as_uint(v[j][1] * g.step) & 0xFFFF0000u);
+  }
+  reinterpret_cast<u32x4*>(out)[0] = w[0];
+  reinterpret_cast<u32x4*>(out)[1] = w[1];
+}
+
+__device__ __forceinline__ void load_group(const uint16_t* src, float* x) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const u32x4 w = reinterpret_cast<const u32x4*>(src)[half];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[8 * half + 2 * j] = bf_lo(w[j]);
+      x[8 * half + 2 * j + 1] = bf_hi(w[j]);
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void kv4_write_kernel(Kv4WriteParams p) {
+  const int b = blockIdx.z, hk = blockIdx.y;
+  const int64_t t0 = p.cu_seqlens[b];
+  const int n = p.cu_seqlens[b + 1] - (int)t0;
+  const int g = threadIdx.x & 7, i = blockIdx.x * kWriteTokens + (threadIdx.x >> 3);
+  if (i >= n) return;
+  const int64_t t = t0 + i;
+  const int64_t slot = p.slot_mapping[t];
+  float k[16], v[16], m[16];
+  load_group(p.k + t * p.k_stride + hk * kD + 16 * g, k);
+  load_group(p.v + t * p.v_stride + hk * kD + 16 * g, v);
+  const float tk = p.k_tscale[b * p.h_kv + hk], tv = p.v_tscale[b * p.h_kv + hk];
+  const int ek = -ilog2f(tk), ev = -ilog2f(tv);
+  if (p.smooth) {
+    load_group(p.k_mean + ((int64_t)b * p.h_kv + hk) * kD + 16 * g, m);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) k[e] -= m[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    k[e] = __builtin_ldexpf(k[e], ek);
+    v[e] = __builtin_ldexpf(v[e], ev);
+  }
+  const Group gk = quantize_group(k, tk), gv = quantize_group(v, tv);
+  if (slot >= 0 && slot < p.num_pages * kPage) {   // else a padded token: nothing to keep
+    const int o = (int)(slot & (kPage - 1));
+    const int64_t row = kv4_row(slot / kPage, p.h_kv, hk);
+    *reinterpret_cast<uint2*>(p.cache.k_codes + (row * kPage + o) * 64 + 8 * g) = make_uint2(gk.lo, gk.hi);
+    p.cache.k_scales[(row * kPage + o) * 8 + g] = (uint8_t)gk.sc;
+    uint32_t* vq = reinterpret_cast<uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256) + 8 * g + (o & 3);
+    vq[0] = gv.lo;
+    vq[4] = gv.hi;
+    p.cache.v_scales[(row * 8 + g) * kPage + o] = (uint8_t)gv.sc;
+    if (p.cache.weights && g == 0) p.cache.weights[row * kPage + o] = 0.0f;
+  }
+  const int64_t out = (t * p.h_kv + hk) * kD + 16 * g;
+  if (p.k_out) store_values(p.k_out + out, gk);
+  if (p.v_out) store_values(p.v_out + out, gv);
+}
+
+}  // namespace
+
+hipError_t launch_kv4_write(const Kv4WriteParams& p, hipStream_t stream) {
+  if (p.total_tokens == 0 || p.max_seqlen == 0) return hipSuccess;
+  if (p.compute_stats) {
+    const int blocks = (p.max_seqlen + kKv4StatTokens - 1) / kKv4StatTokens;
+    kv4_stats_kernel<<<dim3(blocks, p.h_kv, p.batch), 256, 0, stream>>>(p);
+    kv4_stats_final_kernel<<<dim3(p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  }
+  const int chunks = (p.max_seqlen + kWriteTokens - 1) / kWriteTokens;
+  kv4_write_kernel<<<dim3(chunks, p.h_kv, p.batch), 256, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace mpfa

@@ -1,0 +1,432 @@
+"""The 4-bit cache's writer, attentions and eviction against the formats' definitions in
+64 bits (tests/kv4_ref.py, where the tolerances are derived)."""
+import math
+
+import pytest
+import torch
+
+from tests import kv4_ref as R
+
+pytestmark = pytest.mark.gpu
+
+D, PAGE = 128, 64
+
+
+@pytest.fixture(scope="module")
+def mp():
+    import paper_2609_33135_amd as mp
+    assert torch.cuda.is_available()
+    mp.lib()
+    return mp
+
+
+def i32(x):
+    return torch.as_tensor(x, dtype=torch.int32).cuda()
+
+
+def cumulative(lens):
+    return i32([sum(lens[:i]) for i in range(len(lens) + 1)])
+
+
+def slots_of(rows, starts, lens):
+    """Slots of `lens` tokens from key `starts` on, per sequence."""
+    out = []
+    for b, (s, n) in enumerate(zip(starts, lens)):
+        j = torch.arange(s, s + n)
+        out.append(rows[b][j // PAGE].long() * PAGE + j % PAGE)
+    return torch.cat(out).cuda() if out else torch.zeros(0, dtype=torch.int64).cuda()
+
+
+# ------------------------------------------------------------------ the writer: every byte
+def check_write(mp, cache, rows, start, lens, k, v, stats, smooth, cu):
+    for b, n in enumerate(lens):
+        if n == 0:
+            continue
+        kk, vv = k[cu[b]:cu[b] + n].double(), v[cu[b]:cu[b] + n].double()
+        if smooth:
+            kk = (k[cu[b]:cu[b] + n].float() - stats.k_mean[b].float()).double()   # one FP32 subtraction
+        got = R.Tokens(cache, rows[b].cuda(), start[b] + n)
+        for x, t, codes, scales in ((kk, stats.k_tscale[b], got.k_codes, got.k_scales), (vv, stats.v_tscale[b], got.v_codes, got.v_scales)):
+            y, s = R.quantize(x, t.double()[None, :].expand(n, -1))
+            c = codes[start[b]:]
+            have = R.e2m1_value(torch.stack([c & 15, c >> 4], -1).flatten(-2))
+            assert torch.equal(R.e4m3_value(scales[start[b]:]), s), f"scales of sequence {b}"
+            assert torch.equal(have, y), f"codes of sequence {b}"
+
+
+def check_stats(stats, before, lens, k, v, smooth, cu):
+    for b, n in enumerate(lens):
+        if n == 0:   # as they were
+            assert torch.equal(stats.k_mean[b], before[0][b]) and torch.equal(stats.k_tscale[b], before[1][b])
+            continue
+        kk, vv = k[cu[b]:cu[b] + n], v[cu[b]:cu[b] + n]
+        mean = (kk.double().sum(0) / n).float().to(torch.bfloat16) if smooth else torch.zeros_like(stats.k_mean[b])
+        assert torch.equal(stats.k_mean[b], mean)
+        kt = R.tensor_scale((kk.float() - mean.float()).double().abs().amax((0, 2)))
+        assert torch.equal(stats.k_tscale[b].double(), kt)
+        assert torch.equal(stats.v_tscale[b].double(), R.tensor_scale(vv.double().abs().amax((0, 2))))
+
+
+WRITES = [([1], 1), ([2, 1, 3], 2), ([63, 64, 65], 3), ([127, 128, 129, 0, 1], 2), ([1000, 0, 31, 33], 8), ([300], 32), ([5000], 1)]
+
+
+@pytest.mark.parametrize("smooth", [False, True])
+@pytest.mark.parametrize("first", [False, True])
+@pytest.mark.parametrize("lens,h_kv", WRITES)
+def test_write(mp, lens, h_kv, first, smooth):
+    print(f"write {lens} x {h_kv}, first {first}, smooth {smooth}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(len(lens) + h_kv)
+    T, B = sum(lens), len(lens)
+    start = [0 if first else 5 * b + 1 for b in range(B)]
+    rows = R.page_rows([s + n for s, n in zip(start, lens)], sum(-(-(s + n) // PAGE) for s, n in zip(start, lens)) + 2, 3)
+    k = (torch.randn(T, h_kv, D, generator=gen, device="cuda") * 3 + 2 * torch.randn(1, h_kv, D, generator=gen, device="cuda")).bfloat16()
+    v = torch.randn(T, h_kv, D, generator=gen, device="cuda").bfloat16()
+    k[0, :, :16] = 0       # a group without a scale
+    v[-1, 0, 16:32] = -0.0
+    k[T // 2, :, 5] = 60   # an outlier
+    cache = mp.PagedCache4(rows.max().item() + 3, h_kv, weights=True)
+    for n in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        getattr(cache, n).fill_(0xAB)
+    cache.weights.fill_(7.0)
+    stats = mp.SeqStats4(B, h_kv)
+    stats.k_mean.copy_(torch.randn(B, h_kv, D, generator=gen, device="cuda"))
+    stats.k_tscale.fill_(2.0 ** -6)   # below what the outlier needs: it saturates
+    stats.v_tscale.fill_(2.0 ** -9)
+    before = [x.clone() for x in (stats.k_mean, stats.k_tscale)]
+    cu = cumulative(lens)
+    flags = (mp.SMOOTH if smooth else 0) | (mp.COMPUTE_STATS if first else 0)
+    ws = torch.full((mp.kv4_write_workspace_size(B, T, h_kv),), 255, dtype=torch.uint8, device="cuda")
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    slots = slots_of(rows, start, lens)
+    mp.kv4_write(k, v, cu, slots, cache, stats, flags, max(lens), workspace=ws, k_out=ko, v_out=vo)
+    torch.cuda.synchronize()
+    if first:
+        check_stats(stats, before, lens, k, v, smooth, cu)
+    check_write(mp, cache, rows, start, lens, k, v, stats, smooth, cu)
+    # the values handed back are the cache's
+    for b, n in enumerate(lens):
+        got = R.Tokens(cache, rows[b].cuda(), start[b] + n)
+        assert torch.equal(ko[cu[b]:cu[b] + n].double(), (got.k() * stats.k_tscale[b].double()[None, :, None])[start[b]:])
+        assert torch.equal(vo[cu[b]:cu[b] + n].double(), (got.v() * stats.v_tscale[b].double()[None, :, None])[start[b]:])
+    # every other slot is as it was, written ones weigh nothing
+    used = torch.zeros(cache.num_pages * PAGE, dtype=torch.bool, device="cuda")
+    used[slots] = True
+    used = used.view(-1, PAGE)
+    assert (cache.k_codes.transpose(1, 2)[~used] == 0xAB).all() and (cache.k_scales.transpose(1, 2)[~used] == 0xAB).all()
+    assert (cache.v_scales.permute(0, 3, 1, 2)[~used] == 0xAB).all()
+    vc = cache.v_codes.view(-1, h_kv, 16, 16, 4, 4).permute(0, 2, 4, 1, 3, 5).reshape(-1, PAGE, h_kv, 64)
+    assert (vc[~used] == 0xAB).all()
+    w = cache.weights.transpose(1, 2)
+    assert (w[used] == 0).all() and (w[~used] == 7).all()
+
+
+def test_write_slices_of_a_fused_projection_and_padded_tokens(mp):
+    print("write: strided K and V, padded slots", flush=True)
+    T, h_kv = 77, 2
+    qkv = torch.randn(T, 12, D, device="cuda").bfloat16()
+    k, v = qkv[:, 8:10], qkv[:, 10:12]
+    cu = cumulative([T])
+    rows = R.page_rows([T], 4, 1)
+    slots = slots_of(rows, [0], [T])
+    slots[5], slots[40], slots[76] = -1, 4 * PAGE, 1 << 40
+    out = {}
+    for name, kk, vv in (("apart", k, v), ("dense", k.contiguous(), v.contiguous())):
+        cache, stats = mp.PagedCache4(4, h_kv), mp.SeqStats4(1, h_kv)
+        ws = torch.empty(mp.kv4_write_workspace_size(1, T, h_kv), dtype=torch.uint8, device="cuda")
+        mp.kv4_write(kk, vv, cu, slots, cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, T, workspace=ws)
+        out[name] = (cache, stats)
+    torch.cuda.synchronize()
+    (c0, s0), (c1, s1) = out["apart"], out["dense"]
+    for n in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        assert torch.equal(getattr(c0, n), getattr(c1, n))
+    assert torch.equal(s0.k_mean, s1.k_mean) and torch.equal(s0.v_tscale, s1.v_tscale)
+    got = R.Tokens(c0, rows[0].cuda(), T)
+    for t in (5, 40, 76):   # padding: nothing stored
+        assert not got.k_codes[t].any() and not got.k_scales[t].any() and not got.v_codes[t].any() and not got.v_scales[t].any()
+    keep = [t for t in range(T) if t not in (5, 40, 76)]
+    y, s = R.quantize((k.float() - s0.k_mean[0].float()).double(), s0.k_tscale[0].double()[None].expand(T, -1))
+    assert torch.equal(R.e4m3_value(got.k_scales[keep]), s[keep])
+
+
+@pytest.mark.parametrize("factor", [2.0 ** -100, 2.0 ** -70, 1.0, 2.0 ** 70, 2.0 ** 120])
+def test_write_extreme_magnitudes(mp, factor):
+    print(f"write: values around {factor}", flush=True)
+    T, h_kv = 40, 1
+    k = (torch.randn(T, h_kv, D, device="cuda") * factor).bfloat16()
+    v = (torch.randn(T, h_kv, D, device="cuda") * factor).bfloat16()
+    rows = R.page_rows([T], 2, 1)
+    cache, stats = mp.PagedCache4(2, h_kv), mp.SeqStats4(1, h_kv)
+    ws = torch.empty(mp.kv4_write_workspace_size(1, T, h_kv), dtype=torch.uint8, device="cuda")
+    cu = cumulative([T])
+    mp.kv4_write(k, v, cu, slots_of(rows, [0], [T]), cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, T, workspace=ws)
+    torch.cuda.synchronize()
+    check_stats(stats, None, [T], k, v, True, cu)
+    check_write(mp, cache, rows, [0], [T], k, v, stats, True, cu)
+
+
+# ------------------------------------------------------------------ attention
+def check_rows(got, want, tol, what):
+    bad = (got.double() - want).abs() > tol
+    assert not bad.any(), f"{what}: {int(bad.sum())} outputs off, worst {float(((got.double() - want).abs() / tol)[bad].max()):.2f} of the tolerance"
+
+
+def attn_case(mp, kv, h_q, h_kv, n_rows, seed, weights=False, sigma=1.0):
+    """Random cache, queries and page table for sequences of kv keys, their last n_rows being the rows."""
+    pages = sum(-(-n // PAGE) for n in kv) + 3
+    rows = R.page_rows(kv, pages, seed, width=max(1, -(-max(kv) // PAGE)) + 1)
+    cache = R.random_cache(mp, pages, h_kv, seed, weights)
+    R.stale(cache, rows, kv)
+    stats = mp.SeqStats4(len(kv), h_kv)
+    e = torch.arange(len(kv) * h_kv, device="cuda").view(len(kv), h_kv) % 3
+    stats.k_tscale.copy_(2.0 ** (-7.0 + e))
+    stats.v_tscale.copy_(2.0 ** (-2.0 - e))
+    gen = torch.Generator(device="cuda").manual_seed(seed + 1)
+    q = (sigma * torch.randn(sum(n_rows), h_q, D, generator=gen, device="cuda")).bfloat16()
+    return rows, cache, stats, q
+
+
+HEADS = [(1, 1), (4, 4), (8, 2), (10, 2), (16, 1), (17, 1), (40, 1), (6, 2)]
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (1, 3), (100, 4), (128, 0), (129, 130), (300, 64), (1000, 2000)])
+@pytest.mark.parametrize("kv,q_tokens", [([1, 2, 63, 64, 65], 1), ([700, 0, 129], 1), ([1500, 3], 4), ([257, 1025], 9)])
+def test_decode(mp, kv, q_tokens, window, sinks):
+    h_q, h_kv = HEADS[(len(kv) * 7 + window + q_tokens) % len(HEADS)]
+    print(f"decode {kv} rows {q_tokens} heads {h_q}:{h_kv} window {window} sinks {sinks}", flush=True)
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [q_tokens] * len(kv), 11 + window)
+    out = torch.full((len(kv) * q_tokens, h_q, D), math.nan, dtype=torch.bfloat16, device="cuda")
+    plan = mp.kv4_decode_plan(kv, h_q, h_kv, q_tokens, window, sinks)
+    if plan.workspace is not None:
+        plan.workspace.fill_(255)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    for b, n in enumerate(kv):
+        x = slice(b * q_tokens, (b + 1) * q_tokens)
+        want, tol, _, _ = R.attention(q[x], R.Tokens(cache, rows[b].cuda(), n), stats.k_tscale[b], stats.v_tscale[b], n - q_tokens,
+                                      window, sinks)
+        check_rows(out[x], want, tol, f"sequence {b}")
+
+
+@pytest.mark.parametrize("h_q,h_kv", HEADS)
+def test_decode_heads(mp, h_q, h_kv):
+    print(f"decode heads {h_q}:{h_kv}", flush=True)
+    kv = [333, 90]
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [2, 2], 5)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, mp.kv4_decode_plan(kv, h_q, h_kv, 2))
+    torch.cuda.synchronize()
+    for b, n in enumerate(kv):
+        want, tol, _, _ = R.attention(q[2 * b:2 * b + 2], R.Tokens(cache, rows[b].cuda(), n), stats.k_tscale[b], stats.v_tscale[b],
+                                      n - 2, 0, 0)
+        check_rows(out[2 * b:2 * b + 2], want, tol, f"sequence {b}")
+
+
+@pytest.mark.parametrize("part", [128, 256, 640, 8192])
+def test_decode_partitions(mp, part):
+    """Partitions of one tile up to ones that need several windows of the page table, and a
+    workspace for longer sequences than the call's."""
+    print(f"decode partitions of {part}", flush=True)
+    kv, h_q, h_kv = [9001, 130], 8, 2
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [1, 1], 9)
+    plan = mp.kv4_decode_plan([12000, 12000], h_q, h_kv)
+    plan.partition_tokens, plan.max_partitions = part, -(-12000 // part)
+    plan.workspace = torch.full((2 * h_q * plan.max_partitions * 130 * 4 + 256,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, math.nan)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan)
+    torch.cuda.synchronize()
+    for b, n in enumerate(kv):
+        want, tol, _, _ = R.attention(q[b:b + 1], R.Tokens(cache, rows[b].cuda(), n), stats.k_tscale[b], stats.v_tscale[b], n - 1, 0, 0)
+        check_rows(out[b:b + 1], want, tol, f"sequence {b}")
+
+
+@pytest.mark.parametrize("kv,q_tokens,window,sinks", [([1, 700, 65], 1, 0, 0), ([2000, 0, 130], 3, 200, 70), ([513], 20, 0, 0)])
+def test_decode_weights(mp, kv, q_tokens, window, sinks):
+    h_q, h_kv = 10, 2
+    print(f"decode weights {kv} rows {q_tokens} window {window}", flush=True)
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [q_tokens] * len(kv), 21, weights=True, sigma=2.0)
+    before = cache.weights.clone()
+    plan = mp.kv4_decode_plan(kv, h_q, h_kv, q_tokens, window, sinks, weights=True)
+    plan.workspace.fill_(255)
+    out = torch.full_like(q, math.nan)
+    for _ in range(2):   # they accumulate
+        mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    touched = torch.zeros_like(before, dtype=torch.bool)
+    for b, n in enumerate(kv):
+        x = slice(b * q_tokens, (b + 1) * q_tokens)
+        toks = R.Tokens(cache, rows[b].cuda(), n)
+        want, tol, share, stol = R.attention(q[x], toks, stats.k_tscale[b], stats.v_tscale[b], n - q_tokens, window, sinks)
+        check_rows(out[x], want, tol, f"sequence {b}")
+        i = torch.arange(n, device="cuda")
+        pg, o = rows[b].cuda()[i // PAGE].long(), i % PAGE
+        w0 = before[pg, :, o].double()
+        # two additions in FP32
+        off = (toks.weights.double() - (w0 + 2 * share)).abs() > 2 * stol + 2 * 2.0 ** -24 * (w0 + 2 * share)
+        assert not off.any(), f"sequence {b}: {int(off.sum())} weights off"
+        touched[pg, :, o] = True
+    assert torch.equal(cache.weights[~touched].nan_to_num(5.0), before[~touched].nan_to_num(5.0))
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1, 0), (65, 1), (128, 129), (300, 64), (5000, 9000)])
+@pytest.mark.parametrize("new,ctx", [([1], [0]), ([5, 0, 64], [0, 9, 63]), ([130, 257], [0, 500]), ([600], [1000]), ([51, 52], [77, 128])])
+def test_prefill(mp, new, ctx, window, sinks):
+    h_q, h_kv = HEADS[(sum(new) + window) % len(HEADS)]
+    print(f"prefill {new} behind {ctx} heads {h_q}:{h_kv} window {window} sinks {sinks}", flush=True)
+    kv = [a + b for a, b in zip(new, ctx)]
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, new, 31 + window)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_prefill(q, cache, stats, cumulative(new), i32(ctx), i32(kv), rows.cuda(), out, window=window, sinks=sinks,
+                   max_seqlen_q=max(new))
+    torch.cuda.synchronize()
+    check_prefill(q, out, rows, cache, stats, new, ctx, window, sinks)
+
+
+def check_prefill(q, out, rows, cache, stats, new, ctx, window, sinks):
+    at = 0
+    for b, (r, c) in enumerate(zip(new, ctx)):
+        x = slice(at, at + r)
+        at += r
+        if r:
+            want, tol, _, _ = R.attention(q[x], R.Tokens(cache, rows[b].cuda(), c + r), stats.k_tscale[b], stats.v_tscale[b], c, window, sinks)
+            check_rows(out[x], want, tol, f"sequence {b}")
+
+
+@pytest.mark.parametrize("h_q,h_kv", HEADS + [(32, 8), (200, 1)])
+def test_prefill_heads(mp, h_q, h_kv):
+    print(f"prefill heads {h_q}:{h_kv}", flush=True)
+    new, ctx = [70, 3], [10, 200]
+    rows, cache, stats, q = attn_case(mp, [80, 203], h_q, h_kv, new, 41)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_prefill(q, cache, stats, cumulative(new), i32(ctx), i32([80, 203]), rows.cuda(), out)
+    torch.cuda.synchronize()
+    check_prefill(q, out, rows, cache, stats, new, ctx, 0, 0)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 130)])
+@pytest.mark.parametrize("part", [0, 128, 384, 1 << 14])
+def test_prefill_partitions(mp, part, window, sinks):
+    """Few rows behind long contexts: the plan's own cut (0) and others, merged."""
+    print(f"prefill partitions of {part}, window {window}", flush=True)
+    new, ctx, h_q, h_kv = [33, 1, 0, 66], [5000, 130, 40, 0], 8, 2
+    kv = [a + b for a, b in zip(new, ctx)]
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, new, 51)
+    plan = mp.kv4_prefill_plan(new, kv, h_q, h_kv, window, sinks)
+    if part:
+        plan.partition_tokens, plan.max_partitions = part, -(-max(kv) // part)
+        plan.workspace = torch.full((sum(new) * h_q * plan.max_partitions * 130 * 4,), 255, dtype=torch.uint8, device="cuda")
+    else:
+        assert plan.partition_tokens > 0
+        plan.workspace.fill_(255)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_prefill(q, cache, stats, cumulative(new), i32(ctx), i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    check_prefill(q, out, rows, cache, stats, new, ctx, window, sinks)
+
+
+def test_attention_of_extreme_scores(mp):
+    """Scores of thousands (one key takes all), rows of zeros, rows far below and above bf16's middle."""
+    print("attention: extreme scores", flush=True)
+    kv, h_q, h_kv = [300], 4, 2
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [6], 61)
+    stats.k_tscale.fill_(1.0)
+    q[0] *= 100
+    q[1] = 0
+    q[2] *= 2.0 ** -60
+    q[3] *= 2.0 ** -120
+    q[4, :, 1:] *= 2.0 ** -40
+    out = torch.full_like(q, math.nan)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, mp.kv4_decode_plan(kv, h_q, h_kv, 6))
+    pre = torch.full_like(q, math.nan)
+    mp.kv4_prefill(q, cache, stats, cumulative([6]), i32([294]), i32(kv), rows.cuda(), pre)
+    torch.cuda.synchronize()
+    want, tol, _, _ = R.attention(q, R.Tokens(cache, rows[0].cuda(), 300), stats.k_tscale[0], stats.v_tscale[0], 294, 0, 0)
+    check_rows(out, want, tol, "decode")
+    check_rows(pre, want, tol, "prefill")
+
+
+def test_queries_of_a_fused_projection(mp):
+    print("attention: strided queries", flush=True)
+    kv, h_q, h_kv = [200], 8, 2
+    rows, cache, stats, _ = attn_case(mp, kv, h_q, h_kv, [50], 71)
+    qkv = torch.randn(50, h_q + 4, D, device="cuda").bfloat16()
+    q = qkv[:, :h_q]
+    outs = []
+    for x in (q, q.contiguous()):
+        out = torch.full((50, h_q, D), math.nan, dtype=torch.bfloat16, device="cuda")
+        mp.kv4_prefill(x, cache, stats, cumulative([50]), i32([150]), i32(kv), rows.cuda(), out)
+        dec = torch.full((50, h_q, D), math.nan, dtype=torch.bfloat16, device="cuda")
+        mp.kv4_decode(x, cache, stats, i32(kv), rows.cuda(), dec, mp.kv4_decode_plan(kv, h_q, h_kv, 50))
+        outs += [out, dec]
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+    want, tol, _, _ = R.attention(q, R.Tokens(cache, rows[0].cuda(), 200), stats.k_tscale[0], stats.v_tscale[0], 150, 0, 0)
+    check_rows(outs[0], want, tol, "prefill")
+    check_rows(outs[1], want, tol, "decode")
+
+
+# ------------------------------------------------------------------ eviction
+def snapshot(cache, row, n):
+    t = R.Tokens(cache, row.cuda(), n)
+    return [x.clone() for x in (t.k_codes, t.k_scales, t.v_codes, t.v_scales, t.weights)]
+
+
+def fill_weights(cache, kind):
+    w = cache.weights
+    if kind == "ties":
+        w.copy_((w * 4).floor())
+    elif kind == "zero":
+        w.zero_()
+        w.view(-1)[::5] = -0.0
+    elif kind == "signed":
+        w.sub_(0.5).mul_(1e3)
+    elif kind == "special":
+        w.view(-1)[::7] = math.inf
+        w.view(-1)[::11] = -math.inf
+        w.view(-1)[::13] = math.nan
+    elif kind == "close":   # equal in the leading bytes
+        w.copy_((1.0 + (w * 300).floor() * 2.0 ** -23))
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("kind", ["random", "ties", "zero", "signed", "special", "close"])
+@pytest.mark.parametrize("kv,budget,sinks,recent", [([1, 64, 65, 0, 200], 64, 4, 10), ([1500, 700], 129, 0, 0), ([5000], 1000, 100, 900),
+                                                    ([4097, 4096, 4095], 4096, 0, 1), ([300], 1, 1, 0), ([70], 1, 0, 0)])
+def test_evict(mp, kv, budget, sinks, recent, kind, in_place):
+    print(f"evict {kv} to {budget}, {sinks} first, {recent} last, {kind}, in place {in_place}", flush=True)
+    h_kv = 3
+    new = [min(n, budget) for n in kv]
+    pages = sum(-(-n // PAGE) for n in kv + new) + 2
+    cache = R.random_cache(mp, pages, h_kv, budget, weights=True)
+    fill_weights(cache, kind)
+    both = R.page_rows(kv + new, pages, 7)
+    rows = both[:len(kv)]
+    dst = rows if in_place else both[len(kv):, :max(1, -(-max(new) // PAGE))].contiguous()
+    src = [snapshot(cache, rows[b], n) for b, n in enumerate(kv)]
+    whole = {n: getattr(cache, n).clone() for n in ("k_codes", "k_scales", "v_codes", "v_scales", "weights")}
+    kept = torch.full((len(kv), h_kv, budget), 99, dtype=torch.int32, device="cuda")
+    kv_len, new_len = i32(kv), i32([77] * len(kv))
+    mp.kv4_evict(cache, kv_len, rows.cuda(), dst.cuda(), budget, kept, new_len, sinks=sinks, recent=recent, in_place=in_place)
+    torch.cuda.synchronize()
+    assert new_len.tolist() == new
+    touched = torch.zeros(pages, PAGE, dtype=torch.bool)
+    for b, n in enumerate(kv):
+        i = torch.arange(new[b])
+        touched[dst[b][i // PAGE].long(), i % PAGE] = True
+        got = snapshot(cache, dst[b], new[b])
+        for h in range(h_kv):
+            want = R.keep(src[b][4][:, h].cpu(), budget, sinks, recent)
+            assert kept[b, h].tolist() == want + [-1] * (budget - len(want)), f"sequence {b} head {h}"
+            idx = torch.tensor(want, dtype=torch.long, device="cuda")
+            for x, y in zip(got, src[b]):
+                a, c = x[:, h], y[idx, h]
+                if a.dtype == torch.float32:
+                    a, c = a.contiguous().view(torch.int32), c.contiguous().view(torch.int32)
+                assert torch.equal(a, c), f"sequence {b} head {h}"
+    rest = ~touched.cuda()
+    assert torch.equal(cache.k_codes.transpose(1, 2)[rest], whole["k_codes"].transpose(1, 2)[rest])
+    assert torch.equal(cache.k_scales.transpose(1, 2)[rest], whole["k_scales"].transpose(1, 2)[rest])
+    assert torch.equal(cache.v_scales.permute(0, 3, 1, 2)[rest], whole["v_scales"].permute(0, 3, 1, 2)[rest])
+    view = lambda t: t.view(pages, h_kv, 16, 16, 4, 4).permute(0, 2, 4, 1, 3, 5).reshape(pages, PAGE, h_kv, 64)
+    assert torch.equal(view(cache.v_codes)[rest], view(whole["v_codes"])[rest])
+    bits = lambda t: t.transpose(1, 2).contiguous().view(torch.int32)
+    assert torch.equal(bits(cache.weights)[rest], bits(whole["weights"])[rest])
