@@ -4,16 +4,25 @@
 //
 // Choice (kv4_select_kernel, one workgroup per (sequence, KV head)): the first `sinks` and
 // the last `recent` tokens stay; of the others those of the largest weights, ties to the
-// lower index.  The threshold is found by a radix selection over order-preserving 32-bit
-// images of the weights (8 bits a pass, one histogram per wave so that weights with the
-// same leading byte do not meet on one counter), then two sweeps count and write the
-// indices in order, each wave over a segment of its own.  What bounds it: six sweeps over
-// 4 bytes per token, from L2 after the first.
+// lower index.  Weights become 32-bit images in the same order, tokens that stay the
+// largest image, so the threshold is simply the budget-th largest.  It is found by a radix
+// selection, 8 bits a pass, over histograms with 16 columns that lanes take in turn (most
+// weights share their leading byte and would meet on one counter).  Once at most 256 images
+// share the leading bytes (usually after two passes), each is compared with all of them.
+// Then two sweeps count and write the indices in order, each wave over a segment of its own.
+// The images stay in LDS, 32768 of them; what a longer sequence has more is read again each
+// sweep.  What bounds it: latency, of the passes over LDS and of one read of the weights by
+// a single compute unit.  32768 tokens to 4096, 8 heads: 24 us (76 with a histogram per
+// wave and the weights read each sweep; 32 with the images in registers, whose unrolled
+// sweeps outgrow the instruction cache).
 //
 // Move (kv4_move_kernel): destination place i takes source token kept[i] >= i.  With
-// separate pages the places are shared among workgroups; in place, one workgroup per plane
-// goes through them in order, reading a chunk before it writes it: a later chunk's sources
-// lie at or after its own places, so no write reaches a token that is still to be read.
+// separate pages the places are shared among workgroups; in place, a workgroup per half of
+// the planes goes through them in order, reading a chunk before it writes it: a later
+// chunk's sources lie at or after its own places, so no write reaches a token that is still
+// to be read.  What bounds it: HBM lines.  A kept token brings the 256-byte V quad and the
+// 128-byte line of K codes that it lies in, about 450 bytes read for 148 where one token
+// in six stays; 24 sequences to 2048 tokens, 8 heads: 48 us, 4.9 TB/s of such lines.
 #include "kv4_device.h"
 
 namespace mpfa {
@@ -21,7 +30,15 @@ namespace mpfa {
 namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
-constexpr int kMoveChunk = 64;   // places per step of the move: 16 threads each (1024)
+constexpr int kHeld = 32;        // pages per wave whose images stay in LDS (128 KB, 32768 tokens)
+constexpr int kLoads = 16;       // pages in flight when they are filled
+constexpr int kAhead = 8;        // pages per step of a sweep
+constexpr int kListed = 256;     // images compared with each other (each thread one)
+constexpr int kColumns = 16;     // histogram columns
+constexpr int kMoveTokens = 4;   // tokens per thread and step of the move (64 at a time, 16 threads each)
+constexpr int kMoveChunk = 64 * kMoveTokens;
+static_assert(256 * kColumns == 4 * kSelectThreads, "one 16-byte word of the histogram per thread");
+static_assert(kHeld % kLoads == 0 && kHeld % kAhead == 0 && kHeld <= 64, "whole reads of held pages");
 
 // FP32 order as unsigned order; -0 as +0; NaN above everything.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -30,121 +47,159 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
+constexpr uint32_t kStays = 0xFFFFFFFFu, kNone = 0u;   // images of a token that stays anyway, and of no token
+
 __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictParams p) {
-  __shared__ uint32_t hist[kSelectWaves][256];
+  __shared__ __attribute__((aligned(16))) uint32_t hist[256 * kColumns];   // [bin][column]
+  __shared__ uint32_t images[kSelectWaves * kHeld * 64];
   __shared__ uint32_t total[256];
-  __shared__ uint32_t s_prefix, s_need;
+  __shared__ uint32_t s_prefix, s_need, s_count, s_listed;
   __shared__ int above[kSelectWaves], equal[kSelectWaves];
-  const int hk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int hk = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = max(p.kv_len[b], 0);
   int32_t* kept = p.kept + ((int64_t)b * p.h_kv + hk) * p.budget;
-  if (tid == 0 && hk == 0) p.new_len[b] = min(n, p.budget);
   if (n <= p.budget) {   // everything stays
     for (int i = tid; i < p.budget; i += kSelectThreads) kept[i] = i < n ? i : -1;
     return;
   }
   const int32_t* pt = p.page_table + (int64_t)b * p.max_pages;
-  const int lo = p.sinks, hi = n - p.recent;             // tokens that compete: lo .. hi - 1
-  const int want = p.budget - p.sinks - p.recent;        // of them stay (>= 0, < hi - lo since n > budget)
-  auto key_of = [&](int i) {
-    return weight_key(p.cache.weights[kv4_row(pt[i >> 6], p.h_kv, hk) * kPage + (i & (kPage - 1))]);
-  };
+  const int lo = p.sinks, hi = n - p.recent;   // tokens that compete: lo .. hi - 1
   // waves own segments of whole pages, in order
   const int pages = (n + 63) >> 6, seg = (pages + kSelectWaves - 1) / kSelectWaves;
-  const int g0 = wave * seg, g1 = min(pages, g0 + seg);
-
-  // ---- threshold: the want-th largest key (want == 0: above every key)
-  uint32_t prefix = 0xFFFFFFFFu, need = 0;
-  if (want > 0) {
-    if (tid == 0) {
-      s_prefix = 0u;
-      s_need = (uint32_t)want;
-    }
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < kSelectWaves * 256; i += kSelectThreads) hist[0][i] = 0u;
-      __syncthreads();
-      const uint32_t base = s_prefix, left = s_need;
-      for (int g = g0; g < g1; ++g) {
-        const int i = g * 64 + lane;
-        if (i >= lo && i < hi) {
-          const uint32_t k = key_of(i);
-          if (shift == 24 || (k >> (shift + 8)) == (base >> (shift + 8))) atomicAdd(&hist[wave][(k >> shift) & 255u], 1u);
-        }
-      }
-      __syncthreads();
-      if (tid < 256) {
-        uint32_t t = 0;
-        for (int w = 0; w < kSelectWaves; ++w) t += hist[w][tid];
-        total[tid] = t;
-      }
-      __syncthreads();
-      if (wave == 0) {   // lane l holds bins 4l .. 4l + 3; counts of the bins above
-        uint32_t c[4], sum = 0;
+  const int g0 = wave * seg, mine = max(0, min(pages - g0, seg));
+  auto image_of = [&](int g, float w) {
+    const int i = g * 64 + lane;
+    return i >= n ? kNone : (i < lo || i >= hi ? kStays : weight_key(w));
+  };
+  uint32_t* own = images + wave * kHeld * 64 + lane;   // the wave's images, one page per 64
+  const int my_page = mine > 0 ? pt[g0 + min(lane & (kHeld - 1), mine - 1)] : 0;
+  for (int j0 = 0; j0 < min(mine, kHeld); j0 += kLoads) {
+    float w[kLoads];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          c[i] = total[4 * lane + i];
-          sum += c[i];
-        }
-        uint32_t up = sum;   // inclusive suffix sum over the lanes
-        for (int off = 1; off < 64; off <<= 1) {
-          const uint32_t o = __shfl_down(up, off);
-          if (lane + off < 64) up += o;
-        }
-        uint32_t over = up - sum;   // keys in bins of higher lanes
+    for (int j = 0; j < kLoads; ++j)
+      w[j] = p.cache.weights[kv4_row(__builtin_amdgcn_readlane(my_page, j0 + j), p.h_kv, hk) * kPage + lane];
 #pragma unroll
-        for (int i = 3; i >= 0; --i) {
-          if (over < left && left <= over + c[i]) {
-            s_prefix = base | ((uint32_t)(4 * lane + i) << shift);
-            s_need = left - over;
-          }
-          over += c[i];
-        }
-      }
-      __syncthreads();
-    }
-    prefix = s_prefix;
-    need = s_need;   // of the keys equal to the threshold, the first `need` stay
+    for (int j = 0; j < kLoads; ++j) own[(j0 + j) * 64] = j0 + j < mine ? image_of(g0 + j0 + j, w[j]) : kNone;
   }
+  // f(j, image) for the wave's pages in order
+  auto sweep = [&](auto&& f) {
+    const int here = min(mine, kHeld);
+    for (int j0 = 0; j0 < here; j0 += kAhead) {   // past `mine` no token's image
+      uint32_t k[kAhead];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) k[j] = own[(j0 + j) * 64];
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) f(j0 + j, k[j]);
+    }
+    for (int j = kHeld; j < mine; ++j)
+      f(j, image_of(g0 + j, p.cache.weights[kv4_row(pt[g0 + j], p.h_kv, hk) * kPage + lane]));
+  };
+
+  // ---- threshold: the budget-th largest image
+  if (tid == 0) {
+    s_prefix = 0u;
+    s_need = (uint32_t)p.budget;
+    s_count = (uint32_t)n;
+  }
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    reinterpret_cast<u32x4*>(hist)[tid] = (u32x4){0u, 0u, 0u, 0u};
+    if (tid == 0) s_listed = 0u;
+    __syncthreads();
+    const uint32_t base = s_prefix, left = s_need, count = s_count;
+    auto inside = [&](uint32_t k) { return shift == 24 || (k >> (shift + 8)) == (base >> (shift + 8)); };
+    if (count <= kListed) {   // few enough: each image against all of them
+      uint32_t* list = hist;         // its first words are zero: no image
+      sweep([&](int, uint32_t k) {
+        if (k != kNone && inside(k)) list[atomicAdd(&s_listed, 1u)] = k;
+      });
+      __syncthreads();
+      if (tid < count) {
+        const uint32_t k = list[tid];
+        uint32_t gt = 0, ge = 0;
+#pragma unroll 1
+        for (uint32_t i = 0; i < count; i += 4) {
+          const u32x4 o = reinterpret_cast<const u32x4*>(list)[i >> 2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            gt += o[e] > k;
+            ge += o[e] >= k;
+          }
+        }
+        if (gt < left && left <= ge) {   // the equal ones all write the same
+          s_prefix = k;
+          s_need = left - gt;
+        }
+      }
+      __syncthreads();
+      break;
+    }
+    sweep([&](int, uint32_t k) {
+      if (inside(k)) atomicAdd(&hist[((k >> shift) & 255u) * kColumns + (lane & (kColumns - 1))], 1u);
+    });
+    __syncthreads();
+    {   // four threads per bin, a quarter of its columns each
+      const u32x4 w = reinterpret_cast<const u32x4*>(hist)[tid];
+      uint32_t t = (w[0] + w[1]) + (w[2] + w[3]);
+      t += __shfl_xor(t, 1);
+      t += __shfl_xor(t, 2);
+      if ((tid & 3) == 0) total[tid >> 2] = t;
+    }
+    __syncthreads();
+    if (wave == 0) {   // lane l holds bins 4l .. 4l + 3
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] = total[4 * lane + i];
+        sum += c[i];
+      }
+      uint32_t up = sum;   // inclusive suffix sum over the lanes
+      for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t o = __shfl_down(up, off);
+        if (lane + off < 64) up += o;
+      }
+      uint32_t over = up - sum;   // images in bins of higher lanes
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {
+        if (over < left && left <= over + c[i]) {
+          s_prefix = base | ((uint32_t)(4 * lane + i) << shift);
+          s_need = left - over;
+          s_count = c[i];
+        }
+        over += c[i];
+      }
+    }
+    __syncthreads();
+  }
+  const uint32_t prefix = s_prefix;
+  const int need = (int)s_need;   // of the images equal to the threshold, the first `need` stay
 
   // ---- counts per wave, then places
   int na = 0, ne = 0;
-  for (int g = g0; g < g1; ++g) {
-    const int i = g * 64 + lane;
-    bool a = i < n && (i < lo || i >= hi), e = false;
-    if (want > 0 && i >= lo && i < hi) {
-      const uint32_t k = key_of(i);
-      a = k > prefix;
-      e = k == prefix;
-    }
-    na += __popcll(__ballot(a));
-    ne += __popcll(__ballot(e));
-  }
+  sweep([&](int, uint32_t k) {
+    na += __popcll(__ballot(k > prefix));
+    ne += __popcll(__ballot(k == prefix));
+  });
   if (lane == 0) {
     above[wave] = na;
     equal[wave] = ne;
   }
   __syncthreads();
-  int place = 0, eq = 0;   // places taken and equal keys met before this wave's segment
+  int place = 0, eq = 0;   // places taken and equal images met before this wave's segment
   for (int w = 0; w < wave; ++w) {
-    const int take = min(equal[w], max(0, (int)need - eq));
-    place += above[w] + take;
+    place += above[w] + min(equal[w], max(0, need - eq));
     eq += equal[w];
   }
-  for (int g = g0; g < g1; ++g) {
-    const int i = g * 64 + lane;
-    bool a = i < n && (i < lo || i >= hi), e = false;
-    if (want > 0 && i >= lo && i < hi) {
-      const uint32_t k = key_of(i);
-      a = k > prefix;
-      e = k == prefix;
-    }
-    const uint64_t below = (1ull << lane) - 1ull, em = __ballot(e);
-    if (e && eq + __popcll(em & below) < (int)need) a = true;
+  const uint64_t below = (1ull << lane) - 1ull;
+  sweep([&](int j, uint32_t k) {
+    const uint64_t em = __ballot(k == prefix);
+    bool a = k > prefix;
+    if (em) a = a || (k == prefix && eq + __popcll(em & below) < need);
     const uint64_t am = __ballot(a);
-    if (a) kept[place + __popcll(am & below)] = i;
+    if (a) kept[place + __popcll(am & below)] = (g0 + j) * 64 + lane;
     place += __popcll(am);
     eq += __popcll(em);
-  }
+  });
 }
 
 // A thread's part of a token: of every plane the piece that `piece` (0 .. 15) names.
@@ -153,42 +208,61 @@ struct Moved {
   uint8_t sk, sv;
 };
 
+// Grid x: the workgroups that share the places, or in place one; y: the KV head and, in
+// place, which half of the planes (0: K and the weights, 1: V; both: 2).
+template <bool IN_PLACE>
 __global__ __launch_bounds__(1024) void kv4_move_kernel(Kv4EvictParams p) {
-  const int hk = blockIdx.y, b = blockIdx.z, piece = threadIdx.x & 15, slot = threadIdx.x >> 4;
+  const int b = blockIdx.z, piece = threadIdx.x & 15, slot = threadIdx.x >> 4;
+  const int hk = IN_PLACE ? blockIdx.y >> 1 : blockIdx.y;
+  const bool do_k = !IN_PLACE || (blockIdx.y & 1) == 0, do_v = !IN_PLACE || (blockIdx.y & 1) == 1;
   const int n = min(max(p.kv_len[b], 0), p.budget);
   const int32_t* kept = p.kept + ((int64_t)b * p.h_kv + hk) * p.budget;
   const int32_t* src_pt = p.page_table + (int64_t)b * p.max_pages;
   const int32_t* dst_pt = p.dst_page_table + (int64_t)b * p.dst_max_pages;
   const int steps = (n + kMoveChunk - 1) / kMoveChunk;
   for (int c = blockIdx.x; c < steps; c += gridDim.x) {
-    const int i = c * kMoveChunk + slot;
-    const bool have = i < n;
-    Moved m = {};
-    if (have) {
-      const int s = kept[i], o = s & (kPage - 1);
+    Moved m[kMoveTokens] = {};
+    bool have[kMoveTokens];
+#pragma unroll
+    for (int t = 0; t < kMoveTokens; ++t) {
+      const int i = c * kMoveChunk + t * 64 + slot;
+      have[t] = i < n;
+      const int s = have[t] ? kept[i] : 0;
+      if (IN_PLACE && s == i) have[t] = false;   // it stays where it is
+      if (!have[t]) continue;
+      const int o = s & (kPage - 1);
       const int64_t row = kv4_row(src_pt[s >> 6], p.h_kv, hk);
-      m.k = reinterpret_cast<const uint32_t*>(p.cache.k_codes + (row * kPage + o) * 64)[piece];
-      m.v = reinterpret_cast<const uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256)[piece * 4 + (o & 3)];
-      if (piece < 8) {
-        m.sk = p.cache.k_scales[(row * kPage + o) * 8 + piece];
-        m.sv = p.cache.v_scales[(row * 8 + piece) * kPage + o];
+      if (do_k) {
+        m[t].k = reinterpret_cast<const uint32_t*>(p.cache.k_codes + (row * kPage + o) * 64)[piece];
+        if (piece < 8) m[t].sk = p.cache.k_scales[(row * kPage + o) * 8 + piece];
+        if (piece == 8) m[t].w = __float_as_uint(p.cache.weights[row * kPage + o]);
       }
-      if (piece == 8) m.w = __float_as_uint(p.cache.weights[row * kPage + o]);
+      if (do_v) {
+        m[t].v = reinterpret_cast<const uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256)[piece * 4 + (o & 3)];
+        if (piece < 8) m[t].sv = p.cache.v_scales[(row * 8 + piece) * kPage + o];
+      }
     }
-    if (p.in_place) __syncthreads();   // the chunk is read before any of it is written
-    if (have) {
-      const int o = i & (kPage - 1);
+    if (IN_PLACE) __syncthreads();   // the chunk is read before any of it is written
+#pragma unroll
+    for (int t = 0; t < kMoveTokens; ++t) {
+      if (!have[t]) continue;
+      const int i = c * kMoveChunk + t * 64 + slot, o = i & (kPage - 1);
       const int64_t row = kv4_row(dst_pt[i >> 6], p.h_kv, hk);
-      reinterpret_cast<uint32_t*>(p.cache.k_codes + (row * kPage + o) * 64)[piece] = m.k;
-      reinterpret_cast<uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256)[piece * 4 + (o & 3)] = m.v;
-      if (piece < 8) {
-        p.cache.k_scales[(row * kPage + o) * 8 + piece] = m.sk;
-        p.cache.v_scales[(row * 8 + piece) * kPage + o] = m.sv;
+      if (do_k) {
+        reinterpret_cast<uint32_t*>(p.cache.k_codes + (row * kPage + o) * 64)[piece] = m[t].k;
+        if (piece < 8) p.cache.k_scales[(row * kPage + o) * 8 + piece] = m[t].sk;
+        if (piece == 8) p.cache.weights[row * kPage + o] = __uint_as_float(m[t].w);
       }
-      if (piece == 8) p.cache.weights[row * kPage + o] = __uint_as_float(m.w);
+      if (do_v) {
+        reinterpret_cast<uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256)[piece * 4 + (o & 3)] = m[t].v;
+        if (piece < 8) p.cache.v_scales[(row * 8 + piece) * kPage + o] = m[t].sv;
+      }
     }
-    if (p.in_place) __syncthreads();
+    if (IN_PLACE) __syncthreads();
   }
+  // new_len may be kv_len: this kernel gets the same n from either value, and the choice has
+  // read the lengths before it
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.new_len[b] = n;
 }
 
 }  // namespace
@@ -196,7 +270,8 @@ __global__ __launch_bounds__(1024) void kv4_move_kernel(Kv4EvictParams p) {
 hipError_t launch_kv4_evict(const Kv4EvictParams& p, hipStream_t stream) {
   kv4_select_kernel<<<dim3(p.h_kv, p.batch), kSelectThreads, 0, stream>>>(p);
   const int steps = (p.budget + kMoveChunk - 1) / kMoveChunk;
-  kv4_move_kernel<<<dim3(p.in_place ? 1 : steps, p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  if (p.in_place) kv4_move_kernel<true><<<dim3(1, 2 * p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  else kv4_move_kernel<false><<<dim3(steps, p.h_kv, p.batch), 1024, 0, stream>>>(p);
   return hipGetLastError();
 }
 

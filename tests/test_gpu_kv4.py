@@ -430,3 +430,34 @@ def test_evict(mp, kv, budget, sinks, recent, kind, in_place):
     assert torch.equal(view(cache.v_codes)[rest], view(whole["v_codes"])[rest])
     bits = lambda t: t.transpose(1, 2).contiguous().view(torch.int32)
     assert torch.equal(bits(cache.weights)[rest], bits(whole["weights"])[rest])
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_long_sequences_and_lengths_written_in_place(mp, in_place):
+    """More tokens than the choice holds on the chip, in a batch whose new lengths go over the old."""
+    print(f"evict long sequences, in place {in_place}", flush=True)
+    kv, h_kv, budget = [40001, 33000, 500, 32768, 70000], 8, 700
+    new = [min(n, budget) for n in kv]
+    pages = sum(-(-n // PAGE) for n in kv + new) + 1
+    cache = R.random_cache(mp, pages, h_kv, 17, weights=True)
+    both = R.page_rows(kv + new, pages, 8)
+    rows = both[:len(kv)]
+    dst = rows if in_place else both[len(kv):, :-(-budget // PAGE)].contiguous()
+    src = [snapshot(cache, rows[b], n) for b, n in enumerate(kv)]
+    kept = torch.empty(len(kv), h_kv, budget, dtype=torch.int32, device="cuda")
+    kv_len = i32(kv)
+    mp.kv4_evict(cache, kv_len, rows.cuda(), dst.cuda(), budget, kept, kv_len, sinks=3, recent=100, in_place=in_place)
+    torch.cuda.synchronize()
+    assert kv_len.tolist() == new
+    for b, n in enumerate(kv):
+        got = snapshot(cache, dst[b], new[b])
+        for h in range(h_kv):
+            w = src[b][4][:, h].cpu()
+            if n > budget:
+                w[:3] = w[n - 100:] = math.inf
+                want = torch.sort(w, descending=True, stable=True).indices[:budget].sort().values
+            else:
+                want = torch.arange(n)
+            assert kept[b, h, :new[b]].tolist() == want.tolist(), f"sequence {b} head {h}"
+            for x, y in zip(got, src[b]):
+                assert torch.equal(x[:, h], y[want.cuda(), h])
