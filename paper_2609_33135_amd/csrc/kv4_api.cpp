@@ -273,7 +273,7 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* a, void* workspace, size_t
 mpfa_status mpfa_kv4_prefill_plan(int32_t batch, const int32_t* rows_host, const int32_t* kv_len_host, int32_t h_q, int32_t h_kv,
                                   int32_t window, int32_t sinks, int32_t num_cus, int32_t* partition_tokens,
                                   int32_t* max_partitions, size_t* workspace_bytes) {
-  if (batch < 1 || !rows_host || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS || h_q % h_kv ||
+  if (batch < 1 || batch > 65535 || !rows_host || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS || h_q % h_kv ||
       window < 0 || sinks < 0 || num_cus < 1 || !partition_tokens || !max_partitions || !workspace_bytes)
     return MPFA_ERR_INVALID;
   const int tm = mpfa::kKv4Rows / (h_q / h_kv);
@@ -330,21 +330,36 @@ mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* a, void* workspace, size_
 mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int32_t h_q, int32_t h_kv, int32_t q_tokens,
                                  int32_t window, int32_t sinks, uint32_t flags, int32_t num_cus, int32_t* partition_tokens,
                                  int32_t* max_partitions, size_t* workspace_bytes) {
-  if (batch < 1 || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS || h_q % h_kv || q_tokens < 1 ||
+  if (batch < 1 || batch > 65535 || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS || h_q % h_kv || q_tokens < 1 ||
       window < 0 || sinks < 0 || (flags & ~MPFA_KV4_WEIGHTS) || num_cus < 1 || !partition_tokens || !max_partitions ||
       !workspace_bytes)
     return MPFA_ERR_INVALID;
   const int64_t chunks = ((int64_t)q_tokens * (h_q / h_kv) + 15) / 16;
-  int64_t tiles = 0, most = 1;
+  auto seen = [&](int b) {
+    return seen_tiles((int64_t)kv_len_host[b] - q_tokens, (int64_t)kv_len_host[b] - 1, window, sinks);
+  };
+  int64_t most = 1;
   for (int b = 0; b < batch; ++b) {
     if (kv_len_host[b] < 0) return MPFA_ERR_INVALID;
-    const int64_t nt = seen_tiles((int64_t)kv_len_host[b] - q_tokens, (int64_t)kv_len_host[b] - 1, window, sinks);
-    tiles += nt * h_kv * chunks;
-    most = std::max(most, nt);
+    most = std::max(most, seen(b));
   }
-  // about 16 waves per compute unit, at least two tiles each
-  int64_t part = (tiles + 16LL * num_cus - 1) / (16LL * num_cus);
-  part = std::min<int64_t>(std::max<int64_t>(part, 2), 128);
+  // A workgroup holds four partitions (waves) of a KV head.  The units of the card take
+  // equally many workgroups, rounded up, of `part` tiles and about one tile's time to start
+  // and store each: the smallest such sum wins.  (32 contexts of 16K to 64K keys, 32:8 heads:
+  // 10 tiles 222 us, 12 tiles, with a last round of few, 260; 4 of 32K: 8 tiles 35 us, 5
+  // tiles 40, 2 tiles 46; one of 64K, 40:8: 4 tiles 25.5, 3 tiles 32; 64 of 2100: 5 tiles
+  // 38.8, 10 tiles 41.9.)
+  int64_t part = 1, best = INT64_MAX;
+  for (int64_t t = 1; t <= 128; ++t) {
+    int64_t groups = 0;
+    for (int b = 0; b < batch; ++b) groups += ((seen(b) + t - 1) / t * chunks + 3) / 4 * h_kv;
+    const int64_t cost = (groups + num_cus - 1) / num_cus * (t + 1);
+    if (cost < best) {
+      best = cost;
+      part = t;
+    }
+    if (t >= most) break;   // one partition each: longer ones change nothing
+  }
   const int64_t parts = (most + part - 1) / part;
   DecodeSpace s;
   if (!decode_space(batch, h_q, q_tokens, (int)part * MPFA_KV_TILE, (int)parts, flags & MPFA_KV4_WEIGHTS, &s)) return MPFA_ERR_INVALID;

@@ -13,11 +13,12 @@
 //   O^T += V^T P^T   16x16x32 FP16 MFMA
 //
 // K and V go from memory to registers, 16 bytes per lane and load, no LDS.  Inside a
-// 128-key tile MFMA row r of key block mb is key 32 (r/4) + 4 mb + r%4, so lane group g
-// (lanes 16g .. +15) ends up with the scores of keys 32g .. 32g+31 of its column, and
-// these are the keys it supplies to the PV product.  For V a lane holds the octet of
-// channels 8 lr .. +7 of those 32 keys: all its values share one scale group, and MFMA
-// row lr of channel block db is channel 8 lr + db.
+// 128-key tile (two pages) MFMA row r of key block mb is key 64 (mb/4) + 16 (r/4) + 4 (mb%4)
+// + r%4, so lane group g (lanes 16g .. +15) ends up with the scores of keys 16g .. 16g+15 of
+// either page of its column, and these are the keys it supplies to the PV product; every
+// load of a wave lies in one page, whose address is in scalar registers.  For V a lane
+// holds the octet of channels 8 lr .. +7 of those keys: all its values share one scale
+// group, and MFMA row lr of channel block db is channel 8 lr + db.
 //
 // What bounds it: HBM reads, 144 bytes per (token, KV head).
 #include "kv4_device.h"
@@ -30,13 +31,58 @@ namespace {
 
 constexpr int kDecodeWaves = 4;
 
-template <bool WEIGHTS>
+// Workgroups of a sequence of kvl keys for one KV head: partitions times column chunks,
+// four waves each.
+__device__ __forceinline__ int groups_of(const Kv4AttnParams& p, int kvl, int chunks) {
+  const int nt = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks).nt;
+  const int parts = min((nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
+  return (parts * chunks + kDecodeWaves - 1) / kDecodeWaves;
+}
+
+// Sequence and workgroup of position `pos` in a grid whose first workgroups are the ones
+// with work, sequence by sequence; false past them.  Spread over a grid by sequence, the
+// empty workgroups of the shorter ones take places on the card, and others get two: 16
+// contexts of 10K to 32K keys, 8:2 heads, 23.1 us so, 30.3 before; 32 of
+// 16K to 64K, 32:8, 210 us, 222 before.
+__device__ __forceinline__ bool find_group(const Kv4AttnParams& p, int pos, int chunks, int& b, int& group) {
+  const int lane = threadIdx.x & 63;
+  for (int base = 0; base < p.batch; base += 64) {
+    const int mine = base + lane < p.batch ? groups_of(p, p.kv_len[base + lane], chunks) : 0;
+    int incl = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(incl, d);
+      if (lane >= d) incl += up;
+    }
+    const uint64_t past = __ballot(incl > pos);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      b = base + at;
+      group = pos - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(mine, at));
+      return true;
+    }
+    pos -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return false;
+}
+
+// PACKED: one grid dimension, see find_group; else sequences on z (a batch whose lengths
+// would take long to scan; a single sequence, which needs none: 1 us less).
+constexpr int kPackedBatch = 512;
+
+template <bool WEIGHTS, bool PACKED>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4AttnParams p) {
   const int lane = threadIdx.x & 63, g = lane >> 4, lr = lane & 15;
   const int grp = p.h_q / p.h_kv, cols = p.q_tokens * grp;
   const int chunks = (cols + 15) >> 4;
-  const int b = blockIdx.z, hk = blockIdx.y / chunks, chunk = blockIdx.y - hk * chunks;
-  const int part = __builtin_amdgcn_readfirstlane(blockIdx.x * kDecodeWaves + (threadIdx.x >> 6));
+  int b = blockIdx.z, hk = blockIdx.y, group = blockIdx.x;
+  if (PACKED) {
+    hk = blockIdx.x % p.h_kv;
+    if (!find_group(p, blockIdx.x / p.h_kv, chunks, b, group)) return;
+  }
+  // the waves that take the column chunks of one partition are neighbours: they read the
+  // same tiles at about the same time
+  const int item = __builtin_amdgcn_readfirstlane(group * kDecodeWaves + (threadIdx.x >> 6));
+  const int part = item / chunks, chunk = item - part * chunks;
   const int kvl = p.kv_len[b];
   const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
   const int v0 = part * p.partition_tiles, v1 = min(tiles.nt, v0 + p.partition_tiles);
@@ -49,6 +95,57 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
   // keys below it are outside the window (unless they are sinks)
   const int low = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
   const int64_t row = (int64_t)b * p.q_tokens + tok;
+
+  const int32_t* pt = p.page_table + (int64_t)b * p.max_pages;
+  const int npg = (kvl + 63) >> 6;
+  // the pages of 32 visible tiles, one per lane, read back with v_readlane: the loop has
+  // no page-table loads, whose results would drain the loads in flight
+  int win = 0, win_base = 0;
+  auto load_window = [&](int v) {
+    win_base = v;
+    const int x = v + (lane >> 1);
+    win = pt[min(2 * tiles.tile(min(x, tiles.nt - 1)) + (lane & 1), npg - 1)];
+  };
+  int64_t c0, c1;   // (page, KV head) rows of the tile
+  auto tile_pages = [&](int v) {
+    if (v - win_base >= 32) load_window(v);
+    c0 = kv4_row(__builtin_amdgcn_readlane(win, 2 * (v - win_base)), p.h_kv, hk);
+    c1 = kv4_row(__builtin_amdgcn_readlane(win, 2 * (v - win_base) + 1), p.h_kv, hk);
+  };
+
+  // offsets of the lane's bytes in a page: the rest is scalar or constant
+  const uint32_t krow = 16 * (lr >> 2) + (lr & 3);   // + 4 (mb % 4): key of MFMA row lr
+  const uint32_t k_off = krow * 64 + 16 * g, ks_off = krow * 8 + 2 * g;
+  const uint32_t v_off = g * 1024 + lr * 16, vs_off = (lr >> 1) * 64 + 16 * g;
+  u32x4 kc[8];
+  uint32_t ksc[8];
+  auto load_k = [&]() {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int64_t r = half ? c1 : c0;
+      const uint8_t *codes = p.cache.k_codes + r * 4096, *scales = p.cache.k_scales + r * 512;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ksc[4 * half + i] = *reinterpret_cast<const uint16_t*>(scales + ks_off + 32 * i);
+        kc[4 * half + i] = *reinterpret_cast<const u32x4*>(codes + k_off + 256 * i);
+      }
+    }
+  };
+  u32x4 vc[8], vsc[2];
+  auto load_v = [&]() {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int64_t r = half ? c1 : c0;
+      const uint8_t *codes = p.cache.v_codes + r * 4096, *scales = p.cache.v_scales + r * 512;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vc[4 * half + i] = *reinterpret_cast<const u32x4*>(codes + v_off + 256 * i);
+      vsc[half] = *reinterpret_cast<const u32x4*>(scales + vs_off);
+    }
+  };
+
+  load_window(v0);
+  tile_pages(v0);
+  load_k();
 
   // ---- Q: channels 32g .. +31 of the lane's column
   f16x8 qop[4];
@@ -68,56 +165,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     lam = score_scale(p.lam, p.k_tscale[b * p.h_kv + hk], shift);
   }
 
-  const int32_t* pt = p.page_table + (int64_t)b * p.max_pages;
-  const int npg = (kvl + 63) >> 6;
-  // the pages of 32 visible tiles, one per lane, read back with v_readlane: the loop has
-  // no page-table loads, whose results would drain the loads in flight
-  int win = 0, win_base = 0;
-  auto load_window = [&](int v) {
-    win_base = v;
-    const int x = v + (lane >> 1);
-    win = pt[min(2 * tiles.tile(min(x, tiles.nt - 1)) + (lane & 1), npg - 1)];
-  };
-  auto tile_pages = [&](int v, int& q0, int& q1) {
-    if (v - win_base >= 32) load_window(v);
-    q0 = __builtin_amdgcn_readlane(win, 2 * (v - win_base));
-    q1 = __builtin_amdgcn_readlane(win, 2 * (v - win_base) + 1);
-  };
-
-  const int krow = (32 * (lr >> 2) + (lr & 3)) & 63;   // + 4 mb: key of MFMA row lr in its page
-  u32x4 kc[8];
-  uint32_t ksc[8];
-  auto load_k = [&](int q0, int q1) {
-    const int64_t base = kv4_row((lr >> 3) ? q1 : q0, p.h_kv, hk) * kPage + krow;
-#pragma unroll
-    for (int mb = 0; mb < 8; ++mb) {
-      ksc[mb] = *reinterpret_cast<const uint16_t*>(p.cache.k_scales + (base + 4 * mb) * 8 + 2 * g);
-      kc[mb] = *reinterpret_cast<const u32x4*>(p.cache.k_codes + (base + 4 * mb) * 64 + 16 * g);
-    }
-  };
-  u32x4 vc[8], vsc[2];
-  auto load_v = [&](int q0, int q1) {
-    const int64_t base = kv4_row((g >> 1) ? q1 : q0, p.h_kv, hk);
-    const uint8_t* src = p.cache.v_codes + (base * 16 + 8 * (g & 1)) * 256 + 16 * lr;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) vc[i] = *reinterpret_cast<const u32x4*>(src + 256 * i);
-    const uint8_t* sc = p.cache.v_scales + (base * 8 + (lr >> 1)) * kPage + 32 * (g & 1);
-    vsc[0] = reinterpret_cast<const u32x4*>(sc)[0];
-    vsc[1] = reinterpret_cast<const u32x4*>(sc)[1];
-  };
-
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l = 0.0f;   // m in accumulator units (times lam: log2)
   f32x4 o[8];
 #pragma unroll
   for (int db = 0; db < 8; ++db) o[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
-  int c0, c1;
-  load_window(v0);
-  tile_pages(v0, c0, c1);
-  load_k(c0, c1);
   for (int v = v0; v < v1; ++v) {
     const int key0 = tiles.tile(v) * kTile;
-    load_v(c0, c1);
+    load_v();
     __builtin_amdgcn_sched_barrier(0);   // the waits for K below leave V in flight
     f32x4 s[8];
 #pragma unroll
@@ -129,29 +184,26 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
       c = mfma_f16(dequant8h(kc[mb][2], sc[1]), qop[2], c);
       s[mb] = mfma_f16(dequant8h(kc[mb][3], sc[1]), qop[3], c);
     }
-    tile_pages(min(v + 1, v1 - 1), c0, c1);
-    load_k(c0, c1);                      // past the last tile: it again
-    // ---- scores in log2 units; masked ones (which may come from stale bytes) by selection
-    const int k0 = key0 + 32 * g;
+    tile_pages(min(v + 1, v1 - 1));
+    load_k();                            // past the last tile: it again
+    // ---- masked scores (which may come from stale bytes) by selection
+    const int k0 = key0 + 16 * g;
     if (key0 + kTile - 1 > kvl - p.q_tokens || (p.window > 0 && key0 < kvl - p.window)) {   // uniform
 #pragma unroll
       for (int mb = 0; mb < 8; ++mb)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int key = k0 + 4 * mb + i;
+          const int key = k0 + 64 * (mb >> 2) + 4 * (mb & 3) + i;
           const bool seen = key <= pos && (key >= low || key < p.sinks);
-          s[mb][i] = seen ? s[mb][i] * lam : -INFINITY;
+          s[mb][i] = seen ? s[mb][i] : -INFINITY;
         }
-    } else {
-#pragma unroll
-      for (int mb = 0; mb < 8; ++mb) s[mb] *= lam;
     }
     if (WEIGHTS) {
       if (valid) {
         float* dst = p.scores + (((int64_t)b * p.h_kv + hk) * cols + col) * ((int64_t)p.max_partitions * p.partition_tiles * kTile) +
-                     (int64_t)v * kTile + 32 * g;
+                     (int64_t)v * kTile + 16 * g;
 #pragma unroll
-        for (int mb = 0; mb < 8; ++mb) *reinterpret_cast<f32x4*>(dst + 4 * mb) = s[mb];
+        for (int mb = 0; mb < 8; ++mb) *reinterpret_cast<f32x4*>(dst + 64 * (mb >> 2) + 4 * (mb & 3)) = s[mb] * lam;
       }
     }
     float mxa = -INFINITY, mxb = -INFINITY;
@@ -164,9 +216,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     }
     const float mnew = fmaxf(m, wave_max16(fmaxf(mxa, mxb)));
     const float muse = mnew == -INFINITY ? 0.0f : mnew;
-    const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - muse);
+    const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - muse) * lam);
     m = mnew;
-    const float bias = kLog2P - muse;
+    const float bias = __builtin_fmaf(-muse, lam, kLog2P);
     float ps = 0.0f;
     f16x8 pb[4];
 #pragma unroll
@@ -174,7 +226,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
       float e[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(s[mb][i] + bias);
+        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][i], lam, bias));
         pb[mb >> 1][4 * (mb & 1) + i] = (_Float16)e[i];
       }
       ps += (e[0] + e[1]) + (e[2] + e[3]);
@@ -187,15 +239,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     // ---- V: keys past the end hold stale bytes, P = 0 there: their scales are cleared so
     // that 0 * NaN cannot occur
     if (key0 + kTile > kvl) {
-      const int nv = kvl - k0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int keep = nv - 4 * i;
+        const int keep = kvl - k0 - 64 * (i >> 2) - 4 * (i & 3);
         vsc[i >> 2][i & 3] &= keep >= 4 ? 0xFFFFFFFFu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
       }
     }
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {        // keys 32g + 8t .. +7
+    for (int t = 0; t < 4; ++t) {        // keys 64 (t/2) + 16g + 8 (t%2) .. +7
       uint32_t ev[4], od[4];
       f16x2 sc[4];
 #pragma unroll
@@ -228,7 +279,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
   const float lt = wave_sum16(l);
   if (valid) {
     float* st = p.states + ((row * p.h_q + h) * p.max_partitions + part) * kKv4State;
-    if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m, lt);
+    if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m * lam, lt);
     // accumulator row 4g + i of block db is channel 8 (4g + i) + db
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -238,14 +289,18 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
   }
 }
 
-// One wave per row (token, query head).
-__global__ __launch_bounds__(64) void kv4_decode_merge_kernel(Kv4AttnParams p) {
+// One workgroup per row (token, query head): one wave, or four where there are many
+// partitions (a wave keeps eight in flight).
+constexpr int kManyPartitions = 16;
+
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void kv4_decode_merge_kernel(Kv4AttnParams p) {
   const int h = blockIdx.x, tok = blockIdx.y, b = blockIdx.z;
   const int kvl = p.kv_len[b];
   const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
   const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
   const int64_t r = ((int64_t)b * p.q_tokens + tok) * p.h_q + h;
-  kv4_merge_row(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD,
+  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD,
                 p.stats ? p.stats + 2 * r : nullptr);
 }
 
@@ -278,12 +333,23 @@ __global__ __launch_bounds__(256) void kv4_weights_kernel(Kv4AttnParams p) {
 
 }  // namespace
 
-hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream) {
+template <bool WEIGHTS>
+void launch_partitions(const Kv4AttnParams& p, hipStream_t stream) {
   const int chunks = (p.q_tokens * (p.h_q / p.h_kv) + 15) / 16;
-  const dim3 grid((p.max_partitions + kDecodeWaves - 1) / kDecodeWaves, p.h_kv * chunks, p.batch);
-  if (p.scores) kv4_decode_kernel<true><<<grid, 64 * kDecodeWaves, 0, stream>>>(p);
-  else kv4_decode_kernel<false><<<grid, 64 * kDecodeWaves, 0, stream>>>(p);
-  kv4_decode_merge_kernel<<<dim3(p.h_q, p.q_tokens, p.batch), 64, 0, stream>>>(p);
+  const int64_t groups = ((int64_t)p.max_partitions * chunks + kDecodeWaves - 1) / kDecodeWaves;
+  const int64_t all = groups * p.h_kv * p.batch;
+  if (p.batch > 1 && p.batch <= kPackedBatch && all * 64 * kDecodeWaves <= UINT32_MAX)
+    kv4_decode_kernel<WEIGHTS, true><<<dim3((unsigned)all), 64 * kDecodeWaves, 0, stream>>>(p);
+  else
+    kv4_decode_kernel<WEIGHTS, false><<<dim3((unsigned)groups, p.h_kv, p.batch), 64 * kDecodeWaves, 0, stream>>>(p);
+}
+
+hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream) {
+  if (p.scores) launch_partitions<true>(p, stream);
+  else launch_partitions<false>(p, stream);
+  const dim3 rows(p.h_q, p.q_tokens, p.batch);
+  if (p.max_partitions > kManyPartitions) kv4_decode_merge_kernel<4><<<rows, 256, 0, stream>>>(p);
+  else kv4_decode_merge_kernel<1><<<rows, 64, 0, stream>>>(p);
   if (p.scores) {
     const int64_t keys = (int64_t)p.max_partitions * p.partition_tiles * kTile;
     kv4_weights_kernel<<<dim3((unsigned)((keys + 1023) / 1024), p.h_kv, p.batch), 256, 0, stream>>>(p);

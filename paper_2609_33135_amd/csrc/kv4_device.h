@@ -60,33 +60,50 @@ __device__ __forceinline__ float q_amax(u32x4 w) {
   return a;
 }
 
-// Merge of the partition states of one row (query token and head) by a wave: M is the
-// largest m, L = sum f l, O = sum f O with f = 2^(m - M), partitions in order; the row is
-// O / L * tv, or 0 where nothing was visible.  Lane l owns channels 2l and 2l + 1.
-// stats (or null) receives M and 1 / L.
+// Merge of the partition states of one row (query token and head) by WAVES waves: M is the
+// largest m, L = sum f l, O = sum f O with f = 2^(m - M); wave w sums partitions w, w +
+// WAVES, .. in order, the waves' sums add in order.  The row is O / L * tv, or 0 where
+// nothing was visible.  Lane l owns channels 2l and 2l + 1.  stats (or null) receives M and
+// 1 / L.
+template <int WAVES>
 __device__ __forceinline__ void kv4_merge_row(const float* st, int np, float tv, uint16_t* out, float* stats) {
-  const int lane = threadIdx.x & 63;
+  __shared__ float part[WAVES][kKv4State];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float M = -INFINITY;
   for (int q = lane; q < np; q += 64) M = fmaxf(M, st[(int64_t)q * kKv4State]);
   for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
   float L = 0.0f, o0 = 0.0f, o1 = 0.0f;
   if (M > -INFINITY) {
     constexpr int kAhead = 8;
-    for (int q0 = 0; q0 < np; q0 += kAhead) {
+    for (int q0 = wave; q0 < np; q0 += kAhead * WAVES) {
       float2 ml[kAhead], o[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const float* s = st + (int64_t)min(q0 + j, np - 1) * kKv4State;
+        const float* s = st + (int64_t)min(q0 + j * WAVES, np - 1) * kKv4State;
         ml[j] = *reinterpret_cast<const float2*>(s);
         o[j] = *reinterpret_cast<const float2*>(s + 2 + 2 * lane);
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const float f = q0 + j < np ? __builtin_amdgcn_exp2f(ml[j].x - M) : 0.0f;
+        const float f = q0 + j * WAVES < np ? __builtin_amdgcn_exp2f(ml[j].x - M) : 0.0f;
         L = __builtin_fmaf(f, ml[j].y, L);
         o0 = __builtin_fmaf(f, o[j].x, o0);
         o1 = __builtin_fmaf(f, o[j].y, o1);
       }
+    }
+  }
+  if (WAVES > 1) {
+    if (lane == 0) part[wave][0] = L;
+    part[wave][2 + 2 * lane] = o0;
+    part[wave][3 + 2 * lane] = o1;
+    __syncthreads();
+    if (wave != 0) return;
+    L = o0 = o1 = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      L += part[w][0];
+      o0 += part[w][2 + 2 * lane];
+      o1 += part[w][3 + 2 * lane];
     }
   }
   const float inv = L > 0.0f ? __frcp_rn(L) : 0.0f;

@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64) void kv4_prefill_merge_kernel(Kv4AttnParams p) 
   const Kv4Tiles tiles = kv4_tiles(qs + tok0, qs + min(tok0 + tm, nq) - 1, p.window, p.sinks);
   const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
   const int64_t r = (int64_t)(q0 + tok) * p.h_q + h;
-  kv4_merge_row(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD, nullptr);
+  kv4_merge_row<1>(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD, nullptr);
 }
 
 }  // namespace
