@@ -435,12 +435,17 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, siz
  * Keys at or past kv_len are never used, whatever their slots hold.
  *
  * mpfa_kv4_prefill: query i of sequence b (token cu_seqlens_q[b] + i) is at
- * position q_start[b] + i; q_start[b] + its rows <= kv_len[b].  With
- * partition_tokens = 0 every row is computed in one pass and no workspace is
- * needed; with a multiple of 128 the tiles that a block of rows sees are cut
- * into at most max_partitions parts of that many keys, whose states are
- * merged (for few rows behind long contexts).  mpfa_kv4_prefill_plan chooses
- * for lengths known on the host (rows and kv_len after the call's tokens).
+ * position q_start[b] + i; q_start[b] + its rows <= kv_len[b].  Without items
+ * every block of rows is computed in one pass, later rows first, and no
+ * workspace is needed.  With the items of mpfa_kv4_prefill_plan, made for
+ * these lengths (rows, and kv_len = q_start + rows), the blocks are taken
+ * longest first, and where they would leave units of the card idle some are
+ * cut along the keys, whose parts are merged, or all are halved.
+ *
+ * mpfa_kv4_prefill_plan: reports the counts, and with items fills
+ * items[0 .. n_items + n_merges - 1] (host memory of `capacity` entries; too
+ * few: MPFA_ERR_WORKSPACE).  The caller copies them to the device.  half tells
+ * which item size the plan uses and is passed on with the items.
  *
  * mpfa_kv4_decode: q_tokens rows per sequence (1, or a few drafted tokens),
  * row t at position kv_len[b] - q_tokens + t; rows b * q_tokens + t.
@@ -458,6 +463,13 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, siz
  * arguments; its contents on entry are ignored.  Calls (and captured graphs)
  * that may overlap need workspaces of their own.
  */
+typedef struct {       /* a block of rows, or a part of one (prefill plans)               */
+    int32_t seq, row;  /* sequence and its first row                                      */
+    int32_t first, last;   /* of the tiles that the block sees: first .. last - 1         */
+    int32_t state;     /* where the part's state is kept; -1: it is the whole block       */
+    int32_t parts;     /* parts of the block (consecutive states)                         */
+} mpfa_kv4_item;
+
 typedef struct {
     int32_t batch;               /* 1 .. 65535                                     */
     int32_t h_q, h_kv;           /* h_q <= 256, h_kv <= 32, h_q % h_kv == 0        */
@@ -468,12 +480,15 @@ typedef struct {
     int32_t q_tokens;            /* decode: rows per sequence                      */
     int32_t window;              /* 0: no window                                   */
     int32_t sinks;               /* first keys that stay visible (with a window)   */
-    int32_t partition_tokens;    /* multiple of 128; prefill: 0 = one pass         */
-    int32_t max_partitions;
+    int32_t partition_tokens;    /* decode: multiple of 128                        */
+    int32_t max_partitions;      /* decode                                         */
+    int32_t n_items, n_merges;   /* prefill with items: the plan's                 */
+    int32_t n_states, half;
     uint32_t flags;              /* decode: MPFA_KV4_WEIGHTS; prefill: 0           */
     int64_t q_stride;            /* elements between tokens of q (multiple of 8)   */
     const int32_t* cu_seqlens_q; /* prefill: [batch+1]                             */
     const int32_t* q_start;      /* prefill: [batch]                               */
+    const mpfa_kv4_item* items;  /* prefill: a plan on the device, or NULL         */
     const int32_t* kv_len;       /* [batch]                                        */
     const int32_t* page_table;   /* [batch][max_pages]                             */
     const void* q;               /* bf16 [rows][h_q][128], 16-byte aligned         */
@@ -486,7 +501,8 @@ typedef struct {
 mpfa_status mpfa_kv4_prefill_plan(int32_t batch, const int32_t* rows_host,
                                   const int32_t* kv_len_host, int32_t h_q, int32_t h_kv,
                                   int32_t window, int32_t sinks, int32_t num_cus,
-                                  int32_t* partition_tokens, int32_t* max_partitions,
+                                  mpfa_kv4_item* items, int32_t capacity, int32_t* n_items,
+                                  int32_t* n_merges, int32_t* n_states, int32_t* half,
                                   size_t* workspace_bytes);
 mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* args, void* workspace,
                              size_t workspace_bytes, mpfa_stream_t stream);

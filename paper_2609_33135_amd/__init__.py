@@ -76,6 +76,10 @@ class Kv4Cache(C.Structure):
                 ("v_scales", C.c_void_p), ("weights", C.c_void_p), ("num_pages", C.c_int64)]
 
 
+class Kv4Item(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("seq", "row", "first", "last", "state", "parts")]
+
+
 class Kv4WriteArgs(C.Structure):
     _fields_ = [("batch", C.c_int32), ("total_tokens", C.c_int32), ("max_seqlen", C.c_int32),
                 ("h_kv", C.c_int32), ("head_dim", C.c_int32), ("flags", C.c_uint32),
@@ -89,8 +93,9 @@ class Kv4AttnArgs(C.Structure):
     _fields_ = [("batch", C.c_int32), ("h_q", C.c_int32), ("h_kv", C.c_int32), ("head_dim", C.c_int32),
                 ("max_pages", C.c_int32), ("total_tokens", C.c_int32), ("max_seqlen_q", C.c_int32),
                 ("q_tokens", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32),
-                ("partition_tokens", C.c_int32), ("max_partitions", C.c_int32), ("flags", C.c_uint32),
-                ("q_stride", C.c_int64), ("cu_seqlens_q", C.c_void_p), ("q_start", C.c_void_p),
+                ("partition_tokens", C.c_int32), ("max_partitions", C.c_int32), ("n_items", C.c_int32),
+                ("n_merges", C.c_int32), ("n_states", C.c_int32), ("half", C.c_int32), ("flags", C.c_uint32),
+                ("q_stride", C.c_int64), ("cu_seqlens_q", C.c_void_p), ("q_start", C.c_void_p), ("items", C.c_void_p),
                 ("kv_len", C.c_void_p), ("page_table", C.c_void_p), ("q", C.c_void_p), ("cache", Kv4Cache),
                 ("k_tscale", C.c_void_p), ("v_tscale", C.c_void_p), ("out", C.c_void_p)]
 
@@ -144,13 +149,14 @@ def _load(path):
                                       C.c_size_t, C.c_void_p]
         L.mpfa_convert.restype = C.c_int
         L.mpfa_convert.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
-        i32, sized = C.c_int32, [C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_size_t)]
+        i32, out, size = C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_size_t)
         for name, args in (
-                ("mpfa_kv4_write_workspace_size", [i32, i32, i32, C.POINTER(C.c_size_t)]),
+                ("mpfa_kv4_write_workspace_size", [i32, i32, i32, size]),
                 ("mpfa_kv4_write", [C.POINTER(Kv4WriteArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
-                ("mpfa_kv4_prefill_plan", [i32, C.c_void_p, C.c_void_p, i32, i32, i32, i32, i32, *sized]),
+                ("mpfa_kv4_prefill_plan", [i32, C.c_void_p, C.c_void_p, i32, i32, i32, i32, i32, C.c_void_p, i32,
+                                           out, out, out, out, size]),
                 ("mpfa_kv4_prefill", [C.POINTER(Kv4AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
-                ("mpfa_kv4_decode_plan", [i32, C.c_void_p, i32, i32, i32, i32, i32, C.c_uint32, i32, *sized]),
+                ("mpfa_kv4_decode_plan", [i32, C.c_void_p, i32, i32, i32, i32, i32, C.c_uint32, i32, out, out, size]),
                 ("mpfa_kv4_decode", [C.POINTER(Kv4AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
                 ("mpfa_kv4_evict", [C.POINTER(Kv4EvictArgs), C.c_void_p])):
             getattr(L, name).restype = C.c_int
@@ -412,12 +418,15 @@ class SeqStats4:
 
 
 class Kv4Plan:
-    """How a prefill or decode call is cut, and its workspace.  A plan serves one call at a time;
-    lengths up to those it was made for are fine."""
+    """How a prefill or decode call is cut, and its workspace.  A plan serves one call at a time.
+    A decode plan holds for every length up to those it was made for, a prefill plan for its
+    row counts and lengths alone."""
 
-    def __init__(self, what, partition_tokens, max_partitions, workspace):
-        self.what, self.partition_tokens, self.max_partitions = what, partition_tokens, max_partitions
-        self.workspace = workspace
+    def __init__(self, what, workspace, **kw):
+        self.what, self.workspace = what, workspace
+        self.partition_tokens = self.max_partitions = self.n_items = self.n_merges = self.n_states = self.half = 0
+        self.items = None
+        self.__dict__.update(kw)
 
 
 def _host_ints(x):
@@ -425,36 +434,52 @@ def _host_ints(x):
     return np.ascontiguousarray(x, dtype=np.int32)
 
 
-def _plan(name, what, device, call):
+def _units(device):
     import torch
     dev = torch.device(device)
-    part, maxp, size = C.c_int32(0), C.c_int32(0), C.c_size_t(0)
-    cus = torch.cuda.get_device_properties(dev).multi_processor_count
-    _check(call(cus, C.byref(part), C.byref(maxp), C.byref(size)), name)
-    ws = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
-    return Kv4Plan(what, part.value, maxp.value, ws)
+    return dev, torch.cuda.get_device_properties(dev).multi_processor_count
+
+
+def _workspace(size, dev):
+    import torch
+    return torch.empty(size, dtype=torch.uint8, device=dev) if size else None
 
 
 def kv4_prefill_plan(rows_host, kv_len_host, h_q: int, h_kv: int, window=0, sinks=0, device="cuda") -> Kv4Plan:
-    """mpfa_kv4_prefill_plan with its workspace: rows and keys (the call's tokens included) per sequence."""
+    """mpfa_kv4_prefill_plan, its items on the device and its workspace: rows and keys (the call's
+    rows included) per sequence."""
+    import numpy as np
+    import torch
     rows, kv = _host_ints(rows_host), _host_ints(kv_len_host)
     _want(rows.size == kv.size, "kv4_prefill_plan: as many row counts as lengths are wanted")
-    plan = _plan("mpfa_kv4_prefill_plan", ("prefill", rows.size, h_q, h_kv, window, sinks), device,
-                 lambda cus, *out: lib().mpfa_kv4_prefill_plan(rows.size, rows.ctypes.data, kv.ctypes.data, h_q, h_kv,
-                                                               window, sinks, cus, *out))
-    plan.max_rows = int(rows.max())
-    return plan
+    dev, cus = _units(device)
+    n, merges, states, half, size = C.c_int32(0), C.c_int32(0), C.c_int32(0), C.c_int32(0), C.c_size_t(0)
+    room = 256
+    while True:
+        items = np.empty((room, 6), np.int32)
+        rc = lib().mpfa_kv4_prefill_plan(rows.size, rows.ctypes.data, kv.ctypes.data, h_q, h_kv, window, sinks, cus,
+                                         items.ctypes.data, room, C.byref(n), C.byref(merges), C.byref(states), C.byref(half),
+                                         C.byref(size))
+        if rc != MPFA_ERR_WORKSPACE or n.value + merges.value <= room:
+            break
+        room = n.value + merges.value
+    _check(rc, "mpfa_kv4_prefill_plan")
+    used = items[:n.value + merges.value]
+    return Kv4Plan(("prefill", rows.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), n_items=n.value,
+                   n_merges=merges.value, n_states=states.value, half=half.value, max_rows=int(rows.max()),
+                   items=torch.from_numpy(used).to(dev) if n.value else None)
 
 
 def kv4_decode_plan(kv_len_host, h_q: int, h_kv: int, q_tokens=1, window=0, sinks=0, weights=False,
                     device="cuda") -> Kv4Plan:
     """mpfa_kv4_decode_plan with its workspace; weights: the calls accumulate attention weights."""
     kv, flags = _host_ints(kv_len_host), KV4_WEIGHTS if weights else 0
-    plan = _plan("mpfa_kv4_decode_plan", ("decode", kv.size, h_q, h_kv, window, sinks), device,
-                 lambda cus, *out: lib().mpfa_kv4_decode_plan(kv.size, kv.ctypes.data, h_q, h_kv, q_tokens, window, sinks,
-                                                              flags, cus, *out))
-    plan.q_tokens, plan.flags = q_tokens, flags
-    return plan
+    dev, cus = _units(device)
+    part, maxp, size = C.c_int32(0), C.c_int32(0), C.c_size_t(0)
+    _check(lib().mpfa_kv4_decode_plan(kv.size, kv.ctypes.data, h_q, h_kv, q_tokens, window, sinks, flags, cus, C.byref(part),
+                                      C.byref(maxp), C.byref(size)), "mpfa_kv4_decode_plan")
+    return Kv4Plan(("decode", kv.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), partition_tokens=part.value,
+                   max_partitions=maxp.value, q_tokens=q_tokens, flags=flags)
 
 
 def kv4_write_workspace_size(batch: int, total_tokens: int, h_kv: int) -> int:
@@ -501,9 +526,10 @@ def _kv4_attn(what, q, cache, stats, cu, q_start, kv_len, page_table, out, plan,
           f"{what}: the plan was made for another call: {plan and plan.what}")
     ws = plan.workspace if plan is not None else None
     _want(ws is None or ws.get_device() == dev, f"{what}: the plan is of another device")
+    cut = (0,) * 6 if plan is None else (plan.partition_tokens, plan.max_partitions, plan.n_items, plan.n_merges,
+                                         plan.n_states, plan.half)
     a = Kv4AttnArgs(batch, h_q, cache.h_kv, HEAD_DIM, page_table.shape[1], q.shape[0], max_seqlen_q, q_tokens, window, sinks,
-                    plan.partition_tokens if plan is not None else 0, plan.max_partitions if plan is not None else 0, flags,
-                    stride, _ptr(cu), _ptr(q_start), _ptr(kv_len), _ptr(page_table), _ptr(q), cache._c(), _ptr(stats.k_tscale),
+                    *cut, flags, stride, _ptr(cu), _ptr(q_start), None if plan is None else _ptr(plan.items), _ptr(kv_len), _ptr(page_table), _ptr(q), cache._c(), _ptr(stats.k_tscale),
                     _ptr(stats.v_tscale), _ptr(out))
     _call("mpfa_kv4_" + kind, dev, stream, C.byref(a), _ptr(ws), 0 if ws is None else ws.numel())
 

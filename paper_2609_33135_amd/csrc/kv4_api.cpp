@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <new>
 
 #include "kv4_internal.h"
 
@@ -87,7 +88,6 @@ mpfa_status attn_params(const mpfa_kv4_attn_args* a, mpfa::Kv4AttnParams& p) {
   p.max_partitions = a->max_partitions;
   p.window = far(a->window);
   p.sinks = far(a->sinks);
-  p.xcd_remap = a->h_kv % 8 == 0;
   p.lam = kLambda;
   p.q_stride = a->q_stride;
   p.cu_seqlens_q = a->cu_seqlens_q;
@@ -105,6 +105,78 @@ mpfa_status attn_params(const mpfa_kv4_attn_args* a, mpfa::Kv4AttnParams& p) {
 // Tiles seen from a block of rows at positions first .. last.
 int64_t seen_tiles(int64_t first, int64_t last, int window, int sinks) {
   return mpfa::kv4_tiles((int)std::max<int64_t>(first, 0), (int)last, far(window), far(sinks)).nt;
+}
+
+// ---- prefill plans
+// tokens per item of 256 rows, or of 128; 0 where a token's heads do not fit
+int item_tokens(int grp, int half) { return (half ? mpfa::kKv4Rows / 2 : mpfa::kKv4Rows) / grp; }
+
+// of one part of an item, over the KV heads
+size_t state_bytes(int h_kv, int half) {
+  return (size_t)(half ? mpfa::kKv4Rows / 2 : mpfa::kKv4Rows) * h_kv * mpfa::kKv4State * sizeof(float);
+}
+
+struct PlanBlock {
+  int32_t seq, row, tiles;
+};
+
+// Which blocks are cut: those longer than `most` tiles into equal parts of at most that
+// (0: none), and the last `tail` ones in the order into `ways` parts; with its pieces, the
+// number of blocks cut, and its estimated time in tiles.
+struct PlanCut {
+  float cost;
+  int most, tail, ways;
+  int64_t pieces, cut;
+};
+
+int parts_of(int tiles, int64_t i, int64_t n, const PlanCut& c) {
+  int parts = c.most > 0 ? (tiles + c.most - 1) / c.most : 1;
+  if (i >= n - c.tail) parts = std::max(parts, c.ways);
+  return std::max(1, std::min(parts, tiles));
+}
+
+// Estimated time of a cut, in the time of one tile of a 256-row item (3.3 us): a piece takes
+// its tiles (0.55 for 128 rows) and about 1.5 to start and store; the units take the pieces
+// in order as they come free; a merge adds its launch and the states' bytes, 133 KB per
+// piece and KV head written and read at 5 TB/s.
+void price(const PlanBlock* s, int64_t n, int64_t units, int h_kv, int half, float* ends, PlanCut* c) {
+  const float tile = half ? 0.55f : 1.0f, start = 1.5f;
+  std::fill(ends, ends + units, 0.0f);   // a heap, the earliest end on top
+  auto later = [](float x, float y) { return x > y; };
+  float last = 0.0f;
+  int64_t states = 0;
+  c->pieces = c->cut = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    const int parts = parts_of(s[i].tiles, i, n, *c);
+    const float len = start + tile * s[i].tiles / parts;
+    for (int k = 0; k < parts; ++k) {
+      std::pop_heap(ends, ends + units, later);
+      last = std::max(last, ends[units - 1] += len);
+      std::push_heap(ends, ends + units, later);
+    }
+    c->pieces += parts;
+    if (parts > 1) {
+      ++c->cut;
+      states += parts;
+    }
+  }
+  c->cost = last;
+  if (c->cut) c->cost += 1.2f + 0.016f * (half ? 0.5f : 1.0f) * states * h_kv;
+}
+
+PlanCut choose_cut(const PlanBlock* s, int64_t n, int64_t units, int h_kv, int half, float* ends) {
+  PlanCut best = {0.0f, 0, 0, 0, 0, 0};
+  price(s, n, units, h_kv, half, ends, &best);
+  if (n > 16 * units) return best;   // many blocks per unit balance themselves
+  auto consider = [&](PlanCut c) {
+    price(s, n, units, h_kv, half, ends, &c);
+    if (c.cost < best.cost) best = c;
+  };
+  const int longest = s[0].tiles, rest = (int)(n % units);
+  for (int k = 2; k <= 64 && k <= longest; k += k / 2)   // 2, 3, 4, 6, 9, 13, ..
+    if (n * k <= 24 * units || n <= units) consider({0.0f, std::max(1, (longest + k - 1) / k), 0, 0, 0, 0});
+  for (int ways = 2; ways <= 8 && rest > 0 && n > units; ways += ways / 2) consider({0.0f, 0, rest, ways, 0, 0});
+  return best;
 }
 
 #ifdef MPFA_DEBUG_CHECKS
@@ -163,23 +235,45 @@ mpfa_status check_write(const mpfa_kv4_write_args* a, hipStream_t s) {
 mpfa_status check_attn(const mpfa_kv4_attn_args* a, bool decode, hipStream_t s) {
   if (hipStreamSynchronize(s) != hipSuccess) return MPFA_ERR_HIP;
   std::vector<int32_t> cu, qs, kv, pt;
+  std::vector<mpfa_kv4_item> items;
   if (!to_host(a->kv_len, (size_t)a->batch, kv) || !to_host(a->page_table, (size_t)a->batch * a->max_pages, pt)) return MPFA_ERR_HIP;
-  if (!decode && (!to_host(a->cu_seqlens_q, (size_t)a->batch + 1, cu) || !to_host(a->q_start, (size_t)a->batch, qs)))
+  if (!decode && (!to_host(a->cu_seqlens_q, (size_t)a->batch + 1, cu) || !to_host(a->q_start, (size_t)a->batch, qs) ||
+                  (a->items && !to_host(a->items, (size_t)a->n_items + a->n_merges, items))))
     return MPFA_ERR_HIP;
-  const int tm = mpfa::kKv4Rows / (a->h_q / a->h_kv);
   for (int b = 0; b < a->batch; ++b) {
     if (kv[b] < 0 || !row_pages_ok(pt, b, a->max_pages, ((int64_t)kv[b] + 63) / 64, a->cache.num_pages)) return MPFA_ERR_DATA;
-    const int64_t room = (int64_t)a->max_partitions * (a->partition_tokens / MPFA_KV_TILE);
     if (decode) {
+      const int64_t room = (int64_t)a->max_partitions * (a->partition_tokens / MPFA_KV_TILE);
       if (seen_tiles((int64_t)kv[b] - a->q_tokens, kv[b] - 1, a->window, a->sinks) > room) return MPFA_ERR_DATA;
       continue;
     }
     const int n = cu[b + 1] - cu[b];
     if (n < 0 || n > a->max_seqlen_q || qs[b] < 0 || (int64_t)qs[b] + n > kv[b]) return MPFA_ERR_DATA;
-    for (int t = 0; a->partition_tokens > 0 && t < n; t += tm)
-      if (seen_tiles(qs[b] + t, qs[b] + std::min(t + tm, n) - 1, a->window, a->sinks) > room) return MPFA_ERR_DATA;
   }
-  if (!decode && cu[0] != 0) return MPFA_ERR_DATA;
+  if (!decode && (cu[0] != 0 || cu[a->batch] != a->total_tokens)) return MPFA_ERR_DATA;
+  if (!items.empty()) {   // every block once, with all the tiles that it sees, its states inside the workspace
+    const int tm = item_tokens(a->h_q / a->h_kv, a->half);
+    const int64_t room = a->n_states;
+    int64_t seen = 0, planned = 0, blocks = 0;
+    for (int b = 0; b < a->batch; ++b)
+      for (int t = 0; t < cu[b + 1] - cu[b]; t += tm, ++blocks)
+        seen += seen_tiles(qs[b] + t, qs[b] + std::min(t + tm, cu[b + 1] - cu[b]) - 1, a->window, a->sinks);
+    for (int i = 0; i < a->n_items + a->n_merges; ++i) {
+      const mpfa_kv4_item& x = items[i];
+      if (x.seq < 0 || x.seq >= a->batch || x.row < 0 || x.row % tm || x.row >= cu[x.seq + 1] - cu[x.seq]) return MPFA_ERR_DATA;
+      const int n = cu[x.seq + 1] - cu[x.seq], nt =
+          (int)seen_tiles(qs[x.seq] + x.row, qs[x.seq] + std::min(x.row + tm, n) - 1, a->window, a->sinks);
+      if (x.first < 0 || x.first >= x.last || x.last > nt || x.parts < 1) return MPFA_ERR_DATA;
+      if (x.parts > 1 ? x.state < 0 || x.state + (i < a->n_items ? 1 : x.parts) > room : x.state != -1) return MPFA_ERR_DATA;
+      if (i < a->n_items) {
+        planned += x.last - x.first;
+        blocks -= x.parts == 1;
+      } else {
+        --blocks;
+      }
+    }
+    if (seen != planned || blocks != 0) return MPFA_ERR_DATA;
+  }
   const int64_t rows = decode ? (int64_t)a->batch * a->q_tokens : cu[a->batch];
   return scan_rows(a->q, rows, (int64_t)a->h_q * MPFA_HEAD_DIM, a->q_stride, s);
 }
@@ -271,37 +365,91 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* a, void* workspace, size_t
 }
 
 mpfa_status mpfa_kv4_prefill_plan(int32_t batch, const int32_t* rows_host, const int32_t* kv_len_host, int32_t h_q, int32_t h_kv,
-                                  int32_t window, int32_t sinks, int32_t num_cus, int32_t* partition_tokens,
-                                  int32_t* max_partitions, size_t* workspace_bytes) {
-  if (batch < 1 || batch > 65535 || !rows_host || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS || h_q % h_kv ||
-      window < 0 || sinks < 0 || num_cus < 1 || !partition_tokens || !max_partitions || !workspace_bytes)
+                                  int32_t window, int32_t sinks, int32_t num_cus, mpfa_kv4_item* items, int32_t capacity,
+                                  int32_t* n_items, int32_t* n_merges, int32_t* n_states, int32_t* half,
+                                  size_t* workspace_bytes) {
+  if (batch < 1 || batch > 65535 || !rows_host || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS ||
+      h_q % h_kv || window < 0 || sinks < 0 || num_cus < 1 || capacity < 0 || !n_items || !n_merges || !n_states || !half ||
+      !workspace_bytes)
     return MPFA_ERR_INVALID;
-  const int tm = mpfa::kKv4Rows / (h_q / h_kv);
-  int64_t items = 0, tiles = 0, most = 0, total_rows = 0, max_rows = 0;
+  const int grp = h_q / h_kv;
+  int64_t blocks[2] = {0, 0};
   for (int b = 0; b < batch; ++b) {
     if (rows_host[b] < 0 || rows_host[b] > kv_len_host[b]) return MPFA_ERR_INVALID;
-    const int64_t n = rows_host[b], start = (int64_t)kv_len_host[b] - n;
-    total_rows += n;
-    max_rows = std::max(max_rows, n);
-    for (int64_t t = 0; t < n; t += tm) {
-      const int64_t nt = seen_tiles(start + t, start + std::min(t + tm, n) - 1, window, sinks);
-      items += h_kv;
-      tiles += nt * h_kv;
-      most = std::max(most, nt);
+    for (int h = 0; h < 2; ++h)
+      if (const int tm = item_tokens(grp, h)) blocks[h] += ((int64_t)rows_host[b] + tm - 1) / tm;
+  }
+  *n_items = *n_merges = *n_states = *half = 0;
+  *workspace_bytes = 0;
+  if (blocks[0] == 0) return MPFA_OK;
+  if (blocks[1] > INT32_MAX / 64) return MPFA_ERR_UNSUPPORTED;
+
+  // Blocks of either size, longest first; per size the cut that finishes first.
+  const int64_t units = std::max(1, num_cus / h_kv);   // every unit stands for the KV heads of a block
+  PlanBlock* sorted[2] = {nullptr, nullptr};
+  float* ends = new (std::nothrow) float[units];
+  PlanCut best = {1e30f, 0, 0, 0, 0, 0};
+  int best_half = 0;
+  bool ok = ends != nullptr;
+  for (int h = 0; h < 2 && ok; ++h) {
+    const int tm = item_tokens(grp, h);
+    // halves pay where the card has units for them all, or nearly
+    if (tm == 0 || (h == 1 && blocks[1] > 4 * units)) continue;
+    PlanBlock* s = sorted[h] = new (std::nothrow) PlanBlock[blocks[h]];
+    if (!s) {
+      ok = false;
+      break;
+    }
+    int64_t n = 0;
+    for (int b = 0; b < batch; ++b)
+      for (int64_t t = 0; t < rows_host[b]; t += tm) {
+        const int64_t start = (int64_t)kv_len_host[b] - rows_host[b];
+        s[n++] = {b, (int32_t)t,
+                  (int32_t)seen_tiles(start + t, start + std::min<int64_t>(t + tm, rows_host[b]) - 1, window, sinks)};
+      }
+    std::sort(s, s + n, [](const PlanBlock& x, const PlanBlock& y) {
+      return x.tiles != y.tiles ? x.tiles > y.tiles : x.seq != y.seq ? x.seq < y.seq : x.row > y.row;
+    });
+    const PlanCut c = choose_cut(s, n, units, h_kv, h, ends);
+    if (c.cost < best.cost) {
+      best = c;
+      best_half = h;
     }
   }
-  *partition_tokens = *max_partitions = 0;
-  *workspace_bytes = 0;
-  // One workgroup fills a compute unit.  Items are split where they leave units idle
-  // and the longest of them is much longer than a unit's share of all tiles.
-  const int64_t share = (tiles + num_cus - 1) / num_cus;
-  if (items == 0 || max_rows > 65535 || 2 * share + 2 >= most) return MPFA_OK;
-  const int64_t part = std::max<int64_t>(share, 4);
-  const int64_t parts = (most + part - 1) / part;
-  *partition_tokens = (int32_t)(part * MPFA_KV_TILE);
-  *max_partitions = (int32_t)parts;
-  *workspace_bytes = (size_t)total_rows * h_q * parts * mpfa::kKv4State * sizeof(float);
-  return MPFA_OK;
+  mpfa_status st = ok ? MPFA_OK : MPFA_ERR_WORKSPACE;
+  if (ok) {
+    const PlanBlock* s = sorted[best_half];
+    const int64_t n = blocks[best_half];
+    *n_items = (int32_t)best.pieces;
+    *n_merges = (int32_t)best.cut;
+    *half = best_half;
+    *n_states = (int32_t)(best.pieces - (n - best.cut));
+    *workspace_bytes = *n_states * state_bytes(h_kv, best_half);
+    if (items) {
+      if (capacity < best.pieces + best.cut) {
+        st = MPFA_ERR_WORKSPACE;
+      } else {
+        int64_t at = 0, state = 0, merge = best.pieces;
+        for (int64_t i = 0; i < n; ++i) {
+          const int parts = parts_of(s[i].tiles, i, n, best);
+          if (parts > 1) items[merge++] = {s[i].seq, s[i].row, 0, s[i].tiles, (int32_t)state, parts};
+          for (int k = 0; k < parts; ++k)
+            items[at++] = {s[i].seq, s[i].row, (int32_t)((int64_t)s[i].tiles * k / parts),
+                           (int32_t)((int64_t)s[i].tiles * (k + 1) / parts), parts > 1 ? (int32_t)(state + k) : -1, parts};
+          if (parts > 1) state += parts;
+        }
+        // longest first: the card takes them in this order
+        std::sort(items, items + best.pieces, [](const mpfa_kv4_item& x, const mpfa_kv4_item& y) {
+          const int a = x.last - x.first, b = y.last - y.first;
+          return a != b ? a > b : x.seq != y.seq ? x.seq < y.seq : x.row != y.row ? x.row > y.row : x.first > y.first;
+        });
+      }
+    }
+  }
+  delete[] sorted[0];
+  delete[] sorted[1];
+  delete[] ends;
+  return st;
 }
 
 mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* a, void* workspace, size_t workspace_bytes, mpfa_stream_t stream) {
@@ -311,16 +459,24 @@ mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* a, void* workspace, size_
   if (a->total_tokens == 0) return MPFA_OK;
   if (!a->cu_seqlens_q || !a->q_start) return MPFA_ERR_INVALID;
   p.max_seqlen_q = a->max_seqlen_q;
-  const int tm = mpfa::kKv4Rows / (a->h_q / a->h_kv);
-  const int64_t items = ((int64_t)a->max_seqlen_q + tm - 1) / tm * a->h_kv * a->batch;
-  if (p.partition_tiles) {
-    if (a->max_partitions < 1) return MPFA_ERR_INVALID;
-    if (a->max_seqlen_q > 65535) return MPFA_ERR_UNSUPPORTED;
-    const double need = (double)a->total_tokens * a->h_q * a->max_partitions * mpfa::kKv4State * sizeof(float);
-    if (!workspace || (double)workspace_bytes < need || !aligned16(workspace)) return MPFA_ERR_WORKSPACE;
+  if (a->items) {
+    if (a->n_items < 1 || a->n_merges < 0 || a->n_merges > a->n_items || a->n_states < 0 || a->n_states > a->n_items ||
+        (a->half != 0 && a->half != 1))
+      return MPFA_ERR_INVALID;
+    if (a->half && item_tokens(a->h_q / a->h_kv, 1) == 0) return MPFA_ERR_INVALID;
+    if (a->n_merges > 65535 || (int64_t)a->n_items * a->h_kv > (int64_t)UINT32_MAX / 512) return MPFA_ERR_UNSUPPORTED;
+    if (a->n_states > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < a->n_states * state_bytes(a->h_kv, a->half)))
+      return MPFA_ERR_WORKSPACE;
+    p.items = a->items;
+    p.n_items = a->n_items;
+    p.n_merges = a->n_merges;
+    p.half = a->half;
     p.states = static_cast<float*>(workspace);
+  } else {
+    const int tm = item_tokens(a->h_q / a->h_kv, 0);
+    const int64_t items = ((int64_t)a->max_seqlen_q + tm - 1) / tm * a->h_kv * a->batch;
+    if (items > (int64_t)UINT32_MAX / 512) return MPFA_ERR_UNSUPPORTED;
   }
-  if (items * (p.partition_tiles ? a->max_partitions : 1) > (int64_t)UINT32_MAX / 512) return MPFA_ERR_UNSUPPORTED;
 #ifdef MPFA_DEBUG_CHECKS
   if (const mpfa_status st = check_attn(a, false, reinterpret_cast<hipStream_t>(stream))) return st;
 #endif

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64 * WAVES) void kv4_decode_merge_kernel(Kv4AttnPar
   const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
   const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
   const int64_t r = ((int64_t)b * p.q_tokens + tok) * p.h_q + h;
-  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD,
+  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD,
                 p.stats ? p.stats + 2 * r : nullptr);
 }
 

@@ -60,17 +60,18 @@ __device__ __forceinline__ float q_amax(u32x4 w) {
   return a;
 }
 
-// Merge of the partition states of one row (query token and head) by WAVES waves: M is the
+// Merge of the partition states of one row (query token and head), `stride` floats apart,
+// by WAVES waves: M is the
 // largest m, L = sum f l, O = sum f O with f = 2^(m - M); wave w sums partitions w, w +
 // WAVES, .. in order, the waves' sums add in order.  The row is O / L * tv, or 0 where
 // nothing was visible.  Lane l owns channels 2l and 2l + 1.  stats (or null) receives M and
 // 1 / L.
 template <int WAVES>
-__device__ __forceinline__ void kv4_merge_row(const float* st, int np, float tv, uint16_t* out, float* stats) {
+__device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, int np, float tv, uint16_t* out, float* stats) {
   __shared__ float part[WAVES][kKv4State];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = WAVES > 1 ? threadIdx.x >> 6 : 0;
   float M = -INFINITY;
-  for (int q = lane; q < np; q += 64) M = fmaxf(M, st[(int64_t)q * kKv4State]);
+  for (int q = lane; q < np; q += 64) M = fmaxf(M, st[q * stride]);
   for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
   float L = 0.0f, o0 = 0.0f, o1 = 0.0f;
   if (M > -INFINITY) {
@@ -79,7 +80,7 @@ __device__ __forceinline__ void kv4_merge_row(const float* st, int np, float tv,
       float2 ml[kAhead], o[kAhead];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const float* s = st + (int64_t)min(q0 + j * WAVES, np - 1) * kKv4State;
+        const float* s = st + min(q0 + j * WAVES, np - 1) * stride;
         ml[j] = *reinterpret_cast<const float2*>(s);
         o[j] = *reinterpret_cast<const float2*>(s + 2 + 2 * lane);
       }

@@ -6,13 +6,15 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mpfa.h"
+
 namespace mpfa {
 
 constexpr int kKv4StatTokens = 128;   // tokens per statistics partial
 // per partial of one KV head: FP64 sums, FP32 maxima and minima of K per channel, and
 // the largest |V| (padded to 16 bytes)
 constexpr int kKv4StatBytes = 128 * (8 + 4 + 4) + 16;
-constexpr int kKv4Rows = 256;         // query rows (tokens x heads of one KV head) per prefill workgroup
+constexpr int kKv4Rows = 256;         // most query rows (tokens x heads of one KV head) of a prefill item
 constexpr int kKv4State = 130;        // floats of a partition state: m, l, O[128]
 
 // Planes of the cache; page pg, KV head h, slot o.
@@ -45,9 +47,9 @@ struct Kv4AttnParams {
   int batch, h_q, h_kv, max_pages;
   int q_tokens;                          // decode: rows per sequence
   int max_seqlen_q;                      // prefill
-  int partition_tiles, max_partitions;   // partition_tiles 0 (prefill): one pass, no states
+  int partition_tiles, max_partitions;   // decode
+  int n_items, n_merges, half;           // prefill by a plan: its items (half: of 128 rows)
   int window, sinks;
-  int xcd_remap;
   float lam;                             // log2(e) / sqrt(128)
   int64_t q_stride;
   const int32_t* cu_seqlens_q;           // prefill
@@ -59,7 +61,8 @@ struct Kv4AttnParams {
   const float* k_tscale;
   const float* v_tscale;
   uint16_t* out;
-  float* states;                         // [row][h_q][max_partitions][130]
+  const mpfa_kv4_item* items;            // prefill: the plan, or null
+  float* states;                         // decode [row][h_q][max_partitions][130], prefill [state][h_kv][rows][130]
   float* stats;                          // weights: [row][h_q][2]: the merged M and 1 / l
   float* scores;                         // weights: [b][h_kv][q_tokens * G][max_partitions * partition tokens]
 };

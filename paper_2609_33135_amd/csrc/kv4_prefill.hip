@@ -5,6 +5,10 @@
 // the G query heads that share it, 32 rows per wave, one per lane pair.  Packing the heads
 // of a KV head makes the item short in tokens: fewer keys outside the diagonal and the
 // window, more items for short prompts, and one dequantization of K and V for all of them.
+// A plan (made on the host, where the lengths are known) orders the items by length, cuts
+// some of them along the keys, whose parts are merged, and may halve the items: of 128
+// rows, the waves of either half of the workgroup take the same rows and half of every
+// tile's keys, and join at the end.
 //
 // Per 128-key tile K and V are loaded as codes a tile ahead, dequantized exactly to FP16
 // (6 bits) on their way into LDS, and multiplied on the 32x32x16 FP16 MFMA:
@@ -96,21 +100,27 @@ struct Kv4Item {
   int lane, hf, lc;
   int pos, low, sinks;      // the lane's row sees keys <= pos that are >= low or < sinks
   int wpos_min, wlow_max;   // smallest pos and largest low of the wave's rows
+  int kb0;                  // first of the wave's 32-key blocks in a tile
   float lam;
   f16x8 q[8];               // channels 16 ks + 8 hf .. +7
 };
 
+// 32-key blocks of a tile per wave
+template <bool HALF>
+constexpr int kBlocks = HALF ? 2 : 4;
+
 __device__ __forceinline__ void qk_block(f32x16& s, int kb, const Kv4Smem& sm, int buf, const Kv4Item& it) {
-  const uint8_t* kp = sm.k[buf] + (32 * kb + it.lc) * kStride + 16 * it.hf;
+  const uint8_t* kp = sm.k[buf] + (32 * (it.kb0 + kb) + it.lc) * kStride + 16 * it.hf;
   s = (f32x16){};
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) s = mfma32_f16(*reinterpret_cast<const f16x8*>(kp + 32 * ks), it.q[ks], s);
 }
 
-__device__ __forceinline__ void mask_tile(f32x16 (&s)[4], int key0, const Kv4Item& it) {
-  const int k0 = key0 + 8 * it.hf;
+template <int NB>
+__device__ __forceinline__ void mask_tile(f32x16 (&s)[NB], int key0, const Kv4Item& it) {
+  const int k0 = key0 + 32 * it.kb0 + 8 * it.hf;
 #pragma unroll
-  for (int kb = 0; kb < 4; ++kb) {
+  for (int kb = 0; kb < NB; ++kb) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
 #pragma unroll
@@ -128,10 +138,11 @@ struct Kv4Soft {
   float m, l, bias;   // running maximum (accumulator units), row sum, exponent bias
 };
 
-__device__ __forceinline__ float max_tile(const f32x16 (&s)[4], const Kv4Item& it, Kv4Soft& ss) {
+template <int NB>
+__device__ __forceinline__ float max_tile(const f32x16 (&s)[NB], const Kv4Item& it, Kv4Soft& ss) {
   float mxa = -INFINITY, mxb = -INFINITY;
 #pragma unroll
-  for (int kb = 0; kb < 4; kb += 2) {
+  for (int kb = 0; kb < NB; kb += 2) {
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       mxa = fmaxf(fmaxf(mxa, s[kb][r]), s[kb][r + 1]);
@@ -146,8 +157,9 @@ __device__ __forceinline__ float max_tile(const f32x16 (&s)[4], const Kv4Item& i
   return alpha;
 }
 
-// P of one 32-key block: ph[2 kb + t] are keys 32 kb + 16 t + 8 hf .. +7
-__device__ __forceinline__ float exp_block(const f32x16& s, int kb, const Kv4Item& it, const Kv4Soft& ss, f16x8 (&ph)[8]) {
+// P of one 32-key block: ph[2 kb + t] are keys 32 (kb0 + kb) + 16 t + 8 hf .. +7
+template <int NP>
+__device__ __forceinline__ float exp_block(const f32x16& s, int kb, const Kv4Item& it, const Kv4Soft& ss, f16x8 (&ph)[NP]) {
   float ps = 0.0f;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
@@ -175,37 +187,69 @@ __device__ __forceinline__ void rescale(f32x16 (&o)[4], float alpha) {
   }
 }
 
-__device__ __forceinline__ void pv_tile(const Kv4Smem& sm, int buf, const f16x8 (&ph)[8], f32x16 (&o)[4], const Kv4Item& it) {
-  const uint8_t* vp = sm.v[buf] + it.lc * kStride + 16 * it.hf;
+template <int NP>
+__device__ __forceinline__ void pv_tile(const Kv4Smem& sm, int buf, const f16x8 (&ph)[NP], f32x16 (&o)[4], const Kv4Item& it) {
+  const uint8_t* vp = sm.v[buf] + it.lc * kStride + 16 * it.hf + 64 * it.kb0;
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
+  for (int t = 0; t < NP; ++t)
 #pragma unroll
     for (int db = 0; db < 4; ++db)
       o[db] = mfma32_f16(*reinterpret_cast<const f16x8*>(vp + 32 * db * kStride + 32 * t), ph[t], o[db]);
 }
 
-// Tokens tok0 .. of sequence b, KV head hk, visible tiles v0 .. v1 - 1 of the item.
-template <bool SPLIT>
+// Joins the halves of an item of 128 rows: the waves of the second half leave their states
+// in LDS, those of the first add them to their own.
+__device__ __forceinline__ bool join_halves(Kv4Smem& sm, int wave, const Kv4Item& it, Kv4Soft& ss, f32x16 (&o)[4]) {
+  static_assert(4 * 66 * 64 * sizeof(float) <= sizeof(Kv4Smem), "states of four waves");
+  float* st = reinterpret_cast<float*>(&sm) + (wave & 3) * 66 * 64 + it.lane;
+  __syncthreads();   // the tiles are read
+  if (wave >= 4) {
+    st[0] = ss.m;
+    st[64] = ss.l;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[64 * (2 + 16 * db + r)] = o[db][r];
+  }
+  __syncthreads();
+  if (wave >= 4) return false;
+  const float m1 = st[0], l1 = st[64], M = fmaxf(ss.m, m1), use = M == -INFINITY ? 0.0f : M;
+  const float f0 = __builtin_amdgcn_exp2f((ss.m - use) * it.lam), f1 = __builtin_amdgcn_exp2f((m1 - use) * it.lam);
+  ss.m = M;
+  ss.l = f0 * ss.l + f1 * l1;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = f0 * o[db][r] + f1 * st[64 * (2 + 16 * db + r)];
+  return true;
+}
+
+// Tokens tok0 .. of sequence b, KV head hk, visible tiles v0 .. v1 - 1 of the item; state:
+// where the item's parts leave their states for the merge, or null: the output.
+template <bool HALF>
 __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm, int b, int hk, int tok0, int tm, int nq, int q0,
-                                             const Kv4Tiles& tiles, int v0, int v1, int part) {
+                                             const Kv4Tiles& tiles, int v0, int v1, float* state) {
+  constexpr int kNb = kBlocks<HALF>;
   const int grp = p.h_q / p.h_kv;
   Kv4Item it;
   it.lane = threadIdx.x & 63;
   it.hf = it.lane >> 5;
   it.lc = it.lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = wave * 32 + it.lc;
+  const int wrow = 32 * (HALF ? wave & 3 : wave);    // the wave's first row
+  it.kb0 = HALF ? 2 * (wave >> 2) : 0;
+  const int r = wrow + it.lc;
   const int last = min(tok0 + tm, nq) - 1;           // last token of the item
   const int qs = p.q_start[b], kvl = p.kv_len[b];
   const int tok = min(tok0 + r / grp, last);         // rows past the item repeat its last token
   const bool valid = r < (last + 1 - tok0) * grp;
   const int h = hk * grp + r % grp;
-  const bool active = wave * 32 < (last + 1 - tok0) * grp;
+  const bool active = wrow < (last + 1 - tok0) * grp;
   it.pos = qs + tok;
   it.low = p.window > 0 ? max(it.pos - p.window + 1, 0) : 0;
   it.sinks = p.sinks;
-  it.wpos_min = qs + min(tok0 + wave * 32 / grp, last);
-  it.wlow_max = p.window > 0 ? max(qs + min(tok0 + (wave * 32 + 31) / grp, last) - p.window + 1, 0) : 0;
+  it.wpos_min = qs + min(tok0 + wrow / grp, last);
+  it.wlow_max = p.window > 0 ? max(qs + min(tok0 + (wrow + 31) / grp, last) - p.window + 1, 0) : 0;
   {
     const u32x4* src = reinterpret_cast<const u32x4*>(p.q + (int64_t)(q0 + tok) * p.q_stride + h * kD);
     u32x4 w[8];
@@ -261,13 +305,17 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
       put_v(v - 1);
       __syncthreads();
     }
+    if (HALF) {   // the barriers of join_halves
+      __syncthreads();
+      __syncthreads();
+    }
     return;
   }
 
-  f32x16 s[4];
-  f16x8 ph[8];
+  f32x16 s[kNb];
+  f16x8 ph[2 * kNb];
 #pragma unroll
-  for (int kb = 0; kb < 4; ++kb) qk_block(s[kb], kb, sm, vh & 1, it);
+  for (int kb = 0; kb < kNb; ++kb) qk_block(s[kb], kb, sm, vh & 1, it);
   if (vh > v0) __syncthreads();
   auto mask = [&](int v) {
     const int key0 = tiles.tile(v) * kTile;
@@ -282,13 +330,13 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
     fetch_v(kr, p, pgv, hk, u);   // tile v - 1
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kb = 0; kb < 3; ++kb) {
+    for (int kb = 0; kb < kNb - 1; ++kb) {
       qk_block(s[kb], kb, sm, (v - 1) & 1, it);
       ps += exp_block(s[kb + 1], kb + 1, it, ss, ph);
       __builtin_amdgcn_sched_barrier(0);
     }
     ss.l = __builtin_fmaf(alpha, ss.l, ps);
-    qk_block(s[3], 3, sm, (v - 1) & 1, it);
+    qk_block(s[kNb - 1], kNb - 1, sm, (v - 1) & 1, it);
     store_k(sm, v & 1, kr, half, u);
     put_v(v - 1);
     __builtin_amdgcn_sched_barrier(0);
@@ -300,18 +348,18 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
     __syncthreads();
   }
 #pragma unroll
-  for (int kb = 1; kb < 4; ++kb) ps += exp_block(s[kb], kb, it, ss, ph);
+  for (int kb = 1; kb < kNb; ++kb) ps += exp_block(s[kb], kb, it, ss, ph);
   ss.l = __builtin_fmaf(alpha, ss.l, ps);
   rescale(o, alpha);
   pv_tile(sm, v0 & 1, ph, o, it);
 #pragma unroll
   for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(o[db]));
+  if (HALF && !join_halves(sm, wave, it, ss, o)) return;
   const float lt = ss.l + __shfl_xor(ss.l, 32);
   if (!valid) return;
   // accumulator register 4a + i of block db is channel 64 (a%2) + 32 hf + 8 i + 2 db + a/2
-  const int64_t row = (int64_t)(q0 + tok) * p.h_q + h;
-  if (SPLIT) {
-    float* st = p.states + (row * p.max_partitions + part) * kKv4State;
+  if (state) {
+    float* st = state + (int64_t)r * kKv4State;
     if (it.hf == 0) *reinterpret_cast<float2*>(st) = make_float2(ss.m * it.lam, lt);
 #pragma unroll
     for (int a = 0; a < 2; ++a)
@@ -323,7 +371,7 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
               make_float2(o[db][4 * a + i], o[db][8 + 4 * a + i]);
   } else {
     const float inv = lt > 0.0f ? __frcp_rn(lt) * p.v_tscale[b * p.h_kv + hk] : 0.0f;
-    uint16_t* dst = p.out + row * kD + 32 * it.hf;
+    uint16_t* dst = p.out + ((int64_t)(q0 + tok) * p.h_q + h) * kD + 32 * it.hf;
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -337,63 +385,71 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
   }
 }
 
-template <bool SPLIT>
+// floats of the states of one part of an item, for one KV head
+__device__ __forceinline__ int64_t state_floats(bool half) { return (half ? kKv4Rows / 2 : kKv4Rows) * kKv4State; }
+
+// Items of a plan, in its order.
+template <bool HALF>
+__global__ __launch_bounds__(512, 2) void kv4_prefill_plan_kernel(Kv4AttnParams p) {
+  __shared__ Kv4Smem sm;
+  const int tm = (HALF ? kKv4Rows / 2 : kKv4Rows) / (p.h_q / p.h_kv);
+  const int hk = blockIdx.x % p.h_kv;
+  const mpfa_kv4_item x = p.items[blockIdx.x / p.h_kv];
+  const int q0 = p.cu_seqlens_q[x.seq], nq = p.cu_seqlens_q[x.seq + 1] - q0, qs = p.q_start[x.seq];
+  if (x.row >= nq) return;
+  const Kv4Tiles tiles = kv4_tiles(qs + x.row, qs + min(x.row + tm, nq) - 1, p.window, p.sinks);
+  const int v1 = min(x.last, tiles.nt);
+  if (x.first >= v1) return;
+  prefill_item<HALF>(p, sm, x.seq, hk, x.row, tm, nq, q0, tiles, x.first, v1,
+                     x.state < 0 ? nullptr : p.states + ((int64_t)x.state * p.h_kv + hk) * state_floats(HALF));
+}
+
+// Without one: items of 256 rows, the later (longer) ones first.  Blocks are dealt
+// round-robin to the 8 XCDs: with a multiple of 8 KV heads each XCD gets the items of its
+// own heads, whose tiles share that XCD's L2.
 __global__ __launch_bounds__(512, 2) void kv4_prefill_kernel(Kv4AttnParams p) {
   __shared__ Kv4Smem sm;
   const int tm = kKv4Rows / (p.h_q / p.h_kv);
   const int n_items = (p.max_seqlen_q + tm - 1) / tm;
-  // Largest token tiles first.  Blocks are dealt round-robin to the 8 XCDs: with a
-  // multiple of 8 KV heads each XCD gets the items of its own heads, whose tiles share
-  // that XCD's L2.
-  int x = blockIdx.x, hk, b;
-  if (p.xcd_remap) {
-    const int per = p.h_kv / 8;
-    hk = (x & 7) * per;
-    x >>= 3;
-    hk += x % per;
-    x /= per;
-  } else {
-    hk = x % p.h_kv;
-    x /= p.h_kv;
-  }
-  b = x % p.batch;
-  x /= p.batch;
-  const int part = SPLIT ? x % p.max_partitions : 0;
-  if (SPLIT) x /= p.max_partitions;
-  const int tok0 = (n_items - 1 - x) * tm;
+  int x = blockIdx.x;
+  const int hk = x % p.h_kv;
+  x /= p.h_kv;
+  const int b = x % p.batch, tok0 = (n_items - 1 - x / p.batch) * tm;
   const int q0 = p.cu_seqlens_q[b], nq = p.cu_seqlens_q[b + 1] - q0;
   if (tok0 >= nq) return;
   const int qs = p.q_start[b];
   const Kv4Tiles tiles = kv4_tiles(qs + tok0, qs + min(tok0 + tm, nq) - 1, p.window, p.sinks);
-  const int v0 = SPLIT ? part * p.partition_tiles : 0;
-  const int v1 = SPLIT ? min(tiles.nt, v0 + p.partition_tiles) : tiles.nt;
-  if (v0 >= v1) return;
-  prefill_item<SPLIT>(p, sm, b, hk, tok0, tm, nq, q0, tiles, v0, v1, part);
+  prefill_item<false>(p, sm, b, hk, tok0, tm, nq, q0, tiles, 0, tiles.nt, nullptr);
 }
 
-// One wave per row of the packed batch.
-__global__ __launch_bounds__(64) void kv4_prefill_merge_kernel(Kv4AttnParams p) {
-  const int h = blockIdx.x, tok = blockIdx.y, b = blockIdx.z;
-  const int q0 = p.cu_seqlens_q[b], nq = p.cu_seqlens_q[b + 1] - q0;
-  if (tok >= nq) return;
-  const int tm = kKv4Rows / (p.h_q / p.h_kv), tok0 = tok / tm * tm, qs = p.q_start[b];
-  const Kv4Tiles tiles = kv4_tiles(qs + tok0, qs + min(tok0 + tm, nq) - 1, p.window, p.sinks);
-  const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
-  const int64_t r = (int64_t)(q0 + tok) * p.h_q + h;
-  kv4_merge_row<1>(p.states + r * p.max_partitions * kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD, nullptr);
+// Items that the plan cut: four rows per workgroup, one per wave.
+__global__ __launch_bounds__(256) void kv4_prefill_merge_kernel(Kv4AttnParams p) {
+  const int hk = blockIdx.y, grp = p.h_q / p.h_kv;
+  const mpfa_kv4_item x = p.items[p.n_items + blockIdx.z];
+  const int r = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), tok = x.row + r / grp;
+  const int tm = (p.half ? kKv4Rows / 2 : kKv4Rows) / grp;
+  const int q0 = p.cu_seqlens_q[x.seq], nq = p.cu_seqlens_q[x.seq + 1] - q0;
+  if (r >= tm * grp || tok >= nq) return;
+  const int64_t one = state_floats(p.half);
+  kv4_merge_row<1>(p.states + ((int64_t)x.state * p.h_kv + hk) * one + (int64_t)r * kKv4State, one * p.h_kv, x.parts,
+                   p.v_tscale[x.seq * p.h_kv + hk], p.out + ((int64_t)(q0 + tok) * p.h_q + hk * grp + r % grp) * kD, nullptr);
 }
 
 }  // namespace
 
 hipError_t launch_kv4_prefill(const Kv4AttnParams& p, hipStream_t stream) {
-  if (p.max_seqlen_q == 0) return hipSuccess;
-  const int tm = kKv4Rows / (p.h_q / p.h_kv);
-  const int64_t items = (int64_t)((p.max_seqlen_q + tm - 1) / tm) * p.h_kv * p.batch;
-  if (p.partition_tiles) {
-    kv4_prefill_kernel<true><<<dim3((unsigned)(items * p.max_partitions)), 512, 0, stream>>>(p);
-    kv4_prefill_merge_kernel<<<dim3(p.h_q, p.max_seqlen_q, p.batch), 64, 0, stream>>>(p);
-  } else {
-    kv4_prefill_kernel<false><<<dim3((unsigned)items), 512, 0, stream>>>(p);
+  if (p.items) {
+    const unsigned blocks = (unsigned)p.n_items * p.h_kv;
+    if (p.half) kv4_prefill_plan_kernel<true><<<dim3(blocks), 512, 0, stream>>>(p);
+    else kv4_prefill_plan_kernel<false><<<dim3(blocks), 512, 0, stream>>>(p);
+    if (p.n_merges) {
+      const int rows = p.half ? kKv4Rows / 2 : kKv4Rows;
+      kv4_prefill_merge_kernel<<<dim3(rows / 4, p.h_kv, p.n_merges), 256, 0, stream>>>(p);
+    }
+  } else if (p.max_seqlen_q > 0) {
+    const int tm = kKv4Rows / (p.h_q / p.h_kv);
+    const int64_t items = (int64_t)((p.max_seqlen_q + tm - 1) / tm) * p.h_kv * p.batch;
+    kv4_prefill_kernel<<<dim3((unsigned)items), 512, 0, stream>>>(p);
   }
   return hipGetLastError();
 }

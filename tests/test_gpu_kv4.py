@@ -302,20 +302,57 @@ def test_prefill_heads(mp, h_q, h_kv):
     check_prefill(q, out, rows, cache, stats, new, ctx, 0, 0)
 
 
-@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 130)])
-@pytest.mark.parametrize("part", [0, 128, 384, 1 << 14])
-def test_prefill_partitions(mp, part, window, sinks):
-    """Few rows behind long contexts: the plan's own cut (0) and others, merged."""
-    print(f"prefill partitions of {part}, window {window}", flush=True)
-    new, ctx, h_q, h_kv = [33, 1, 0, 66], [5000, 130, 40, 0], 8, 2
+def make_plan(mp, new, ctx, h_q, h_kv, window, sinks, part, half):
+    """A plan by hand: items of 128 or 256 rows, cut into parts of at most `part` tiles."""
+    tm = (128 if half else 256) // (h_q // h_kv)
+    items, merges, states = [], [], 0
+    for b, (r, c) in enumerate(zip(new, ctx)):
+        for t in range(0, r, tm):
+            nt = visible_tiles(c + t, c + min(t + tm, r) - 1, window, sinks)
+            n = -(-nt // part)
+            if n > 1:
+                merges.append((b, t, 0, nt, states, n))
+            items += [(b, t, k * part, min(nt, (k + 1) * part), states + k if n > 1 else -1, n) for k in range(n)]
+            states += n if n > 1 else 0
+    size = states * h_kv * (128 if half else 256) * 130 * 4
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda") if size else None
+    return mp.Kv4Plan(("prefill", len(new), h_q, h_kv, window, sinks), ws, n_items=len(items), n_merges=len(merges), n_states=states,
+                      half=half, max_rows=max(new), items=i32(items + merges))
+
+
+def visible_tiles(first, last, window, sinks):
+    tiles = set()
+    for pos in range(first, last + 1):
+        tiles |= set(range((max(0, pos - window + 1) if window else 0) // 128, pos // 128 + 1))
+        if window:
+            tiles |= set(range(0, (min(sinks, pos + 1) + 127) // 128))
+    return len(tiles)
+
+
+@pytest.mark.parametrize("half", [0, 1])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (700, 130), (1, 0)])
+@pytest.mark.parametrize("part", [1, 3, 1 << 14])
+def test_prefill_by_hand_made_plans(mp, part, window, sinks, half):
+    print(f"prefill in parts of {part} tiles, window {window}, half {half}", flush=True)
+    new, ctx, h_q, h_kv = [33, 1, 0, 200], [5000, 130, 40, 300], 10, 2
     kv = [a + b for a, b in zip(new, ctx)]
     rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, new, 51)
+    plan = make_plan(mp, new, ctx, h_q, h_kv, window, sinks, part, half)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_prefill(q, cache, stats, cumulative(new), i32(ctx), i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    check_prefill(q, out, rows, cache, stats, new, ctx, window, sinks)
+
+
+@pytest.mark.parametrize("h_q,h_kv", HEADS + [(32, 8), (200, 1)])
+@pytest.mark.parametrize("new,ctx,window,sinks", [([33, 1, 0, 66], [5000, 130, 40, 0], 0, 0), ([700], [0], 0, 0), ([1, 1], [9000, 20000], 3000, 4),
+                                                  ([300, 130], [700, 2000], 500, 200)])
+def test_prefill_by_plan(mp, new, ctx, window, sinks, h_q, h_kv):
+    print(f"prefill {new} behind {ctx} by plan, heads {h_q}:{h_kv}, window {window}", flush=True)
+    kv = [a + b for a, b in zip(new, ctx)]
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, new, 53)
     plan = mp.kv4_prefill_plan(new, kv, h_q, h_kv, window, sinks)
-    if part:
-        plan.partition_tokens, plan.max_partitions = part, -(-max(kv) // part)
-        plan.workspace = torch.full((sum(new) * h_q * plan.max_partitions * 130 * 4,), 255, dtype=torch.uint8, device="cuda")
-    else:
-        assert plan.partition_tokens > 0
+    if plan.workspace is not None:
         plan.workspace.fill_(255)
     out = torch.full_like(q, math.nan)
     mp.kv4_prefill(q, cache, stats, cumulative(new), i32(ctx), i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)

@@ -229,10 +229,17 @@ def test_debug_library_accepts_the_run_and_refuses_bad_data(mp, monkeypatch):
     bad = s.q.clone()
     bad[0, 0, 0] = math.nan
     refused(dec, q=bad)
-    pre = lambda start: mp.kv4_prefill(s.q, s.cache, s.stats, s.one, start, s.kv_len, s.table, s.out)
+    pre = lambda start, plan=None: mp.kv4_prefill(s.q, s.cache, s.stats, s.one, start, s.kv_len, s.table, s.out, plan)
     pre(s.kv_len - 1)
     refused(pre, s.kv_len)
     refused(pre, s.kv_len * 0 - 1)
+    plan = mp.kv4_prefill_plan([1, 1], s.kv, H_Q, H_KV)
+    pre(s.kv_len - 1, plan)
+    for at, value in ((0, 2), (0, -1), (1, 64), (3, 9), (2, 1), (4, 0), (4, -2)):   # sequence, row, last, first, state
+        items = plan.items.clone()
+        items[0, at] = value
+        refused(pre, s.kv_len - 1, mp.Kv4Plan(plan.what, plan.workspace, n_items=plan.n_items, n_merges=plan.n_merges,
+                                              n_states=plan.n_states, half=plan.half, max_rows=1, items=items))
     evict = lambda dst, in_place: mp.kv4_evict(s.cache, s.kv_len, s.table, dst, 64, kept, s.kv_len.clone(), in_place=in_place)
     refused(evict, s.table, False)
     refused(evict, s.table.flip(1).contiguous(), True)

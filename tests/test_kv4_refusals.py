@@ -89,15 +89,20 @@ ATTN_BAD = [
 @pytest.mark.parametrize("kw,status", ATTN_BAD + [
     (dict(flags=512), INVALID), (dict(flags=1), INVALID), (dict(q_tokens=1), INVALID), (dict(cu_seqlens_q=None), INVALID),
     (dict(q_start=None), INVALID), (dict(max_seqlen_q=-1), INVALID), (dict(total_tokens=-1), INVALID),
-    (dict(partition_tokens=128), INVALID), (dict(partition_tokens=128, max_partitions=2, max_seqlen_q=65536), UNSUPPORTED),
+    (dict(items=0x1000), INVALID), (dict(items=0x1000, n_items=2, n_merges=3), INVALID),
+    (dict(items=0x1000, n_items=2, n_merges=-1), INVALID), (dict(items=0x1000, n_items=2, n_states=3), INVALID),
+    (dict(items=0x1000, n_items=2, n_states=-1), INVALID), (dict(items=0x1000, n_items=2, half=2), INVALID),
+    (dict(items=0x1000, n_items=2, half=1, h_q=256, h_kv=1, q_stride=256 * 128), INVALID),
+    (dict(items=0x1000, n_items=1 << 22), UNSUPPORTED), (dict(items=0x1000, n_items=70000, n_merges=65536), UNSUPPORTED),
     (dict(max_seqlen_q=2 ** 31 - 1, batch=65535), UNSUPPORTED)])
 def test_prefill(mp, kw, status):
     assert mp.lib().mpfa_kv4_prefill(C.byref(_attn(mp, **kw)), 0x1000, 1 << 60, None) == status
 
 
-def test_prefill_workspace(mp):
-    a = _attn(mp, partition_tokens=128, max_partitions=3)
-    need = 10 * 8 * 3 * 130 * 4
+@pytest.mark.parametrize("half", [0, 1])
+def test_prefill_workspace(mp, half):
+    a = _attn(mp, items=0x1000, n_items=5, n_merges=2, n_states=4, half=half)
+    need = 4 * 2 * (128 if half else 256) * 130 * 4
     for ws, size in ((None, need), (0x1000, need - 1), (0x1008, need)):
         assert mp.lib().mpfa_kv4_prefill(C.byref(a), ws, size, None) == WORKSPACE
     assert mp.lib().mpfa_kv4_prefill(None, None, 0, None) == INVALID
@@ -141,13 +146,28 @@ def test_calls_without_tokens_do_nothing(mp):
     assert mp.lib().mpfa_kv4_prefill(C.byref(_attn(mp, total_tokens=0, q=None)), None, 0, None) == 0
 
 
-def _plan(mp, name, *args):
+def _plan(mp, name, *args, outs=2):
     import numpy as np
     arrays = [np.asarray(a, np.int32) if isinstance(a, list) else a for a in args]
-    out = C.c_int32(-7), C.c_int32(-7), C.c_size_t(7)
+    out = *(C.c_int32(-7) for _ in range(outs)), C.c_size_t(7)
     ptrs = [a.ctypes.data if hasattr(a, "ctypes") else a for a in arrays]
     rc = getattr(mp.lib(), name)(*ptrs, *(C.byref(o) for o in out))
     return rc, [o.value for o in out]
+
+
+def _prefill_plan(mp, rows, kv, h_q, h_kv, window, sinks, cus=256):
+    """The plan's items and merges, the number of states and whether the items are halved."""
+    import numpy as np
+    rc, (n, merges, states, half, size) = _plan(mp, "mpfa_kv4_prefill_plan", len(rows), rows, kv, h_q, h_kv, window, sinks, cus,
+                                                None, 0, outs=4)
+    assert rc == 0 and size == states * h_kv * (128 if half else 256) * 130 * 4
+    table = np.full((n + merges, 6), -9, np.int32)
+    few = np.empty((max(n + merges - 1, 0), 6), np.int32)
+    args = (len(rows), rows, kv, h_q, h_kv, window, sinks, cus)
+    if n + merges:
+        assert _plan(mp, "mpfa_kv4_prefill_plan", *args, few.ctypes.data, n + merges - 1, outs=4)[0] == WORKSPACE
+    assert _plan(mp, "mpfa_kv4_prefill_plan", *args, table.ctypes.data, n + merges, outs=4) == (0, [n, merges, states, half, size])
+    return table[:n].tolist(), table[n:].tolist(), states, half
 
 
 @pytest.mark.parametrize("args", [
@@ -159,11 +179,12 @@ def test_decode_plan_refuses(mp, args):
 
 
 @pytest.mark.parametrize("args", [
-    (0, [1], [1], 8, 2, 0, 0, 256), (1, None, [1], 8, 2, 0, 0, 256), (1, [1], None, 8, 2, 0, 0, 256),
-    (1, [2], [1], 8, 2, 0, 0, 256), (1, [-1], [1], 8, 2, 0, 0, 256), (1, [1], [1], 8, 3, 0, 0, 256),
-    (1, [1], [1], 8, 2, -1, 0, 256), (1, [1], [1], 8, 2, 0, 0, 0)])
+    (0, [1], [1], 8, 2, 0, 0, 256, None, 0), (1, None, [1], 8, 2, 0, 0, 256, None, 0), (1, [1], None, 8, 2, 0, 0, 256, None, 0),
+    (1, [2], [1], 8, 2, 0, 0, 256, None, 0), (1, [-1], [1], 8, 2, 0, 0, 256, None, 0), (1, [1], [1], 8, 3, 0, 0, 256, None, 0),
+    (1, [1], [1], 8, 2, -1, 0, 256, None, 0), (1, [1], [1], 8, 2, 0, 0, 0, None, 0), (1, [1], [1], 8, 2, 0, 0, 256, None, -1),
+    (65536, [1], [1], 8, 2, 0, 0, 256, None, 0)])
 def test_prefill_plan_refuses(mp, args):
-    assert _plan(mp, "mpfa_kv4_prefill_plan", *args)[0] == INVALID
+    assert _plan(mp, "mpfa_kv4_prefill_plan", *args, outs=4)[0] == INVALID
 
 
 def _visible_tiles(first, last, window, sinks):
@@ -189,14 +210,38 @@ def test_decode_plan_covers_the_visible_tiles(mp, kv, q_tokens, window, sinks):
     assert size >= rows * (maxp * 130 + 2 + maxp * part) * 4
 
 
-@pytest.mark.parametrize("rows,kv,window,sinks", [([1], [50000], 0, 0), ([70], [30000], 0, 0), ([5, 0], [9000, 1], 700, 70)])
-def test_prefill_plan_covers_the_visible_tiles(mp, rows, kv, window, sinks):
-    rc, (part, maxp, size) = _plan(mp, "mpfa_kv4_prefill_plan", len(rows), rows, kv, 8, 2, window, sinks, 256)
-    assert rc == 0
-    if part:
-        most = max(_visible_tiles(n - r + t, n - r + min(t + 64, r) - 1, window, sinks)
-                   for r, n in zip(rows, kv) for t in range(0, r, 64))
-        assert part % 128 == 0 and maxp * part >= most * 128 and size == sum(rows) * 8 * maxp * 130 * 4
+@pytest.mark.parametrize("rows,kv,h_q,h_kv,window,sinks", [
+    ([1], [50000], 8, 2, 0, 0), ([70], [30000], 8, 2, 0, 0), ([5, 0], [9000, 1], 8, 2, 700, 70), ([777], [777], 32, 8, 0, 0),
+    ([8192], [8192], 32, 8, 0, 0), ([512, 2048, 1000], [15512, 7049, 13345], 40, 8, 4096, 4), ([300] * 9, [300] * 9, 16, 1, 0, 0),
+    ([40], [20000], 256, 1, 0, 0), ([3], [3], 32, 32, 1, 0), ([0], [7], 8, 8, 0, 0), ([20000], [90000], 10, 2, 0, 0)])
+def test_prefill_plan_has_every_tile_once(mp, rows, kv, h_q, h_kv, window, sinks):
+    items, merges, states, half = _prefill_plan(mp, rows, kv, h_q, h_kv, window, sinks)
+    tm = (128 if half else 256) // (h_q // h_kv)
+    want = {}
+    for b, (r, n) in enumerate(zip(rows, kv)):
+        for t in range(0, r, tm):
+            want[b, t] = _visible_tiles(n - r + t, n - r + min(t + tm, r) - 1, window, sinks)
+    got, kept = {}, {}
+    for seq, row, first, last, state, parts in items:
+        got.setdefault((seq, row), []).append((first, last))
+        if parts > 1:
+            kept.setdefault((seq, row), []).append((first, state, parts))
+        else:
+            assert state == -1
+    assert got.keys() == want.keys()
+    for k, spans in got.items():
+        spans.sort()
+        assert spans[0][0] == 0 and spans[-1][1] == want[k]
+        assert all(a < b for a, b in spans) and all(x[1] == y[0] for x, y in zip(spans, spans[1:]))
+    assert {(s, r) for s, r, *_ in merges} == kept.keys() and len(merges) == len(kept)
+    used = []
+    for seq, row, first, last, state, parts in merges:
+        spans = sorted(kept[seq, row])
+        assert [x[1] for x in spans] == list(range(state, state + parts)) and {x[2] for x in spans} == {parts}
+        used += [x[1] for x in spans]
+    assert sorted(used) == list(range(states))
+    lengths = [x[3] - x[2] for x in items]
+    assert lengths == sorted(lengths, reverse=True)
 
 
 def _struct(mp, data, cls):
@@ -240,8 +285,7 @@ def test_binding_refuses_what_it_cannot_pass_on(mp):
         mp.PagedCache4(3, 2, planes=dict(k_codes=c.k_codes, k_scales=c.k_scales, v_codes=c.v_codes, v_scales=c.v_scales))
     i32 = dict(dtype=torch.int32)
     table, one = torch.zeros(1, 1, **i32), torch.ones(1, **i32)
-    plan = mp.Kv4Plan(("decode", 1, 4, 2, 0, 0), 128, 1, None)
-    plan.q_tokens, plan.flags = 1, 0
+    plan = mp.Kv4Plan(("decode", 1, 4, 2, 0, 0), None, partition_tokens=128, max_partitions=1, q_tokens=1, flags=0)
     q = torch.zeros(1, 4, 128, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         mp.kv4_decode(q, c, s, one, table, torch.empty_like(q), plan, window=5)                    # a plan of another window
