@@ -350,11 +350,12 @@ def _rows(what, t, heads, dev):
     """Token stride of a bf16 [T][heads][128] tensor whose tokens may lie apart (a slice of a
     fused projection), or ValueError."""
     import torch
-    if (t.dtype is not torch.bfloat16 or t.get_device() != dev or t.dim() != 3 or t.shape[1] != heads or
-            t.shape[2] != HEAD_DIM or t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM)):
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is not torch.bfloat16 or t.get_device() != dev or len(shape) != 3 or shape[1] != heads or
+            shape[2] != HEAD_DIM or stride[2] != 1 or (heads > 1 and stride[1] != HEAD_DIM)):
         raise ValueError(f"{what}: bf16 [T][{heads}][{HEAD_DIM}] on device {dev} with contiguous heads is wanted, got "
-                         f"{t.dtype} {tuple(t.shape)} strides {tuple(t.stride())} on device {t.get_device()}")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * HEAD_DIM)
+                         f"{t.dtype} {tuple(shape)} strides {stride} on device {t.get_device()}")
+    return stride[0] if shape[0] > 1 else max(stride[0], heads * HEAD_DIM)
 
 
 def _want(ok, what):
@@ -368,53 +369,66 @@ def _call(name, dev, stream, *args):
     if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             return _check(getattr(lib(), name)(*args, _stream(stream)), name)
-    return _check(getattr(lib(), name)(*args, _stream(stream)), name)
+    rc = getattr(lib(), name)(*args, _stream(stream))
+    if rc:
+        _check(rc, name)
 
 
-class PagedCache4:
+class _Tensors:
+    """Tensors named once: they are read as attributes, and their addresses are taken when the
+    object is made (a call of a few tokens takes 2 us less so)."""
+
+    def __init__(self, tensors):
+        object.__setattr__(self, "_at", {n: _ptr(t) for n, t in tensors.items()})
+        self.__dict__.update(tensors)
+
+    def __setattr__(self, name, value):
+        if name in self._at:
+            raise AttributeError(f"{name} belongs to the object: make a new one for other tensors")
+        object.__setattr__(self, name, value)
+
+
+class PagedCache4(_Tensors):
     """Planes of the paged 4-bit cache (NVFP4 K and V); weights: with the FP32 weight per
     token that decode accumulates and eviction reads.  planes: existing tensors by plane
     name instead of new zeroed ones."""
 
     def __init__(self, num_pages: int, h_kv: int, device="cuda", weights=False, planes=None):
         import torch
-        self.num_pages, self.h_kv = num_pages, h_kv
         shapes = dict(k_codes=(PAGE, 64), k_scales=(PAGE, 8), v_codes=(PAGE, 64), v_scales=(8, PAGE), weights=(PAGE,))
         if planes is None:
             planes = {n: torch.zeros((num_pages, h_kv, *s), device=device,
                                      dtype=torch.float32 if n == "weights" else torch.uint8)
                       for n, s in shapes.items() if weights or n != "weights"}
-        self.device = planes["k_codes"].get_device()
-        for n, s in shapes.items():
-            t = planes.get(n)
+        found = {n: planes.get(n) for n in shapes}
+        _want(all(t is not None or n == "weights" for n, t in found.items()), "PagedCache4: a plane is missing")
+        dev = found["k_codes"].get_device()
+        for n, t in found.items():
             if t is not None:
-                _same("PagedCache4", torch.float32 if n == "weights" else torch.uint8, self.device, t)
-                _want(tuple(t.shape) == (num_pages, h_kv, *s), f"PagedCache4: {n} has shape {tuple(t.shape)}")
-            else:
-                _want(n == "weights", f"PagedCache4: no plane {n}")
-            setattr(self, n, t)
-
-    def _c(self):
-        return Kv4Cache(_ptr(self.k_codes), _ptr(self.k_scales), _ptr(self.v_codes), _ptr(self.v_scales),
-                        _ptr(self.weights), self.num_pages)
+                _same("PagedCache4", torch.float32 if n == "weights" else torch.uint8, dev, t)
+                _want(tuple(t.shape) == (num_pages, h_kv, *shapes[n]), f"PagedCache4: {n} has shape {tuple(t.shape)}")
+        super().__init__(found)
+        self.num_pages, self.h_kv, self.device = num_pages, h_kv, dev
+        self._c = Kv4Cache(*self._at.values(), num_pages)
 
 
-class SeqStats4:
+class SeqStats4(_Tensors):
     """Per-sequence statistics of the 4-bit cache, frozen after a sequence's first write: K mean
     and the tensor scales of K and V (existing tensors may be given)."""
 
     def __init__(self, batch: int, h_kv: int, device="cuda", k_mean=None, k_tscale=None, v_tscale=None):
         import torch
         new = dict(dtype=torch.float32, device=device)
-        self.k_tscale = torch.ones((batch, h_kv), **new) if k_tscale is None else k_tscale
-        self.v_tscale = torch.ones((batch, h_kv), **new) if v_tscale is None else v_tscale
-        dev = self.k_tscale.device
-        self.k_mean = torch.zeros((batch, h_kv, HEAD_DIM), dtype=torch.bfloat16, device=dev) if k_mean is None else k_mean
-        self.batch, self.h_kv, self.device = batch, h_kv, self.k_tscale.get_device()
-        _same("SeqStats4", torch.float32, self.device, self.k_tscale, self.v_tscale)
-        _same("SeqStats4", torch.bfloat16, self.device, self.k_mean)
-        _want(tuple(self.k_tscale.shape) == tuple(self.v_tscale.shape) == (batch, h_kv) and
-              tuple(self.k_mean.shape) == (batch, h_kv, HEAD_DIM), "SeqStats4: shapes")
+        kt = torch.ones((batch, h_kv), **new) if k_tscale is None else k_tscale
+        vt = torch.ones((batch, h_kv), **new) if v_tscale is None else v_tscale
+        mean = torch.zeros((batch, h_kv, HEAD_DIM), dtype=torch.bfloat16, device=kt.device) if k_mean is None else k_mean
+        dev = kt.get_device()
+        _same("SeqStats4", torch.float32, dev, kt, vt)
+        _same("SeqStats4", torch.bfloat16, dev, mean)
+        _want(tuple(kt.shape) == tuple(vt.shape) == (batch, h_kv) and tuple(mean.shape) == (batch, h_kv, HEAD_DIM),
+              "SeqStats4: shapes")
+        super().__init__(dict(k_mean=mean, k_tscale=kt, v_tscale=vt))
+        self.batch, self.h_kv, self.device = batch, h_kv, dev
 
 
 class Kv4Plan:
@@ -425,8 +439,14 @@ class Kv4Plan:
     def __init__(self, what, workspace, **kw):
         self.what, self.workspace = what, workspace
         self.partition_tokens = self.max_partitions = self.n_items = self.n_merges = self.n_states = self.half = 0
+        self.q_tokens = self.flags = 0
         self.items = None
         self.__dict__.update(kw)
+
+    def cut(self):
+        """The fields of Kv4AttnArgs that the plan sets: q_tokens, then partition_tokens .. flags."""
+        return (self.q_tokens, self.partition_tokens, self.max_partitions, self.n_items, self.n_merges, self.n_states,
+                self.half, self.flags)
 
 
 def _host_ints(x):
@@ -493,44 +513,50 @@ def kv4_write(k, v, cu_seqlens, slot_mapping, cache: PagedCache4, stats: SeqStat
     """mpfa_kv4_write: k, v bf16 [T][Hkv][128] (tokens may lie apart) into the 4-bit cache; workspace:
     kv4_write_workspace_size bytes, with COMPUTE_STATS."""
     import torch
-    dev, T, batch = cache.device, k.shape[0], cu_seqlens.numel() - 1
-    ks, vs = _rows("kv4_write: k", k, cache.h_kv, dev), _rows("kv4_write: v", v, cache.h_kv, dev)
+    dev, h_kv, T, batch = cache.device, cache.h_kv, k.shape[0], cu_seqlens.numel() - 1
+    ks, vs = _rows("kv4_write: k", k, h_kv, dev), _rows("kv4_write: v", v, h_kv, dev)
     _same("kv4_write", torch.int32, dev, cu_seqlens)
     _same("kv4_write", torch.int64, dev, slot_mapping)
-    _want(v.shape[0] == T and slot_mapping.numel() == T, "kv4_write: as many V rows and slots as K rows are wanted")
-    _want(stats.batch == batch and stats.h_kv == cache.h_kv and stats.device == dev, "kv4_write: stats of another batch")
-    for t in (k_out, v_out):
+    if v.shape[0] != T or slot_mapping.numel() != T:
+        raise ValueError("kv4_write: as many V rows and slots as K rows are wanted")
+    if stats.batch != batch or stats.h_kv != h_kv or stats.device != dev:
+        raise ValueError("kv4_write: stats of another batch")
+    out, size = [None, None], 0
+    for i, t in enumerate((k_out, v_out)):
         if t is not None:
             _same("kv4_write", torch.bfloat16, dev, t)
             _want(t.numel() == k.numel(), "kv4_write: k_out and v_out have the shape of k")
+            out[i] = t.data_ptr()
     if workspace is not None:
         _same("kv4_write: workspace", workspace.dtype, dev, workspace)
-    a = Kv4WriteArgs(batch, T, max_seqlen, cache.h_kv, HEAD_DIM, flags, ks, vs, _ptr(cu_seqlens), _ptr(k), _ptr(v),
-                     _ptr(slot_mapping), _ptr(stats.k_mean), _ptr(stats.k_tscale), _ptr(stats.v_tscale), cache._c(),
-                     _ptr(k_out), _ptr(v_out))
-    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        size = workspace.numel() * workspace.element_size()
+    at = stats._at
+    a = Kv4WriteArgs(batch, T, max_seqlen, h_kv, HEAD_DIM, flags, ks, vs, cu_seqlens.data_ptr(), k.data_ptr(), v.data_ptr(),
+                     slot_mapping.data_ptr(), at["k_mean"], at["k_tscale"], at["v_tscale"], cache._c, *out)
     _call("mpfa_kv4_write", dev, stream, C.byref(a), _ptr(workspace), size)
 
 
-def _kv4_attn(what, q, cache, stats, cu, q_start, kv_len, page_table, out, plan, max_seqlen_q, q_tokens, window, sinks,
-              flags, stream):
+def _kv4_attn(what, kind, q, cache, stats, cu, q_start, kv_len, page_table, out, plan, max_seqlen_q, window, sinks, stream):
     import torch
-    dev, batch, h_q = cache.device, kv_len.numel(), q.shape[1] if q.dim() == 3 else 0
+    dev, h_kv, batch, shape = cache.device, cache.h_kv, kv_len.numel(), q.shape
+    h_q = shape[1] if len(shape) == 3 else 0
     stride = _rows(what, q, h_q, dev)
     _same(what, torch.int32, dev, kv_len, page_table)
     _same(what, torch.bfloat16, dev, out)
-    _want(out.numel() == q.numel() and page_table.dim() == 2 and page_table.shape[0] == batch, f"{what}: shapes")
-    _want(stats.batch == batch and stats.h_kv == cache.h_kv and stats.device == dev, f"{what}: stats of another batch")
-    kind = "decode" if q_tokens else "prefill"
-    _want(plan is None or plan.what == (kind, batch, h_q, cache.h_kv, window, sinks),
-          f"{what}: the plan was made for another call: {plan and plan.what}")
-    ws = plan.workspace if plan is not None else None
-    _want(ws is None or ws.get_device() == dev, f"{what}: the plan is of another device")
-    cut = (0,) * 6 if plan is None else (plan.partition_tokens, plan.max_partitions, plan.n_items, plan.n_merges,
-                                         plan.n_states, plan.half)
-    a = Kv4AttnArgs(batch, h_q, cache.h_kv, HEAD_DIM, page_table.shape[1], q.shape[0], max_seqlen_q, q_tokens, window, sinks,
-                    *cut, flags, stride, _ptr(cu), _ptr(q_start), None if plan is None else _ptr(plan.items), _ptr(kv_len), _ptr(page_table), _ptr(q), cache._c(), _ptr(stats.k_tscale),
-                    _ptr(stats.v_tscale), _ptr(out))
+    if out.numel() != q.numel() or page_table.dim() != 2 or page_table.shape[0] != batch:
+        raise ValueError(f"{what}: shapes")
+    if stats.batch != batch or stats.h_kv != h_kv or stats.device != dev:
+        raise ValueError(f"{what}: stats of another batch")
+    ws, items, cut = None, None, (0,) * 8
+    if plan is not None:
+        if plan.what != (kind, batch, h_q, h_kv, window, sinks):
+            raise ValueError(f"{what}: the plan was made for another call: {plan.what}")
+        cut, ws, items = plan.cut(), plan.workspace, _ptr(plan.items)
+        if ws is not None and ws.get_device() != dev:
+            raise ValueError(f"{what}: the plan is of another device")
+    a = Kv4AttnArgs(batch, h_q, h_kv, HEAD_DIM, page_table.shape[1], shape[0], max_seqlen_q, cut[0], window, sinks, *cut[1:],
+                    stride, cu, q_start, items, kv_len.data_ptr(), page_table.data_ptr(), q.data_ptr(), cache._c,
+                    stats._at["k_tscale"], stats._at["v_tscale"], out.data_ptr())
     _call("mpfa_kv4_" + kind, dev, stream, C.byref(a), _ptr(ws), 0 if ws is None else ws.numel())
 
 
@@ -543,18 +569,19 @@ def kv4_prefill(q, cache: PagedCache4, stats: SeqStats4, cu_seqlens_q, q_start, 
     if max_seqlen_q is None:
         max_seqlen_q = q.shape[0] if plan is None else plan.max_rows
     _same("kv4_prefill", torch.int32, cache.device, cu_seqlens_q, q_start)
-    _want(cu_seqlens_q.numel() == kv_len.numel() + 1 and q_start.numel() == kv_len.numel(), "kv4_prefill: shapes")
-    _kv4_attn("kv4_prefill", q, cache, stats, cu_seqlens_q, q_start, kv_len, page_table, out, plan,
-              max_seqlen_q, 0, window, sinks, 0, stream)
+    if cu_seqlens_q.numel() != kv_len.numel() + 1 or q_start.numel() != kv_len.numel():
+        raise ValueError("kv4_prefill: shapes")
+    _kv4_attn("kv4_prefill", "prefill", q, cache, stats, cu_seqlens_q.data_ptr(), q_start.data_ptr(), kv_len, page_table, out,
+              plan, max_seqlen_q, window, sinks, stream)
 
 
 def kv4_decode(q, cache: PagedCache4, stats: SeqStats4, kv_len, page_table, out, plan: Kv4Plan, window=0, sinks=0,
                stream=None):
     """mpfa_kv4_decode: the plan's q_tokens rows per sequence, the last ones of its kv_len keys; with a
     plan made for weights the attention weights are added to cache.weights."""
-    _want(q.shape[0] == kv_len.numel() * plan.q_tokens, "kv4_decode: q has q_tokens rows per sequence")
-    _kv4_attn("kv4_decode", q, cache, stats, None, None, kv_len, page_table, out, plan, 0, plan.q_tokens, window, sinks,
-              plan.flags, stream)
+    if q.shape[0] != kv_len.numel() * plan.q_tokens:
+        raise ValueError("kv4_decode: q has q_tokens rows per sequence")
+    _kv4_attn("kv4_decode", "decode", q, cache, stats, None, None, kv_len, page_table, out, plan, 0, window, sinks, stream)
 
 
 def kv4_evict(cache: PagedCache4, kv_len, page_table, dst_page_table, budget: int, kept, new_len, sinks=0, recent=0,
@@ -562,11 +589,11 @@ def kv4_evict(cache: PagedCache4, kv_len, page_table, dst_page_table, budget: in
     """mpfa_kv4_evict: cuts every sequence to the `budget` tokens of the largest cache.weights (per KV head;
     the first `sinks` and last `recent` always stay); kept int32 [B][Hkv][budget] and new_len [B] are written."""
     import torch
-    dev, batch = cache.device, kv_len.numel()
+    dev, h_kv, batch, src, dst = cache.device, cache.h_kv, kv_len.numel(), page_table.shape, dst_page_table.shape
     _same("kv4_evict", torch.int32, dev, kv_len, page_table, dst_page_table, kept, new_len)
-    _want(page_table.dim() == dst_page_table.dim() == 2 and page_table.shape[0] == dst_page_table.shape[0] == batch and
-          tuple(kept.shape) == (batch, cache.h_kv, budget) and new_len.numel() == batch, "kv4_evict: shapes")
-    a = Kv4EvictArgs(batch, cache.h_kv, page_table.shape[1], dst_page_table.shape[1], budget, sinks, recent,
-                     KV4_IN_PLACE if in_place else 0, _ptr(kv_len), _ptr(page_table), _ptr(dst_page_table), cache._c(),
-                     _ptr(kept), _ptr(new_len))
+    if (len(src) != 2 or len(dst) != 2 or src[0] != batch or dst[0] != batch or kept.shape != (batch, h_kv, budget) or
+            new_len.numel() != batch):
+        raise ValueError("kv4_evict: shapes")
+    a = Kv4EvictArgs(batch, h_kv, src[1], dst[1], budget, sinks, recent, KV4_IN_PLACE if in_place else 0, kv_len.data_ptr(),
+                     page_table.data_ptr(), dst_page_table.data_ptr(), cache._c, kept.data_ptr(), new_len.data_ptr())
     _call("mpfa_kv4_evict", dev, stream, C.byref(a))
