@@ -344,6 +344,8 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* a, void* workspace, size_t
   p.h_kv = a->h_kv;
   p.smooth = smooth;
   p.compute_stats = stats;
+  // from 32768 tokens on 512 per partial: workgroups enough, and a quarter of the partials
+  p.stat_tokens = a->total_tokens >= 32768 ? 4 * mpfa::kKv4StatTokens : mpfa::kKv4StatTokens;
   p.num_pages = a->cache.num_pages;
   p.k_stride = a->k_stride;
   p.v_stride = a->v_stride;

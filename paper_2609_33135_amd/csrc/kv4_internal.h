@@ -10,7 +10,7 @@
 
 namespace mpfa {
 
-constexpr int kKv4StatTokens = 128;   // tokens per statistics partial
+constexpr int kKv4StatTokens = 128;   // fewest tokens per statistics partial
 // per partial of one KV head: FP64 sums, FP32 maxima and minima of K per channel, and
 // the largest |V| (padded to 16 bytes)
 constexpr int kKv4StatBytes = 128 * (8 + 4 + 4) + 16;
@@ -29,6 +29,7 @@ struct Kv4Cache {
 struct Kv4WriteParams {
   int batch, total_tokens, max_seqlen, h_kv;
   int smooth, compute_stats;
+  int stat_tokens;                    // tokens per statistics partial, a multiple of kKv4StatTokens
   int64_t num_pages, k_stride, v_stride;
   const int32_t* cu_seqlens;
   const uint16_t* k;

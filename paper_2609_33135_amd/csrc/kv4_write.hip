@@ -13,16 +13,22 @@ namespace mpfa {
 
 namespace {
 
+constexpr int64_t kLastLevelCache = (int64_t)256 << 20;
 constexpr int kWriteTokens = 32;   // tokens per workgroup: eight per wave, eight lanes (groups of 16) each
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+__device__ __forceinline__ u32x4 load16(const uint16_t* src, bool stream) {
+  const u32x4* at = reinterpret_cast<const u32x4*>(src);
+  return stream ? __builtin_nontemporal_load(at) : *at;
+}
+
 // Statistics partial of block blk of sequence b (the blocks of a batch are numbered so
-// that no two sequences share one: floor(t0 / 128) + b, since ceil(n / 128) more of them
-// end at or before the next sequence's first).
+// that no two sequences share one: floor(t0 / tokens) + b, since ceil(n / tokens) more of
+// them end at or before the next sequence's first).
 __device__ __forceinline__ uint8_t* stat_block(const Kv4WriteParams& p, int64_t t0, int b, int blk, int hk) {
-  return p.ws + ((t0 / kKv4StatTokens + b + blk) * p.h_kv + hk) * kKv4StatBytes;
+  return p.ws + ((t0 / p.stat_tokens + b + blk) * p.h_kv + hk) * kKv4StatBytes;
 }
 
 struct StatPtrs {
@@ -34,15 +40,19 @@ __device__ __forceinline__ StatPtrs stat_ptrs(uint8_t* s) {
           reinterpret_cast<float*>(s + kD * 16)};
 }
 
-// One workgroup per (128 tokens, KV head): 16 lanes per token row, 16 rows at a time.
+// One workgroup per (stat_tokens tokens, KV head): 16 lanes per token row, 128 rows at a time.
+// STREAM: the rows are read past the caches' ordinary replacement.  What does not fit the
+// last-level cache is lost to the write pass anyway: 65536 tokens, 8 heads, 182 us of the
+// whole call so, 195 not; 16384 tokens, which fit, 52.9 and 51.2.
+template <bool STREAM>
 __global__ __launch_bounds__(256) void kv4_stats_kernel(Kv4WriteParams p) {
   __shared__ double s_sum[4][kD];
   __shared__ float s_mx[4][kD], s_mn[4][kD], s_v[4];
   const int b = blockIdx.z, hk = blockIdx.y, blk = blockIdx.x;
   const int64_t t0 = p.cu_seqlens[b];
   const int n = p.cu_seqlens[b + 1] - (int)t0;
-  const int tb = blk * kKv4StatTokens, te = min(n, tb + kKv4StatTokens);
-  if (tb >= n) return;
+  const int begin = blk * p.stat_tokens, te = min(n, begin + p.stat_tokens);
+  if (begin >= n) return;
   const int c = threadIdx.x & 15, row = threadIdx.x >> 4, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   double sum[8];
   float mx[8], mn[8], va = 0.0f;
@@ -52,17 +62,25 @@ __global__ __launch_bounds__(256) void kv4_stats_kernel(Kv4WriteParams p) {
     mx[e] = -INFINITY;
     mn[e] = INFINITY;
   }
+  // eight rows of K and V in flight; rows past the end repeat the last one, whose values
+  // change no extreme, and are left out of the sums
+  constexpr int kRows = kKv4StatTokens / 16;
+  for (int tb = begin; tb < te; tb += kKv4StatTokens) {
+    u32x4 kw[kRows], vw[kRows];
 #pragma unroll
-  for (int i = 0; i < kKv4StatTokens / 16; ++i) {
-    const int t = tb + 16 * i + row;
-    if (t < te) {
-      const u32x4 kw = *reinterpret_cast<const u32x4*>(p.k + (t0 + t) * p.k_stride + hk * kD + 8 * c);
-      const u32x4 vw = *reinterpret_cast<const u32x4*>(p.v + (t0 + t) * p.v_stride + hk * kD + 8 * c);
-      va = fmaxf(va, q_amax(vw));
+    for (int i = 0; i < kRows; ++i) {
+      const int64_t t = t0 + min(tb + 16 * i + row, te - 1);
+      kw[i] = load16(p.k + t * p.k_stride + hk * kD + 8 * c, STREAM);
+      vw[i] = load16(p.v + t * p.v_stride + hk * kD + 8 * c, STREAM);
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const bool mine = tb + 16 * i + row < te;
+      va = fmaxf(va, q_amax(vw[i]));
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = e & 1 ? bf_hi(kw[e >> 1]) : bf_lo(kw[e >> 1]);
-        sum[e] += (double)x;
+        const float x = e & 1 ? bf_hi(kw[i][e >> 1]) : bf_lo(kw[i][e >> 1]);
+        sum[e] += mine ? (double)x : 0.0;
         mx[e] = fmaxf(mx[e], x);
         mn[e] = fminf(mn[e], x);
       }
@@ -107,15 +125,26 @@ __global__ __launch_bounds__(1024) void kv4_stats_final_kernel(Kv4WriteParams p)
   const int64_t t0 = p.cu_seqlens[b];
   const int n = p.cu_seqlens[b + 1] - (int)t0;
   if (n <= 0) return;   // no tokens: the statistics stay as they are
-  const int nblk = (n + kKv4StatTokens - 1) / kKv4StatTokens;
+  const int nblk = (n + p.stat_tokens - 1) / p.stat_tokens;
+  constexpr int kAhead = 8;
   double sum = 0.0;
   float mx = -INFINITY, mn = INFINITY, va = 0.0f;
-#pragma unroll 4
-  for (int blk = part; blk < nblk; blk += 8) {
-    const StatPtrs s = stat_ptrs(stat_block(p, t0, b, blk, hk));
-    sum += s.sum[c];
-    mx = fmaxf(mx, s.mx[c]);
-    mn = fminf(mn, s.mn[c]);
+  for (int blk0 = part; blk0 < nblk; blk0 += 8 * kAhead) {   // past the last block it again, without its sum
+    double sums[kAhead];
+    float mxs[kAhead], mns[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const StatPtrs s = stat_ptrs(stat_block(p, t0, b, min(blk0 + 8 * i, nblk - 1), hk));
+      sums[i] = s.sum[c];
+      mxs[i] = s.mx[c];
+      mns[i] = s.mn[c];
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      sum += blk0 + 8 * i < nblk ? sums[i] : 0.0;
+      mx = fmaxf(mx, mxs[i]);
+      mn = fminf(mn, mns[i]);
+    }
   }
   for (int blk = threadIdx.x; blk < nblk; blk += 1024) va = fmaxf(va, stat_ptrs(stat_block(p, t0, b, blk, hk)).v[0]);
   for (int off = 32; off >= 1; off >>= 1) va = fmaxf(va, __shfl_xor(va, off));
@@ -185,7 +214,9 @@ __device__ __forceinline__ Group quantize_group(const float* x, float t) {
   return g;
 }
 
-// The values that a group's codes stand for, as bf16 (exact: six bits).
+// The values that a group's codes stand for, as bf16 (exact: six bits).  Nothing here reads
+// them again: stored past the caches they leave K and V there (16384 tokens, 8 heads, 31
+// us, 37 not).
 __device__ __forceinline__ void store_values(uint16_t* out, const Group& g) {
   u32x4 w[2];
 #pragma unroll
@@ -197,8 +228,8 @@ __device__ __forceinline__ void store_values(uint16_t* out, const Group& g) {
     for (int j = 0; j < 4; ++j)
       w[half][j] = (__float_as_uint(v[j][0] * g.step) >> 16) | (__float_as_uint(v[j][1] * g.step) & 0xFFFF0000u);
   }
-  reinterpret_cast<u32x4*>(out)[0] = w[0];
-  reinterpret_cast<u32x4*>(out)[1] = w[1];
+  __builtin_nontemporal_store(w[0], reinterpret_cast<u32x4*>(out));
+  __builtin_nontemporal_store(w[1], reinterpret_cast<u32x4*>(out) + 1);
 }
 
 __device__ __forceinline__ void load_group(const uint16_t* src, float* x) {
@@ -258,8 +289,10 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4WriteParams p) {
 hipError_t launch_kv4_write(const Kv4WriteParams& p, hipStream_t stream) {
   if (p.total_tokens == 0 || p.max_seqlen == 0) return hipSuccess;
   if (p.compute_stats) {
-    const int blocks = (p.max_seqlen + kKv4StatTokens - 1) / kKv4StatTokens;
-    kv4_stats_kernel<<<dim3(blocks, p.h_kv, p.batch), 256, 0, stream>>>(p);
+    const int blocks = (p.max_seqlen + p.stat_tokens - 1) / p.stat_tokens;
+    const dim3 grid(blocks, p.h_kv, p.batch);
+    if ((int64_t)p.total_tokens * p.h_kv * kD * 4 >= kLastLevelCache) kv4_stats_kernel<true><<<grid, 256, 0, stream>>>(p);
+    else kv4_stats_kernel<false><<<grid, 256, 0, stream>>>(p);
     kv4_stats_final_kernel<<<dim3(p.h_kv, p.batch), 1024, 0, stream>>>(p);
   }
   const int chunks = (p.max_seqlen + kWriteTokens - 1) / kWriteTokens;
