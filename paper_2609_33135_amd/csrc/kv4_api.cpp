@@ -492,7 +492,8 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
       window < 0 || sinks < 0 || (flags & ~MPFA_KV4_WEIGHTS) || num_cus < 1 || !partition_tokens || !max_partitions ||
       !workspace_bytes)
     return MPFA_ERR_INVALID;
-  const int64_t chunks = ((int64_t)q_tokens * (h_q / h_kv) + 15) / 16;
+  const int64_t cols = (int64_t)q_tokens * (h_q / h_kv), per = mpfa::kv4_wide_columns(cols) ? 32 : 16;
+  const int64_t chunks = (cols + per - 1) / per;
   auto seen = [&](int b) {
     return seen_tiles((int64_t)kv_len_host[b] - q_tokens, (int64_t)kv_len_host[b] - 1, window, sinks);
   };
@@ -535,8 +536,7 @@ mpfa_status mpfa_kv4_decode(const mpfa_kv4_attn_args* a, void* workspace, size_t
   if (a->q_tokens < 1 || a->q_tokens > 65535 || a->partition_tokens < 1 || a->max_partitions < 1) return MPFA_ERR_INVALID;
   if (weights && !a->cache.weights) return MPFA_ERR_INVALID;
   p.q_tokens = a->q_tokens;
-  const int64_t chunks = ((int64_t)a->q_tokens * (a->h_q / a->h_kv) + 15) / 16;
-  if (chunks * a->h_kv > 65535) return MPFA_ERR_UNSUPPORTED;
+  if ((int64_t)a->q_tokens * a->h_q > 65535 * 16) return MPFA_ERR_UNSUPPORTED;
   if ((int64_t)a->max_partitions * a->partition_tokens > ((int64_t)1 << 30)) return MPFA_ERR_UNSUPPORTED;
   DecodeSpace s;
   if (!decode_space(a->batch, a->h_q, a->q_tokens, a->partition_tokens, a->max_partitions, weights, &s)) return MPFA_ERR_INVALID;

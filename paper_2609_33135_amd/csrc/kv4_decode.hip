@@ -2,8 +2,8 @@
 // 4-bit cache for gfx950, the merge of its partitions, and the accumulation of the
 // attention weights.
 //
-// One wave takes one (sequence, KV head, 16 columns, partition of the visible tiles).  A
-// column is a query row: (token, query head of the KV head).  Keys are centered by their
+// One wave takes one (sequence, KV head, 16 or 32 columns, partition of the visible tiles).
+// A column is a query row: (token, query head of the KV head).  Keys are centered by their
 // sequence's mean when they are written; the term q . mean is the same for every key of a
 // row, so the softmax does not see it and bf16 queries need no compensation.
 //
@@ -69,11 +69,14 @@ __device__ __forceinline__ bool find_group(const Kv4AttnParams& p, int pos, int 
 // would take long to scan; a single sequence, which needs none: 1 us less).
 constexpr int kPackedBatch = 512;
 
-template <bool WEIGHTS, bool PACKED>
+// COLS: columns per wave, 16 or 32: two MFMA column blocks that share the dequantized K and
+// V, in steps of one page instead of a tile of two (whose registers would spill).
+template <int COLS, bool WEIGHTS, bool PACKED>
 __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4AttnParams p) {
+  constexpr int kN = COLS / 16, kP = 2 / kN, kB = 4 * kP;   // column blocks; pages and key blocks per step
   const int lane = threadIdx.x & 63, g = lane >> 4, lr = lane & 15;
   const int grp = p.h_q / p.h_kv, cols = p.q_tokens * grp;
-  const int chunks = (cols + 15) >> 4;
+  const int chunks = (cols + COLS - 1) / COLS;
   int b = blockIdx.z, hk = blockIdx.y, group = blockIdx.x;
   if (PACKED) {
     hk = blockIdx.x % p.h_kv;
@@ -88,14 +91,6 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
   const int v0 = part * p.partition_tiles, v1 = min(tiles.nt, v0 + p.partition_tiles);
   if (v0 >= v1 || part >= p.max_partitions) return;
 
-  const int col = chunk * 16 + lr;
-  const bool valid = col < cols;
-  const int tok = valid ? col / grp : 0, h = hk * grp + (valid ? col - tok * grp : 0);
-  const int pos = kvl - p.q_tokens + tok;            // last visible key; negative: none
-  // keys below it are outside the window (unless they are sinks)
-  const int low = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
-  const int64_t row = (int64_t)b * p.q_tokens + tok;
-
   const int32_t* pt = p.page_table + (int64_t)b * p.max_pages;
   const int npg = (kvl + 63) >> 6;
   // the pages of 32 visible tiles, one per lane, read back with v_readlane: the loop has
@@ -106,24 +101,24 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     const int x = v + (lane >> 1);
     win = pt[min(2 * tiles.tile(min(x, tiles.nt - 1)) + (lane & 1), npg - 1)];
   };
-  int64_t c0, c1;   // (page, KV head) rows of the tile
-  auto tile_pages = [&](int v) {
+  int64_t c[kP];   // (page, KV head) rows of a step
+  auto step_pages = [&](int u) {   // step u: kP pages from page kP u of the visible tiles on
+    const int v = u * kP / 2;
     if (v - win_base >= 32) load_window(v);
-    c0 = kv4_row(__builtin_amdgcn_readlane(win, 2 * (v - win_base)), p.h_kv, hk);
-    c1 = kv4_row(__builtin_amdgcn_readlane(win, 2 * (v - win_base) + 1), p.h_kv, hk);
+#pragma unroll
+    for (int i = 0; i < kP; ++i) c[i] = kv4_row(__builtin_amdgcn_readlane(win, kP * u + i - 2 * win_base), p.h_kv, hk);
   };
 
   // offsets of the lane's bytes in a page: the rest is scalar or constant
   const uint32_t krow = 16 * (lr >> 2) + (lr & 3);   // + 4 (mb % 4): key of MFMA row lr
   const uint32_t k_off = krow * 64 + 16 * g, ks_off = krow * 8 + 2 * g;
   const uint32_t v_off = g * 1024 + lr * 16, vs_off = (lr >> 1) * 64 + 16 * g;
-  u32x4 kc[8];
-  uint32_t ksc[8];
+  u32x4 kc[kB];
+  uint32_t ksc[kB];
   auto load_k = [&]() {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int64_t r = half ? c1 : c0;
-      const uint8_t *codes = p.cache.k_codes + r * 4096, *scales = p.cache.k_scales + r * 512;
+    for (int half = 0; half < kP; ++half) {
+      const uint8_t *codes = p.cache.k_codes + c[half] * 4096, *scales = p.cache.k_scales + c[half] * 512;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         ksc[4 * half + i] = *reinterpret_cast<const uint16_t*>(scales + ks_off + 32 * i);
@@ -131,27 +126,34 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
       }
     }
   };
-  u32x4 vc[8], vsc[2];
+  u32x4 vc[kB], vsc[kP];
   auto load_v = [&]() {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int64_t r = half ? c1 : c0;
-      const uint8_t *codes = p.cache.v_codes + r * 4096, *scales = p.cache.v_scales + r * 512;
+    for (int half = 0; half < kP; ++half) {
+      const uint8_t *codes = p.cache.v_codes + c[half] * 4096, *scales = p.cache.v_scales + c[half] * 512;
 #pragma unroll
       for (int i = 0; i < 4; ++i) vc[4 * half + i] = *reinterpret_cast<const u32x4*>(codes + v_off + 256 * i);
       vsc[half] = *reinterpret_cast<const u32x4*>(scales + vs_off);
     }
   };
 
+  const int u0 = v0 * 2 / kP, u1 = v1 * 2 / kP;
   load_window(v0);
-  tile_pages(v0);
+  step_pages(u0);
   load_k();
 
-  // ---- Q: channels 32g .. +31 of the lane's column
-  f16x8 qop[4];
-  float lam;
-  {
-    const u32x4* src = reinterpret_cast<const u32x4*>(p.q + row * p.q_stride + h * kD + 32 * g);
+  // ---- Q: channels 32g .. +31 of the lane's columns, and what they see
+  f16x8 qop[kN][4];
+  float lam[kN], m[kN], l[kN];   // m in accumulator units (times lam: log2)
+  int pos[kN];                   // last visible key; negative: none
+  f32x4 o[kN][8];
+  auto col_of = [&](int n) { return chunk * COLS + 16 * n + lr; };
+#pragma unroll
+  for (int n = 0; n < kN; ++n) {
+    const int col = min(col_of(n), cols - 1), tok = col / grp;
+    pos[n] = kvl - p.q_tokens + tok;
+    const u32x4* src = reinterpret_cast<const u32x4*>(p.q + ((int64_t)b * p.q_tokens + tok) * p.q_stride +
+                                                      (hk * grp + col - tok * grp) * kD + 32 * g);
     u32x4 w[4];
     float a = 0.0f;
 #pragma unroll
@@ -161,92 +163,100 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     }
     const int shift = q_shift(wave_max16(a));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) qop[i] = q_operand(w[i], shift);
-    lam = score_scale(p.lam, p.k_tscale[b * p.h_kv + hk], shift);
+    for (int i = 0; i < 4; ++i) qop[n][i] = q_operand(w[i], shift);
+    lam[n] = score_scale(p.lam, p.k_tscale[b * p.h_kv + hk], shift);
+    m[n] = -INFINITY;
+    l[n] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < 8; ++db) o[n][db] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
 
-  float m = -INFINITY, l = 0.0f;   // m in accumulator units (times lam: log2)
-  f32x4 o[8];
-#pragma unroll
-  for (int db = 0; db < 8; ++db) o[db] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-  for (int v = v0; v < v1; ++v) {
-    const int key0 = tiles.tile(v) * kTile;
+  for (int u = u0; u < u1; ++u) {
+    const int key0 = tiles.tile(u * kP / 2) * kTile + (kP == 1 ? kPage * (u & 1) : 0);
     load_v();
     __builtin_amdgcn_sched_barrier(0);   // the waits for K below leave V in flight
-    f32x4 s[8];
+    f32x4 s[kN][kB];
 #pragma unroll
-    for (int mb = 0; mb < 8; ++mb) {
+    for (int mb = 0; mb < kB; ++mb) {
       const f16x2 sc = e4m3_pair_f16(ksc[mb]);
-      f32x4 c = {0.f, 0.f, 0.f, 0.f};
-      c = mfma_f16(dequant8h(kc[mb][0], sc[0]), qop[0], c);
-      c = mfma_f16(dequant8h(kc[mb][1], sc[0]), qop[1], c);
-      c = mfma_f16(dequant8h(kc[mb][2], sc[1]), qop[2], c);
-      s[mb] = mfma_f16(dequant8h(kc[mb][3], sc[1]), qop[3], c);
-    }
-    tile_pages(min(v + 1, v1 - 1));
-    load_k();                            // past the last tile: it again
-    // ---- masked scores (which may come from stale bytes) by selection
-    const int k0 = key0 + 16 * g;
-    if (key0 + kTile - 1 > kvl - p.q_tokens || (p.window > 0 && key0 < kvl - p.window)) {   // uniform
+      const f16x8 k[4] = {dequant8h(kc[mb][0], sc[0]), dequant8h(kc[mb][1], sc[0]), dequant8h(kc[mb][2], sc[1]),
+                          dequant8h(kc[mb][3], sc[1])};
 #pragma unroll
-      for (int mb = 0; mb < 8; ++mb)
+      for (int n = 0; n < kN; ++n) {
+        s[n][mb] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][mb] = mfma_f16(k[i], qop[n][i], s[n][mb]);
+      }
+    }
+    step_pages(min(u + 1, u1 - 1));
+    load_k();                            // past the last step: it again
+    const int k0 = key0 + 16 * g;
+    f16x8 pb[kN][2 * kP];
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      // ---- masked scores (which may come from stale bytes) by selection
+      if (key0 + kPage * kP - 1 > kvl - p.q_tokens || (p.window > 0 && key0 < kvl - p.window)) {   // uniform
+        // keys below it are outside the window (unless they are sinks)
+        const int low = p.window > 0 ? max(pos[n] - p.window + 1, 0) : 0;
+#pragma unroll
+        for (int mb = 0; mb < kB; ++mb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = k0 + 64 * (mb >> 2) + 4 * (mb & 3) + i;
+            const bool seen = key <= pos[n] && (key >= low || key < p.sinks);
+            s[n][mb][i] = seen ? s[n][mb][i] : -INFINITY;
+          }
+      }
+      if (WEIGHTS) {
+        if (col_of(n) < cols) {
+          float* dst = p.scores +
+                       (((int64_t)b * p.h_kv + hk) * cols + col_of(n)) * ((int64_t)p.max_partitions * p.partition_tiles * kTile) +
+                       (int64_t)u * (kPage * kP) + 16 * g;
+#pragma unroll
+          for (int mb = 0; mb < kB; ++mb) *reinterpret_cast<f32x4*>(dst + 64 * (mb >> 2) + 4 * (mb & 3)) = s[n][mb] * lam[n];
+        }
+      }
+      float mxa = -INFINITY, mxb = -INFINITY;
+#pragma unroll
+      for (int mb = 0; mb < kB; mb += 2) {
+        mxa = fmaxf(fmaxf(mxa, s[n][mb][0]), s[n][mb][1]);
+        mxa = fmaxf(fmaxf(mxa, s[n][mb][2]), s[n][mb][3]);
+        mxb = fmaxf(fmaxf(mxb, s[n][mb + 1][0]), s[n][mb + 1][1]);
+        mxb = fmaxf(fmaxf(mxb, s[n][mb + 1][2]), s[n][mb + 1][3]);
+      }
+      const float mnew = fmaxf(m[n], wave_max16(fmaxf(mxa, mxb)));
+      const float muse = mnew == -INFINITY ? 0.0f : mnew;
+      const float alpha = m[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[n] - muse) * lam[n]);
+      m[n] = mnew;
+      const float bias = __builtin_fmaf(-muse, lam[n], kLog2P);
+      float ps = 0.0f;
+#pragma unroll
+      for (int mb = 0; mb < kB; ++mb) {
+        float e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int key = k0 + 64 * (mb >> 2) + 4 * (mb & 3) + i;
-          const bool seen = key <= pos && (key >= low || key < p.sinks);
-          s[mb][i] = seen ? s[mb][i] : -INFINITY;
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][mb][i], lam[n], bias));
+          pb[n][mb >> 1][4 * (mb & 1) + i] = (_Float16)e[i];
         }
-    }
-    if (WEIGHTS) {
-      if (valid) {
-        float* dst = p.scores + (((int64_t)b * p.h_kv + hk) * cols + col) * ((int64_t)p.max_partitions * p.partition_tiles * kTile) +
-                     (int64_t)v * kTile + 16 * g;
-#pragma unroll
-        for (int mb = 0; mb < 8; ++mb) *reinterpret_cast<f32x4*>(dst + 64 * (mb >> 2) + 4 * (mb & 3)) = s[mb] * lam;
+        ps += (e[0] + e[1]) + (e[2] + e[3]);
       }
-    }
-    float mxa = -INFINITY, mxb = -INFINITY;
+      l[n] = alpha * l[n] + ps;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
-    for (int mb = 0; mb < 8; mb += 2) {
-      mxa = fmaxf(fmaxf(mxa, s[mb][0]), s[mb][1]);
-      mxa = fmaxf(fmaxf(mxa, s[mb][2]), s[mb][3]);
-      mxb = fmaxf(fmaxf(mxb, s[mb + 1][0]), s[mb + 1][1]);
-      mxb = fmaxf(fmaxf(mxb, s[mb + 1][2]), s[mb + 1][3]);
-    }
-    const float mnew = fmaxf(m, wave_max16(fmaxf(mxa, mxb)));
-    const float muse = mnew == -INFINITY ? 0.0f : mnew;
-    const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - muse) * lam);
-    m = mnew;
-    const float bias = __builtin_fmaf(-muse, lam, kLog2P);
-    float ps = 0.0f;
-    f16x8 pb[4];
-#pragma unroll
-    for (int mb = 0; mb < 8; ++mb) {
-      float e[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[mb][i], lam, bias));
-        pb[mb >> 1][4 * (mb & 1) + i] = (_Float16)e[i];
+        for (int db = 0; db < 8; ++db) o[n][db] *= alpha;
       }
-      ps += (e[0] + e[1]) + (e[2] + e[3]);
-    }
-    l = alpha * l + ps;
-    if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
-#pragma unroll
-      for (int db = 0; db < 8; ++db) o[db] *= alpha;
     }
     // ---- V: keys past the end hold stale bytes, P = 0 there: their scales are cleared so
     // that 0 * NaN cannot occur
-    if (key0 + kTile > kvl) {
+    if (key0 + kPage * kP > kvl) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < kB; ++i) {
         const int keep = kvl - k0 - 64 * (i >> 2) - 4 * (i & 3);
         vsc[i >> 2][i & 3] &= keep >= 4 ? 0xFFFFFFFFu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
       }
     }
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {        // keys 64 (t/2) + 16g + 8 (t%2) .. +7
+    for (int t = 0; t < 2 * kP; ++t) {   // keys 64 (t/2) + 16g + 8 (t%2) .. +7
       uint32_t ev[4], od[4];
       f16x2 sc[4];
 #pragma unroll
@@ -257,51 +267,60 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
         const uint32_t w = vsc[t >> 1][2 * (t & 1) + (i >> 1)];
         sc[i] = e4m3_pair_f16((i & 1) ? w >> 16 : w);
       }
-      auto pv = [&](const uint32_t (&w)[4], auto sel, f32x4& acc) {
+      auto pv = [&](const uint32_t (&w)[4], auto sel, int db) {
         constexpr int S = decltype(sel)::value;
         const f16x2 x0 = fp4_pair_f16<S>(w[0], sc[0]), x1 = fp4_pair_f16<S>(w[1], sc[1]);
         const f16x2 x2 = fp4_pair_f16<S>(w[2], sc[2]), x3 = fp4_pair_f16<S>(w[3], sc[3]);
-        acc = mfma_f16((f16x8){x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]}, pb[t], acc);
+        const f16x8 x = {x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+#pragma unroll
+        for (int n = 0; n < kN; ++n) o[n][db] = mfma_f16(x, pb[n][t], o[n][db]);
       };
-      pv(ev, std::integral_constant<int, 0>{}, o[0]);
-      pv(od, std::integral_constant<int, 0>{}, o[1]);
-      pv(ev, std::integral_constant<int, 1>{}, o[2]);
-      pv(od, std::integral_constant<int, 1>{}, o[3]);
-      pv(ev, std::integral_constant<int, 2>{}, o[4]);
-      pv(od, std::integral_constant<int, 2>{}, o[5]);
-      pv(ev, std::integral_constant<int, 3>{}, o[6]);
-      pv(od, std::integral_constant<int, 3>{}, o[7]);
+      pv(ev, std::integral_constant<int, 0>{}, 0);
+      pv(od, std::integral_constant<int, 0>{}, 1);
+      pv(ev, std::integral_constant<int, 1>{}, 2);
+      pv(od, std::integral_constant<int, 1>{}, 3);
+      pv(ev, std::integral_constant<int, 2>{}, 4);
+      pv(od, std::integral_constant<int, 2>{}, 5);
+      pv(ev, std::integral_constant<int, 3>{}, 6);
+      pv(od, std::integral_constant<int, 3>{}, 7);
     }
   }
-  // keep the products in full-wave control flow (the store below is under a branch)
 #pragma unroll
-  for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(o[db]));
-  const float lt = wave_sum16(l);
-  if (valid) {
-    float* st = p.states + ((row * p.h_q + h) * p.max_partitions + part) * kKv4State;
-    if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m * lam, lt);
-    // accumulator row 4g + i of block db is channel 8 (4g + i) + db
+  for (int n = 0; n < kN; ++n) {
+    // keep the products in full-wave control flow (the store below is under a branch)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(o[n][db]));
+    const float lt = wave_sum16(l[n]);
+    const int col = col_of(n);
+    if (col < cols) {
+      const int tok = col / grp;
+      float* st = p.states + ((((int64_t)b * p.q_tokens + tok) * p.h_q + hk * grp + col - tok * grp) * p.max_partitions + part) * kKv4State;
+      if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m[n] * lam[n], lt);
+      // accumulator row 4g + i of block db is channel 8 (4g + i) + db
 #pragma unroll
-      for (int db = 0; db < 8; db += 2)
-        *reinterpret_cast<float2*>(st + 2 + 32 * g + 8 * i + db) = make_float2(o[db][i], o[db + 1][i]);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int db = 0; db < 8; db += 2)
+          *reinterpret_cast<float2*>(st + 2 + 32 * g + 8 * i + db) = make_float2(o[n][db][i], o[n][db + 1][i]);
+    }
   }
 }
 
-// One workgroup per row (token, query head): one wave, or four where there are many
-// partitions (a wave keeps eight in flight).
+// Rows (token, query head): a wave each, four to a workgroup, or a workgroup of four waves
+// each where there are many partitions (a wave keeps eight in flight).
 constexpr int kManyPartitions = 16;
 
 template <int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void kv4_decode_merge_kernel(Kv4AttnParams p) {
-  const int h = blockIdx.x, tok = blockIdx.y, b = blockIdx.z;
+__global__ __launch_bounds__(256) void kv4_decode_merge_kernel(Kv4AttnParams p) {
+  const int b = blockIdx.y, rows = p.q_tokens * p.h_q;
+  const int i = WAVES > 1 ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (i >= rows) return;
   const int kvl = p.kv_len[b];
   const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
   const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
-  const int64_t r = ((int64_t)b * p.q_tokens + tok) * p.h_q + h;
-  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, np, p.v_tscale[b * p.h_kv + h / (p.h_q / p.h_kv)], p.out + r * kD,
-                p.stats ? p.stats + 2 * r : nullptr);
+  const int64_t r = (int64_t)b * rows + i;
+  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, np,
+                       p.v_tscale[b * p.h_kv + i % p.h_q / (p.h_q / p.h_kv)], p.out + r * kD, p.stats ? p.stats + 2 * r : nullptr);
 }
 
 // Adds every visible key's share of the attention, summed over the rows of its KV head in
@@ -333,23 +352,24 @@ __global__ __launch_bounds__(256) void kv4_weights_kernel(Kv4AttnParams p) {
 
 }  // namespace
 
-template <bool WEIGHTS>
+template <int COLS, bool WEIGHTS>
 void launch_partitions(const Kv4AttnParams& p, hipStream_t stream) {
-  const int chunks = (p.q_tokens * (p.h_q / p.h_kv) + 15) / 16;
+  const int chunks = (p.q_tokens * (p.h_q / p.h_kv) + COLS - 1) / COLS;
   const int64_t groups = ((int64_t)p.max_partitions * chunks + kDecodeWaves - 1) / kDecodeWaves;
   const int64_t all = groups * p.h_kv * p.batch;
   if (p.batch > 1 && p.batch <= kPackedBatch && all * 64 * kDecodeWaves <= UINT32_MAX)
-    kv4_decode_kernel<WEIGHTS, true><<<dim3((unsigned)all), 64 * kDecodeWaves, 0, stream>>>(p);
+    kv4_decode_kernel<COLS, WEIGHTS, true><<<dim3((unsigned)all), 64 * kDecodeWaves, 0, stream>>>(p);
   else
-    kv4_decode_kernel<WEIGHTS, false><<<dim3((unsigned)groups, p.h_kv, p.batch), 64 * kDecodeWaves, 0, stream>>>(p);
+    kv4_decode_kernel<COLS, WEIGHTS, false><<<dim3((unsigned)groups, p.h_kv, p.batch), 64 * kDecodeWaves, 0, stream>>>(p);
 }
 
 hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream) {
-  if (p.scores) launch_partitions<true>(p, stream);
-  else launch_partitions<false>(p, stream);
-  const dim3 rows(p.h_q, p.q_tokens, p.batch);
-  if (p.max_partitions > kManyPartitions) kv4_decode_merge_kernel<4><<<rows, 256, 0, stream>>>(p);
-  else kv4_decode_merge_kernel<1><<<rows, 64, 0, stream>>>(p);
+  const bool wide = kv4_wide_columns(p.q_tokens * (p.h_q / p.h_kv));
+  if (p.scores) wide ? launch_partitions<32, true>(p, stream) : launch_partitions<16, true>(p, stream);
+  else wide ? launch_partitions<32, false>(p, stream) : launch_partitions<16, false>(p, stream);
+  const int rows = p.q_tokens * p.h_q;
+  if (p.max_partitions > kManyPartitions) kv4_decode_merge_kernel<4><<<dim3(rows, p.batch), 256, 0, stream>>>(p);
+  else kv4_decode_merge_kernel<1><<<dim3((rows + 3) / 4, p.batch), 256, 0, stream>>>(p);
   if (p.scores) {
     const int64_t keys = (int64_t)p.max_partitions * p.partition_tiles * kTile;
     kv4_weights_kernel<<<dim3((unsigned)((keys + 1023) / 1024), p.h_kv, p.batch), 256, 0, stream>>>(p);

@@ -100,6 +100,9 @@ __host__ __device__ inline Kv4Tiles kv4_tiles(int first, int last, int window, i
   return t;
 }
 
+// Whether decode waves take 32 columns (rows times heads of a KV head) each, or 16.
+__host__ __device__ inline bool kv4_wide_columns(int64_t cols) { return cols > 16; }
+
 hipError_t launch_kv4_write(const Kv4WriteParams& p, hipStream_t stream);
 hipError_t launch_kv4_prefill(const Kv4AttnParams& p, hipStream_t stream);
 hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream);
