@@ -12,13 +12,12 @@
 //                    eighth of the bf16 output's own 2^-8; FP8 would be 2^-4)
 //   O^T += V^T P^T   16x16x32 FP16 MFMA
 //
-// K and V go from memory to registers, 16 bytes per lane and load, no LDS.  Inside a
-// 128-key tile (two pages) MFMA row r of key block mb is key 64 (mb/4) + 16 (r/4) + 4 (mb%4)
-// + r%4, so lane group g (lanes 16g .. +15) ends up with the scores of keys 16g .. 16g+15 of
-// either page of its column, and these are the keys it supplies to the PV product; every
-// load of a wave lies in one page, whose address is in scalar registers.  For V a lane
-// holds the octet of channels 8 lr .. +7 of those keys: all its values share one scale
-// group, and MFMA row lr of channel block db is channel 8 lr + db.
+// K and V go from memory to registers, 16 bytes per lane and load, no LDS, a page of 64 keys
+// per step, whose address is in scalar registers.  MFMA row r of key block mb is key
+// 16 (r/4) + 4 mb + r%4, so lane group g (lanes 16g .. +15) ends up with the scores of keys
+// 16g .. 16g+15 of its column, and these are the keys it supplies to the PV product.  For V
+// a lane holds the octet of channels 8 lr .. +7 of those keys: all its values share one
+// scale group, and MFMA row lr of channel block db is channel 8 lr + db.
 //
 // What bounds it: HBM reads, 144 bytes per (token, KV head).
 #include "kv4_device.h"
@@ -69,11 +68,13 @@ __device__ __forceinline__ bool find_group(const Kv4AttnParams& p, int pos, int 
 // would take long to scan; a single sequence, which needs none: 1 us less).
 constexpr int kPackedBatch = 512;
 
-// COLS: columns per wave, 16 or 32: two MFMA column blocks that share the dequantized K and
-// V, in steps of one page instead of a tile of two (whose registers would spill).
+// COLS: columns per wave, 16 or 32 (two MFMA column blocks that share the dequantized K and
+// V).  In steps of one page three waves of 16 columns fit a SIMD, or two of 32; with tiles of
+// two pages two of 16, and 32 spilled (one context of 64K keys, 40:8 heads, 20.8 us, 21.8 so;
+// 16 contexts of 10K to 32K, 8:2 heads, 21.4 and 22.8).
 template <int COLS, bool WEIGHTS, bool PACKED>
-__global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4AttnParams p) {
-  constexpr int kN = COLS / 16, kP = 2 / kN, kB = 4 * kP;   // column blocks; pages and key blocks per step
+__global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_decode_kernel(Kv4AttnParams p) {
+  constexpr int kN = COLS / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4, lr = lane & 15;
   const int grp = p.h_q / p.h_kv, cols = p.q_tokens * grp;
   const int chunks = (cols + COLS - 1) / COLS;
@@ -101,45 +102,37 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     const int x = v + (lane >> 1);
     win = pt[min(2 * tiles.tile(min(x, tiles.nt - 1)) + (lane & 1), npg - 1)];
   };
-  int64_t c[kP];   // (page, KV head) rows of a step
-  auto step_pages = [&](int u) {   // step u: kP pages from page kP u of the visible tiles on
-    const int v = u * kP / 2;
-    if (v - win_base >= 32) load_window(v);
-#pragma unroll
-    for (int i = 0; i < kP; ++i) c[i] = kv4_row(__builtin_amdgcn_readlane(win, kP * u + i - 2 * win_base), p.h_kv, hk);
+  int64_t c;   // (page, KV head) row of a step
+  auto step_page = [&](int u) {   // step u: page u of the visible tiles
+    if ((u >> 1) - win_base >= 32) load_window(u >> 1);
+    c = kv4_row(__builtin_amdgcn_readlane(win, u - 2 * win_base), p.h_kv, hk);
   };
 
   // offsets of the lane's bytes in a page: the rest is scalar or constant
-  const uint32_t krow = 16 * (lr >> 2) + (lr & 3);   // + 4 (mb % 4): key of MFMA row lr
+  const uint32_t krow = 16 * (lr >> 2) + (lr & 3);   // + 4 mb: key of MFMA row lr
   const uint32_t k_off = krow * 64 + 16 * g, ks_off = krow * 8 + 2 * g;
   const uint32_t v_off = g * 1024 + lr * 16, vs_off = (lr >> 1) * 64 + 16 * g;
-  u32x4 kc[kB];
-  uint32_t ksc[kB];
+  u32x4 kc[4];
+  uint32_t ksc[4];
   auto load_k = [&]() {
+    const uint8_t *codes = p.cache.k_codes + c * 4096, *scales = p.cache.k_scales + c * 512;
 #pragma unroll
-    for (int half = 0; half < kP; ++half) {
-      const uint8_t *codes = p.cache.k_codes + c[half] * 4096, *scales = p.cache.k_scales + c[half] * 512;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ksc[4 * half + i] = *reinterpret_cast<const uint16_t*>(scales + ks_off + 32 * i);
-        kc[4 * half + i] = *reinterpret_cast<const u32x4*>(codes + k_off + 256 * i);
-      }
+    for (int i = 0; i < 4; ++i) {
+      ksc[i] = *reinterpret_cast<const uint16_t*>(scales + ks_off + 32 * i);
+      kc[i] = *reinterpret_cast<const u32x4*>(codes + k_off + 256 * i);
     }
   };
-  u32x4 vc[kB], vsc[kP];
+  u32x4 vc[4], vsc;
   auto load_v = [&]() {
+    const uint8_t *codes = p.cache.v_codes + c * 4096, *scales = p.cache.v_scales + c * 512;
 #pragma unroll
-    for (int half = 0; half < kP; ++half) {
-      const uint8_t *codes = p.cache.v_codes + c[half] * 4096, *scales = p.cache.v_scales + c[half] * 512;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) vc[4 * half + i] = *reinterpret_cast<const u32x4*>(codes + v_off + 256 * i);
-      vsc[half] = *reinterpret_cast<const u32x4*>(scales + vs_off);
-    }
+    for (int i = 0; i < 4; ++i) vc[i] = *reinterpret_cast<const u32x4*>(codes + v_off + 256 * i);
+    vsc = *reinterpret_cast<const u32x4*>(scales + vs_off);
   };
 
-  const int u0 = v0 * 2 / kP, u1 = v1 * 2 / kP;
+  const int u0 = 2 * v0, u1 = 2 * v1;
   load_window(v0);
-  step_pages(u0);
+  step_page(u0);
   load_k();
 
   // ---- Q: channels 32g .. +31 of the lane's columns, and what they see
@@ -172,12 +165,12 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
   }
 
   for (int u = u0; u < u1; ++u) {
-    const int key0 = tiles.tile(u * kP / 2) * kTile + (kP == 1 ? kPage * (u & 1) : 0);
+    const int key0 = tiles.tile(u >> 1) * kTile + kPage * (u & 1);
     load_v();
     __builtin_amdgcn_sched_barrier(0);   // the waits for K below leave V in flight
-    f32x4 s[kN][kB];
+    f32x4 s[kN][4];
 #pragma unroll
-    for (int mb = 0; mb < kB; ++mb) {
+    for (int mb = 0; mb < 4; ++mb) {
       const f16x2 sc = e4m3_pair_f16(ksc[mb]);
       const f16x8 k[4] = {dequant8h(kc[mb][0], sc[0]), dequant8h(kc[mb][1], sc[0]), dequant8h(kc[mb][2], sc[1]),
                           dequant8h(kc[mb][3], sc[1])};
@@ -188,21 +181,21 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
         for (int i = 0; i < 4; ++i) s[n][mb] = mfma_f16(k[i], qop[n][i], s[n][mb]);
       }
     }
-    step_pages(min(u + 1, u1 - 1));
+    step_page(min(u + 1, u1 - 1));
     load_k();                            // past the last step: it again
     const int k0 = key0 + 16 * g;
-    f16x8 pb[kN][2 * kP];
+    f16x8 pb[kN][2];
 #pragma unroll
     for (int n = 0; n < kN; ++n) {
       // ---- masked scores (which may come from stale bytes) by selection
-      if (key0 + kPage * kP - 1 > kvl - p.q_tokens || (p.window > 0 && key0 < kvl - p.window)) {   // uniform
+      if (key0 + kPage - 1 > kvl - p.q_tokens || (p.window > 0 && key0 < kvl - p.window)) {   // uniform
         // keys below it are outside the window (unless they are sinks)
         const int low = p.window > 0 ? max(pos[n] - p.window + 1, 0) : 0;
 #pragma unroll
-        for (int mb = 0; mb < kB; ++mb)
+        for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int key = k0 + 64 * (mb >> 2) + 4 * (mb & 3) + i;
+            const int key = k0 + 4 * mb + i;
             const bool seen = key <= pos[n] && (key >= low || key < p.sinks);
             s[n][mb][i] = seen ? s[n][mb][i] : -INFINITY;
           }
@@ -211,14 +204,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
         if (col_of(n) < cols) {
           float* dst = p.scores +
                        (((int64_t)b * p.h_kv + hk) * cols + col_of(n)) * ((int64_t)p.max_partitions * p.partition_tiles * kTile) +
-                       (int64_t)u * (kPage * kP) + 16 * g;
+                       (int64_t)u * kPage + 16 * g;
 #pragma unroll
-          for (int mb = 0; mb < kB; ++mb) *reinterpret_cast<f32x4*>(dst + 64 * (mb >> 2) + 4 * (mb & 3)) = s[n][mb] * lam[n];
+          for (int mb = 0; mb < 4; ++mb) *reinterpret_cast<f32x4*>(dst + 4 * mb) = s[n][mb] * lam[n];
         }
       }
       float mxa = -INFINITY, mxb = -INFINITY;
 #pragma unroll
-      for (int mb = 0; mb < kB; mb += 2) {
+      for (int mb = 0; mb < 4; mb += 2) {
         mxa = fmaxf(fmaxf(mxa, s[n][mb][0]), s[n][mb][1]);
         mxa = fmaxf(fmaxf(mxa, s[n][mb][2]), s[n][mb][3]);
         mxb = fmaxf(fmaxf(mxb, s[n][mb + 1][0]), s[n][mb + 1][1]);
@@ -231,7 +224,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
       const float bias = __builtin_fmaf(-muse, lam[n], kLog2P);
       float ps = 0.0f;
 #pragma unroll
-      for (int mb = 0; mb < kB; ++mb) {
+      for (int mb = 0; mb < 4; ++mb) {
         float e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -248,15 +241,15 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
     }
     // ---- V: keys past the end hold stale bytes, P = 0 there: their scales are cleared so
     // that 0 * NaN cannot occur
-    if (key0 + kPage * kP > kvl) {
+    if (key0 + kPage > kvl) {
 #pragma unroll
-      for (int i = 0; i < kB; ++i) {
-        const int keep = kvl - k0 - 64 * (i >> 2) - 4 * (i & 3);
-        vsc[i >> 2][i & 3] &= keep >= 4 ? 0xFFFFFFFFu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
+      for (int i = 0; i < 4; ++i) {
+        const int keep = kvl - k0 - 4 * i;
+        vsc[i] &= keep >= 4 ? 0xFFFFFFFFu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2 * kP; ++t) {   // keys 64 (t/2) + 16g + 8 (t%2) .. +7
+    for (int t = 0; t < 2; ++t) {        // keys 16g + 8t .. +7
       uint32_t ev[4], od[4];
       f16x2 sc[4];
 #pragma unroll
@@ -264,7 +257,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, 2) void kv4_decode_kernel(Kv4Att
         const uint32_t a = vc[2 * t + (i >> 1)][2 * (i & 1)], c = vc[2 * t + (i >> 1)][2 * (i & 1) + 1];
         ev[i] = keys_even(a, c);
         od[i] = keys_odd(a, c);
-        const uint32_t w = vsc[t >> 1][2 * (t & 1) + (i >> 1)];
+        const uint32_t w = vsc[2 * t + (i >> 1)];
         sc[i] = e4m3_pair_f16((i & 1) ? w >> 16 : w);
       }
       auto pv = [&](const uint32_t (&w)[4], auto sel, int db) {
