@@ -51,18 +51,17 @@ int far(int x) { return x < kFar ? x : kFar; }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Bytes of the three parts of a decode workspace: partition states, then with weights the
-// merged statistics and the scores.  False where a size does not fit.
+// Bytes of the two parts of a decode workspace: partition states, then with weights the
+// scores.  False where a size does not fit.
 struct DecodeSpace {
-  size_t states, stats, scores;
+  size_t states, scores;
 };
 bool decode_space(int batch, int h_q, int q_tokens, int partition_tokens, int max_partitions, bool weights, DecodeSpace* s) {
   const double rows = (double)batch * q_tokens * h_q;
   const double keys = (double)max_partitions * partition_tokens;
-  if (rows * max_partitions * mpfa::kKv4State * 4 + (weights ? rows * (8 + keys * 4) : 0) > 9e18) return false;
+  if (rows * max_partitions * mpfa::kKv4State * 4 + (weights ? rows * keys * 4 : 0) > 9e18) return false;
   const size_t r = (size_t)batch * q_tokens * h_q;
   s->states = align256(r * max_partitions * mpfa::kKv4State * sizeof(float));
-  s->stats = weights ? align256(r * 2 * sizeof(float)) : 0;
   s->scores = weights ? r * (size_t)max_partitions * partition_tokens * sizeof(float) : 0;
   return true;
 }
@@ -524,7 +523,7 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
   if (!decode_space(batch, h_q, q_tokens, (int)part * MPFA_KV_TILE, (int)parts, flags & MPFA_KV4_WEIGHTS, &s)) return MPFA_ERR_INVALID;
   *partition_tokens = (int32_t)(part * MPFA_KV_TILE);
   *max_partitions = (int32_t)parts;
-  *workspace_bytes = s.states + s.stats + s.scores;
+  *workspace_bytes = s.states + s.scores;
   return MPFA_OK;
 }
 
@@ -540,13 +539,10 @@ mpfa_status mpfa_kv4_decode(const mpfa_kv4_attn_args* a, void* workspace, size_t
   if ((int64_t)a->max_partitions * a->partition_tokens > ((int64_t)1 << 30)) return MPFA_ERR_UNSUPPORTED;
   DecodeSpace s;
   if (!decode_space(a->batch, a->h_q, a->q_tokens, a->partition_tokens, a->max_partitions, weights, &s)) return MPFA_ERR_INVALID;
-  if (!workspace || workspace_bytes < s.states + s.stats + s.scores || !aligned16(workspace)) return MPFA_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < s.states + s.scores || !aligned16(workspace)) return MPFA_ERR_WORKSPACE;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.states = reinterpret_cast<float*>(ws);
-  if (weights) {
-    p.stats = reinterpret_cast<float*>(ws + s.states);
-    p.scores = reinterpret_cast<float*>(ws + s.states + s.stats);
-  }
+  if (weights) p.scores = reinterpret_cast<float*>(ws + s.states);
 #ifdef MPFA_DEBUG_CHECKS
   if (const mpfa_status st = check_attn(a, true, reinterpret_cast<hipStream_t>(stream))) return st;
 #endif

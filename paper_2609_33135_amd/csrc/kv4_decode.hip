@@ -299,43 +299,72 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
   }
 }
 
+// ---- after the partitions: the rows' merge and, with weights, the keys' shares.  One launch
+// for both: the shares' workgroups derive the merged maximum and sum of every row from the
+// partitions themselves (a launch of their own after the merge took 4 us more).
+
 // Rows (token, query head): a wave each, four to a workgroup, or a workgroup of four waves
 // each where there are many partitions (a wave keeps eight in flight).
 constexpr int kManyPartitions = 16;
+constexpr int kWeightKeys = 1024;   // per workgroup, four per thread
+constexpr int kWeightRows = 64;     // whose maxima and sums are held at a time
+
+__device__ __forceinline__ int partitions_of(const Kv4AttnParams& p, const Kv4Tiles& tiles) {
+  return min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
+}
 
 template <int WAVES>
-__global__ __launch_bounds__(256) void kv4_decode_merge_kernel(Kv4AttnParams p) {
-  const int b = blockIdx.y, rows = p.q_tokens * p.h_q;
-  const int i = WAVES > 1 ? blockIdx.x : __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+__device__ __forceinline__ void merge_rows(const Kv4AttnParams& p, int b, int block, const Kv4Tiles& tiles) {
+  const int rows = p.q_tokens * p.h_q;
+  const int i = WAVES > 1 ? block : __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6));
   if (i >= rows) return;
-  const int kvl = p.kv_len[b];
-  const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
-  const int np = min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
   const int64_t r = (int64_t)b * rows + i;
-  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, np,
-                       p.v_tscale[b * p.h_kv + i % p.h_q / (p.h_q / p.h_kv)], p.out + r * kD, p.stats ? p.stats + 2 * r : nullptr);
+  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, partitions_of(p, tiles),
+                       p.v_tscale[b * p.h_kv + i % p.h_q / (p.h_q / p.h_kv)], p.out + r * kD);
 }
 
 // Adds every visible key's share of the attention, summed over the rows of its KV head in
-// order, to the cache's weights: four keys per thread.
-__global__ __launch_bounds__(256) void kv4_weights_kernel(Kv4AttnParams p) {
-  const int b = blockIdx.z, hk = blockIdx.y, kvl = p.kv_len[b];
-  const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
+// order, to the cache's weights.
+__device__ __forceinline__ void add_weights(const Kv4AttnParams& p, int b, int hk, int block, const Kv4Tiles& tiles) {
+  __shared__ float2 stats[kWeightRows];   // a row's maximum, and 2^15 / its sum (0: it sees nothing)
+  const int kvl = p.kv_len[b], grp = p.h_q / p.h_kv, cols = p.q_tokens * grp, np = partitions_of(p, tiles);
   const int64_t per_col = (int64_t)p.max_partitions * p.partition_tiles * kTile;
-  const int vk = (blockIdx.x * 256 + threadIdx.x) * 4;
-  if (vk >= min((int64_t)tiles.nt * kTile, per_col)) return;
-  const int key = tiles.tile(vk / kTile) * kTile + (vk & (kTile - 1));
-  if (key >= kvl) return;
-  const int grp = p.h_q / p.h_kv, cols = p.q_tokens * grp;
-  const float* src = p.scores + ((int64_t)b * p.h_kv + hk) * cols * per_col + vk;
+  if ((int64_t)block * kWeightKeys >= min((int64_t)tiles.nt * kTile, per_col)) return;
+  const int vk = block * kWeightKeys + threadIdx.x * 4;
+  const bool mine = vk < min((int64_t)tiles.nt * kTile, per_col);
+  const int key = mine ? tiles.tile(vk / kTile) * kTile + (vk & (kTile - 1)) : kvl;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   f32x4 w = {0.f, 0.f, 0.f, 0.f};
-  for (int c = 0; c < cols; ++c) {
-    const float2 st = *reinterpret_cast<const float2*>(p.stats + 2 * (((int64_t)b * p.q_tokens + c / grp) * p.h_q + hk * grp + c % grp));
-    if (!(st.y > 0.0f)) continue;   // a row that sees nothing
-    const f32x4 s = *reinterpret_cast<const f32x4*>(src + c * per_col);
+  for (int c0 = 0; c0 < cols; c0 += kWeightRows) {
+    const int n = min(cols - c0, kWeightRows);
+    __syncthreads();
+    for (int c = wave; c < n; c += 4) {
+      const int tok = (c0 + c) / grp, h = hk * grp + (c0 + c) - tok * grp;
+      const float* st = p.states + (((int64_t)b * p.q_tokens + tok) * p.h_q + h) * p.max_partitions * kKv4State;
+      float M = -INFINITY, L = 0.0f;
+      for (int q = lane; q < np; q += 64) M = fmaxf(M, st[(int64_t)q * kKv4State]);
+      for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+      if (M > -INFINITY)
+        for (int q = lane; q < np; q += 64) {
+          const float2 ml = *reinterpret_cast<const float2*>(st + (int64_t)q * kKv4State);
+          L = __builtin_fmaf(__builtin_amdgcn_exp2f(ml.x - M), ml.y, L);
+        }
+      for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off);
+      if (lane == 0) stats[c] = make_float2(M, L > 0.0f ? __fdiv_rn(0x1p15f, L) : 0.0f);
+    }
+    __syncthreads();
+    if (key < kvl) {
+      const float* src = p.scores + (((int64_t)b * p.h_kv + hk) * cols + c0) * per_col + vk;
+      for (int c = 0; c < n; ++c) {
+        const float2 st = stats[c];
+        if (!(st.y > 0.0f)) continue;
+        const f32x4 s = *reinterpret_cast<const f32x4*>(src + c * per_col);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(s[i] - st.x + kLog2P), st.y, w[i]);
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_fmaf(__builtin_amdgcn_exp2f(s[i] - st.x), st.y, w[i]);
+      }
+    }
   }
+  if (key >= kvl) return;
   const int32_t pg = p.page_table[(int64_t)b * p.max_pages + (key >> 6)];
   float* dst = p.cache.weights + kv4_row(pg, p.h_kv, hk) * kPage + (key & (kPage - 1));
 #pragma unroll
@@ -343,7 +372,16 @@ __global__ __launch_bounds__(256) void kv4_weights_kernel(Kv4AttnParams p) {
     if (key + i < kvl) dst[i] += w[i];
 }
 
-}  // namespace
+// Grid x: the blocks of rows, then with weights those of keys per KV head; y: sequences.
+template <int WAVES, bool WEIGHTS>
+__global__ __launch_bounds__(256) void kv4_decode_finish_kernel(Kv4AttnParams p) {
+  const int b = blockIdx.y, kvl = p.kv_len[b];
+  const int rows = p.q_tokens * p.h_q, blocks = WAVES > 1 ? rows : (rows + 3) / 4;
+  const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
+  const int x = blockIdx.x;
+  if (!WEIGHTS || x < blocks) merge_rows<WAVES>(p, b, x, tiles);
+  else add_weights(p, b, (x - blocks) % p.h_kv, (x - blocks) / p.h_kv, tiles);
+}
 
 template <int COLS, bool WEIGHTS>
 void launch_partitions(const Kv4AttnParams& p, hipStream_t stream) {
@@ -356,17 +394,20 @@ void launch_partitions(const Kv4AttnParams& p, hipStream_t stream) {
     kv4_decode_kernel<COLS, WEIGHTS, false><<<dim3((unsigned)groups, p.h_kv, p.batch), 64 * kDecodeWaves, 0, stream>>>(p);
 }
 
+}  // namespace
+
 hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream) {
   const bool wide = kv4_wide_columns(p.q_tokens * (p.h_q / p.h_kv));
   if (p.scores) wide ? launch_partitions<32, true>(p, stream) : launch_partitions<16, true>(p, stream);
   else wide ? launch_partitions<32, false>(p, stream) : launch_partitions<16, false>(p, stream);
-  const int rows = p.q_tokens * p.h_q;
-  if (p.max_partitions > kManyPartitions) kv4_decode_merge_kernel<4><<<dim3(rows, p.batch), 256, 0, stream>>>(p);
-  else kv4_decode_merge_kernel<1><<<dim3((rows + 3) / 4, p.batch), 256, 0, stream>>>(p);
-  if (p.scores) {
-    const int64_t keys = (int64_t)p.max_partitions * p.partition_tiles * kTile;
-    kv4_weights_kernel<<<dim3((unsigned)((keys + 1023) / 1024), p.h_kv, p.batch), 256, 0, stream>>>(p);
-  }
+  const bool many = p.max_partitions > kManyPartitions;
+  const int64_t rows = (int64_t)p.q_tokens * p.h_q, keys = (int64_t)p.max_partitions * p.partition_tiles * kTile;
+  const int64_t blocks = (many ? rows : (rows + 3) / 4) + (p.scores ? (keys + kWeightKeys - 1) / kWeightKeys * p.h_kv : 0);
+  const dim3 grid((unsigned)blocks, p.batch);
+  if (p.scores && many) kv4_decode_finish_kernel<4, true><<<grid, 256, 0, stream>>>(p);
+  else if (p.scores) kv4_decode_finish_kernel<1, true><<<grid, 256, 0, stream>>>(p);
+  else if (many) kv4_decode_finish_kernel<4, false><<<grid, 256, 0, stream>>>(p);
+  else kv4_decode_finish_kernel<1, false><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 

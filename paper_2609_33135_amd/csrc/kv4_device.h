@@ -64,10 +64,9 @@ __device__ __forceinline__ float q_amax(u32x4 w) {
 // by WAVES waves: M is the
 // largest m, L = sum f l, O = sum f O with f = 2^(m - M); wave w sums partitions w, w +
 // WAVES, .. in order, the waves' sums add in order.  The row is O / L * tv, or 0 where
-// nothing was visible.  Lane l owns channels 2l and 2l + 1.  stats (or null) receives M and
-// 1 / L.
+// nothing was visible.  Lane l owns channels 2l and 2l + 1.
 template <int WAVES>
-__device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, int np, float tv, uint16_t* out, float* stats) {
+__device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, int np, float tv, uint16_t* out) {
   __shared__ float part[WAVES][kKv4State];
   const int lane = threadIdx.x & 63, wave = WAVES > 1 ? threadIdx.x >> 6 : 0;
   float M = -INFINITY;
@@ -110,10 +109,6 @@ __device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, i
   const float inv = L > 0.0f ? __frcp_rn(L) : 0.0f;
   const uint32_t lo = bf16_rne(o0 * inv * tv), hi = bf16_rne(o1 * inv * tv);
   *reinterpret_cast<uint32_t*>(out + 2 * lane) = lo | (hi << 16);
-  if (stats && lane == 0) {
-    stats[0] = M;
-    stats[1] = inv;
-  }
 }
 
 }  // namespace

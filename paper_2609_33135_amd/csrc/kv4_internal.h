@@ -64,7 +64,6 @@ struct Kv4AttnParams {
   uint16_t* out;
   const mpfa_kv4_item* items;            // prefill: the plan, or null
   float* states;                         // decode [row][h_q][max_partitions][130], prefill [state][h_kv][rows][130]
-  float* stats;                          // weights: [row][h_q][2]: the merged M and 1 / l
   float* scores;                         // weights: [b][h_kv][q_tokens * G][max_partitions * partition tokens]
 };
 

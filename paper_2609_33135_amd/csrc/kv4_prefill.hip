@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256) void kv4_prefill_merge_kernel(Kv4AttnParams p)
   if (r >= tm * grp || tok >= nq) return;
   const int64_t one = state_floats(p.half);
   kv4_merge_row<1>(p.states + ((int64_t)x.state * p.h_kv + hk) * one + (int64_t)r * kKv4State, one * p.h_kv, x.parts,
-                   p.v_tscale[x.seq * p.h_kv + hk], p.out + ((int64_t)(q0 + tok) * p.h_q + hk * grp + r % grp) * kD, nullptr);
+                   p.v_tscale[x.seq * p.h_kv + hk], p.out + ((int64_t)(q0 + tok) * p.h_q + hk * grp + r % grp) * kD);
 }
 
 }  // namespace

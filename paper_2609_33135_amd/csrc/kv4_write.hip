@@ -14,6 +14,12 @@ namespace mpfa {
 namespace {
 
 constexpr int64_t kLastLevelCache = (int64_t)256 << 20;
+// Where every workgroup of the write pass reads the partials of its sequence itself: up to so
+// many of them, and so many reads of one by all workgroups (2 KB each, from L2).  One launch
+// less: 777 tokens, 8 heads, 12.1 us, 14.9 not; one prompt of 4000 18.7 and 20.5; but four of
+// 4000, 128000 reads, 50.8 and 48.0.
+constexpr int kFusedPartials = 32;
+constexpr int64_t kFusedReads = 50000;
 constexpr int kWriteTokens = 32;   // tokens per workgroup: eight per wave, eight lanes (groups of 16) each
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
@@ -116,62 +122,87 @@ __global__ __launch_bounds__(256) void kv4_stats_kernel(Kv4WriteParams p) {
   if (t == 0) o.v[0] = fmaxf(fmaxf(s_v[0], s_v[1]), fmaxf(s_v[2], s_v[3]));
 }
 
-// The partials of one (sequence, KV head): means and tensor scales.  128 lanes hold the
-// channels, eight of them share the blocks.
-__global__ __launch_bounds__(1024) void kv4_stats_final_kernel(Kv4WriteParams p) {
-  __shared__ double s_sum[8][kD];
-  __shared__ float s_mx[8][kD], s_mn[8][kD], s_v[16], s_k[2];
-  const int b = blockIdx.y, hk = blockIdx.x, c = threadIdx.x & (kD - 1), part = threadIdx.x >> 7;
-  const int64_t t0 = p.cu_seqlens[b];
-  const int n = p.cu_seqlens[b + 1] - (int)t0;
-  if (n <= 0) return;   // no tokens: the statistics stay as they are
+// What the partials of a (sequence, KV head) come to: the means (BF16, in LDS) and the
+// tensor scales, by a workgroup of PARTS x 128 threads: 128 lanes hold the channels, PARTS of
+// them share the blocks.
+template <int PARTS>
+struct StatSmem {
+  double sum[PARTS][kD];
+  float mx[PARTS][kD], mn[PARTS][kD], v[2 * PARTS], k[2], scale[2];
+  __attribute__((aligned(16))) uint16_t mean[kD];
+};
+
+template <int PARTS>
+__device__ __forceinline__ void finish_stats(const Kv4WriteParams& p, StatSmem<PARTS>& sm, int b, int hk, int64_t t0, int n) {
+  const int c = threadIdx.x & (kD - 1), part = threadIdx.x >> 7;
   const int nblk = (n + p.stat_tokens - 1) / p.stat_tokens;
   constexpr int kAhead = 8;
   double sum = 0.0;
   float mx = -INFINITY, mn = INFINITY, va = 0.0f;
-  for (int blk0 = part; blk0 < nblk; blk0 += 8 * kAhead) {   // past the last block it again, without its sum
+  for (int blk = threadIdx.x; blk < nblk; blk += PARTS * kD) va = fmaxf(va, stat_ptrs(stat_block(p, t0, b, blk, hk)).v[0]);
+  for (int blk0 = part; blk0 < nblk; blk0 += PARTS * kAhead) {   // past the last block it again, without its sum
     double sums[kAhead];
     float mxs[kAhead], mns[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const StatPtrs s = stat_ptrs(stat_block(p, t0, b, min(blk0 + 8 * i, nblk - 1), hk));
+      const StatPtrs s = stat_ptrs(stat_block(p, t0, b, min(blk0 + PARTS * i, nblk - 1), hk));
       sums[i] = s.sum[c];
       mxs[i] = s.mx[c];
       mns[i] = s.mn[c];
     }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      sum += blk0 + 8 * i < nblk ? sums[i] : 0.0;
+      sum += blk0 + PARTS * i < nblk ? sums[i] : 0.0;
       mx = fmaxf(mx, mxs[i]);
       mn = fminf(mn, mns[i]);
     }
   }
-  for (int blk = threadIdx.x; blk < nblk; blk += 1024) va = fmaxf(va, stat_ptrs(stat_block(p, t0, b, blk, hk)).v[0]);
   for (int off = 32; off >= 1; off >>= 1) va = fmaxf(va, __shfl_xor(va, off));
-  s_sum[part][c] = sum;
-  s_mx[part][c] = mx;
-  s_mn[part][c] = mn;
-  if ((threadIdx.x & 63) == 0) s_v[threadIdx.x >> 6] = va;
+  sm.sum[part][c] = sum;
+  sm.mx[part][c] = mx;
+  sm.mn[part][c] = mn;
+  if ((threadIdx.x & 63) == 0) sm.v[threadIdx.x >> 6] = va;
   __syncthreads();
   if (threadIdx.x < kD) {
-    for (int i = 1; i < 8; ++i) {
-      sum += s_sum[i][c];
-      mx = fmaxf(mx, s_mx[i][c]);
-      mn = fminf(mn, s_mn[i][c]);
+    for (int i = 1; i < PARTS; ++i) {
+      sum += sm.sum[i][c];
+      mx = fmaxf(mx, sm.mx[i][c]);
+      mn = fminf(mn, sm.mn[i][c]);
     }
-    const uint16_t m = p.smooth ? bf16_rne((float)(sum / (double)n)) : 0;
-    p.k_mean[((int64_t)b * p.h_kv + hk) * kD + c] = m;
-    const float mean = bf16_to_f32(m);
+    sm.mean[c] = p.smooth ? bf16_rne((float)(sum / (double)n)) : 0;
+    const float mean = bf16_to_f32(sm.mean[c]);
     float a = fmaxf(__builtin_fabsf(mx - mean), __builtin_fabsf(mn - mean));
     for (int off = 32; off >= 1; off >>= 1) a = fmaxf(a, __shfl_xor(a, off));
-    if ((threadIdx.x & 63) == 0) s_k[threadIdx.x >> 6] = a;
+    if ((threadIdx.x & 63) == 0) sm.k[threadIdx.x >> 6] = a;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 16; ++i) va = fmaxf(va, s_v[i]);
-    p.k_tscale[b * p.h_kv + hk] = tensor_scale(fmaxf(s_k[0], s_k[1]));
-    p.v_tscale[b * p.h_kv + hk] = tensor_scale(va);
+    for (int i = 0; i < 2 * PARTS; ++i) va = fmaxf(va, sm.v[i]);
+    sm.scale[0] = tensor_scale(fmaxf(sm.k[0], sm.k[1]));
+    sm.scale[1] = tensor_scale(va);
   }
+  __syncthreads();
+}
+
+template <int PARTS>
+__device__ __forceinline__ void store_stats(const Kv4WriteParams& p, const StatSmem<PARTS>& sm, int b, int hk) {
+  const int at = b * p.h_kv + hk;
+  if (threadIdx.x < kD) p.k_mean[(int64_t)at * kD + threadIdx.x] = sm.mean[threadIdx.x];
+  if (threadIdx.x == 0) {
+    p.k_tscale[at] = sm.scale[0];
+    p.v_tscale[at] = sm.scale[1];
+  }
+}
+
+// Sequences without tokens keep their statistics.
+__global__ __launch_bounds__(1024) void kv4_stats_final_kernel(Kv4WriteParams p) {
+  __shared__ StatSmem<8> sm;
+  const int b = blockIdx.y, hk = blockIdx.x;
+  const int64_t t0 = p.cu_seqlens[b];
+  const int n = p.cu_seqlens[b + 1] - (int)t0;
+  if (n <= 0) return;
+  finish_stats(p, sm, b, hk, t0, n);
+  store_stats(p, sm, b, hk);
 }
 
 // One group of 16 values: codes of channels 0..7 and 8..15, and the scale byte.
@@ -244,26 +275,36 @@ __device__ __forceinline__ void load_group(const uint16_t* src, float* x) {
   }
 }
 
+// FUSED: every workgroup finishes the statistics itself (see kFusedPartials) and the first of each (sequence, KV head) stores them.
+template <bool FUSED>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4WriteParams p) {
-  const int b = blockIdx.z, hk = blockIdx.y;
+  const int b = blockIdx.z, hk = blockIdx.y, first = blockIdx.x * kWriteTokens;
   const int64_t t0 = p.cu_seqlens[b];
   const int n = p.cu_seqlens[b + 1] - (int)t0;
-  const int g = threadIdx.x & 7, i = blockIdx.x * kWriteTokens + (threadIdx.x >> 3);
-  if (i >= n) return;
-  const int64_t t = t0 + i;
+  if (first >= n) return;
+  const int g = threadIdx.x & 7, i = first + (threadIdx.x >> 3);
+  const int64_t t = t0 + min(i, n - 1);
   const int64_t slot = p.slot_mapping[t];
-  float k[16], v[16], m[16];
+  float k[16], v[16], m[16], tk, tv;
   load_group(p.k + t * p.k_stride + hk * kD + 16 * g, k);
   load_group(p.v + t * p.v_stride + hk * kD + 16 * g, v);
-  const float tk = p.k_tscale[b * p.h_kv + hk], tv = p.v_tscale[b * p.h_kv + hk];
-  const int ek = -ilog2f(tk), ev = -ilog2f(tv);
-  if (p.smooth) {
-    load_group(p.k_mean + ((int64_t)b * p.h_kv + hk) * kD + 16 * g, m);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) k[e] -= m[e];
+  if (FUSED) {
+    __shared__ StatSmem<2> sm;
+    finish_stats(p, sm, b, hk, t0, n);
+    if (first == 0) store_stats(p, sm, b, hk);
+    load_group(sm.mean + 16 * g, m);
+    tk = sm.scale[0];
+    tv = sm.scale[1];
+  } else {
+    if (p.smooth) load_group(p.k_mean + ((int64_t)b * p.h_kv + hk) * kD + 16 * g, m);
+    tk = p.k_tscale[b * p.h_kv + hk];
+    tv = p.v_tscale[b * p.h_kv + hk];
   }
+  if (i >= n) return;
+  const int ek = -ilog2f(tk), ev = -ilog2f(tv);
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
+    if (p.smooth) k[e] -= m[e];
     k[e] = __builtin_ldexpf(k[e], ek);
     v[e] = __builtin_ldexpf(v[e], ev);
   }
@@ -288,15 +329,22 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4WriteParams p) {
 
 hipError_t launch_kv4_write(const Kv4WriteParams& p, hipStream_t stream) {
   if (p.total_tokens == 0 || p.max_seqlen == 0) return hipSuccess;
-  if (p.compute_stats) {
-    const int blocks = (p.max_seqlen + p.stat_tokens - 1) / p.stat_tokens;
-    const dim3 grid(blocks, p.h_kv, p.batch);
-    if ((int64_t)p.total_tokens * p.h_kv * kD * 4 >= kLastLevelCache) kv4_stats_kernel<true><<<grid, 256, 0, stream>>>(p);
-    else kv4_stats_kernel<false><<<grid, 256, 0, stream>>>(p);
-    kv4_stats_final_kernel<<<dim3(p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  const dim3 chunks((p.max_seqlen + kWriteTokens - 1) / kWriteTokens, p.h_kv, p.batch);
+  if (!p.compute_stats) {
+    kv4_write_kernel<false><<<chunks, 256, 0, stream>>>(p);
+    return hipGetLastError();
   }
-  const int chunks = (p.max_seqlen + kWriteTokens - 1) / kWriteTokens;
-  kv4_write_kernel<<<dim3(chunks, p.h_kv, p.batch), 256, 0, stream>>>(p);
+  const int blocks = (p.max_seqlen + p.stat_tokens - 1) / p.stat_tokens;
+  const dim3 grid(blocks, p.h_kv, p.batch);
+  if ((int64_t)p.total_tokens * p.h_kv * kD * 4 >= kLastLevelCache) kv4_stats_kernel<true><<<grid, 256, 0, stream>>>(p);
+  else kv4_stats_kernel<false><<<grid, 256, 0, stream>>>(p);
+  const int64_t reads = (int64_t)p.total_tokens / kWriteTokens * p.h_kv * blocks;
+  if (blocks <= kFusedPartials && reads <= kFusedReads) {
+    kv4_write_kernel<true><<<chunks, 256, 0, stream>>>(p);
+  } else {
+    kv4_stats_final_kernel<<<dim3(p.h_kv, p.batch), 1024, 0, stream>>>(p);
+    kv4_write_kernel<false><<<chunks, 256, 0, stream>>>(p);
+  }
   return hipGetLastError();
 }
 

@@ -121,7 +121,7 @@ def test_decode_workspace(mp):
     states = 2 * 8 * 2 * 130 * 4
     for ws, size in ((None, states), (0x1000, states - 1), (0x1008, 1 << 30)):
         assert mp.lib().mpfa_kv4_decode(C.byref(_decode(mp)), ws, size, None) == WORKSPACE
-    with_scores = (states + 255) // 256 * 256 + 256 + 2 * 8 * 2 * 128 * 4
+    with_scores = (states + 255) // 256 * 256 + 2 * 8 * 2 * 128 * 4
     assert mp.lib().mpfa_kv4_decode(C.byref(_decode(mp, flags=512)), 0x1000, with_scores - 1, None) == WORKSPACE
     assert mp.lib().mpfa_kv4_decode(None, 0x1000, 1 << 30, None) == INVALID
 
@@ -207,7 +207,7 @@ def test_decode_plan_covers_the_visible_tiles(mp, kv, q_tokens, window, sinks):
     most = max(_visible_tiles(n - q_tokens, n - 1, window, sinks) for n in kv)
     assert maxp * part >= most * 128 and (maxp - 1) * part < max(most, 1) * 128
     rows = len(kv) * q_tokens * 8
-    assert size >= rows * (maxp * 130 + 2 + maxp * part) * 4
+    assert size >= rows * (maxp * 130 + maxp * part) * 4
 
 
 @pytest.mark.parametrize("rows,kv,h_q,h_kv,window,sinks", [
