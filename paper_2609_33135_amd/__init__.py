@@ -366,6 +366,8 @@ def _want(ok, what):
 def _call(name, dev, stream, *args):
     """The library call on the tensors' device (made current for it) and its current stream."""
     import torch
+    if dev < 0:
+        raise ValueError(f"{name}: tensors on a GPU are wanted")
     if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             return _check(getattr(lib(), name)(*args, _stream(stream)), name)

@@ -21,6 +21,7 @@ namespace {
 constexpr int kMaxKvHeads = 32;
 constexpr int kFar = 1 << 30;   // windows and sinks from here on see every key there can be
 constexpr float kLambda = 0.12751743074173085f;   // log2(e) / sqrt(128)
+constexpr int kMostTokens = 1 << 28;   // of one call: its grids stay below 2^32 threads
 constexpr int64_t kMaxStride = (int64_t)1 << 31;  // elements between tokens
 
 mpfa_status dim_ok(int head_dim) {
@@ -330,7 +331,7 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* a, void* workspace, size_t
     return MPFA_ERR_INVALID;
   if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->k_mean) || !aligned16(a->k_out) || !aligned16(a->v_out))
     return MPFA_ERR_INVALID;
-  if (a->batch > 65535) return MPFA_ERR_UNSUPPORTED;
+  if (a->batch > 65535 || a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
   if (stats) {
     size_t need = 0;
     if (mpfa_kv4_write_workspace_size(a->batch, a->total_tokens, a->h_kv, &need) != MPFA_OK) return MPFA_ERR_INVALID;
@@ -339,7 +340,7 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* a, void* workspace, size_t
   mpfa::Kv4WriteParams p{};
   p.batch = a->batch;
   p.total_tokens = a->total_tokens;
-  p.max_seqlen = a->max_seqlen;
+  p.max_seqlen = std::min(a->max_seqlen, a->total_tokens);
   p.h_kv = a->h_kv;
   p.smooth = smooth;
   p.compute_stats = stats;
@@ -459,7 +460,8 @@ mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* a, void* workspace, size_
   if (a->q_tokens != 0 || a->max_seqlen_q < 0 || a->total_tokens < 0 || a->flags) return MPFA_ERR_INVALID;
   if (a->total_tokens == 0) return MPFA_OK;
   if (!a->cu_seqlens_q || !a->q_start) return MPFA_ERR_INVALID;
-  p.max_seqlen_q = a->max_seqlen_q;
+  if (a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
+  p.max_seqlen_q = std::min(a->max_seqlen_q, a->total_tokens);
   if (a->items) {
     if (a->n_items < 1 || a->n_merges < 0 || a->n_merges > a->n_items || a->n_states < 0 || a->n_states > a->n_items ||
         (a->half != 0 && a->half != 1))
@@ -475,7 +477,7 @@ mpfa_status mpfa_kv4_prefill(const mpfa_kv4_attn_args* a, void* workspace, size_
     p.states = static_cast<float*>(workspace);
   } else {
     const int tm = item_tokens(a->h_q / a->h_kv, 0);
-    const int64_t items = ((int64_t)a->max_seqlen_q + tm - 1) / tm * a->h_kv * a->batch;
+    const int64_t items = ((int64_t)p.max_seqlen_q + tm - 1) / tm * a->h_kv * a->batch;
     if (items > (int64_t)UINT32_MAX / 512) return MPFA_ERR_UNSUPPORTED;
   }
 #ifdef MPFA_DEBUG_CHECKS
@@ -535,7 +537,8 @@ mpfa_status mpfa_kv4_decode(const mpfa_kv4_attn_args* a, void* workspace, size_t
   if (a->q_tokens < 1 || a->q_tokens > 65535 || a->partition_tokens < 1 || a->max_partitions < 1) return MPFA_ERR_INVALID;
   if (weights && !a->cache.weights) return MPFA_ERR_INVALID;
   p.q_tokens = a->q_tokens;
-  if ((int64_t)a->q_tokens * a->h_q > 65535 * 16) return MPFA_ERR_UNSUPPORTED;
+  // partitions times column chunks: their grid stays below 2^32 threads
+  if ((int64_t)a->max_partitions * (((int64_t)a->q_tokens * (a->h_q / a->h_kv) + 15) / 16) > (1 << 24)) return MPFA_ERR_UNSUPPORTED;
   if ((int64_t)a->max_partitions * a->partition_tokens > ((int64_t)1 << 30)) return MPFA_ERR_UNSUPPORTED;
   DecodeSpace s;
   if (!decode_space(a->batch, a->h_q, a->q_tokens, a->partition_tokens, a->max_partitions, weights, &s)) return MPFA_ERR_INVALID;

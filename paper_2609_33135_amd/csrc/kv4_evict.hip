@@ -269,9 +269,9 @@ __global__ __launch_bounds__(1024) void kv4_move_kernel(Kv4EvictParams p) {
 
 hipError_t launch_kv4_evict(const Kv4EvictParams& p, hipStream_t stream) {
   kv4_select_kernel<<<dim3(p.h_kv, p.batch), kSelectThreads, 0, stream>>>(p);
-  const int steps = (p.budget + kMoveChunk - 1) / kMoveChunk;
+  const int steps = (int)(((int64_t)p.budget + kMoveChunk - 1) / kMoveChunk);
   if (p.in_place) kv4_move_kernel<true><<<dim3(1, 2 * p.h_kv, p.batch), 1024, 0, stream>>>(p);
-  else kv4_move_kernel<false><<<dim3(steps, p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  else kv4_move_kernel<false><<<dim3(min(steps, 4096), p.h_kv, p.batch), 1024, 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -120,6 +120,24 @@ def test_write(mp, lens, h_kv, first, smooth):
     assert (w[used] == 0).all() and (w[~used] == 7).all()
 
 
+@pytest.mark.parametrize("lens,h_kv", [([33000, 1, 500], 1), ([16400, 0, 16399, 7], 2), ([65537], 8)])
+def test_write_long_prompts(mp, lens, h_kv):
+    """Larger statistics partials, and reads past the caches."""
+    print(f"write {lens} x {h_kv}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(h_kv)
+    T, B = sum(lens), len(lens)
+    rows = R.page_rows(lens, sum(-(-n // PAGE) for n in lens) + 2, 3)
+    k = (torch.randn(T, h_kv, D, generator=gen, device="cuda") + 2 * torch.randn(1, h_kv, D, generator=gen, device="cuda")).bfloat16()
+    v = torch.randn(T, h_kv, D, generator=gen, device="cuda").bfloat16()
+    cache, stats, cu = mp.PagedCache4(int(rows.max()) + 1, h_kv), mp.SeqStats4(B, h_kv), cumulative(lens)
+    before = [x.clone() for x in (stats.k_mean, stats.k_tscale)]
+    ws = torch.full((mp.kv4_write_workspace_size(B, T, h_kv),), 255, dtype=torch.uint8, device="cuda")
+    mp.kv4_write(k, v, cu, slots_of(rows, [0] * B, lens), cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, max(lens), workspace=ws)
+    torch.cuda.synchronize()
+    check_stats(stats, before, lens, k, v, True, cu)
+    check_write(mp, cache, rows, [0] * B, lens, k, v, stats, True, cu)
+
+
 def test_write_slices_of_a_fused_projection_and_padded_tokens(mp):
     print("write: strided K and V, padded slots", flush=True)
     T, h_kv = 77, 2
@@ -498,3 +516,85 @@ def test_evict_long_sequences_and_lengths_written_in_place(mp, in_place):
             assert kept[b, h, :new[b]].tolist() == want.tolist(), f"sequence {b} head {h}"
             for x, y in zip(got, src[b]):
                 assert torch.equal(x[:, h], y[want.cuda(), h])
+
+
+# ------------------------------------------------------------------ far pages, many sequences
+def test_pages_past_32_bits_of_bytes(mp):
+    """Pages whose code bytes lie past 4 GiB of their plane, through all four operators."""
+    print("pages past 4 GiB", flush=True)
+    h_q, h_kv, kv, pages = 16, 8, [300, 70], 140000
+    assert pages * h_kv * 4096 > 1 << 32
+    cache, stats = mp.PagedCache4(pages, h_kv, weights=True), mp.SeqStats4(2, h_kv)
+    rows = torch.full((2, 6), -1, dtype=torch.int32)
+    rows[0, :5] = torch.tensor([139999, 3, 139000, 131072, 138888], dtype=torch.int32)
+    rows[1, :2] = torch.tensor([139998, 131071], dtype=torch.int32)
+    cu, T = cumulative(kv), sum(kv)
+    k, v = torch.randn(T, h_kv, D, device="cuda").bfloat16(), torch.randn(T, h_kv, D, device="cuda").bfloat16()
+    ws = torch.empty(mp.kv4_write_workspace_size(2, T, h_kv), dtype=torch.uint8, device="cuda")
+    mp.kv4_write(k, v, cu, slots_of(rows, [0, 0], kv), cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, 300, workspace=ws)
+    torch.cuda.synchronize()
+    check_write(mp, cache, rows, [0, 0], kv, k, v, stats, True, cu)
+    q = torch.randn(T, h_q, D, device="cuda").bfloat16()
+    out = torch.full_like(q, math.nan)
+    mp.kv4_prefill(q, cache, stats, cu, i32([0, 0]), i32(kv), rows.cuda(), out, mp.kv4_prefill_plan(kv, kv, h_q, h_kv))
+    torch.cuda.synchronize()
+    check_prefill(q, out, rows, cache, stats, kv, [0, 0], 0, 0)
+    last = q[[299, 369]].contiguous()
+    dec = torch.full_like(last, math.nan)
+    mp.kv4_decode(last, cache, stats, i32(kv), rows.cuda(), dec, mp.kv4_decode_plan(kv, h_q, h_kv, weights=True))
+    torch.cuda.synchronize()
+    for b, n in enumerate(kv):
+        toks = R.Tokens(cache, rows[b].cuda(), n)
+        want, tol, share, stol = R.attention(last[b:b + 1], toks, stats.k_tscale[b], stats.v_tscale[b], n - 1, 0, 0)
+        check_rows(dec[b:b + 1], want, tol, f"sequence {b}")
+        assert ((toks.weights.double() - share).abs() <= stol + 2.0 ** -24 * share).all()
+    src = [snapshot(cache, rows[b], n) for b, n in enumerate(kv)]
+    dst = i32([[139990, 139991], [5, 139992]])
+    kept, new_len = torch.empty(2, h_kv, 100, dtype=torch.int32, device="cuda"), i32([0, 0])
+    mp.kv4_evict(cache, i32(kv), rows.cuda(), dst, 100, kept, new_len)
+    torch.cuda.synchronize()
+    for b, n in enumerate(kv):
+        got = snapshot(cache, dst[b].cpu(), min(n, 100))
+        for h in range(h_kv):
+            idx = torch.tensor(R.keep(src[b][4][:, h].cpu(), 100, 0, 0), device="cuda")
+            assert all(torch.equal(x[:, h], y[idx, h]) for x, y in zip(got, src[b]))
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (64, 2)])
+def test_many_sequences(mp, window, sinks):
+    """More sequences than the packed decode grid looks through."""
+    print(f"600 sequences, window {window}", flush=True)
+    kv = [(i * 37) % 211 for i in range(600)]
+    h_q, h_kv = 4, 2
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [1] * len(kv), 81, weights=True)
+    before = cache.weights.clone()
+    out = torch.full_like(q, math.nan)
+    plan = mp.kv4_decode_plan(kv, h_q, h_kv, 1, window, sinks, weights=True)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    for b in range(0, 600, 7):
+        n = kv[b]
+        toks = R.Tokens(cache, rows[b].cuda(), n)
+        want, tol, share, stol = R.attention(q[b:b + 1], toks, stats.k_tscale[b], stats.v_tscale[b], n - 1, window, sinks)
+        check_rows(out[b:b + 1], want, tol, f"sequence {b}")
+        i = torch.arange(n, device="cuda")
+        w0 = before[rows[b].cuda()[i // PAGE].long(), :, i % PAGE].double()
+        assert ((toks.weights.double() - w0 - share).abs() <= stol + 2.0 ** -24 * (w0 + share)).all()
+
+
+def test_evict_many_sequences(mp):
+    print("evict 600 sequences", flush=True)
+    kv, h_kv, budget = [(i * 37) % 211 for i in range(600)], 2, 50
+    pages = sum(-(-n // PAGE) for n in kv) + 1
+    cache = R.random_cache(mp, pages, h_kv, 91, weights=True)
+    rows = R.page_rows(kv, pages, 9)
+    src = [snapshot(cache, rows[b], n) for b, n in enumerate(kv)]
+    kept, kv_len = torch.empty(600, h_kv, budget, dtype=torch.int32, device="cuda"), i32(kv)
+    mp.kv4_evict(cache, kv_len, rows.cuda(), rows.cuda(), budget, kept, kv_len, sinks=1, recent=9, in_place=True)
+    torch.cuda.synchronize()
+    assert kv_len.tolist() == [min(n, budget) for n in kv]
+    for b in range(0, 600, 5):
+        got = snapshot(cache, rows[b], min(kv[b], budget))
+        for h in range(h_kv):
+            idx = torch.tensor(R.keep(src[b][4][:, h].cpu(), budget, 1, 9), dtype=torch.long, device="cuda")
+            assert all(torch.equal(x[:, h], y[idx, h]) for x, y in zip(got, src[b])), f"sequence {b}"

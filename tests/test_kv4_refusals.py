@@ -60,7 +60,8 @@ BAD_CACHE = [dict(cache={n: v}) for n in PLANES[:4] for v in (None, 0x1008)] + \
     (dict(v_stride=260), INVALID), (dict(k_stride=1 << 31), INVALID), (dict(cu_seqlens=None), INVALID), (dict(k=None), INVALID),
     (dict(v=None), INVALID), (dict(slot_mapping=None), INVALID), (dict(k_mean=None), INVALID), (dict(k_tscale=None), INVALID),
     (dict(v_tscale=None), INVALID), (dict(k=0x1002), INVALID), (dict(v=0x1008), INVALID), (dict(k_out=0x1008), INVALID),
-    (dict(v_out=0x1004), INVALID), (dict(batch=65536), UNSUPPORTED)] + [(c, INVALID) for c in BAD_CACHE])
+    (dict(v_out=0x1004), INVALID), (dict(batch=65536), UNSUPPORTED),
+    (dict(total_tokens=(1 << 28) + 1), UNSUPPORTED)] + [(c, INVALID) for c in BAD_CACHE])
 def test_write(mp, kw, status):
     assert mp.lib().mpfa_kv4_write(C.byref(_write(mp, **kw)), 0x1000, 1 << 40, None) == status
 
@@ -94,7 +95,8 @@ ATTN_BAD = [
     (dict(items=0x1000, n_items=2, n_states=-1), INVALID), (dict(items=0x1000, n_items=2, half=2), INVALID),
     (dict(items=0x1000, n_items=2, half=1, h_q=256, h_kv=1, q_stride=256 * 128), INVALID),
     (dict(items=0x1000, n_items=1 << 22), UNSUPPORTED), (dict(items=0x1000, n_items=70000, n_merges=65536), UNSUPPORTED),
-    (dict(max_seqlen_q=2 ** 31 - 1, batch=65535), UNSUPPORTED)])
+    (dict(total_tokens=1 << 28, max_seqlen_q=2 ** 31 - 1, batch=65535), UNSUPPORTED),
+    (dict(total_tokens=(1 << 28) + 1), UNSUPPORTED)])
 def test_prefill(mp, kw, status):
     assert mp.lib().mpfa_kv4_prefill(C.byref(_attn(mp, **kw)), 0x1000, 1 << 60, None) == status
 
@@ -111,7 +113,7 @@ def test_prefill_workspace(mp, half):
 @pytest.mark.parametrize("kw,status", ATTN_BAD + [
     (dict(flags=1), INVALID), (dict(flags=256), INVALID), (dict(q_tokens=0), INVALID), (dict(q_tokens=-1), INVALID),
     (dict(q_tokens=65536), INVALID), (dict(partition_tokens=0), INVALID), (dict(max_partitions=0), INVALID),
-    (dict(flags=512, cache=dict(weights=None)), INVALID), (dict(q_tokens=65535, h_q=256, h_kv=32, q_stride=256 * 128), UNSUPPORTED),
+    (dict(flags=512, cache=dict(weights=None)), INVALID), (dict(q_tokens=65535, h_q=256, h_kv=32, q_stride=256 * 128, max_partitions=8192), UNSUPPORTED),
     (dict(max_partitions=1 << 24), UNSUPPORTED)])
 def test_decode(mp, kw, status):
     assert mp.lib().mpfa_kv4_decode(C.byref(_decode(mp, **kw)), 0x1000, 1 << 60, None) == status
@@ -293,3 +295,14 @@ def test_binding_refuses_what_it_cannot_pass_on(mp):
         mp.kv4_decode(torch.cat([q, q]), c, s, one, table, torch.empty_like(q), plan)
     with pytest.raises(ValueError):
         mp.kv4_evict(c, one, table, table, 4, torch.zeros(1, 2, 5, **i32), one)
+    # tensors of the right shapes in host memory
+    with pytest.raises(ValueError, match="GPU"):
+        mp.kv4_write(k, k, cu, slots, c, s, 0, 3)
+    with pytest.raises(ValueError, match="GPU"):
+        mp.kv4_decode(q, c, s, one, table, torch.empty_like(q), plan)
+    with pytest.raises(ValueError, match="GPU"):
+        mp.kv4_prefill(q, c, s, torch.tensor([0, 1], **i32), one, one, table, torch.empty_like(q))
+    with pytest.raises(ValueError, match="GPU"):
+        mp.kv4_evict(c, one, table, table, 4, torch.zeros(1, 2, 4, **i32), one)
+    with pytest.raises(AttributeError):
+        c.k_codes = c.v_codes   # the addresses are taken once
