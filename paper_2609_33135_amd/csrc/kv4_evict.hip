@@ -18,11 +18,14 @@
 //
 // Move (kv4_move_kernel): destination place i takes source token kept[i] >= i.  With
 // separate pages the places are shared among workgroups; in place, a workgroup per half of
-// the planes goes through them in order, reading a chunk before it writes it: a later
-// chunk's sources lie at or after its own places, so no write reaches a token that is still
-// to be read.  What bounds it: HBM lines.  A kept token brings the 256-byte V quad and the
-// 128-byte line of K codes that it lies in, about 450 bytes read for 148 where one token
-// in six stays; 24 sequences to 2048 tokens, 8 heads: 48 us, 4.9 TB/s of such lines.
+// the planes, or per quarter of either's codes where there are few, goes through them in
+// order, reading a chunk before it writes it: a later chunk's sources lie at or after its own
+// places, so no write reaches a token that is still to be read.  (The whole call in place,
+// by halves and by quarters: 32768 tokens to 4096, 8 heads, 123 and 57 us; 24 sequences to
+// 2048, 107 and 115, as the quarters read every line more than once.)
+// What bounds it: HBM lines.  A kept token brings the 256-byte V quad and the 128-byte line
+// of K codes that it lies in, about 450 bytes read for 148 where one token in six stays; 24
+// sequences to 2048 tokens, 8 heads: 48 us, about 4.9 TB/s of such lines.
 #include "kv4_device.h"
 
 namespace mpfa {
@@ -35,8 +38,8 @@ constexpr int kLoads = 16;       // pages in flight when they are filled
 constexpr int kAhead = 8;        // pages per step of a sweep
 constexpr int kListed = 256;     // images compared with each other (each thread one)
 constexpr int kColumns = 16;     // histogram columns
-constexpr int kMoveTokens = 4;   // tokens per thread and step of the move (64 at a time, 16 threads each)
-constexpr int kMoveChunk = 64 * kMoveTokens;
+constexpr int kManyHeads = 64;   // (sequence, KV head) pairs from which halves of the planes fill the card
+constexpr int kMoveTokens = 4;   // tokens per thread and step of the move
 static_assert(256 * kColumns == 4 * kSelectThreads, "one 16-byte word of the histogram per thread");
 static_assert(kHeld % kLoads == 0 && kHeld % kAhead == 0 && kHeld <= 64, "whole reads of held pages");
 
@@ -202,30 +205,39 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictPara
   });
 }
 
-// A thread's part of a token: of every plane the piece that `piece` (0 .. 15) names.
+// What a thread moves of a token: a 4-byte piece of K's codes, of V's, or both, with some
+// threads SCALES group scales, and with one the weight.
+template <int SCALES>
 struct Moved {
   uint32_t k, v, w;
-  uint8_t sk, sv;
+  uint8_t sk[SCALES], sv[SCALES];
 };
 
 // Grid x: the workgroups that share the places, or in place one; y: the KV head and, in
-// place, which half of the planes (0: K and the weights, 1: V; both: 2).
-template <bool IN_PLACE>
+// place, the part of the planes, whose workgroups do not depend on each other: K's or V's
+// half (PARTS 2), or a quarter of either's codes (8).  PARTS 1: not in place.
+template <int PARTS>
 __global__ __launch_bounds__(1024) void kv4_move_kernel(Kv4EvictParams p) {
-  const int b = blockIdx.z, piece = threadIdx.x & 15, slot = threadIdx.x >> 4;
-  const int hk = IN_PLACE ? blockIdx.y >> 1 : blockIdx.y;
-  const bool do_k = !IN_PLACE || (blockIdx.y & 1) == 0, do_v = !IN_PLACE || (blockIdx.y & 1) == 1;
+  constexpr bool IN_PLACE = PARTS > 1;
+  constexpr int kPieces = PARTS == 8 ? 4 : 16, kSlots = 1024 / kPieces, kChunk = kSlots * kMoveTokens;
+  constexpr int kScales = PARTS == 8 ? 2 : 1;
+  const int b = blockIdx.z, hk = blockIdx.y / PARTS, part = blockIdx.y % PARTS;
+  const int quarter = PARTS == 8 ? part & 3 : 0;
+  const int local = threadIdx.x & (kPieces - 1), piece = local + kPieces * quarter, slot = threadIdx.x / kPieces;
+  const bool do_k = PARTS == 1 || part < PARTS / 2, do_v = PARTS == 1 || part >= PARTS / 2;
+  const bool scales = PARTS == 8 ? quarter == 0 : local < 8;
+  const bool weight = PARTS == 8 ? part == 0 && local == 0 : local == 8;
   const int n = min(max(p.kv_len[b], 0), p.budget);
   const int32_t* kept = p.kept + ((int64_t)b * p.h_kv + hk) * p.budget;
   const int32_t* src_pt = p.page_table + (int64_t)b * p.max_pages;
   const int32_t* dst_pt = p.dst_page_table + (int64_t)b * p.dst_max_pages;
-  const int steps = (n + kMoveChunk - 1) / kMoveChunk;
+  const int steps = (n + kChunk - 1) / kChunk;
   for (int c = blockIdx.x; c < steps; c += gridDim.x) {
-    Moved m[kMoveTokens] = {};
+    Moved<kScales> m[kMoveTokens] = {};
     bool have[kMoveTokens];
 #pragma unroll
     for (int t = 0; t < kMoveTokens; ++t) {
-      const int i = c * kMoveChunk + t * 64 + slot;
+      const int i = c * kChunk + t * kSlots + slot;
       have[t] = i < n;
       const int s = have[t] ? kept[i] : 0;
       if (IN_PLACE && s == i) have[t] = false;   // it stays where it is
@@ -234,28 +246,40 @@ __global__ __launch_bounds__(1024) void kv4_move_kernel(Kv4EvictParams p) {
       const int64_t row = kv4_row(src_pt[s >> 6], p.h_kv, hk);
       if (do_k) {
         m[t].k = reinterpret_cast<const uint32_t*>(p.cache.k_codes + (row * kPage + o) * 64)[piece];
-        if (piece < 8) m[t].sk = p.cache.k_scales[(row * kPage + o) * 8 + piece];
-        if (piece == 8) m[t].w = __float_as_uint(p.cache.weights[row * kPage + o]);
+        if (scales) {
+#pragma unroll
+          for (int g = 0; g < kScales; ++g) m[t].sk[g] = p.cache.k_scales[(row * kPage + o) * 8 + kScales * local + g];
+        }
+        if (weight) m[t].w = __float_as_uint(p.cache.weights[row * kPage + o]);
       }
       if (do_v) {
         m[t].v = reinterpret_cast<const uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256)[piece * 4 + (o & 3)];
-        if (piece < 8) m[t].sv = p.cache.v_scales[(row * 8 + piece) * kPage + o];
+        if (scales) {
+#pragma unroll
+          for (int g = 0; g < kScales; ++g) m[t].sv[g] = p.cache.v_scales[(row * 8 + kScales * local + g) * kPage + o];
+        }
       }
     }
     if (IN_PLACE) __syncthreads();   // the chunk is read before any of it is written
 #pragma unroll
     for (int t = 0; t < kMoveTokens; ++t) {
       if (!have[t]) continue;
-      const int i = c * kMoveChunk + t * 64 + slot, o = i & (kPage - 1);
+      const int i = c * kChunk + t * kSlots + slot, o = i & (kPage - 1);
       const int64_t row = kv4_row(dst_pt[i >> 6], p.h_kv, hk);
       if (do_k) {
         reinterpret_cast<uint32_t*>(p.cache.k_codes + (row * kPage + o) * 64)[piece] = m[t].k;
-        if (piece < 8) p.cache.k_scales[(row * kPage + o) * 8 + piece] = m[t].sk;
-        if (piece == 8) p.cache.weights[row * kPage + o] = __uint_as_float(m[t].w);
+        if (scales) {
+#pragma unroll
+          for (int g = 0; g < kScales; ++g) p.cache.k_scales[(row * kPage + o) * 8 + kScales * local + g] = m[t].sk[g];
+        }
+        if (weight) p.cache.weights[row * kPage + o] = __uint_as_float(m[t].w);
       }
       if (do_v) {
         reinterpret_cast<uint32_t*>(p.cache.v_codes + (row * 16 + (o >> 2)) * 256)[piece * 4 + (o & 3)] = m[t].v;
-        if (piece < 8) p.cache.v_scales[(row * 8 + piece) * kPage + o] = m[t].sv;
+        if (scales) {
+#pragma unroll
+          for (int g = 0; g < kScales; ++g) p.cache.v_scales[(row * 8 + kScales * local + g) * kPage + o] = m[t].sv[g];
+        }
       }
     }
     if (IN_PLACE) __syncthreads();
@@ -269,9 +293,11 @@ __global__ __launch_bounds__(1024) void kv4_move_kernel(Kv4EvictParams p) {
 
 hipError_t launch_kv4_evict(const Kv4EvictParams& p, hipStream_t stream) {
   kv4_select_kernel<<<dim3(p.h_kv, p.batch), kSelectThreads, 0, stream>>>(p);
-  const int steps = (int)(((int64_t)p.budget + kMoveChunk - 1) / kMoveChunk);
-  if (p.in_place) kv4_move_kernel<true><<<dim3(1, 2 * p.h_kv, p.batch), 1024, 0, stream>>>(p);
-  else kv4_move_kernel<false><<<dim3(min(steps, 4096), p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  constexpr int kChunk = 64 * kMoveTokens;   // places per step, 16 threads each
+  const int steps = (int)(((int64_t)p.budget + kChunk - 1) / kChunk);
+  if (!p.in_place) kv4_move_kernel<1><<<dim3(min(steps, 4096), p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  else if (p.h_kv * p.batch >= kManyHeads) kv4_move_kernel<2><<<dim3(1, 2 * p.h_kv, p.batch), 1024, 0, stream>>>(p);
+  else kv4_move_kernel<8><<<dim3(1, 8 * p.h_kv, p.batch), 1024, 0, stream>>>(p);
   return hipGetLastError();
 }
 
