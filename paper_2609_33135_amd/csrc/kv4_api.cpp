@@ -240,8 +240,12 @@ mpfa_status check_attn(const mpfa_kv4_attn_args* a, bool decode, hipStream_t s) 
   if (!decode && (!to_host(a->cu_seqlens_q, (size_t)a->batch + 1, cu) || !to_host(a->q_start, (size_t)a->batch, qs) ||
                   (a->items && !to_host(a->items, (size_t)a->n_items + a->n_merges, items))))
     return MPFA_ERR_HIP;
+  std::vector<uint8_t> used;   // pages whose weights the call adds to
+  if (decode && (a->flags & MPFA_KV4_WEIGHTS)) used.assign((size_t)a->cache.num_pages, 0);
   for (int b = 0; b < a->batch; ++b) {
     if (kv[b] < 0 || !row_pages_ok(pt, b, a->max_pages, ((int64_t)kv[b] + 63) / 64, a->cache.num_pages)) return MPFA_ERR_DATA;
+    for (int64_t i = 0; !used.empty() && i < ((int64_t)kv[b] + 63) / 64; ++i)
+      if (used[pt[(size_t)b * a->max_pages + i]]++) return MPFA_ERR_DATA;
     if (decode) {
       const int64_t room = (int64_t)a->max_partitions * (a->partition_tokens / MPFA_KV_TILE);
       if (seen_tiles((int64_t)kv[b] - a->q_tokens, kv[b] - 1, a->window, a->sinks) > room) return MPFA_ERR_DATA;

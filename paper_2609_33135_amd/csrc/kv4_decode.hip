@@ -41,8 +41,8 @@ __device__ __forceinline__ int groups_of(const Kv4AttnParams& p, int kvl, int ch
 // Sequence and workgroup of position `pos` in a grid whose first workgroups are the ones
 // with work, sequence by sequence; false past them.  Spread over a grid by sequence, the
 // empty workgroups of the shorter ones take places on the card, and others get two: 16
-// contexts of 10K to 32K keys, 8:2 heads, 23.1 us so, 30.3 before; 32 of
-// 16K to 64K, 32:8, 210 us, 222 before.
+// contexts of 10K to 32K keys, 8:2 heads, 23.1 us so, 30.3 before; 32 of 16K to 64K, 32:8,
+// 210 us, 222 before.
 __device__ __forceinline__ bool find_group(const Kv4AttnParams& p, int pos, int chunks, int& b, int& group) {
   const int lane = threadIdx.x & 63;
   for (int base = 0; base < p.batch; base += 64) {
@@ -130,7 +130,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
     vsc = *reinterpret_cast<const u32x4*>(scales + vs_off);
   };
 
-  const int u0 = 2 * v0, u1 = 2 * v1;
+  // the last tile's second page is left out where the sequence ends before it
+  const int u0 = 2 * v0, u1 = 2 * v1 - (tiles.tile(v1 - 1) * kTile + kPage >= kvl ? 1 : 0);
   load_window(v0);
   step_page(u0);
   load_k();

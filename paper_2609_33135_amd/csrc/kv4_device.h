@@ -69,20 +69,25 @@ template <int WAVES>
 __device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, int np, float tv, uint16_t* out) {
   __shared__ float part[WAVES][kKv4State];
   const int lane = threadIdx.x & 63, wave = WAVES > 1 ? threadIdx.x >> 6 : 0;
-  float M = -INFINITY;
-  for (int q = lane; q < np; q += 64) M = fmaxf(M, st[q * stride]);
-  for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
-  float L = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  if (M > -INFINITY) {
-    constexpr int kAhead = 8;
-    for (int q0 = wave; q0 < np; q0 += kAhead * WAVES) {
-      float2 ml[kAhead], o[kAhead];
+  constexpr int kAhead = 8;
+  float2 ml[kAhead], o[kAhead];
+  auto load = [&](int q0) {   // partitions q0, q0 + WAVES, ..; past the last it again (not used)
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) {
-        const float* s = st + min(q0 + j * WAVES, np - 1) * stride;
-        ml[j] = *reinterpret_cast<const float2*>(s);
-        o[j] = *reinterpret_cast<const float2*>(s + 2 + 2 * lane);
-      }
+    for (int j = 0; j < kAhead; ++j) {
+      const float* s = st + min(q0 + j * WAVES, np - 1) * stride;
+      ml[j] = *reinterpret_cast<const float2*>(s);
+      o[j] = *reinterpret_cast<const float2*>(s + 2 + 2 * lane);
+    }
+  };
+  float M = -INFINITY, L = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  if (np > 0) {
+    load(wave);   // the first ones beside the maxima
+    for (int q = lane; q < np; q += 64) M = fmaxf(M, st[q * stride]);
+    for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off));
+  }
+  if (M > -INFINITY) {
+    for (int q0 = wave; q0 < np; q0 += kAhead * WAVES) {
+      if (q0 > wave) load(q0);
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         const float f = q0 + j * WAVES < np ? __builtin_amdgcn_exp2f(ml[j].x - M) : 0.0f;

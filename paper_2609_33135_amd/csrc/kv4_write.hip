@@ -79,18 +79,22 @@ __global__ __launch_bounds__(256) void kv4_stats_kernel(Kv4WriteParams p) {
       kw[i] = load16(p.k + t * p.k_stride + hk * kD + 8 * c, STREAM);
       vw[i] = load16(p.v + t * p.v_stride + hk * kD + 8 * c, STREAM);
     }
+    auto take = [&](bool whole) {
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const bool mine = tb + 16 * i + row < te;
-      va = fmaxf(va, q_amax(vw[i]));
+      for (int i = 0; i < kRows; ++i) {
+        const bool mine = whole || tb + 16 * i + row < te;
+        va = fmaxf(va, q_amax(vw[i]));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = e & 1 ? bf_hi(kw[i][e >> 1]) : bf_lo(kw[i][e >> 1]);
-        sum[e] += mine ? (double)x : 0.0;
-        mx[e] = fmaxf(mx[e], x);
-        mn[e] = fminf(mn[e], x);
+        for (int e = 0; e < 8; ++e) {
+          const float x = e & 1 ? bf_hi(kw[i][e >> 1]) : bf_lo(kw[i][e >> 1]);
+          sum[e] += mine ? (double)x : 0.0;
+          mx[e] = fmaxf(mx[e], x);
+          mn[e] = fminf(mn[e], x);
+        }
       }
-    }
+    };
+    if (tb + kKv4StatTokens <= te) take(true);   // uniform: no selects
+    else take(false);
   }
   // the four rows of a wave, then the four waves
 #pragma unroll

@@ -225,6 +225,7 @@ def test_debug_library_accepts_the_run_and_refuses_bad_data(mp, monkeypatch):
     refused(dec, kv=s.kv_len - 1000)
     refused(dec, kv=s.kv_len + 1000)
     refused(dec, table=torch.full_like(s.table, -1))
+    refused(dec, table=s.table[:1].repeat(2, 1))   # weights of shared pages
     refused(dec, table=torch.full_like(s.table, s.cache.num_pages))
     bad = s.q.clone()
     bad[0, 0, 0] = math.nan
