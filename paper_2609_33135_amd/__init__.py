@@ -441,7 +441,7 @@ class Kv4Plan:
     def __init__(self, what, workspace, **kw):
         self.what, self.workspace = what, workspace
         self.partition_tokens = self.max_partitions = self.n_items = self.n_merges = self.n_states = self.half = 0
-        self.q_tokens = self.flags = 0
+        self.q_tokens = self.flags = self.max_rows = 0
         self.items = None
         self.__dict__.update(kw)
 
@@ -554,8 +554,9 @@ def _kv4_attn(what, kind, q, cache, stats, cu, q_start, kv_len, page_table, out,
         if plan.what != (kind, batch, h_q, h_kv, window, sinks):
             raise ValueError(f"{what}: the plan was made for another call: {plan.what}")
         cut, ws, items = plan.cut(), plan.workspace, _ptr(plan.items)
-        if ws is not None and ws.get_device() != dev:
-            raise ValueError(f"{what}: the plan is of another device")
+        for t in (ws, plan.items):
+            if t is not None and t.get_device() != dev:
+                raise ValueError(f"{what}: the plan is of another device")
     a = Kv4AttnArgs(batch, h_q, h_kv, HEAD_DIM, page_table.shape[1], shape[0], max_seqlen_q, cut[0], window, sinks, *cut[1:],
                     stride, cu, q_start, items, kv_len.data_ptr(), page_table.data_ptr(), q.data_ptr(), cache._c,
                     stats._at["k_tscale"], stats._at["v_tscale"], out.data_ptr())

@@ -107,6 +107,15 @@ int64_t seen_tiles(int64_t first, int64_t last, int window, int sinks) {
   return mpfa::kv4_tiles((int)std::max<int64_t>(first, 0), (int)last, far(window), far(sinks)).nt;
 }
 
+// Most tiles that the last `q_tokens` of any sequence of at most kv_len keys see: with a
+// window a shorter sequence may lie across one tile more.
+int64_t most_tiles(int64_t kv_len, int64_t q_tokens, int window, int sinks) {
+  const int64_t all = (kv_len + 127) / 128;
+  if (window == 0) return all;
+  const int64_t span = (int64_t)far(window) + q_tokens - 1;   // keys of the window
+  return std::min(all, (std::min<int64_t>(sinks, kv_len) + 127) / 128 + (span + 254) / 128);
+}
+
 // ---- prefill plans
 // tokens per item of 256 rows, or of 128; 0 where a token's heads do not fit
 int item_tokens(int grp, int half) { return (half ? mpfa::kKv4Rows / 2 : mpfa::kKv4Rows) / grp; }
@@ -494,7 +503,7 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
                                  int32_t window, int32_t sinks, uint32_t flags, int32_t num_cus, int32_t* partition_tokens,
                                  int32_t* max_partitions, size_t* workspace_bytes) {
   if (batch < 1 || batch > 65535 || !kv_len_host || !kv_heads_ok(h_kv) || h_q < 1 || h_q > MPFA_MAX_HEADS || h_q % h_kv || q_tokens < 1 ||
-      window < 0 || sinks < 0 || (flags & ~MPFA_KV4_WEIGHTS) || num_cus < 1 || !partition_tokens || !max_partitions ||
+      q_tokens > 65535 || window < 0 || sinks < 0 || (flags & ~MPFA_KV4_WEIGHTS) || num_cus < 1 || !partition_tokens || !max_partitions ||
       !workspace_bytes)
     return MPFA_ERR_INVALID;
   const int64_t cols = (int64_t)q_tokens * (h_q / h_kv), per = mpfa::kv4_wide_columns(cols) ? 32 : 16;
@@ -502,11 +511,13 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
   auto seen = [&](int b) {
     return seen_tiles((int64_t)kv_len_host[b] - q_tokens, (int64_t)kv_len_host[b] - 1, window, sinks);
   };
-  int64_t most = 1;
+  int64_t most = 1, bound = 1;
   for (int b = 0; b < batch; ++b) {
     if (kv_len_host[b] < 0) return MPFA_ERR_INVALID;
     most = std::max(most, seen(b));
+    bound = std::max(bound, most_tiles(kv_len_host[b], q_tokens, window, sinks));
   }
+  if ((double)batch * most * chunks * h_kv > 1e15) return MPFA_ERR_INVALID;   // no workspace is as large
   // A workgroup holds four partitions (waves) of a KV head.  The units of the card take
   // equally many workgroups, rounded up, of `part` tiles and about one tile's time to start
   // and store each: the smallest such sum wins.  (32 contexts of 16K to 64K keys, 32:8 heads:
@@ -524,7 +535,7 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
     }
     if (t >= most) break;   // one partition each: longer ones change nothing
   }
-  const int64_t parts = (most + part - 1) / part;
+  const int64_t parts = (bound + part - 1) / part;
   DecodeSpace s;
   if (!decode_space(batch, h_q, q_tokens, (int)part * MPFA_KV_TILE, (int)parts, flags & MPFA_KV4_WEIGHTS, &s)) return MPFA_ERR_INVALID;
   *partition_tokens = (int32_t)(part * MPFA_KV_TILE);

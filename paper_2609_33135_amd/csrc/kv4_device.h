@@ -61,10 +61,9 @@ __device__ __forceinline__ float q_amax(u32x4 w) {
 }
 
 // Merge of the partition states of one row (query token and head), `stride` floats apart,
-// by WAVES waves: M is the
-// largest m, L = sum f l, O = sum f O with f = 2^(m - M); wave w sums partitions w, w +
-// WAVES, .. in order, the waves' sums add in order.  The row is O / L * tv, or 0 where
-// nothing was visible.  Lane l owns channels 2l and 2l + 1.
+// by WAVES waves: M is the largest m, L = sum f l, O = sum f O with f = 2^(m - M); wave w
+// sums partitions w, w + WAVES, .. in order, the waves' sums add in order.  The row is
+// O / L * tv, or 0 where nothing was visible.  Lane l owns channels 2l and 2l + 1.
 template <int WAVES>
 __device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, int np, float tv, uint16_t* out) {
   __shared__ float part[WAVES][kKv4State];

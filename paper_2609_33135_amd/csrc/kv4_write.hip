@@ -279,7 +279,8 @@ __device__ __forceinline__ void load_group(const uint16_t* src, float* x) {
   }
 }
 
-// FUSED: every workgroup finishes the statistics itself (see kFusedPartials) and the first of each (sequence, KV head) stores them.
+// FUSED: every workgroup finishes the statistics itself (see kFusedPartials) and the first of
+// each (sequence, KV head) stores them.
 template <bool FUSED>
 __global__ __launch_bounds__(256) void kv4_write_kernel(Kv4WriteParams p) {
   const int b = blockIdx.z, hk = blockIdx.y, first = blockIdx.x * kWriteTokens;

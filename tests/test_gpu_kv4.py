@@ -257,6 +257,28 @@ def test_decode_partitions(mp, part):
         check_rows(out[b:b + 1], want, tol, f"sequence {b}")
 
 
+@pytest.mark.parametrize("longest,q_tokens,window,sinks", [(640, 1, 128, 0), (1024, 3, 126, 5), (896, 2, 255, 200), (768, 1, 1, 0)])
+def test_decode_by_a_plan_for_longer_sequences(mp, longest, q_tokens, window, sinks):
+    """Shorter sequences may lie across one tile more than the longest one."""
+    print(f"decode by a plan for {longest} keys, rows {q_tokens} window {window} sinks {sinks}", flush=True)
+    kv, h_q, h_kv = list(range(longest, longest - 260, -13)), 4, 2
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [q_tokens] * len(kv), 17, weights=True)
+    before = cache.weights.clone()
+    plan = mp.kv4_decode_plan([longest] * len(kv), h_q, h_kv, q_tokens, window, sinks, weights=True)
+    plan.workspace.fill_(255)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    for b, n in enumerate(kv):
+        x = slice(b * q_tokens, (b + 1) * q_tokens)
+        toks = R.Tokens(cache, rows[b].cuda(), n)
+        want, tol, share, stol = R.attention(q[x], toks, stats.k_tscale[b], stats.v_tscale[b], n - q_tokens, window, sinks)
+        check_rows(out[x], want, tol, f"sequence of {n}")
+        i = torch.arange(n, device="cuda")
+        w0 = before[rows[b].cuda()[i // PAGE].long(), :, i % PAGE].double()
+        assert ((toks.weights.double() - w0 - share).abs() <= stol + 2.0 ** -24 * (w0 + share)).all()
+
+
 @pytest.mark.parametrize("kv,q_tokens,window,sinks", [([1, 700, 65], 1, 0, 0), ([2000, 0, 130], 3, 200, 70), ([513], 20, 0, 0)])
 def test_decode_weights(mp, kv, q_tokens, window, sinks):
     h_q, h_kv = 10, 2

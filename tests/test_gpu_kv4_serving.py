@@ -246,3 +246,68 @@ def test_debug_library_accepts_the_run_and_refuses_bad_data(mp, monkeypatch):
     refused(evict, s.table.flip(1).contiguous(), True)
     refused(evict, s.table.flip(0).contiguous(), True)
     evict(s.table, True)
+
+
+def test_prompt_and_prefill_in_graphs(mp):
+    """A prompt's write and its prefill, by a plan and in one pass, captured once and replayed on other
+    values with eager work between the replays; rows behind the last sequence stay as they were."""
+    print("prompt in graphs", flush=True)
+    lens, window, sinks = [1500, 3, 260], 600, 7
+    T, B = sum(lens), len(lens)
+    rows = R.page_rows(lens, 32, 4)
+    table, slots, cu, kv = rows.cuda(), slots_of(rows, [0] * B, lens), cumulative(lens), i32(lens)
+    zero = i32([0] * B)
+    bf16 = dict(dtype=torch.bfloat16, device="cuda")
+    q, k, v = torch.empty(T + 9, H_Q, D, **bf16), torch.empty(T, H_KV, D, **bf16), torch.empty(T, H_KV, D, **bf16)
+    made = lambda: (mp.PagedCache4(32, H_KV), mp.SeqStats4(B, H_KV), torch.empty_like(q), torch.empty_like(q))
+    plan = mp.kv4_prefill_plan(lens, lens, H_Q, H_KV, window, sinks)
+    ws = torch.empty(mp.kv4_write_workspace_size(B, T, H_KV), dtype=torch.uint8, device="cuda")
+
+    def run(cache, stats, by_plan, one_pass):
+        mp.kv4_write(k, v, cu, slots, cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, max(lens), workspace=ws)
+        att = dict(window=window, sinks=sinks)
+        mp.kv4_prefill(q, cache, stats, cu, zero, kv, table, by_plan, plan, **att)
+        mp.kv4_prefill(q, cache, stats, cu, zero, kv, table, one_pass, max_seqlen_q=max(lens), **att)
+
+    gen = torch.Generator(device="cuda").manual_seed(12)
+
+    def fill():
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+
+    fill()
+    captured, eager = made(), made()
+    run(*eager)   # warm
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(*captured)
+    for _ in range(4):
+        fill()
+        for x in (captured, eager):
+            for out in x[2:]:
+                out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        run(*eager)
+        torch.cuda.synchronize()
+        for n in ("k_codes", "k_scales", "v_codes", "v_scales"):
+            assert torch.equal(getattr(captured[0], n), getattr(eager[0], n))
+        assert torch.equal(captured[1].k_mean, eager[1].k_mean)
+        for a, b in zip(captured[2:], eager[2:]):
+            assert torch.equal(a, b) and (a[T:] == 7).all()
+    at = 0
+    for b, n in enumerate(lens):
+        want, tol, _, _ = R.attention(q[at:at + n], R.Tokens(eager[0], table[b], n), eager[1].k_tscale[b], eager[1].v_tscale[b], 0,
+                                      window, sinks)
+        for out in captured[2:]:
+            check_rows(out[at:at + n], want, tol, f"prompt {b}")
+        at += n
+
+
+def test_plan_of_another_device_is_refused(mp):
+    s = Server(mp, [200, 70], 320, seed=9)
+    plan = mp.kv4_prefill_plan([1, 1], s.kv, H_Q, H_KV)
+    plan.items, plan.workspace = plan.items.cpu(), None
+    with pytest.raises(ValueError, match="another device"):
+        mp.kv4_prefill(s.q, s.cache, s.stats, s.one, s.kv_len - 1, s.kv_len, s.table, s.out, plan)

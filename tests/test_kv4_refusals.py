@@ -175,7 +175,8 @@ def _prefill_plan(mp, rows, kv, h_q, h_kv, window, sinks, cus=256):
 @pytest.mark.parametrize("args", [
     (0, [1], 8, 2, 1, 0, 0, 0, 256), (1, None, 8, 2, 1, 0, 0, 0, 256), (1, [-1], 8, 2, 1, 0, 0, 0, 256),
     (1, [1], 7, 2, 1, 0, 0, 0, 256), (1, [1], 8, 2, 0, 0, 0, 0, 256), (1, [1], 8, 2, 1, -1, 0, 0, 256),
-    (1, [1], 8, 2, 1, 0, -1, 0, 256), (1, [1], 8, 2, 1, 0, 0, 1, 256), (1, [1], 8, 2, 1, 0, 0, 0, 0)])
+    (1, [1], 8, 2, 1, 0, -1, 0, 256), (1, [1], 8, 2, 1, 0, 0, 1, 256), (1, [1], 8, 2, 1, 0, 0, 0, 0), (1, [1], 8, 2, 65536, 0, 0, 0, 256),
+    (65535, [2 ** 31 - 1] * 65535, 256, 32, 65535, 0, 0, 0, 256)])
 def test_decode_plan_refuses(mp, args):
     assert _plan(mp, "mpfa_kv4_decode_plan", *args)[0] == INVALID
 
@@ -202,11 +203,12 @@ def _visible_tiles(first, last, window, sinks):
 
 @pytest.mark.parametrize("kv,q_tokens,window,sinks", [
     ([1, 129, 5000], 1, 0, 0), ([100000], 1, 1000, 4), ([100000], 8, 1, 300), ([700, 0, 3], 4, 128, 128), ([65536] * 3, 1, 0, 9),
-    ([900], 1, 2 ** 31 - 1, 2 ** 31 - 1)])
+    ([900], 1, 2 ** 31 - 1, 2 ** 31 - 1), ([4096], 1, 128, 0), ([4096, 200], 3, 126, 5), ([640], 1, 130, 513)])
 def test_decode_plan_covers_the_visible_tiles(mp, kv, q_tokens, window, sinks):
     rc, (part, maxp, size) = _plan(mp, "mpfa_kv4_decode_plan", len(kv), kv, 8, 2, q_tokens, window, sinks, 512, 256)
     assert rc == 0 and part % 128 == 0 and maxp >= 1
-    most = max(_visible_tiles(n - q_tokens, n - 1, window, sinks) for n in kv)
+    # of these lengths and of every shorter one (which may lie across one tile more)
+    most = max(_visible_tiles(m - q_tokens, m - 1, window, sinks) for n in kv for m in range(max(n - 128, 0), n + 1))
     assert maxp * part >= most * 128 and (maxp - 1) * part < max(most, 1) * 128
     rows = len(kv) * q_tokens * 8
     assert size >= rows * (maxp * 130 + maxp * part) * 4
@@ -295,6 +297,8 @@ def test_binding_refuses_what_it_cannot_pass_on(mp):
         mp.kv4_decode(torch.cat([q, q]), c, s, one, table, torch.empty_like(q), plan)
     with pytest.raises(ValueError):
         mp.kv4_evict(c, one, table, table, 4, torch.zeros(1, 2, 5, **i32), one)
+    with pytest.raises(ValueError, match="another call"):
+        mp.kv4_prefill(q, c, s, torch.tensor([0, 1], **i32), one, one, table, torch.empty_like(q), plan)   # a decode's plan
     # tensors of the right shapes in host memory
     with pytest.raises(ValueError, match="GPU"):
         mp.kv4_write(k, k, cu, slots, c, s, 0, 3)
