@@ -22,6 +22,7 @@ constexpr int kMaxKvHeads = 32;
 constexpr int kFar = 1 << 30;   // windows and sinks from here on see every key there can be
 constexpr float kLambda = 0.12751743074173085f;   // log2(e) / sqrt(128)
 constexpr int kMostTokens = 1 << 28;   // of one call: its grids stay below 2^32 threads
+constexpr int64_t kMergeTiles = 2;   // time of a decode's second launch, in tiles
 constexpr int64_t kMaxStride = (int64_t)1 << 31;  // elements between tokens
 
 mpfa_status dim_ok(int head_dim) {
@@ -520,15 +521,18 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
   if ((double)batch * most * chunks * h_kv > 1e15) return MPFA_ERR_INVALID;   // no workspace is as large
   // A workgroup holds four partitions (waves) of a KV head.  The units of the card take
   // equally many workgroups, rounded up, of `part` tiles and about one tile's time to start
-  // and store each: the smallest such sum wins.  (32 contexts of 16K to 64K keys, 32:8 heads:
+  // and store each; where a row has more than four there is a launch that merges them: the
+  // smallest such sum wins.  (32 contexts of 16K to 64K keys, 32:8 heads:
   // 10 tiles 222 us, 12 tiles, with a last round of few, 260; 4 of 32K: 8 tiles 35 us, 5
-  // tiles 40, 2 tiles 46; one of 64K, 40:8: 4 tiles 25.5, 3 tiles 32; 64 of 2100: 5 tiles
-  // 38.8, 10 tiles 41.9.)
+  // tiles 40, 2 tiles 46; one of 64K, 40:8: 4 tiles 25.5, 3 tiles 32; one of 1000 or eight:
+  // 2 tiles, four partitions, 9.2 and 9.9, 1 tile 11.3 and 11.1; 16 of 2000: 2 tiles 13.8, 4
+  // tiles, without the merge, 15.0.)
   int64_t part = 1, best = INT64_MAX;
   for (int64_t t = 1; t <= 128; ++t) {
     int64_t groups = 0;
     for (int b = 0; b < batch; ++b) groups += ((seen(b) + t - 1) / t * chunks + 3) / 4 * h_kv;
-    const int64_t cost = (groups + num_cus - 1) / num_cus * (t + 1);
+    const int64_t cost = (groups + num_cus - 1) / num_cus * (t + 1) +
+                         (mpfa::kv4_direct(chunks, (bound + t - 1) / t, flags & MPFA_KV4_WEIGHTS) ? 0 : kMergeTiles);
     if (cost < best) {
       best = cost;
       part = t;

@@ -28,14 +28,37 @@ namespace mpfa {
 
 namespace {
 
-constexpr int kDecodeWaves = 4;
+constexpr int kDecodeWaves = kKv4DecodeWaves;
+
+__device__ __forceinline__ int partitions_of(const Kv4AttnParams& p, const Kv4Tiles& tiles) {
+  return min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
+}
+
+// Where one wave holds all columns of a KV head, the waves of a workgroup have partitions of
+// the same rows and can join them in LDS.  They do where that
+//  - leaves the output itself (four partitions at most), with no launch to merge them: 64
+//    contexts of four rows and 2048 keys, 40:8 heads, 43 us, 54 with it; 64 of 2100, 32:8,
+//    32.3 and 38.7; or
+//  - a fourth of many states: one context of 64K keys, 40:8, 19.6 us, 21.1 not.  (In between
+//    the waves that wait for the others cost more: 4 of 32K, 32:8, 35.4 us, 33.8 not.)
+constexpr int kJoinPartitions = 64;
+__host__ __device__ inline bool direct(const Kv4AttnParams& p, int chunks) {
+  return kv4_direct(chunks, p.max_partitions, p.scores != nullptr);
+}
+__host__ __device__ inline bool joined(const Kv4AttnParams& p, int chunks) {
+  return direct(p, chunks) || (chunks == 1 && !p.scores && p.max_partitions > kJoinPartitions);
+}
+// States per row
+__device__ __forceinline__ int states_of(const Kv4AttnParams& p, const Kv4Tiles& tiles, int chunks) {
+  const int parts = partitions_of(p, tiles);
+  return joined(p, chunks) ? (parts + kDecodeWaves - 1) / kDecodeWaves : parts;
+}
 
 // Workgroups of a sequence of kvl keys for one KV head: partitions times column chunks,
-// four waves each.
+// four waves each; one for the zeros of a sequence without keys where nothing follows.
 __device__ __forceinline__ int groups_of(const Kv4AttnParams& p, int kvl, int chunks) {
-  const int nt = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks).nt;
-  const int parts = min((nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
-  return (parts * chunks + kDecodeWaves - 1) / kDecodeWaves;
+  const int parts = partitions_of(p, kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks));
+  return max((parts * chunks + kDecodeWaves - 1) / kDecodeWaves, direct(p, chunks) ? 1 : 0);
 }
 
 // Sequence and workgroup of position `pos` in a grid whose first workgroups are the ones
@@ -72,7 +95,7 @@ constexpr int kPackedBatch = 512;
 // V).  In steps of one page three waves of 16 columns fit a SIMD, or two of 32; with tiles of
 // two pages two of 16, and 32 spilled (one context of 64K keys, 40:8 heads, 20.8 us, 21.8 so;
 // 16 contexts of 10K to 32K, 8:2 heads, 21.4 and 22.8).
-template <int COLS, bool WEIGHTS, bool PACKED>
+template <int COLS, bool JOIN, bool WEIGHTS, bool PACKED>
 __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_decode_kernel(Kv4AttnParams p) {
   constexpr int kN = COLS / 16;
   const int lane = threadIdx.x & 63, g = lane >> 4, lr = lane & 15;
@@ -89,8 +112,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
   const int part = item / chunks, chunk = item - part * chunks;
   const int kvl = p.kv_len[b];
   const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
-  const int v0 = part * p.partition_tiles, v1 = min(tiles.nt, v0 + p.partition_tiles);
-  if (v0 >= v1 || part >= p.max_partitions) return;
+  const int v0 = part * p.partition_tiles, v1 = part < p.max_partitions ? min(tiles.nt, v0 + p.partition_tiles) : 0;
+  const bool idle = v0 >= v1;
+  if (!JOIN && idle) return;
 
   const int32_t* pt = p.page_table + (int64_t)b * p.max_pages;
   const int npg = (kvl + 63) >> 6;
@@ -132,9 +156,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
 
   // the last tile's second page is left out where the sequence ends before it
   const int u0 = 2 * v0, u1 = 2 * v1 - (tiles.tile(v1 - 1) * kTile + kPage >= kvl ? 1 : 0);
-  load_window(v0);
-  step_page(u0);
-  load_k();
+  if (!idle) {
+    load_window(v0);
+    step_page(u0);
+    load_k();
+  }
 
   // ---- Q: channels 32g .. +31 of the lane's columns, and what they see
   f16x8 qop[kN][4];
@@ -279,23 +305,53 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
       pv(od, std::integral_constant<int, 3>{}, 7);
     }
   }
+  // where a column's state goes: to LDS, or to the workspace
+  __shared__ float joint[JOIN ? kDecodeWaves : 1][JOIN ? COLS : 1][kKv4State];
+  const int64_t row0 = (int64_t)b * p.q_tokens * p.h_q + hk * grp;
+  auto row_of = [&](int col) { return row0 + (int64_t)(col / grp) * p.h_q + col % grp; };
+  auto state_of = [&](int col, int at) { return p.states + (row_of(col) * p.max_partitions + at) * kKv4State; };
+  if (!idle) {
 #pragma unroll
-  for (int n = 0; n < kN; ++n) {
-    // keep the products in full-wave control flow (the store below is under a branch)
+    for (int n = 0; n < kN; ++n) {
+      // keep the products in full-wave control flow (the store below is under a branch)
 #pragma unroll
-    for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(o[n][db]));
-    const float lt = wave_sum16(l[n]);
-    const int col = col_of(n);
-    if (col < cols) {
-      const int tok = col / grp;
-      float* st = p.states + ((((int64_t)b * p.q_tokens + tok) * p.h_q + hk * grp + col - tok * grp) * p.max_partitions + part) * kKv4State;
-      if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m[n] * lam[n], lt);
-      // accumulator row 4g + i of block db is channel 8 (4g + i) + db
+      for (int db = 0; db < 8; ++db) asm volatile("" : "+v"(o[n][db]));
+      const float lt = wave_sum16(l[n]);
+      const int col = col_of(n);
+      if (col < cols) {
+        float* st = JOIN ? joint[threadIdx.x >> 6][col] : state_of(col, part);
+        if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m[n] * lam[n], lt);
+        // accumulator row 4g + i of block db is channel 8 (4g + i) + db
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int db = 0; db < 8; db += 2)
-          *reinterpret_cast<float2*>(st + 2 + 32 * g + 8 * i + db) = make_float2(o[n][db][i], o[n][db + 1][i]);
+          for (int db = 0; db < 8; db += 2)
+            *reinterpret_cast<float2*>(st + 2 + 32 * g + 8 * i + db) = make_float2(o[n][db][i], o[n][db + 1][i]);
+      }
+    }
+  }
+  if (!JOIN) return;
+  __syncthreads();
+  const int live = max(min(partitions_of(p, tiles) - group * kDecodeWaves, kDecodeWaves), 0);
+  const float tv = p.v_tscale[b * p.h_kv + hk];
+  for (int col = threadIdx.x >> 6; col < cols; col += kDecodeWaves) {
+    float M = -INFINITY, L = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    for (int q = 0; q < live; ++q) M = fmaxf(M, joint[q][col][0]);
+    if (M > -INFINITY)
+      for (int q = 0; q < live; ++q) {
+        const float2 ml = *reinterpret_cast<const float2*>(joint[q][col]);
+        const float2 x = *reinterpret_cast<const float2*>(joint[q][col] + 2 + 2 * lane);
+        const float f = __builtin_amdgcn_exp2f(ml.x - M);
+        L = __builtin_fmaf(f, ml.y, L);
+        o0 = __builtin_fmaf(f, x.x, o0);
+        o1 = __builtin_fmaf(f, x.y, o1);
+      }
+    if (direct(p, chunks)) {
+      kv4_store_row(p.out + row_of(col) * kD, L, o0, o1, tv);
+    } else {
+      float* st = state_of(col, group);
+      if (lane == 0) *reinterpret_cast<float2*>(st) = make_float2(M, L);
+      *reinterpret_cast<float2*>(st + 2 + 2 * lane) = make_float2(o0, o1);
     }
   }
 }
@@ -305,30 +361,27 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
 // partitions themselves (a launch of their own after the merge took 4 us more).
 
 // Rows (token, query head): a wave each, four to a workgroup, or a workgroup of four waves
-// each where there are many partitions (a wave keeps eight in flight).
-constexpr int kManyPartitions = 16;
+// each where there are many states (a wave keeps eight in flight).
+constexpr int kManyStates = 16;
 constexpr int kWeightKeys = 1024;   // per workgroup, four per thread
 constexpr int kWeightRows = 64;     // whose maxima and sums are held at a time
 
-__device__ __forceinline__ int partitions_of(const Kv4AttnParams& p, const Kv4Tiles& tiles) {
-  return min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
-}
-
 template <int WAVES>
-__device__ __forceinline__ void merge_rows(const Kv4AttnParams& p, int b, int block, const Kv4Tiles& tiles) {
+__device__ __forceinline__ void merge_rows(const Kv4AttnParams& p, int b, int block, const Kv4Tiles& tiles, int chunks) {
   const int rows = p.q_tokens * p.h_q;
   const int i = WAVES > 1 ? block : __builtin_amdgcn_readfirstlane(block * 4 + (threadIdx.x >> 6));
   if (i >= rows) return;
   const int64_t r = (int64_t)b * rows + i;
-  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, partitions_of(p, tiles),
+  kv4_merge_row<WAVES>(p.states + r * p.max_partitions * kKv4State, kKv4State, states_of(p, tiles, chunks),
                        p.v_tscale[b * p.h_kv + i % p.h_q / (p.h_q / p.h_kv)], p.out + r * kD);
 }
 
 // Adds every visible key's share of the attention, summed over the rows of its KV head in
 // order, to the cache's weights.
-__device__ __forceinline__ void add_weights(const Kv4AttnParams& p, int b, int hk, int block, const Kv4Tiles& tiles) {
+__device__ __forceinline__ void add_weights(const Kv4AttnParams& p, int b, int hk, int block, const Kv4Tiles& tiles,
+                                            int chunks) {
   __shared__ float2 stats[kWeightRows];   // a row's maximum, and 2^15 / its sum (0: it sees nothing)
-  const int kvl = p.kv_len[b], grp = p.h_q / p.h_kv, cols = p.q_tokens * grp, np = partitions_of(p, tiles);
+  const int kvl = p.kv_len[b], grp = p.h_q / p.h_kv, cols = p.q_tokens * grp, np = states_of(p, tiles, chunks);
   const int64_t per_col = (int64_t)p.max_partitions * p.partition_tiles * kTile;
   if ((int64_t)block * kWeightKeys >= min((int64_t)tiles.nt * kTile, per_col)) return;
   const int vk = block * kWeightKeys + threadIdx.x * 4;
@@ -375,40 +428,49 @@ __device__ __forceinline__ void add_weights(const Kv4AttnParams& p, int b, int h
 
 // Grid x: the blocks of rows, then with weights those of keys per KV head; y: sequences.
 template <int WAVES, bool WEIGHTS>
-__global__ __launch_bounds__(256) void kv4_decode_finish_kernel(Kv4AttnParams p) {
+__global__ __launch_bounds__(256) void kv4_decode_finish_kernel(Kv4AttnParams p, int chunks) {
   const int b = blockIdx.y, kvl = p.kv_len[b];
   const int rows = p.q_tokens * p.h_q, blocks = WAVES > 1 ? rows : (rows + 3) / 4;
   const Kv4Tiles tiles = kv4_tiles(kvl - p.q_tokens, kvl - 1, p.window, p.sinks);
   const int x = blockIdx.x;
-  if (!WEIGHTS || x < blocks) merge_rows<WAVES>(p, b, x, tiles);
-  else add_weights(p, b, (x - blocks) % p.h_kv, (x - blocks) / p.h_kv, tiles);
+  if (!WEIGHTS || x < blocks) merge_rows<WAVES>(p, b, x, tiles, chunks);
+  else add_weights(p, b, (x - blocks) % p.h_kv, (x - blocks) / p.h_kv, tiles, chunks);
 }
 
-template <int COLS, bool WEIGHTS>
-void launch_partitions(const Kv4AttnParams& p, hipStream_t stream) {
-  const int chunks = (p.q_tokens * (p.h_q / p.h_kv) + COLS - 1) / COLS;
+template <int COLS, bool JOIN, bool WEIGHTS>
+void launch_partitions(const Kv4AttnParams& p, int chunks, hipStream_t stream) {
   const int64_t groups = ((int64_t)p.max_partitions * chunks + kDecodeWaves - 1) / kDecodeWaves;
   const int64_t all = groups * p.h_kv * p.batch;
   if (p.batch > 1 && p.batch <= kPackedBatch && all * 64 * kDecodeWaves <= UINT32_MAX)
-    kv4_decode_kernel<COLS, WEIGHTS, true><<<dim3((unsigned)all), 64 * kDecodeWaves, 0, stream>>>(p);
+    kv4_decode_kernel<COLS, JOIN, WEIGHTS, true><<<dim3((unsigned)all), 64 * kDecodeWaves, 0, stream>>>(p);
   else
-    kv4_decode_kernel<COLS, WEIGHTS, false><<<dim3((unsigned)groups, p.h_kv, p.batch), 64 * kDecodeWaves, 0, stream>>>(p);
+    kv4_decode_kernel<COLS, JOIN, WEIGHTS, false><<<dim3((unsigned)groups, p.h_kv, p.batch), 64 * kDecodeWaves, 0, stream>>>(p);
+}
+
+template <int COLS>
+void launch_columns(const Kv4AttnParams& p, int chunks, hipStream_t stream) {
+  if (p.scores) launch_partitions<COLS, false, true>(p, chunks, stream);
+  else if (joined(p, chunks)) launch_partitions<COLS, true, false>(p, chunks, stream);
+  else launch_partitions<COLS, false, false>(p, chunks, stream);
 }
 
 }  // namespace
 
 hipError_t launch_kv4_decode(const Kv4AttnParams& p, hipStream_t stream) {
-  const bool wide = kv4_wide_columns(p.q_tokens * (p.h_q / p.h_kv));
-  if (p.scores) wide ? launch_partitions<32, true>(p, stream) : launch_partitions<16, true>(p, stream);
-  else wide ? launch_partitions<32, false>(p, stream) : launch_partitions<16, false>(p, stream);
-  const bool many = p.max_partitions > kManyPartitions;
+  const int cols = p.q_tokens * (p.h_q / p.h_kv);
+  const bool wide = kv4_wide_columns(cols);
+  const int chunks = wide ? (cols + 31) / 32 : 1;
+  wide ? launch_columns<32>(p, chunks, stream) : launch_columns<16>(p, chunks, stream);
+  if (direct(p, chunks)) return hipGetLastError();
+  const int states = joined(p, chunks) ? (p.max_partitions + kDecodeWaves - 1) / kDecodeWaves : p.max_partitions;
+  const bool many = states > kManyStates;
   const int64_t rows = (int64_t)p.q_tokens * p.h_q, keys = (int64_t)p.max_partitions * p.partition_tiles * kTile;
   const int64_t blocks = (many ? rows : (rows + 3) / 4) + (p.scores ? (keys + kWeightKeys - 1) / kWeightKeys * p.h_kv : 0);
   const dim3 grid((unsigned)blocks, p.batch);
-  if (p.scores && many) kv4_decode_finish_kernel<4, true><<<grid, 256, 0, stream>>>(p);
-  else if (p.scores) kv4_decode_finish_kernel<1, true><<<grid, 256, 0, stream>>>(p);
-  else if (many) kv4_decode_finish_kernel<4, false><<<grid, 256, 0, stream>>>(p);
-  else kv4_decode_finish_kernel<1, false><<<grid, 256, 0, stream>>>(p);
+  if (p.scores && many) kv4_decode_finish_kernel<4, true><<<grid, 256, 0, stream>>>(p, chunks);
+  else if (p.scores) kv4_decode_finish_kernel<1, true><<<grid, 256, 0, stream>>>(p, chunks);
+  else if (many) kv4_decode_finish_kernel<4, false><<<grid, 256, 0, stream>>>(p, chunks);
+  else kv4_decode_finish_kernel<1, false><<<grid, 256, 0, stream>>>(p, chunks);
   return hipGetLastError();
 }
 

@@ -60,10 +60,16 @@ __device__ __forceinline__ float q_amax(u32x4 w) {
   return a;
 }
 
+// Channels 2l and 2l + 1 of a row of the output: O / L * tv, or 0 where nothing was visible.
+__device__ __forceinline__ void kv4_store_row(uint16_t* out, float L, float o0, float o1, float tv) {
+  const float inv = L > 0.0f ? __frcp_rn(L) : 0.0f;
+  const uint32_t lo = bf16_rne(o0 * inv * tv), hi = bf16_rne(o1 * inv * tv);
+  *reinterpret_cast<uint32_t*>(out + 2 * (threadIdx.x & 63)) = lo | (hi << 16);
+}
+
 // Merge of the partition states of one row (query token and head), `stride` floats apart,
 // by WAVES waves: M is the largest m, L = sum f l, O = sum f O with f = 2^(m - M); wave w
-// sums partitions w, w + WAVES, .. in order, the waves' sums add in order.  The row is
-// O / L * tv, or 0 where nothing was visible.  Lane l owns channels 2l and 2l + 1.
+// sums partitions w, w + WAVES, .. in order, the waves' sums add in order.  Lane l owns channels 2l and 2l + 1.
 template <int WAVES>
 __device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, int np, float tv, uint16_t* out) {
   __shared__ float part[WAVES][kKv4State];
@@ -110,9 +116,7 @@ __device__ __forceinline__ void kv4_merge_row(const float* st, int64_t stride, i
       o1 += part[w][3 + 2 * lane];
     }
   }
-  const float inv = L > 0.0f ? __frcp_rn(L) : 0.0f;
-  const uint32_t lo = bf16_rne(o0 * inv * tv), hi = bf16_rne(o1 * inv * tv);
-  *reinterpret_cast<uint32_t*>(out + 2 * lane) = lo | (hi << 16);
+  kv4_store_row(out, L, o0, o1, tv);
 }
 
 }  // namespace

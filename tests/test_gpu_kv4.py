@@ -620,3 +620,29 @@ def test_evict_many_sequences(mp):
         for h in range(h_kv):
             idx = torch.tensor(R.keep(src[b][4][:, h].cpu(), budget, 1, 9), dtype=torch.long, device="cuda")
             assert all(torch.equal(x[:, h], y[idx, h]) for x, y in zip(got, src[b])), f"sequence {b}"
+
+
+@pytest.mark.parametrize("batch,longest", [(600, 500), (3, 500), (1, 500), (2, 9000), (5, 20)])
+def test_decode_without_weights_and_sequences_without_keys(mp, batch, longest):
+    """Few partitions, whose workgroups write the output themselves, and many, joined in fours; the packed
+    grid and the plain one; q rows of several column counts."""
+    kv = [(i * 37 + 11) % 97 * longest // 96 if i % 3 else 0 for i in range(batch)]
+    if batch == 1:
+        kv = [0]
+    for h_q, q_tokens in ((2, 1), (10, 3), (40, 1)):   # of two KV heads: 1, 15 and 20 columns
+        print(f"decode of {batch} sequences up to {longest}, heads {h_q}:2 rows {q_tokens}", flush=True)
+        rows, cache, stats, q = attn_case(mp, kv, h_q, 2, [q_tokens] * batch, 19)
+        plan = mp.kv4_decode_plan([longest] * batch, h_q, 2, q_tokens)
+        for part in (plan.partition_tokens, 128):
+            plan.partition_tokens, plan.max_partitions = part, max(1, -(-longest // part))
+            plan.workspace = torch.full((batch * q_tokens * h_q * plan.max_partitions * 130 * 4 + 256,), 255, dtype=torch.uint8,
+                                        device="cuda")
+            out = torch.full_like(q, math.nan)
+            mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan)
+            torch.cuda.synchronize()
+            for b in list(range(0, batch, 1 + batch // 40)):
+                x = slice(b * q_tokens, (b + 1) * q_tokens)
+                want, tol, _, _ = R.attention(q[x], R.Tokens(cache, rows[b].cuda(), kv[b]), stats.k_tscale[b], stats.v_tscale[b],
+                                              kv[b] - q_tokens, 0, 0)
+                check_rows(out[x], want, tol, f"sequence {b}")
+            assert not out.isnan().any()
