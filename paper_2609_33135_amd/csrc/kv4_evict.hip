@@ -11,21 +11,23 @@
 // share the leading bytes (usually after two passes), each is compared with all of them.
 // Then two sweeps count and write the indices in order, each wave over a segment of its own.
 // The images stay in LDS, 32768 of them; what a longer sequence has more is read again each
-// sweep.  What bounds it: latency, of the passes over LDS and of one read of the weights by
-// a single compute unit.  32768 tokens to 4096, 8 heads: 24 us (76 with a histogram per
-// wave and the weights read each sweep; 32 with the images in registers, whose unrolled
-// sweeps outgrow the instruction cache).
+// sweep.  What bounds it: one compute unit, of whose 37000 cycles for 32768 tokens a third
+// are the read of the weights (beside it the first histogram), a quarter the other sweep for
+// the threshold with the comparisons, a quarter the two sweeps for the indices; each spends
+// 10 to 20 instructions on 64 tokens.  32768 tokens to 4096, 8 heads: 17.7 us (76 with a
+// histogram per wave and the weights read each sweep; 32 with the images in registers; 23
+// with a sweep more for the first histogram and scattered sums in vector registers).
 //
 // Move (kv4_move_kernel): destination place i takes source token kept[i] >= i.  With
 // separate pages the places are shared among workgroups; in place, a workgroup per half of
 // the planes, or per quarter of either's codes where there are few, goes through them in
 // order, reading a chunk before it writes it: a later chunk's sources lie at or after its own
 // places, so no write reaches a token that is still to be read.  (The whole call in place,
-// by halves and by quarters: 32768 tokens to 4096, 8 heads, 123 and 57 us; 24 sequences to
-// 2048, 107 and 115, as the quarters read every line more than once.)
+// by halves and by quarters: 32768 tokens to 4096, 8 heads, 117 and 51 us; 24 sequences to
+// 2048, 104 and 112, as the quarters read every line more than once.)
 // What bounds it: HBM lines.  A kept token brings the 256-byte V quad and the 128-byte line
 // of K codes that it lies in, about 450 bytes read for 148 where one token in six stays; 24
-// sequences to 2048 tokens, 8 heads: 48 us, about 4.9 TB/s of such lines.
+// sequences to 2048 tokens, 8 heads: 47 us, about 5 TB/s of such lines.
 #include "kv4_device.h"
 
 namespace mpfa {
@@ -35,7 +37,7 @@ namespace {
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kHeld = 32;        // pages per wave whose images stay in LDS (128 KB, 32768 tokens)
 constexpr int kLoads = 16;       // pages in flight when they are filled
-constexpr int kAhead = 8;        // pages per step of a sweep
+constexpr int kAhead = 4;        // pages per step of a sweep
 constexpr int kListed = 256;     // images compared with each other (each thread one)
 constexpr int kColumns = 16;     // histogram columns
 constexpr int kManyHeads = 64;   // (sequence, KV head) pairs from which halves of the planes fill the card
@@ -71,76 +73,62 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictPara
   // waves own segments of whole pages, in order
   const int pages = (n + 63) >> 6, seg = (pages + kSelectWaves - 1) / kSelectWaves;
   const int g0 = wave * seg, mine = max(0, min(pages - g0, seg));
-  auto image_of = [&](int g, float w) {
-    const int i = g * 64 + lane;
+  auto image_of = [&](int i, float w) {
     return i >= n ? kNone : (i < lo || i >= hi ? kStays : weight_key(w));
   };
-  uint32_t* own = images + wave * kHeld * 64 + lane;   // the wave's images, one page per 64
+  auto clear = [&] { reinterpret_cast<u32x4*>(hist)[tid] = (u32x4){0u, 0u, 0u, 0u}; };
+  auto count_in = [&](uint32_t k, int shift) {
+    atomicAdd(&hist[((k >> shift) & 255u) * kColumns + (lane & (kColumns - 1))], 1u);
+  };
+  clear();
+  if (tid == 0) {
+    s_prefix = s_listed = 0u;
+    s_need = (uint32_t)p.budget;
+  }
+  __syncthreads();
+  // The images, and beside the loads the histogram of their first byte.  Sixteen lanes read a
+  // page, four tokens each.
+  uint32_t* own = images + wave * kHeld * 64;   // the wave's images, one page per 64
   const int my_page = mine > 0 ? pt[g0 + min(lane & (kHeld - 1), mine - 1)] : 0;
   for (int j0 = 0; j0 < min(mine, kHeld); j0 += kLoads) {
-    float w[kLoads];
+    f32x4 w[kLoads / 4];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      w[j] = p.cache.weights[kv4_row(__builtin_amdgcn_readlane(my_page, j0 + j), p.h_kv, hk) * kPage + lane];
+    for (int j = 0; j < kLoads / 4; ++j)
+      w[j] = reinterpret_cast<const f32x4*>(
+          p.cache.weights + kv4_row(__shfl(my_page, j0 + 4 * j + (lane >> 4)), p.h_kv, hk) * kPage)[lane & 15];
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) own[(j0 + j) * 64] = j0 + j < mine ? image_of(g0 + j0 + j, w[j]) : kNone;
+    for (int j = 0; j < kLoads / 4; ++j) {
+      const int pg = j0 + 4 * j + (lane >> 4), i = (g0 + pg) * 64 + 4 * (lane & 15);
+      u32x4 k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        k[e] = pg < mine ? image_of(i + e, w[j][e]) : kNone;
+        if (pg < mine) count_in(k[e], 24);
+      }
+      reinterpret_cast<u32x4*>(own)[(j0 / 4 + j) * 64 + lane] = k;
+    }
   }
+  auto rest = [&](auto&& f) {   // what is not held
+    for (int j = kHeld; j < mine; ++j)
+      f(j, image_of((g0 + j) * 64 + lane, p.cache.weights[kv4_row(pt[g0 + j], p.h_kv, hk) * kPage + lane]));
+  };
+  rest([&](int, uint32_t k) { count_in(k, 24); });
+  __syncthreads();
   // f(j, image) for the wave's pages in order
   auto sweep = [&](auto&& f) {
-    const int here = min(mine, kHeld);
-    for (int j0 = 0; j0 < here; j0 += kAhead) {   // past `mine` no token's image
+    for (int j0 = 0; j0 < min(mine, kHeld); j0 += kAhead) {   // past `mine` no token's image
       uint32_t k[kAhead];
 #pragma unroll
-      for (int j = 0; j < kAhead; ++j) k[j] = own[(j0 + j) * 64];
+      for (int j = 0; j < kAhead; ++j) k[j] = own[(j0 + j) * 64 + lane];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) f(j0 + j, k[j]);
     }
-    for (int j = kHeld; j < mine; ++j)
-      f(j, image_of(g0 + j, p.cache.weights[kv4_row(pt[g0 + j], p.h_kv, hk) * kPage + lane]));
+    rest(f);
   };
 
   // ---- threshold: the budget-th largest image
-  if (tid == 0) {
-    s_prefix = 0u;
-    s_need = (uint32_t)p.budget;
-    s_count = (uint32_t)n;
-  }
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    reinterpret_cast<u32x4*>(hist)[tid] = (u32x4){0u, 0u, 0u, 0u};
-    if (tid == 0) s_listed = 0u;
-    __syncthreads();
-    const uint32_t base = s_prefix, left = s_need, count = s_count;
-    auto inside = [&](uint32_t k) { return shift == 24 || (k >> (shift + 8)) == (base >> (shift + 8)); };
-    if (count <= kListed) {   // few enough: each image against all of them
-      uint32_t* list = hist;         // its first words are zero: no image
-      sweep([&](int, uint32_t k) {
-        if (k != kNone && inside(k)) list[atomicAdd(&s_listed, 1u)] = k;
-      });
-      __syncthreads();
-      if (tid < count) {
-        const uint32_t k = list[tid];
-        uint32_t gt = 0, ge = 0;
-#pragma unroll 1
-        for (uint32_t i = 0; i < count; i += 4) {
-          const u32x4 o = reinterpret_cast<const u32x4*>(list)[i >> 2];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            gt += o[e] > k;
-            ge += o[e] >= k;
-          }
-        }
-        if (gt < left && left <= ge) {   // the equal ones all write the same
-          s_prefix = k;
-          s_need = left - gt;
-        }
-      }
-      __syncthreads();
-      break;
-    }
-    sweep([&](int, uint32_t k) {
-      if (inside(k)) atomicAdd(&hist[((k >> shift) & 255u) * kColumns + (lane & (kColumns - 1))], 1u);
-    });
-    __syncthreads();
+  for (int shift = 24;; shift -= 8) {
+    const uint32_t base = s_prefix, left = s_need;
     {   // four threads per bin, a quarter of its columns each
       const u32x4 w = reinterpret_cast<const u32x4*>(hist)[tid];
       uint32_t t = (w[0] + w[1]) + (w[2] + w[3]);
@@ -173,6 +161,46 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictPara
       }
     }
     __syncthreads();
+    if (shift == 0) break;
+    const uint32_t found = s_prefix, count = s_count;
+    auto inside = [&](uint32_t k) { return (k >> shift) == (found >> shift); };
+    clear();
+    __syncthreads();
+    if (count <= kListed) {   // few enough: each image against all of them
+      const uint32_t need = s_need;
+      uint32_t* list = hist;         // its first words are zero: no image
+      sweep([&](int, uint32_t k) {
+        if (k != kNone && inside(k)) list[atomicAdd(&s_listed, 1u)] = k;
+      });
+      __syncthreads();
+      {   // four threads per image, every fourth four of the others each
+        const uint32_t k = list[tid >> 2];
+        uint32_t gt = 0, ge = 0;
+#pragma unroll 1
+        for (uint32_t i = 4 * (tid & 3); i < count; i += 16) {
+          const u32x4 o = reinterpret_cast<const u32x4*>(list)[i >> 2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            gt += o[e] > k;
+            ge += o[e] >= k;
+          }
+        }
+        for (int off = 1; off <= 2; off <<= 1) {
+          gt += __shfl_xor(gt, off);
+          ge += __shfl_xor(ge, off);
+        }
+        if (k != kNone && gt < need && need <= ge) {   // the equal ones all write the same
+          s_prefix = k;
+          s_need = need - gt;
+        }
+      }
+      __syncthreads();
+      break;
+    }
+    sweep([&](int, uint32_t k) {
+      if (inside(k)) count_in(k, shift - 8);
+    });
+    __syncthreads();
   }
   const uint32_t prefix = s_prefix;
   const int need = (int)s_need;   // of the images equal to the threshold, the first `need` stay
@@ -193,15 +221,25 @@ __global__ __launch_bounds__(kSelectThreads) void kv4_select_kernel(Kv4EvictPara
     place += above[w] + min(equal[w], max(0, need - eq));
     eq += equal[w];
   }
-  const uint64_t below = (1ull << lane) - 1ull;
-  sweep([&](int j, uint32_t k) {
+  // base + the number of lower lanes in m
+  auto rank = [](uint64_t m, int base) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, base));
+  };
+  place = __builtin_amdgcn_readfirstlane(place);
+  eq = __builtin_amdgcn_readfirstlane(eq);
+  auto choose = [&](uint32_t k) {
+    uint64_t am = __ballot(k > prefix);
     const uint64_t em = __ballot(k == prefix);
-    bool a = k > prefix;
-    if (em) a = a || (k == prefix && eq + __popcll(em & below) < need);
-    const uint64_t am = __ballot(a);
-    if (a) kept[place + __popcll(am & below)] = (g0 + j) * 64 + lane;
+    if (em) {
+      am |= __ballot(k == prefix && rank(em, eq) < need);
+      eq += __popcll(em);
+    }
+    return am;
+  };
+  sweep([&](int j, uint32_t k) {
+    const uint64_t am = choose(k);
+    if (__builtin_amdgcn_inverse_ballot_w64(am)) kept[(uint32_t)rank(am, place)] = (g0 + j) * 64 + lane;
     place += __popcll(am);
-    eq += __popcll(em);
   });
 }
 
