@@ -34,11 +34,11 @@ __device__ __forceinline__ int partitions_of(const Kv4AttnParams& p, const Kv4Ti
   return min((tiles.nt + p.partition_tiles - 1) / p.partition_tiles, p.max_partitions);
 }
 
-// Where one wave holds all columns of a KV head, the waves of a workgroup have partitions of
-// the same rows and can join them in LDS.  They do where that
-//  - leaves the output itself (four partitions at most), with no launch to merge them: 64
-//    contexts of four rows and 2048 keys, 40:8 heads, 43 us, 54 with it; 64 of 2100, 32:8,
-//    32.3 and 38.7; or
+// The waves of a workgroup that have partitions of the same rows can join them in LDS.  They
+// do where that
+//  - leaves the output itself (the workgroup has all partitions of its rows), with no launch
+//    to merge them: 64 contexts of four rows and 2048 keys, 40:8 heads, 43 us, 54 with it; 64
+//    of 2100, 32:8, 32.3 and 38.7, with 40 columns (40:8, eight rows) 62 and 73; or
 //  - a fourth of many states: one context of 64K keys, 40:8, 19.6 us, 21.1 not.  (In between
 //    the waves that wait for the others cost more: 4 of 32K, 32:8, 35.4 us, 33.8 not.)
 constexpr int kJoinPartitions = 64;
@@ -306,7 +306,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
     }
   }
   // where a column's state goes: to LDS, or to the workspace
-  __shared__ float joint[JOIN ? kDecodeWaves : 1][JOIN ? COLS : 1][kKv4State];
+  __shared__ float joint[JOIN ? kDecodeWaves : 1][JOIN ? COLS : 1][kKv4State];   // [wave][column of its chunk]
   const int64_t row0 = (int64_t)b * p.q_tokens * p.h_q + hk * grp;
   auto row_of = [&](int col) { return row0 + (int64_t)(col / grp) * p.h_q + col % grp; };
   auto state_of = [&](int col, int at) { return p.states + (row_of(col) * p.max_partitions + at) * kKv4State; };
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
       const float lt = wave_sum16(l[n]);
       const int col = col_of(n);
       if (col < cols) {
-        float* st = JOIN ? joint[threadIdx.x >> 6][col] : state_of(col, part);
+        float* st = JOIN ? joint[threadIdx.x >> 6][16 * n + lr] : state_of(col, part);
         if (g == 0) *reinterpret_cast<float2*>(st) = make_float2(m[n] * lam[n], lt);
         // accumulator row 4g + i of block db is channel 8 (4g + i) + db
 #pragma unroll
@@ -330,28 +330,32 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
       }
     }
   }
-  if (!JOIN) return;
-  __syncthreads();
-  const int live = max(min(partitions_of(p, tiles) - group * kDecodeWaves, kDecodeWaves), 0);
-  const float tv = p.v_tscale[b * p.h_kv + hk];
-  for (int col = threadIdx.x >> 6; col < cols; col += kDecodeWaves) {
-    float M = -INFINITY, L = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int q = 0; q < live; ++q) M = fmaxf(M, joint[q][col][0]);
-    if (M > -INFINITY)
-      for (int q = 0; q < live; ++q) {
-        const float2 ml = *reinterpret_cast<const float2*>(joint[q][col]);
-        const float2 x = *reinterpret_cast<const float2*>(joint[q][col] + 2 + 2 * lane);
-        const float f = __builtin_amdgcn_exp2f(ml.x - M);
-        L = __builtin_fmaf(f, ml.y, L);
-        o0 = __builtin_fmaf(f, x.x, o0);
-        o1 = __builtin_fmaf(f, x.y, o1);
+  if constexpr (JOIN) {
+    __syncthreads();
+    const int own = kDecodeWaves / chunks;   // partitions of the workgroup
+    const int live = max(min(partitions_of(p, tiles) - group * own, own), 0);
+    const float tv = p.v_tscale[b * p.h_kv + hk];
+    for (int col = threadIdx.x >> 6; col < cols; col += kDecodeWaves) {
+      const float(*st0)[COLS][kKv4State] = joint + col / COLS;   // of the workgroup's first partition
+      const int at = col % COLS;
+      float M = -INFINITY, L = 0.0f, o0 = 0.0f, o1 = 0.0f;
+      for (int q = 0; q < live; ++q) M = fmaxf(M, st0[q * chunks][at][0]);
+      if (M > -INFINITY)
+        for (int q = 0; q < live; ++q) {
+          const float* st = st0[q * chunks][at];
+          const float2 ml = *reinterpret_cast<const float2*>(st), x = *reinterpret_cast<const float2*>(st + 2 + 2 * lane);
+          const float f = __builtin_amdgcn_exp2f(ml.x - M);
+          L = __builtin_fmaf(f, ml.y, L);
+          o0 = __builtin_fmaf(f, x.x, o0);
+          o1 = __builtin_fmaf(f, x.y, o1);
+        }
+      if (direct(p, chunks)) {
+        kv4_store_row(p.out + row_of(col) * kD, L, o0, o1, tv);
+      } else {
+        float* st = state_of(col, group);
+        if (lane == 0) *reinterpret_cast<float2*>(st) = make_float2(M, L);
+        *reinterpret_cast<float2*>(st + 2 + 2 * lane) = make_float2(o0, o1);
       }
-    if (direct(p, chunks)) {
-      kv4_store_row(p.out + row_of(col) * kD, L, o0, o1, tv);
-    } else {
-      float* st = state_of(col, group);
-      if (lane == 0) *reinterpret_cast<float2*>(st) = make_float2(M, L);
-      *reinterpret_cast<float2*>(st + 2 + 2 * lane) = make_float2(o0, o1);
     }
   }
 }

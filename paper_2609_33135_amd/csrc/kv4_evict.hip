@@ -16,7 +16,7 @@
 // the threshold with the comparisons, a quarter the two sweeps for the indices; each spends
 // 10 to 20 instructions on 64 tokens.  32768 tokens to 4096, 8 heads: 17.7 us (76 with a
 // histogram per wave and the weights read each sweep; 32 with the images in registers; 23
-// with a sweep more for the first histogram and scattered sums in vector registers).
+// with a sweep more for the first histogram and the places counted in vector registers).
 //
 // Move (kv4_move_kernel): destination place i takes source token kept[i] >= i.  With
 // separate pages the places are shared among workgroups; in place, a workgroup per half of

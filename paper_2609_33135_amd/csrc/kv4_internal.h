@@ -102,10 +102,11 @@ __host__ __device__ inline Kv4Tiles kv4_tiles(int first, int last, int window, i
 // Whether decode waves take 32 columns (rows times heads of a KV head) each, or 16.
 __host__ __device__ inline bool kv4_wide_columns(int64_t cols) { return cols > 16; }
 
-// Whether a decode workgroup's waves have all of their rows' partitions, and write the output.
+// Whether the four waves of a decode workgroup have all partitions of their rows (in `chunks`
+// parts of 16 or 32 columns), and write the output themselves.
 constexpr int kKv4DecodeWaves = 4;
 __host__ __device__ inline bool kv4_direct(int64_t chunks, int64_t max_partitions, bool weights) {
-  return chunks == 1 && max_partitions <= kKv4DecodeWaves && !weights;
+  return kKv4DecodeWaves % chunks == 0 && max_partitions <= kKv4DecodeWaves / chunks && !weights;
 }
 
 hipError_t launch_kv4_write(const Kv4WriteParams& p, hipStream_t stream);

@@ -629,7 +629,7 @@ def test_decode_without_weights_and_sequences_without_keys(mp, batch, longest):
     kv = [(i * 37 + 11) % 97 * longest // 96 if i % 3 else 0 for i in range(batch)]
     if batch == 1:
         kv = [0]
-    for h_q, q_tokens in ((2, 1), (10, 3), (40, 1)):   # of two KV heads: 1, 15 and 20 columns
+    for h_q, q_tokens in ((2, 1), (10, 3), (40, 1), (24, 3), (64, 3), (32, 8)):   # of two KV heads: 1, 15, 20, 36, 96, 128 columns
         print(f"decode of {batch} sequences up to {longest}, heads {h_q}:2 rows {q_tokens}", flush=True)
         rows, cache, stats, q = attn_case(mp, kv, h_q, 2, [q_tokens] * batch, 19)
         plan = mp.kv4_decode_plan([longest] * batch, h_q, 2, q_tokens)
