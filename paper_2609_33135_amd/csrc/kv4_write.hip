@@ -142,8 +142,9 @@ __device__ __forceinline__ void finish_stats(const Kv4WriteParams& p, StatSmem<P
   const int nblk = (n + p.stat_tokens - 1) / p.stat_tokens;
   constexpr int kAhead = 8;
   double sum = 0.0;
-  float mx = -INFINITY, mn = INFINITY, va = 0.0f;
-  for (int blk = threadIdx.x; blk < nblk; blk += PARTS * kD) va = fmaxf(va, stat_ptrs(stat_block(p, t0, b, blk, hk)).v[0]);
+  float mx = -INFINITY, mn = INFINITY;
+  auto v_of = [&](int blk) { return stat_ptrs(stat_block(p, t0, b, blk, hk)).v[0]; };
+  float va = v_of(min((int)threadIdx.x, nblk - 1));   // in flight beside the loads below
   for (int blk0 = part; blk0 < nblk; blk0 += PARTS * kAhead) {   // past the last block it again, without its sum
     double sums[kAhead];
     float mxs[kAhead], mns[kAhead];
@@ -161,6 +162,7 @@ __device__ __forceinline__ void finish_stats(const Kv4WriteParams& p, StatSmem<P
       mn = fminf(mn, mns[i]);
     }
   }
+  for (int blk = threadIdx.x + PARTS * kD; blk < nblk; blk += PARTS * kD) va = fmaxf(va, v_of(blk));
   for (int off = 32; off >= 1; off >>= 1) va = fmaxf(va, __shfl_xor(va, off));
   sm.sum[part][c] = sum;
   sm.mx[part][c] = mx;
@@ -280,9 +282,10 @@ __device__ __forceinline__ void load_group(const uint16_t* src, float* x) {
 }
 
 // FUSED: every workgroup finishes the statistics itself (see kFusedPartials) and the first of
-// each (sequence, KV head) stores them.
+// each (sequence, KV head) stores them.  Five waves fit a SIMD (four prompts, 4048 tokens
+// together, 8 heads: 19.4 us; 21.3 with four, 21.2 with six, which spill).
 template <bool FUSED>
-__global__ __launch_bounds__(256) void kv4_write_kernel(Kv4WriteParams p) {
+__global__ __launch_bounds__(256, FUSED ? 5 : 1) void kv4_write_kernel(Kv4WriteParams p) {
   const int b = blockIdx.z, hk = blockIdx.y, first = blockIdx.x * kWriteTokens;
   const int64_t t0 = p.cu_seqlens[b];
   const int n = p.cu_seqlens[b + 1] - (int)t0;
