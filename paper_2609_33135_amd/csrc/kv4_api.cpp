@@ -346,6 +346,8 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* a, void* workspace, size_t
   if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->k_mean) || !aligned16(a->k_out) || !aligned16(a->v_out))
     return MPFA_ERR_INVALID;
   if (a->batch > 65535 || a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
+  const int64_t groups = (std::min(a->max_seqlen, a->total_tokens) + mpfa::kKv4WriteTokens - 1) / mpfa::kKv4WriteTokens;
+  if (groups * a->h_kv > (int64_t)UINT32_MAX / 256) return MPFA_ERR_UNSUPPORTED;
   if (stats) {
     size_t need = 0;
     if (mpfa_kv4_write_workspace_size(a->batch, a->total_tokens, a->h_kv, &need) != MPFA_OK) return MPFA_ERR_INVALID;

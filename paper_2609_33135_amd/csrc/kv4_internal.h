@@ -14,6 +14,7 @@ constexpr int kKv4StatTokens = 128;   // fewest tokens per statistics partial
 // per partial of one KV head: FP64 sums, FP32 maxima and minima of K per channel, and
 // the largest |V| (padded to 16 bytes)
 constexpr int kKv4StatBytes = 128 * (8 + 4 + 4) + 16;
+constexpr int kKv4WriteTokens = 32;   // tokens per workgroup of 256 threads of the write pass
 constexpr int kKv4Rows = 256;         // most query rows (tokens x heads of one KV head) of a prefill item
 constexpr int kKv4State = 130;        // floats of a partition state: m, l, O[128]
 

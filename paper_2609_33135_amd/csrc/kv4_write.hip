@@ -16,11 +16,16 @@ namespace {
 constexpr int64_t kLastLevelCache = (int64_t)256 << 20;
 // Where every workgroup of the write pass reads the partials of its sequence itself: up to so
 // many of them, and so many reads of one by all workgroups (2 KB each, from L2).  One launch
-// less: 777 tokens, 8 heads, 12.1 us, 14.9 not; one prompt of 4000 18.7 and 20.5; but four of
-// 4000, 128000 reads, 50.8 and 48.0.
+// less.  8 heads: 777 tokens 12.4 us, 15.1 not; 4000 17.6 and 19.5; eight of 2000, 64000 reads,
+// 44.5 and 48.7; but 6000, 47 partials, 26.4 and 23.7; four of 4000, 128000 reads, 50.3 and
+// 49.5; eight, 256000, 104 and 92.
 constexpr int kFusedPartials = 32;
-constexpr int64_t kFusedReads = 50000;
-constexpr int kWriteTokens = 32;   // tokens per workgroup: eight per wave, eight lanes (groups of 16) each
+constexpr int64_t kFusedReads = 100000;
+// Tokens per workgroup of the write pass: eight per wave, eight lanes (groups of 16) each.  In
+// both passes the KV heads of the same tokens are neighbours in the grid: their rows lie side
+// by side in memory (8 heads: 33000 tokens 100 us, 104 head by head; four prompts, 4048 tokens
+// together, 18.1 and 19.4; but eight of 4000 92 and 90).
+constexpr int kWriteTokens = kKv4WriteTokens;
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -54,7 +59,7 @@ template <bool STREAM>
 __global__ __launch_bounds__(256) void kv4_stats_kernel(Kv4WriteParams p) {
   __shared__ double s_sum[4][kD];
   __shared__ float s_mx[4][kD], s_mn[4][kD], s_v[4];
-  const int b = blockIdx.z, hk = blockIdx.y, blk = blockIdx.x;
+  const int b = blockIdx.y, hk = blockIdx.x % p.h_kv, blk = blockIdx.x / p.h_kv;
   const int64_t t0 = p.cu_seqlens[b];
   const int n = p.cu_seqlens[b + 1] - (int)t0;
   const int begin = blk * p.stat_tokens, te = min(n, begin + p.stat_tokens);
@@ -283,10 +288,11 @@ __device__ __forceinline__ void load_group(const uint16_t* src, float* x) {
 
 // FUSED: every workgroup finishes the statistics itself (see kFusedPartials) and the first of
 // each (sequence, KV head) stores them.  Five waves fit a SIMD (four prompts, 4048 tokens
-// together, 8 heads: 19.4 us; 21.3 with four, 21.2 with six, which spill).
+// together, 8 heads: 19.4 us; 21.3 with four, 21.2 with six, which spill; 18.1 with the heads
+// side by side).
 template <bool FUSED>
 __global__ __launch_bounds__(256, FUSED ? 5 : 1) void kv4_write_kernel(Kv4WriteParams p) {
-  const int b = blockIdx.z, hk = blockIdx.y, first = blockIdx.x * kWriteTokens;
+  const int b = blockIdx.y, hk = blockIdx.x % p.h_kv, first = blockIdx.x / p.h_kv * kWriteTokens;
   const int64_t t0 = p.cu_seqlens[b];
   const int n = p.cu_seqlens[b + 1] - (int)t0;
   if (first >= n) return;
@@ -337,13 +343,13 @@ __global__ __launch_bounds__(256, FUSED ? 5 : 1) void kv4_write_kernel(Kv4WriteP
 
 hipError_t launch_kv4_write(const Kv4WriteParams& p, hipStream_t stream) {
   if (p.total_tokens == 0 || p.max_seqlen == 0) return hipSuccess;
-  const dim3 chunks((p.max_seqlen + kWriteTokens - 1) / kWriteTokens, p.h_kv, p.batch);
+  const dim3 chunks((p.max_seqlen + kWriteTokens - 1u) / kWriteTokens * p.h_kv, p.batch);
   if (!p.compute_stats) {
     kv4_write_kernel<false><<<chunks, 256, 0, stream>>>(p);
     return hipGetLastError();
   }
   const int blocks = (p.max_seqlen + p.stat_tokens - 1) / p.stat_tokens;
-  const dim3 grid(blocks, p.h_kv, p.batch);
+  const dim3 grid((unsigned)blocks * p.h_kv, p.batch);
   if ((int64_t)p.total_tokens * p.h_kv * kD * 4 >= kLastLevelCache) kv4_stats_kernel<true><<<grid, 256, 0, stream>>>(p);
   else kv4_stats_kernel<false><<<grid, 256, 0, stream>>>(p);
   const int64_t reads = (int64_t)p.total_tokens / kWriteTokens * p.h_kv * blocks;

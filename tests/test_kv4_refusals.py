@@ -61,6 +61,7 @@ BAD_CACHE = [dict(cache={n: v}) for n in PLANES[:4] for v in (None, 0x1008)] + \
     (dict(v=None), INVALID), (dict(slot_mapping=None), INVALID), (dict(k_mean=None), INVALID), (dict(k_tscale=None), INVALID),
     (dict(v_tscale=None), INVALID), (dict(k=0x1002), INVALID), (dict(v=0x1008), INVALID), (dict(k_out=0x1008), INVALID),
     (dict(v_out=0x1004), INVALID), (dict(batch=65536), UNSUPPORTED),
+    (dict(total_tokens=1 << 28, max_seqlen=1 << 28), UNSUPPORTED),
     (dict(total_tokens=(1 << 28) + 1), UNSUPPORTED)] + [(c, INVALID) for c in BAD_CACHE])
 def test_write(mp, kw, status):
     assert mp.lib().mpfa_kv4_write(C.byref(_write(mp, **kw)), 0x1000, 1 << 40, None) == status
