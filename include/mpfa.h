@@ -430,7 +430,7 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, siz
  * j < sinks):
  *   S = q . Khat / sqrt(128);  out = BF16(sum_j softmax(S)_j Vhat_j)
  * with FP32 scores, maxima and sums and P rounded to FP16 (2^-11 of each P, or
- * 2^-40 of the row's largest where that is more).
+ * 2^-40 of the row's largest where that is more), for every finite q, K and V.
  * A row that sees no key is 0.  h_q / h_kv may be anything from 1 to 256.
  * Keys at or past kv_len are never used, whatever their slots hold.
  *

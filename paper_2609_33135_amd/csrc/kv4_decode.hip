@@ -248,7 +248,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
       const float muse = mnew == -INFINITY ? 0.0f : mnew;
       const float alpha = m[n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m[n] - muse) * lam[n]);
       m[n] = mnew;
-      const float bias = __builtin_fmaf(-muse, lam[n], kLog2P);
+      float bias = __builtin_fmaf(-muse, lam[n], kLog2P);
+      const bool far = __builtin_fabsf(bias) > kPlainBias;
+      if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+        const float d = far ? muse : 0.0f;
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb) s[n][mb] -= d;
+        bias = far ? kLog2P : bias;
+      }
       float ps = 0.0f;
 #pragma unroll
       for (int mb = 0; mb < 4; ++mb) {

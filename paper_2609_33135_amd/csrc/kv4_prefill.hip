@@ -138,8 +138,10 @@ struct Kv4Soft {
   float m, l, bias;   // running maximum (accumulator units), row sum, exponent bias
 };
 
+// Running maximum and bias of the tile's exponentials (s: the scores, or their distance from the
+// maximum where that is needed, see kPlainBias); returns the factor of what was summed before.
 template <int NB>
-__device__ __forceinline__ float max_tile(const f32x16 (&s)[NB], const Kv4Item& it, Kv4Soft& ss) {
+__device__ __forceinline__ float max_tile(f32x16 (&s)[NB], const Kv4Item& it, Kv4Soft& ss) {
   float mxa = -INFINITY, mxb = -INFINITY;
 #pragma unroll
   for (int kb = 0; kb < NB; kb += 2) {
@@ -154,6 +156,13 @@ __device__ __forceinline__ float max_tile(const f32x16 (&s)[NB], const Kv4Item& 
   const float alpha = ss.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((ss.m - muse) * it.lam);
   ss.m = mnew;
   ss.bias = __builtin_fmaf(-muse, it.lam, kLog2P);
+  const bool far = __builtin_fabsf(ss.bias) > kPlainBias;
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+    const float d = far ? muse : 0.0f;
+#pragma unroll
+    for (int kb = 0; kb < NB; ++kb) s[kb] -= d;
+    ss.bias = far ? kLog2P : ss.bias;
+  }
   return alpha;
 }
 
@@ -238,12 +247,10 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wrow = 32 * (HALF ? wave & 3 : wave);    // the wave's first row
   it.kb0 = HALF ? 2 * (wave >> 2) : 0;
-  const int r = wrow + it.lc;
   const int last = min(tok0 + tm, nq) - 1;           // last token of the item
   const int qs = p.q_start[b], kvl = p.kv_len[b];
-  const int tok = min(tok0 + r / grp, last);         // rows past the item repeat its last token
-  const bool valid = r < (last + 1 - tok0) * grp;
-  const int h = hk * grp + r % grp;
+  const int row = wrow + it.lc;
+  const int tok = min(tok0 + row / grp, last);       // rows past the item repeat its last token
   const bool active = wrow < (last + 1 - tok0) * grp;
   it.pos = qs + tok;
   it.low = p.window > 0 ? max(it.pos - p.window + 1, 0) : 0;
@@ -251,7 +258,7 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
   it.wpos_min = qs + min(tok0 + wrow / grp, last);
   it.wlow_max = p.window > 0 ? max(qs + min(tok0 + (wrow + 31) / grp, last) - p.window + 1, 0) : 0;
   {
-    const u32x4* src = reinterpret_cast<const u32x4*>(p.q + (int64_t)(q0 + tok) * p.q_stride + h * kD);
+    const u32x4* src = reinterpret_cast<const u32x4*>(p.q + (int64_t)(q0 + tok) * p.q_stride + (hk * grp + row % grp) * kD);
     u32x4 w[8];
     float a = 0.0f;
 #pragma unroll
@@ -341,9 +348,10 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
     put_v(v - 1);
     __builtin_amdgcn_sched_barrier(0);
     mask(v - 1);
+    const float next = max_tile(s, it, ss);   // ahead of the PV products: its branch leaves them beside the exponentials
     rescale(o, alpha);
     pv_tile(sm, v & 1, ph, o, it);
-    alpha = max_tile(s, it, ss);
+    alpha = next;
     ps = exp_block(s[0], 0, it, ss, ph);
     __syncthreads();
   }
@@ -356,22 +364,25 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
   for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(o[db]));
   if (HALF && !join_halves(sm, wave, it, ss, o)) return;
   const float lt = ss.l + __shfl_xor(ss.l, 32);
-  if (!valid) return;
+  // the lane's row once more: kept over the loop it would take registers that the loop needs
+  const int lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), hf = lane >> 5, r = wrow + (lane & 31);
+  if (r >= (last + 1 - tok0) * grp) return;
+  const int t = it.pos - qs;   // its token
   // accumulator register 4a + i of block db is channel 64 (a%2) + 32 hf + 8 i + 2 db + a/2
   if (state) {
     float* st = state + (int64_t)r * kKv4State;
-    if (it.hf == 0) *reinterpret_cast<float2*>(st) = make_float2(ss.m * it.lam, lt);
+    if (hf == 0) *reinterpret_cast<float2*>(st) = make_float2(ss.m * it.lam, lt);
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int db = 0; db < 4; ++db)
-          *reinterpret_cast<float2*>(st + 2 + 64 * a + 32 * it.hf + 8 * i + 2 * db) =
+          *reinterpret_cast<float2*>(st + 2 + 64 * a + 32 * hf + 8 * i + 2 * db) =
               make_float2(o[db][4 * a + i], o[db][8 + 4 * a + i]);
   } else {
     const float inv = lt > 0.0f ? __frcp_rn(lt) * p.v_tscale[b * p.h_kv + hk] : 0.0f;
-    uint16_t* dst = p.out + ((int64_t)(q0 + tok) * p.h_q + h) * kD + 32 * it.hf;
+    uint16_t* dst = p.out + ((int64_t)(q0 + t) * p.h_q + hk * grp + r - (t - tok0) * grp) * kD + 32 * hf;
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll

@@ -1,0 +1,56 @@
+"""The 4-bit cache at the ends of its ranges.  Definitions and tolerances: tests/kv4_ref.py."""
+import math
+
+import pytest
+import torch
+
+from tests import kv4_ref as R
+from tests.test_gpu_kv4 import (D, PAGE, attn_case, check_prefill, check_rows, check_stats, check_write, cumulative, i32, mp,  # noqa: F401
+                                slots_of)
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ scores of any size
+def both(mp, q, cache, stats, kv, rows, weights=False):
+    """The call's rows by decode and by prefill, in one pass and in halves that split the keys."""
+    n, (r, h_q) = kv[0], q.shape[:2]
+    dec, pre, cut = (torch.full_like(q, math.nan) for _ in range(3))
+    args = (cumulative([r]), i32([n - r]), i32(kv), rows.cuda())
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), dec, mp.kv4_decode_plan(kv, h_q, cache.h_kv, r, weights=weights))
+    mp.kv4_prefill(q, cache, stats, *args, pre)
+    mp.kv4_prefill(q, cache, stats, *args, cut, mp.kv4_prefill_plan([r], kv, h_q, cache.h_kv))
+    torch.cuda.synchronize()
+    return {"decode": dec, "prefill": pre, "prefill by plan": cut}
+
+
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("q_exp,t_exp", [(10, 0), (16, 0), (20, 0), (30, 3), (60, -3), (100, 0), (60, 63), (110, 63), (-50, 63), (118, -63)])
+def test_one_key_takes_all(mp, q_exp, t_exp, weights):
+    """Queries so large that the best key's weight is 1 and every other one's 0: its V comes out, exactly (a V
+    value has six bits, and 1 times it divided by 1 is off by a few 2^-24 before the rounding to bf16)."""
+    print(f"one key takes all: q about 2^{q_exp}, K in units of 2^{t_exp}, weights {weights}", flush=True)
+    kv, h_q, h_kv, r = [700], 4, 2, 6
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [r], 61, weights=weights)
+    stats.k_tscale.fill_(2.0 ** t_exp)
+    q = (q.double() * 2.0 ** q_exp).bfloat16()
+    toks = R.Tokens(cache, rows[0].cuda(), kv[0])
+    k, v, w0 = toks.k() * 2.0 ** t_exp, toks.v() * stats.v_tscale[0].double()[None, :, None], toks.weights
+    want, share = torch.empty(r, h_q, D, dtype=torch.float64, device="cuda"), torch.zeros(kv[0], h_kv, dtype=torch.float64, device="cuda")
+    for i in range(r):
+        for h in range(h_q):
+            n, hk = kv[0] - r + 1 + i, h // (h_q // h_kv)
+            s = (k[:n, hk] @ q[i, h].double()) / math.sqrt(D)
+            size = (k[:n, hk].abs() @ q[i, h].double().abs()).max() / math.sqrt(D)
+            top = s.topk(2)
+            # the distance outweighs what FP32 sums of 128 products may be off by, and any other key's weight is below
+            # 2^-40 of the best one's, which its FP16 value does not hold
+            assert top.values[0] - top.values[1] > 2 * 136 * 2.0 ** -24 * size + 40
+            want[i, h] = v[top.indices[0], hk]
+            share[top.indices[0], hk] += 1
+    for name, out in both(mp, q, cache, stats, kv, rows, weights).items():
+        assert torch.equal(out.double(), want), f"{name}: {int((out.double() != want).sum())} values off, {int(out.isnan().sum())} NaN"
+    if weights:
+        got = R.Tokens(cache, rows[0].cuda(), kv[0]).weights.double()
+        # a share is 2^15 / L times 2^0: two roundings, then the additions
+        assert ((got - (w0.double() + share)).abs() <= 2.0 ** -20 * (w0.double() + share)).all()
