@@ -168,6 +168,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
   int pos[kN];                   // last visible key; negative: none
   f32x4 o[kN][8];
   auto col_of = [&](int n) { return chunk * COLS + 16 * n + lr; };
+  const float tk = p.k_tscale[b * p.h_kv + hk];
 #pragma unroll
   for (int n = 0; n < kN; ++n) {
     const int col = min(col_of(n), cols - 1), tok = col / grp;
@@ -181,10 +182,10 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
       w[i] = src[i];
       a = fmaxf(a, q_amax(w[i]));
     }
-    const int shift = q_shift(wave_max16(a));
+    const int shift = q_shift(wave_max16(a), tk);
 #pragma unroll
     for (int i = 0; i < 4; ++i) qop[n][i] = q_operand(w[i], shift);
-    lam[n] = score_scale(p.lam, p.k_tscale[b * p.h_kv + hk], shift);
+    lam[n] = score_scale(p.lam, tk, shift);
     m[n] = -INFINITY;
     l[n] = 0.0f;
 #pragma unroll

@@ -35,12 +35,13 @@ __device__ __forceinline__ f16x2 fp4_pair_f16(uint32_t w, f16x2 m) {
   return __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, SEL) * m;
 }
 
-// Exponent shift of a query row whose largest magnitude is a: the row times 2^shift is
-// below 2^15, so its bf16 values are exact in FP16 (11 bits) wherever they are above
-// 2^-28 of the largest, and off by at most 2^-39 of it elsewhere (a row below 2^-46
-// altogether, whose scores are below 2^-30 of a K unit, loses more).
-__device__ __forceinline__ int q_shift(float a) {
-  return a > 0.0f ? min(14 - ilog2f(a), 60) : 0;
+// Exponent shift of a query row whose largest magnitude is a, for keys in units of the tensor
+// scale: the row times 2^shift is below 2^15, so its bf16 values are exact in FP16 (11 bits)
+// wherever they are above 2^-28 of the largest, and off by at most 2^-39 of it elsewhere.  The
+// shift stops where score_scale's factor would leave the normal numbers, 2^(scale's exponent -
+// shift) = 2^-123: rows that small have scores below 2^-90.
+__device__ __forceinline__ int q_shift(float a, float k_tscale) {
+  return a > 0.0f ? min(14 - ilog2f(a), 123 + ilog2f(k_tscale)) : 0;
 }
 // log2(e) / sqrt(128) for scores in units of the K tensor scale and the row's shift.  The
 // exponent stays where the factor is a normal number (2^-126 .. ): 0 times a masked

@@ -266,10 +266,11 @@ __device__ __forceinline__ void prefill_item(const Kv4AttnParams& p, Kv4Smem& sm
       w[ks] = src[2 * ks + it.hf];
       a = fmaxf(a, q_amax(w[ks]));
     }
-    const int shift = q_shift(wave_max32(a));
+    const float tk = p.k_tscale[b * p.h_kv + hk];
+    const int shift = q_shift(wave_max32(a), tk);
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) it.q[ks] = q_operand(w[ks], shift);
-    it.lam = score_scale(p.lam, p.k_tscale[b * p.h_kv + hk], shift);
+    it.lam = score_scale(p.lam, tk, shift);
   }
 
   Kv4Soft ss = {-INFINITY, 0.0f, 0.0f};

@@ -54,3 +54,25 @@ def test_one_key_takes_all(mp, q_exp, t_exp, weights):
         got = R.Tokens(cache, rows[0].cuda(), kv[0]).weights.double()
         # a share is 2^15 / L times 2^0: two roundings, then the additions
         assert ((got - (w0.double() + share)).abs() <= 2.0 ** -20 * (w0.double() + share)).all()
+
+
+# ------------------------------------------------------------------ small queries, large keys
+@pytest.mark.parametrize("q_exp", [-70, -76, -78, -79, -90])
+def test_small_queries_against_large_keys(mp, q_exp):
+    """Queries far below bf16's middle against keys far above it: ordinary scores, to the ordinary tolerance.  Every
+    second key is 0 with V = 1, the others 2688 * 2^63 in all channels with V = -1; every query value is
+    129 / 128 * 2^q_exp, so that a loss of bits would not average out."""
+    print(f"q about 2^{q_exp} against keys in units of 2^63", flush=True)
+    kv, h_q, h_kv, r = [500], 4, 2, 5
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [r], 67)
+    cache.k_codes[:, :, 0::2], cache.k_codes[:, :, 1::2] = 0x00, 0x77
+    vc = cache.v_codes.view(-1, h_kv, 16, 16, 4, 4)
+    vc[:, :, :, :, 0::2], vc[:, :, :, :, 1::2] = 0x22, 0xAA
+    cache.k_scales.fill_(0x7E)
+    cache.v_scales.fill_(0x38)
+    stats.k_tscale.fill_(2.0 ** 63)
+    q.fill_(129 / 128 * 2.0 ** q_exp)
+    want, tol, _, _ = R.attention(q, R.Tokens(cache, rows[0].cuda(), kv[0]), stats.k_tscale[0], stats.v_tscale[0], kv[0] - r, 0, 0)
+    for name, out in both(mp, q, cache, stats, kv, rows).items():
+        assert not out.isnan().any(), name
+        check_rows(out, want, tol, name)
