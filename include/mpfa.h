@@ -461,8 +461,9 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, siz
  *
  * workspace: 16-byte aligned, at least the plan's workspace_bytes for the same
  * arguments; its contents on entry are ignored.  Calls (and captured graphs)
- * that may overlap need workspaces of their own; the workspace and the items
- * of a captured call live as long as its graph.
+ * that may overlap need workspaces of their own.  The workspace and the items
+ * stay as they are until the call has ended on its stream, those of a captured
+ * call as long as its graph.
  */
 typedef struct {       /* a block of rows, or a part of one (prefill plans)               */
     int32_t seq, row;  /* sequence and its first row                                      */

@@ -364,16 +364,19 @@ def _want(ok, what):
 
 
 def _call(name, dev, stream, *args):
-    """The library call on the tensors' device (made current for it) and its current stream."""
+    """The library call on the tensors' device (made current for it) and its current stream, or the
+    given one; returns the stream's handle."""
     import torch
     if dev < 0:
         raise ValueError(f"{name}: tensors on a GPU are wanted")
     if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
-            return _check(getattr(lib(), name)(*args, _stream(stream)), name)
-    rc = getattr(lib(), name)(*args, _stream(stream))
+            return _call(name, dev, stream, *args)
+    on = _stream(stream)
+    rc = getattr(lib(), name)(*args, on)
     if rc:
         _check(rc, name)
+    return on
 
 
 class _Tensors:
@@ -436,10 +439,16 @@ class SeqStats4(_Tensors):
 class Kv4Plan:
     """How a prefill or decode call is cut, and its workspace.  A plan serves one call at a time.
     A decode plan holds for every length up to those it was made for, a prefill plan for its
-    row counts and lengths alone."""
+    row counts and lengths alone.
 
-    def __init__(self, what, workspace, **kw):
+    Its workspace and items are made on the current stream.  A call on another stream waits for
+    that one first, as for any tensor (Stream.wait_stream); the plan may be dropped as soon as
+    the call returns, whichever stream it is on.  The plan of a captured call lives as long as
+    the graph."""
+
+    def __init__(self, what, workspace, home=None, **kw):
         self.what, self.workspace = what, workspace
+        self.home = home   # handle of the stream that the workspace and the items were made on
         self.partition_tokens = self.max_partitions = self.n_items = self.n_merges = self.n_states = self.half = 0
         self.q_tokens = self.flags = self.max_rows = 0
         self.items = None
@@ -467,6 +476,12 @@ def _workspace(size, dev):
     return torch.empty(size, dtype=torch.uint8, device=dev) if size else None
 
 
+def _home(dev):
+    """Handle of the stream that tensors of the device are made on now."""
+    import torch
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
 def kv4_prefill_plan(rows_host, kv_len_host, h_q: int, h_kv: int, window=0, sinks=0, device="cuda") -> Kv4Plan:
     """mpfa_kv4_prefill_plan, its items on the device and its workspace: rows and keys (the call's
     rows included) per sequence."""
@@ -487,7 +502,7 @@ def kv4_prefill_plan(rows_host, kv_len_host, h_q: int, h_kv: int, window=0, sink
         room = n.value + merges.value
     _check(rc, "mpfa_kv4_prefill_plan")
     used = items[:n.value + merges.value]
-    return Kv4Plan(("prefill", rows.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), n_items=n.value,
+    return Kv4Plan(("prefill", rows.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), _home(dev), n_items=n.value,
                    n_merges=merges.value, n_states=states.value, half=half.value, max_rows=int(rows.max()),
                    items=torch.from_numpy(used).to(dev) if n.value else None)
 
@@ -500,7 +515,7 @@ def kv4_decode_plan(kv_len_host, h_q: int, h_kv: int, q_tokens=1, window=0, sink
     part, maxp, size = C.c_int32(0), C.c_int32(0), C.c_size_t(0)
     _check(lib().mpfa_kv4_decode_plan(kv.size, kv.ctypes.data, h_q, h_kv, q_tokens, window, sinks, flags, cus, C.byref(part),
                                       C.byref(maxp), C.byref(size)), "mpfa_kv4_decode_plan")
-    return Kv4Plan(("decode", kv.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), partition_tokens=part.value,
+    return Kv4Plan(("decode", kv.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), _home(dev), partition_tokens=part.value,
                    max_partitions=maxp.value, q_tokens=q_tokens, flags=flags)
 
 
@@ -560,7 +575,11 @@ def _kv4_attn(what, kind, q, cache, stats, cu, q_start, kv_len, page_table, out,
     a = Kv4AttnArgs(batch, h_q, h_kv, HEAD_DIM, page_table.shape[1], shape[0], max_seqlen_q, cut[0], window, sinks, *cut[1:],
                     stride, cu, q_start, items, kv_len.data_ptr(), page_table.data_ptr(), q.data_ptr(), cache._c,
                     stats._at["k_tscale"], stats._at["v_tscale"], out.data_ptr())
-    _call("mpfa_kv4_" + kind, dev, stream, C.byref(a), _ptr(ws), 0 if ws is None else ws.numel())
+    on = _call("mpfa_kv4_" + kind, dev, stream, C.byref(a), _ptr(ws), 0 if ws is None else ws.numel())
+    if plan is not None and on != plan.home:   # the plan's memory is not reused before this stream has passed the call
+        for t in (ws, plan.items):
+            if t is not None:
+                t.record_stream(torch.cuda.ExternalStream(on, device=dev))
 
 
 def kv4_prefill(q, cache: PagedCache4, stats: SeqStats4, cu_seqlens_q, q_start, kv_len, page_table, out, plan=None,

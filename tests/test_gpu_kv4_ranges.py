@@ -76,3 +76,32 @@ def test_small_queries_against_large_keys(mp, q_exp):
     for name, out in both(mp, q, cache, stats, kv, rows).items():
         assert not out.isnan().any(), name
         check_rows(out, want, tol, name)
+
+
+# ------------------------------------------------------------------ plans used on another stream
+@pytest.mark.parametrize("prefill", [False, True])
+def test_plan_dropped_after_a_call_on_another_stream(mp, prefill):
+    """Its memory is not handed out again before the call has ended."""
+    print(f"plan dropped behind a call on another stream, prefill {prefill}", flush=True)
+    kv, h_q, h_kv, r = [9000], 8, 2, 2
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [r], 29)
+    table, kv_len, out = rows.cuda(), i32(kv), torch.full_like(q, math.nan)
+    cu, start = cumulative([r]), i32([kv[0] - r])
+    plan = mp.kv4_prefill_plan([r], kv, h_q, h_kv) if prefill else mp.kv4_decode_plan(kv, h_q, h_kv, r)
+    size, at = plan.workspace.numel(), {t.data_ptr() for t in (plan.workspace, plan.items) if t is not None}
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(200_000_000)   # the call waits behind it
+    if prefill:
+        mp.kv4_prefill(q, cache, stats, cu, start, kv_len, table, out, plan, stream=other)
+    else:
+        mp.kv4_decode(q, cache, stats, kv_len, table, out, plan, stream=other)
+    items = 0 if plan.items is None else plan.items.numel()
+    del plan
+    new = [torch.empty(size, dtype=torch.uint8, device="cuda") for _ in range(3)] + \
+        [torch.empty(items, dtype=torch.int32, device="cuda") for _ in range(3 if items else 0)]
+    assert not other.query(), "the other stream was to be busy still"
+    assert not at & {t.data_ptr() for t in new}
+    other.synchronize()
+    check_prefill(q, out, rows, cache, stats, [r], [kv[0] - r], 0, 0)

@@ -1,0 +1,76 @@
+"""A plan's workspace and items belong to the plan, which a caller may drop as soon as a call
+returns: on a stream other than the one they were made on they are recorded as in use there."""
+import types
+
+import pytest
+import torch
+
+from tests.test_abi_fuzz import mp  # noqa: F401
+
+
+class Memory:
+    """What the binding asks of a plan's tensors."""
+
+    def __init__(self):
+        self.used_on = []
+
+    def get_device(self):
+        return -1
+
+    def data_ptr(self):
+        return 0x1000
+
+    def numel(self):
+        return 1 << 20
+
+    def record_stream(self, stream):
+        self.used_on.append(stream.cuda_stream)
+
+
+class Library:
+    """Accepts every call."""
+
+    def __getattr__(self, name):
+        return lambda *args: 0
+
+
+@pytest.fixture
+def launches(mp, monkeypatch):   # noqa: F811
+    """The binding with host tensors taken for a device's, its stream 7 the current one."""
+    monkeypatch.setattr(mp, "lib", Library)
+    call = mp._call
+    monkeypatch.setattr(mp, "_call", lambda name, dev, stream, *args: call(name, 0, stream, *args))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(mp, "_stream", lambda stream: 7 if stream is None else stream.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: types.SimpleNamespace(cuda_stream=handle))
+    i32 = dict(dtype=torch.int32)
+    c, s = mp.PagedCache4(2, 2, device="cpu"), mp.SeqStats4(1, 2, device="cpu")
+    q, one, table = torch.zeros(1, 4, 128, dtype=torch.bfloat16), torch.ones(1, **i32), torch.zeros(1, 1, **i32)
+
+    def decode(plan, stream=None):
+        mp.kv4_decode(q, c, s, one, table, torch.empty_like(q), plan, stream=stream)
+
+    def prefill(plan, stream=None):
+        mp.kv4_prefill(q, c, s, torch.tensor([0, 1], **i32), one * 0, one, table, torch.empty_like(q), plan, stream=stream)
+
+    return decode, prefill
+
+
+def decode_plan(mp, **kw):   # noqa: F811
+    return mp.Kv4Plan(("decode", 1, 4, 2, 0, 0), Memory(), partition_tokens=128, max_partitions=1, q_tokens=1, **kw)
+
+
+def prefill_plan(mp, **kw):   # noqa: F811
+    return mp.Kv4Plan(("prefill", 1, 4, 2, 0, 0), Memory(), n_items=2, n_merges=1, n_states=2, max_rows=1, items=Memory(), **kw)
+
+
+@pytest.mark.parametrize("home,stream,used_on", [(7, None, []), (3, None, [7]), (7, 5, [5]), (5, 5, []), (None, None, [7])])
+def test_memory_of_a_plan_is_recorded_on_another_stream(mp, launches, home, stream, used_on):   # noqa: F811
+    decode, prefill = launches
+    on = None if stream is None else types.SimpleNamespace(cuda_stream=stream)
+    plan = decode_plan(mp, home=home)
+    decode(plan, on)
+    assert plan.workspace.used_on == used_on
+    plan = prefill_plan(mp, home=home)
+    prefill(plan, on)
+    assert plan.workspace.used_on == used_on and plan.items.used_on == used_on
