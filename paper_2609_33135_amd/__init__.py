@@ -450,7 +450,7 @@ class Kv4Plan:
         self.what, self.workspace = what, workspace
         self.home = home   # handle of the stream that the workspace and the items were made on
         self.partition_tokens = self.max_partitions = self.n_items = self.n_merges = self.n_states = self.half = 0
-        self.q_tokens = self.flags = self.max_rows = 0
+        self.q_tokens = self.flags = self.max_rows = self.rows = 0
         self.items = None
         self.__dict__.update(kw)
 
@@ -503,7 +503,7 @@ def kv4_prefill_plan(rows_host, kv_len_host, h_q: int, h_kv: int, window=0, sink
     _check(rc, "mpfa_kv4_prefill_plan")
     used = items[:n.value + merges.value]
     return Kv4Plan(("prefill", rows.size, h_q, h_kv, window, sinks), _workspace(size.value, dev), _home(dev), n_items=n.value,
-                   n_merges=merges.value, n_states=states.value, half=half.value, max_rows=int(rows.max()),
+                   n_merges=merges.value, n_states=states.value, half=half.value, max_rows=int(rows.max()), rows=int(rows.sum()),
                    items=torch.from_numpy(used).to(dev) if n.value else None)
 
 
@@ -585,11 +585,14 @@ def _kv4_attn(what, kind, q, cache, stats, cu, q_start, kv_len, page_table, out,
 def kv4_prefill(q, cache: PagedCache4, stats: SeqStats4, cu_seqlens_q, q_start, kv_len, page_table, out, plan=None,
                 window=0, sinks=0, max_seqlen_q=None, stream=None):
     """mpfa_kv4_prefill: causal attention of bf16 queries [T][Hq][128] (tokens may lie apart) over the
-    4-bit cache; plan: kv4_prefill_plan of the same window and sinks (None: one pass).  max_seqlen_q: the
-    most rows of one sequence (by default the plan's, or T without one)."""
+    4-bit cache; plan: kv4_prefill_plan of the same window and sinks (None: one pass), whose rows are computed
+    and what q has more is padding.  max_seqlen_q: the most rows of one sequence (by default the plan's, or T
+    without one)."""
     import torch
     if max_seqlen_q is None:
         max_seqlen_q = q.shape[0] if plan is None else plan.max_rows
+    if plan is not None and q.shape[0] < plan.rows:
+        raise ValueError(f"kv4_prefill: q has {q.shape[0]} rows, the plan was made for {plan.rows}")
     _same("kv4_prefill", torch.int32, cache.device, cu_seqlens_q, q_start)
     if cu_seqlens_q.numel() != kv_len.numel() + 1 or q_start.numel() != kv_len.numel():
         raise ValueError("kv4_prefill: shapes")

@@ -411,9 +411,13 @@ __global__ __launch_bounds__(512, 2) void kv4_prefill_plan_kernel(Kv4AttnParams 
   if (x.row >= nq) return;
   const Kv4Tiles tiles = kv4_tiles(qs + x.row, qs + min(x.row + tm, nq) - 1, p.window, p.sinks);
   const int v1 = min(x.last, tiles.nt);
-  if (x.first >= v1) return;
-  prefill_item<HALF>(p, sm, x.seq, hk, x.row, tm, nq, q0, tiles, x.first, v1,
-                     x.state < 0 ? nullptr : p.states + ((int64_t)x.state * p.h_kv + hk) * state_floats(HALF));
+  float* state = x.state < 0 ? nullptr : p.states + ((int64_t)x.state * p.h_kv + hk) * state_floats(HALF);
+  if (x.first >= v1) {   // a plan of a longer prompt: a part without tiles adds nothing to its block
+    if (state)
+      for (int i = threadIdx.x; i < state_floats(HALF); i += 512) state[i] = i % kKv4State == 0 ? -INFINITY : 0.0f;
+    return;
+  }
+  prefill_item<HALF>(p, sm, x.seq, hk, x.row, tm, nq, q0, tiles, x.first, v1, state);
 }
 
 // Without one: items of 256 rows, the later (longer) ones first.  Blocks are dealt

@@ -78,6 +78,25 @@ def test_small_queries_against_large_keys(mp, q_exp):
         check_rows(out, want, tol, name)
 
 
+# ------------------------------------------------------------------ plans of other lengths
+@pytest.mark.parametrize("new,ctx", [([70], [500]), ([40], [0]), ([70], [100])])
+def test_prefill_by_a_plan_for_longer_prompts(mp, new, ctx):
+    """Parts of a cut block that have no tiles left add nothing to it."""
+    print(f"prefill {new} behind {ctx} by a plan for 70 behind 30000", flush=True)
+    h_q, h_kv = 8, 2
+    kv = [a + b for a, b in zip(new, ctx)]
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, new, 43)
+    q = torch.cat([q, torch.zeros(70 - new[0], h_q, D, device="cuda").bfloat16()])
+    plan = mp.kv4_prefill_plan([70], [30000], h_q, h_kv)
+    assert plan.n_merges > 0
+    plan.workspace.fill_(255)
+    out = torch.full_like(q, 7.0)
+    mp.kv4_prefill(q, cache, stats, cumulative(new), i32(ctx), i32(kv), rows.cuda(), out, plan)
+    torch.cuda.synchronize()
+    check_prefill(q[:new[0]], out[:new[0]], rows, cache, stats, new, ctx, 0, 0)
+    assert (out[new[0]:] == 7).all()
+
+
 # ------------------------------------------------------------------ plans used on another stream
 @pytest.mark.parametrize("prefill", [False, True])
 def test_plan_dropped_after_a_call_on_another_stream(mp, prefill):

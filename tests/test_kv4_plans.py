@@ -1,5 +1,6 @@
-"""A plan's workspace and items belong to the plan, which a caller may drop as soon as a call
-returns: on a stream other than the one they were made on they are recorded as in use there."""
+"""Plans and the calls that use them.  A plan's workspace and items belong to the plan, which a
+caller may drop as soon as a call returns: on a stream other than the one they were made on they
+are recorded as in use there."""
 import types
 
 import pytest
@@ -74,3 +75,10 @@ def test_memory_of_a_plan_is_recorded_on_another_stream(mp, launches, home, stre
     plan = prefill_plan(mp, home=home)
     prefill(plan, on)
     assert plan.workspace.used_on == used_on and plan.items.used_on == used_on
+
+
+def test_prefill_plan_of_more_rows_is_refused(mp, launches):   # noqa: F811
+    _, prefill = launches   # one row
+    prefill(prefill_plan(mp, rows=1))
+    with pytest.raises(ValueError, match="rows"):
+        prefill(prefill_plan(mp, rows=2))
