@@ -401,7 +401,8 @@ typedef struct {
  */
 typedef struct {
     int32_t batch;               /* 1 .. 65535                                     */
-    int32_t total_tokens;        /* cu_seqlens[batch] (host copy)                  */
+    int32_t total_tokens;        /* of k, v, slot_mapping: cu_seqlens[batch], or
+                                    more (padding, neither read nor written)       */
     int32_t max_seqlen;          /* most tokens of one sequence in this call       */
     int32_t h_kv;                /* 1 .. 32                                        */
     int32_t head_dim;            /* must be 128                                    */
@@ -477,7 +478,8 @@ typedef struct {
     int32_t h_q, h_kv;           /* h_q <= 256, h_kv <= 32, h_q % h_kv == 0        */
     int32_t head_dim;            /* must be 128                                    */
     int32_t max_pages;           /* page_table row length                          */
-    int32_t total_tokens;        /* prefill: cu_seqlens_q[batch] (host copy)       */
+    int32_t total_tokens;        /* prefill, of q and out: cu_seqlens_q[batch], or
+                                    more (padding, neither read nor written)       */
     int32_t max_seqlen_q;        /* prefill: most rows of one sequence             */
     int32_t q_tokens;            /* decode: rows per sequence                      */
     int32_t window;              /* 0: no window                                   */

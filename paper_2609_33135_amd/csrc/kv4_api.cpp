@@ -229,16 +229,17 @@ mpfa_status check_write(const mpfa_kv4_write_args* a, hipStream_t s) {
   if (hipStreamSynchronize(s) != hipSuccess) return MPFA_ERR_HIP;
   std::vector<int32_t> cu;
   std::vector<int64_t> slots;
-  if (!to_host(a->cu_seqlens, (size_t)a->batch + 1, cu) || !to_host(a->slot_mapping, (size_t)a->total_tokens, slots))
-    return MPFA_ERR_HIP;
-  if (cu[0] != 0 || cu[a->batch] != a->total_tokens) return MPFA_ERR_DATA;
+  if (!to_host(a->cu_seqlens, (size_t)a->batch + 1, cu)) return MPFA_ERR_HIP;
+  if (cu[0] != 0 || cu[a->batch] > a->total_tokens) return MPFA_ERR_DATA;
   for (int b = 0; b < a->batch; ++b)
     if (cu[b + 1] < cu[b] || cu[b + 1] - cu[b] > a->max_seqlen) return MPFA_ERR_DATA;
+  const int64_t tokens = cu[a->batch];   // the rest is padding
+  if (!to_host(a->slot_mapping, (size_t)tokens, slots)) return MPFA_ERR_HIP;
   std::sort(slots.begin(), slots.end());
   for (size_t i = 0; i < slots.size(); ++i)   // negative: padding
     if (slots[i] >= 64 * a->cache.num_pages || (i > 0 && slots[i] >= 0 && slots[i] == slots[i - 1])) return MPFA_ERR_DATA;
-  mpfa_status st = scan_rows(a->k, a->total_tokens, (int64_t)a->h_kv * MPFA_HEAD_DIM, a->k_stride, s);
-  if (st == MPFA_OK) st = scan_rows(a->v, a->total_tokens, (int64_t)a->h_kv * MPFA_HEAD_DIM, a->v_stride, s);
+  mpfa_status st = scan_rows(a->k, tokens, (int64_t)a->h_kv * MPFA_HEAD_DIM, a->k_stride, s);
+  if (st == MPFA_OK) st = scan_rows(a->v, tokens, (int64_t)a->h_kv * MPFA_HEAD_DIM, a->v_stride, s);
   return st;
 }
 
@@ -264,7 +265,7 @@ mpfa_status check_attn(const mpfa_kv4_attn_args* a, bool decode, hipStream_t s) 
     const int n = cu[b + 1] - cu[b];
     if (n < 0 || n > a->max_seqlen_q || qs[b] < 0 || (int64_t)qs[b] + n > kv[b]) return MPFA_ERR_DATA;
   }
-  if (!decode && (cu[0] != 0 || cu[a->batch] != a->total_tokens)) return MPFA_ERR_DATA;
+  if (!decode && (cu[0] != 0 || cu[a->batch] > a->total_tokens)) return MPFA_ERR_DATA;
   if (!items.empty()) {   // every block once, with all the tiles that it sees, its states inside the workspace
     const int tm = item_tokens(a->h_q / a->h_kv, a->half);
     const int64_t room = a->n_states;

@@ -97,6 +97,38 @@ def test_prefill_by_a_plan_for_longer_prompts(mp, new, ctx):
     assert (out[new[0]:] == 7).all()
 
 
+# ------------------------------------------------------------------ padded batches
+def test_debug_library_takes_padded_batches(mp, monkeypatch):
+    """Rows behind the last sequence are neither read nor written, whatever they and their slots hold."""
+    print("debug library: padded batches", flush=True)
+    monkeypatch.setattr(mp, "lib", mp.debug_lib)
+    lens, h_q, h_kv, pad = [70, 5], 8, 2, 9
+    T, B = sum(lens), len(lens)
+    rows = R.page_rows(lens, 6, 2)
+    val = lambda h: torch.randn(T + pad, h, D, device="cuda").bfloat16()
+    q, k, v = val(h_q), val(h_kv), val(h_kv)
+    for x in (q, k, v):
+        x[T:] = math.nan
+    cu, slots = cumulative(lens), torch.cat([slots_of(rows, [0] * B, lens), torch.full((pad,), 5, dtype=torch.int64, device="cuda")])
+    cache, stats = mp.PagedCache4(6, h_kv), mp.SeqStats4(B, h_kv)
+    ws = torch.empty(mp.kv4_write_workspace_size(B, T + pad, h_kv), dtype=torch.uint8, device="cuda")
+    ko = torch.full_like(k, 7.0)
+    mp.kv4_write(k, v, cu, slots, cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, max(lens), workspace=ws, k_out=ko)
+    out = torch.full_like(q, 7.0)
+    args = (q, cache, stats, cu, i32([0] * B), i32(lens), rows.cuda(), out)
+    mp.kv4_prefill(*args)
+    torch.cuda.synchronize()
+    check_write(mp, cache, rows, [0] * B, lens, k, v, stats, True, cu)
+    check_prefill(q[:T], out[:T], rows, cache, stats, lens, [0] * B, 0, 0)
+    mp.kv4_prefill(*args, mp.kv4_prefill_plan(lens, lens, h_q, h_kv))
+    torch.cuda.synchronize()
+    check_prefill(q[:T], out[:T], rows, cache, stats, lens, [0] * B, 0, 0)
+    assert (out[T:] == 7).all() and (ko[T:] == 7).all()
+    with pytest.raises(mp.MpfaError) as e:   # fewer rows than the sequences say
+        mp.kv4_prefill(q[:T - 1], cache, stats, cu, i32([0] * B), i32(lens), rows.cuda(), out[:T - 1])
+    assert e.value.status == mp.MPFA_ERR_DATA
+
+
 # ------------------------------------------------------------------ plans used on another stream
 @pytest.mark.parametrize("prefill", [False, True])
 def test_plan_dropped_after_a_call_on_another_stream(mp, prefill):
