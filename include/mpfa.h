@@ -386,9 +386,10 @@ typedef struct {
  *  - Without MPFA_SMOOTH, K is not centered and k_mean is not read.
  *  - K - Kbar in FP32, then per 16 channels scale = E4M3_RNE_sat(amax / (6 t)),
  *    codes = E2M1_RNE_sat(x / (t * scale)); V the same without a mean.
- *  - A token whose slot is negative or past the cache (padding) is not stored;
- *    it does count in the statistics.  Two tokens of a call may not have the
- *    same slot (the debug library returns MPFA_ERR_DATA).
+ *  - A token whose slot is negative is padding: it is not stored, but does count
+ *    in the statistics.  So it goes with a slot past the cache, which is a
+ *    caller's mistake all the same: the debug library returns MPFA_ERR_DATA
+ *    for it, and where two tokens of a call have the same slot.
  *  - With cache.weights the weight of every stored slot becomes 0.
  *  - k_out, v_out (or NULL): the values that the cache now stands for, K
  *    without its mean (every value is exact in BF16).
