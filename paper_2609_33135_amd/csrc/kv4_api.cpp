@@ -68,6 +68,15 @@ bool decode_space(int batch, int h_q, int q_tokens, int partition_tokens, int ma
   return true;
 }
 
+// Whether a decode's grids stay below 2^32 threads, and its keys within the lengths there can be:
+// partitions times column chunks, and with weights a workgroup per kKv4WeightKeys keys of a KV
+// head beside one per row at most.
+bool decode_grids_ok(int h_q, int h_kv, int q_tokens, int64_t partition_tokens, int64_t max_partitions, bool weights) {
+  const int64_t cols = (int64_t)q_tokens * (h_q / h_kv), keys = max_partitions * partition_tokens;
+  if (max_partitions * ((cols + 15) / 16) > (1 << 24) || keys > ((int64_t)1 << 30)) return false;
+  return !weights || (int64_t)q_tokens * h_q + (keys + mpfa::kKv4WeightKeys - 1) / mpfa::kKv4WeightKeys * h_kv <= (int64_t)UINT32_MAX / 256;
+}
+
 // What prefill and decode share.
 mpfa_status attn_params(const mpfa_kv4_attn_args* a, mpfa::Kv4AttnParams& p) {
   if (!a) return MPFA_ERR_INVALID;
@@ -543,6 +552,7 @@ mpfa_status mpfa_kv4_decode_plan(int32_t batch, const int32_t* kv_len_host, int3
     if (t >= most) break;   // one partition each: longer ones change nothing
   }
   const int64_t parts = (bound + part - 1) / part;
+  if (!decode_grids_ok(h_q, h_kv, q_tokens, part * MPFA_KV_TILE, parts, flags & MPFA_KV4_WEIGHTS)) return MPFA_ERR_UNSUPPORTED;
   DecodeSpace s;
   if (!decode_space(batch, h_q, q_tokens, (int)part * MPFA_KV_TILE, (int)parts, flags & MPFA_KV4_WEIGHTS, &s)) return MPFA_ERR_INVALID;
   *partition_tokens = (int32_t)(part * MPFA_KV_TILE);
@@ -559,9 +569,7 @@ mpfa_status mpfa_kv4_decode(const mpfa_kv4_attn_args* a, void* workspace, size_t
   if (a->q_tokens < 1 || a->q_tokens > 65535 || a->partition_tokens < 1 || a->max_partitions < 1) return MPFA_ERR_INVALID;
   if (weights && !a->cache.weights) return MPFA_ERR_INVALID;
   p.q_tokens = a->q_tokens;
-  // partitions times column chunks: their grid stays below 2^32 threads
-  if ((int64_t)a->max_partitions * (((int64_t)a->q_tokens * (a->h_q / a->h_kv) + 15) / 16) > (1 << 24)) return MPFA_ERR_UNSUPPORTED;
-  if ((int64_t)a->max_partitions * a->partition_tokens > ((int64_t)1 << 30)) return MPFA_ERR_UNSUPPORTED;
+  if (!decode_grids_ok(a->h_q, a->h_kv, a->q_tokens, a->partition_tokens, a->max_partitions, weights)) return MPFA_ERR_UNSUPPORTED;
   DecodeSpace s;
   if (!decode_space(a->batch, a->h_q, a->q_tokens, a->partition_tokens, a->max_partitions, weights, &s)) return MPFA_ERR_INVALID;
   if (!workspace || workspace_bytes < s.states + s.scores || !aligned16(workspace)) return MPFA_ERR_WORKSPACE;

@@ -375,7 +375,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, COLS == 16 ? 3 : 2) void kv4_dec
 // Rows (token, query head): a wave each, four to a workgroup, or a workgroup of four waves
 // each where there are many states (a wave keeps eight in flight).
 constexpr int kManyStates = 16;
-constexpr int kWeightKeys = 1024;   // per workgroup, four per thread
+constexpr int kWeightKeys = kKv4WeightKeys;
 constexpr int kWeightRows = 64;     // whose maxima and sums are held at a time
 
 template <int WAVES>

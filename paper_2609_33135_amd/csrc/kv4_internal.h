@@ -16,6 +16,7 @@ constexpr int kKv4StatTokens = 128;   // fewest tokens per statistics partial
 constexpr int kKv4StatBytes = 128 * (8 + 4 + 4) + 16;
 constexpr int kKv4WriteTokens = 32;   // tokens per workgroup of 256 threads of the write pass
 constexpr int kKv4Rows = 256;         // most query rows (tokens x heads of one KV head) of a prefill item
+constexpr int kKv4WeightKeys = 1024;  // keys of a KV head whose weights a workgroup adds, four per thread
 constexpr int kKv4State = 130;        // floats of a partition state: m, l, O[128]
 
 // Planes of the cache; page pg, KV head h, slot o.

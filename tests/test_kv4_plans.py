@@ -1,6 +1,7 @@
 """Plans and the calls that use them.  A plan's workspace and items belong to the plan, which a
 caller may drop as soon as a call returns: on a stream other than the one they were made on they
 are recorded as in use there."""
+import ctypes as C
 import types
 
 import pytest
@@ -82,3 +83,19 @@ def test_prefill_plan_of_more_rows_is_refused(mp, launches):   # noqa: F811
     prefill(prefill_plan(mp, rows=1))
     with pytest.raises(ValueError, match="rows"):
         prefill(prefill_plan(mp, rows=2))
+
+
+def test_grid_of_the_weights_stays_below_its_bound(mp):   # noqa: F811
+    """2^30 keys of 32 KV heads, 1024 to a workgroup: 2^25 workgroups of 256 threads are more than a grid takes."""
+    a = mp.Kv4AttnArgs(batch=1, h_q=32, h_kv=32, head_dim=128, max_pages=1 << 24, q_tokens=1, q_stride=32 * 128, flags=mp.KV4_WEIGHTS,
+                       partition_tokens=1 << 20, max_partitions=1 << 10, cache=mp.Kv4Cache(num_pages=1 << 24))
+    for n in ("k_codes", "k_scales", "v_codes", "v_scales", "weights"):
+        setattr(a.cache, n, 0x1000)
+    for n in ("kv_len", "page_table", "q", "k_tscale", "v_tscale", "out"):
+        setattr(a, n, 0x1000)   # never dereferenced
+    assert mp.lib().mpfa_kv4_decode(C.byref(a), 0x1000, 1 << 60, None) == mp.MPFA_ERR_UNSUPPORTED
+    out = C.c_int32(0), C.c_int32(0), C.c_size_t(0)
+    for n, flags, status in ((1 << 30, mp.KV4_WEIGHTS, mp.MPFA_ERR_UNSUPPORTED), ((1 << 30) + 1, 0, mp.MPFA_ERR_UNSUPPORTED),
+                             (1 << 28, mp.KV4_WEIGHTS, mp.MPFA_OK), (1 << 30, 0, mp.MPFA_OK)):
+        kv = (C.c_int32 * 1)(n)   # a plan that no call would take is none
+        assert mp.lib().mpfa_kv4_decode_plan(1, C.addressof(kv), 32, 32, 1, 0, 0, flags, 256, *(C.byref(x) for x in out)) == status, n
