@@ -398,7 +398,9 @@ typedef struct {
  * k_mean, k_out, v_out are 16-byte aligned.
  * workspace: at least mpfa_kv4_write_workspace_size bytes with
  * MPFA_COMPUTE_STATS (16-byte aligned), else unused; its contents on entry are
- * ignored.  Deterministic: identical inputs give identical bytes.
+ * ignored.  Deterministic: identical inputs give identical bytes.  A sequence
+ * gets the same bytes whatever shares its call where its sums are exact, which
+ * they are unless the exponents of a K channel span more than 45 - log2(tokens).
  */
 typedef struct {
     int32_t batch;               /* 1 .. 65535                                     */

@@ -1,9 +1,11 @@
 // kv4_write.hip -- K and V into the 4-bit cache for gfx950: on a sequence's first call
 // its statistics (K means, tensor scales), then NVFP4 rows of both.
 //
-// Every rounding is fixed, so the codes are bit-reproducible: the means come from FP64
-// sums (bf16 tokens add exactly in 53 bits, in any order), centering is one FP32
-// subtraction, and x -> fl(x - mean) is monotone, so the largest |K - mean| is reached
+// Every rounding is fixed, so a call's codes are bit-reproducible.  The means come from FP64
+// sums: bf16 tokens add exactly in 53 bits, in any order, where the exponents of a channel span
+// at most 45 - log2(tokens); beyond that the order counts, which is fixed for a call but goes by
+// the call's token counts (how many tokens make a partial, who adds the partials).  Centering is
+// one FP32 subtraction, and x -> fl(x - mean) is monotone, so the largest |K - mean| is reached
 // at a channel's maximum or minimum and the tokens are read once for it.
 #include "kv4_device.h"
 

@@ -11,6 +11,62 @@ from tests.test_gpu_kv4 import (D, PAGE, attn_case, check_prefill, check_rows, c
 pytestmark = pytest.mark.gpu
 
 
+# ------------------------------------------------------------------ weights over many keys and partitions
+@pytest.mark.parametrize("part", [None, 128, 640])
+@pytest.mark.parametrize("h_q,h_kv,q_tokens,window,sinks", [(8, 2, 1, 0, 0), (10, 2, 4, 0, 0), (12, 3, 1, 3000, 70), (80, 1, 1, 0, 0)])
+def test_weights_of_long_contexts(mp, h_q, h_kv, q_tokens, window, sinks, part):
+    """More than 64 partitions, partitions of several tiles, more keys than one workgroup adds, more rows than
+    are held at a time; by the plan's own cut and by others."""
+    kv = [9001, 1030, 130]
+    print(f"weights of {kv}, heads {h_q}:{h_kv}, rows {q_tokens}, window {window}, parts {part}", flush=True)
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, [q_tokens] * len(kv), 23, weights=True)
+    before = cache.weights.clone()
+    longest = 12000
+    plan = mp.kv4_decode_plan([longest] * len(kv), h_q, h_kv, q_tokens, window, sinks, weights=True)
+    if part:
+        plan.partition_tokens, plan.max_partitions = part, -(-longest // part)
+        r = len(kv) * q_tokens * h_q
+        states = (r * plan.max_partitions * 130 * 4 + 255) // 256 * 256
+        plan.workspace = torch.empty(states + r * plan.max_partitions * part * 4, dtype=torch.uint8, device="cuda")
+    plan.workspace.fill_(255)
+    out = torch.full_like(q, math.nan)
+    mp.kv4_decode(q, cache, stats, i32(kv), rows.cuda(), out, plan, window=window, sinks=sinks)
+    torch.cuda.synchronize()
+    touched = torch.zeros_like(before, dtype=torch.bool)
+    for b, n in enumerate(kv):
+        x = slice(b * q_tokens, (b + 1) * q_tokens)
+        toks = R.Tokens(cache, rows[b].cuda(), n)
+        want, tol, share, stol = R.attention(q[x], toks, stats.k_tscale[b], stats.v_tscale[b], n - q_tokens, window, sinks)
+        check_rows(out[x], want, tol, f"sequence {b}")
+        i = torch.arange(n, device="cuda")
+        pg, o = rows[b].cuda()[i // PAGE].long(), i % PAGE
+        w0 = before[pg, :, o].double()
+        off = (toks.weights.double() - (w0 + share)).abs() > stol + 2.0 ** -24 * (w0 + share)
+        assert not off.any(), f"sequence {b}: {int(off.sum())} weights off, the first at {off.nonzero()[0].tolist()}"
+        touched[pg, :, o] = True
+    assert torch.equal(cache.weights[~touched].nan_to_num(5.0), before[~touched].nan_to_num(5.0))
+
+
+# ------------------------------------------------------------------ statistics of many prompts together
+@pytest.mark.parametrize("lens,h_kv", [([(i * 37) % 97 + 500 for i in range(60)] + [0, 1, 1500], 2), ([4100] * 8 + [700], 1)])
+def test_write_of_many_prompts_together(mp, lens, h_kv):
+    """Partials of 512 tokens that the write pass itself finishes."""
+    T, B = sum(lens), len(lens)
+    assert T >= 32768 and -(-max(lens) // 512) <= 32
+    print(f"write {B} prompts, {T} tokens x {h_kv}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(h_kv)
+    rows = R.page_rows(lens, sum(-(-n // PAGE) for n in lens) + 2, 3)
+    k = (torch.randn(T, h_kv, D, generator=gen, device="cuda") + 2 * torch.randn(1, h_kv, D, generator=gen, device="cuda")).bfloat16()
+    v = torch.randn(T, h_kv, D, generator=gen, device="cuda").bfloat16()
+    cache, stats, cu = mp.PagedCache4(int(rows.max()) + 1, h_kv), mp.SeqStats4(B, h_kv), cumulative(lens)
+    before = [x.clone() for x in (stats.k_mean, stats.k_tscale)]
+    ws = torch.full((mp.kv4_write_workspace_size(B, T, h_kv),), 255, dtype=torch.uint8, device="cuda")
+    mp.kv4_write(k, v, cu, slots_of(rows, [0] * B, lens), cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, max(lens), workspace=ws)
+    torch.cuda.synchronize()
+    check_stats(stats, before, lens, k, v, True, cu)
+    check_write(mp, cache, rows, [0] * B, lens, k, v, stats, True, cu)
+
+
 # ------------------------------------------------------------------ scores of any size
 def both(mp, q, cache, stats, kv, rows, weights=False):
     """The call's rows by decode and by prefill, in one pass and in halves that split the keys."""
