@@ -436,7 +436,10 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, siz
  * with FP32 scores, maxima and sums and P rounded to FP16 (2^-11 of each P, or
  * 2^-40 of the row's largest where that is more), for every finite q, K and V.
  * A row that sees no key is 0.  h_q / h_kv may be anything from 1 to 256.
- * Keys at or past kv_len are never used, whatever their slots hold.
+ * Keys at or past kv_len are never used, whatever their slots hold.  The first
+ * ceil(kv_len / 64) entries of a sequence's row of the page table name pages of
+ * the cache also where no row sees them (before a window: they may be read,
+ * and given any written page, such as another sequence's).
  *
  * mpfa_kv4_prefill: query i of sequence b (token cu_seqlens_q[b] + i) is at
  * position q_start[b] + i; q_start[b] + its rows <= kv_len[b].  Without items
@@ -461,7 +464,7 @@ mpfa_status mpfa_kv4_write(const mpfa_kv4_write_args* args, void* workspace, siz
  * With MPFA_KV4_WEIGHTS, cache.weights[slot] += sum over the rows of the call
  * and the query heads of the KV head of softmax(S), for every visible key,
  * summed in a fixed order (no atomics).  Sequences of such a call may not
- * share pages.
+ * share pages, those before a window included.
  *
  * workspace: 16-byte aligned, at least the plan's workspace_bytes for the same
  * arguments; its contents on entry are ignored.  Calls (and captured graphs)
@@ -537,6 +540,10 @@ mpfa_status mpfa_kv4_decode(const mpfa_kv4_attn_args* args, void* workspace,
  *    order, and no two sequences of the call share a page.
  * Keys keep the positions they were rotated with; from then on positions,
  * windows and sinks count what is left in the cache.
+ * Weights come from mpfa_kv4_decode alone: the writer sets them to 0 and the
+ * prefill adds none.  To evict right behind a prompt, decode its last rows with
+ * MPFA_KV4_WEIGHTS first (q_tokens of them, the outputs are the prefill's);
+ * without, all weights tie and the first tokens stay.
  */
 typedef struct {
     int32_t batch;                 /* 1 .. 65535                                   */

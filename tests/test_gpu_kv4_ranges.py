@@ -212,3 +212,58 @@ def test_plan_dropped_after_a_call_on_another_stream(mp, prefill):
     assert not at & {t.data_ptr() for t in new}
     other.synchronize()
     check_prefill(q, out, rows, cache, stats, [r], [kv[0] - r], 0, 0)
+
+
+# ------------------------------------------------------------------ what the interface promises
+@pytest.mark.parametrize("kv,rows_n,window,sinks", [([700, 1500], 1, 100, 0), ([2000, 900], 5, 200, 70), ([1500, 1000], 40, 64, 3)])
+def test_pages_before_a_window_may_hold_anything_written(mp, kv, rows_n, window, sinks):
+    """Entries of pages that no row sees may name other sequences' pages: every output byte stays."""
+    print(f"{kv} keys, {rows_n} rows, window {window}: entries before it replaced", flush=True)
+    h_q, h_kv, n_rows = 8, 2, [rows_n] * len(kv)
+    rows, cache, stats, q = attn_case(mp, kv, h_q, h_kv, n_rows, 73)
+    other = rows.clone()
+    for b, n in enumerate(kv):
+        first = n - rows_n - window + 1   # first key of the first row's window
+        for pg in range(-(-n // PAGE)):
+            if pg * PAGE >= sinks and (pg + 1) * PAGE <= first:
+                other[b, pg] = rows[1 - b, pg % (min(kv) // PAGE)]   # a whole page of the other sequence
+    assert (other != rows).any(1).all()
+    outs = []
+    for table in (rows.cuda(), other.cuda()):
+        dec, pre, cut = (torch.full_like(q, math.nan) for _ in range(3))
+        att = dict(window=window, sinks=sinks)
+        args = (q, cache, stats, cumulative(n_rows), i32([n - rows_n for n in kv]), i32(kv), table)
+        mp.kv4_decode(q, cache, stats, i32(kv), table, dec, mp.kv4_decode_plan(kv, h_q, h_kv, rows_n, window, sinks), **att)
+        mp.kv4_prefill(*args, pre, max_seqlen_q=rows_n, **att)
+        mp.kv4_prefill(*args, cut, mp.kv4_prefill_plan(n_rows, kv, h_q, h_kv, window, sinks), **att)
+        outs.append((dec, pre, cut))
+    torch.cuda.synchronize()
+    for a, b in zip(*outs):
+        assert not a.isnan().any() and torch.equal(a, b)
+
+
+def test_eviction_right_behind_a_prompt(mp):
+    """The prompt's last rows decoded once more give its tokens their weights, and the prefill's outputs."""
+    print("eviction behind a prompt", flush=True)
+    T, n, h_q, h_kv, budget = 500, 32, 8, 2, 100
+    rows = R.page_rows([T], 10, 3)
+    table, kv_len, cu = rows.cuda(), i32([T]), cumulative([T])
+    cache, stats = mp.PagedCache4(10, h_kv, weights=True), mp.SeqStats4(1, h_kv)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn(T, h, D, generator=gen, device="cuda").bfloat16() for h in (h_q, h_kv, h_kv))
+    ws = torch.empty(mp.kv4_write_workspace_size(1, T, h_kv), dtype=torch.uint8, device="cuda")
+    mp.kv4_write(k, v, cu, slots_of(rows, [0], [T]), cache, stats, mp.SMOOTH | mp.COMPUTE_STATS, T, workspace=ws)
+    out, last = torch.empty_like(q), torch.empty_like(q[-n:])
+    mp.kv4_prefill(q, cache, stats, cu, i32([0]), kv_len, table, out, mp.kv4_prefill_plan([T], [T], h_q, h_kv))
+    mp.kv4_decode(q[-n:], cache, stats, kv_len, table, last, mp.kv4_decode_plan([T], h_q, h_kv, n, weights=True))
+    torch.cuda.synchronize()
+    toks = R.Tokens(cache, table[0], T)
+    want, tol, share, stol = R.attention(q[-n:], toks, stats.k_tscale[0], stats.v_tscale[0], T - n, 0, 0)
+    check_rows(last, want, tol, "decode")
+    check_rows(out[-n:], want, tol, "prefill")
+    assert ((toks.weights.double() - share).abs() <= stol + 2.0 ** -24 * share).all()
+    kept = torch.empty(1, h_kv, budget, dtype=torch.int32, device="cuda")
+    mp.kv4_evict(cache, kv_len, table, table, budget, kept, kv_len, sinks=4, recent=20, in_place=True)
+    torch.cuda.synchronize()
+    for h in range(h_kv):
+        assert kept[0, h].tolist() == R.keep(toks.weights[:, h].cpu(), budget, 4, 20)
