@@ -355,7 +355,7 @@ def _rows(what, t, heads, dev):
             shape[2] != HEAD_DIM or stride[2] != 1 or (heads > 1 and stride[1] != HEAD_DIM)):
         raise ValueError(f"{what}: bf16 [T][{heads}][{HEAD_DIM}] on device {dev} with contiguous heads is wanted, got "
                          f"{t.dtype} {tuple(shape)} strides {stride} on device {t.get_device()}")
-    return stride[0] if shape[0] > 1 else max(stride[0], heads * HEAD_DIM)
+    return stride[0] if shape[0] > 1 else heads * HEAD_DIM   # of one token any stride will do
 
 
 def _want(ok, what):

@@ -99,3 +99,10 @@ def test_grid_of_the_weights_stays_below_its_bound(mp):   # noqa: F811
                              (1 << 28, mp.KV4_WEIGHTS, mp.MPFA_OK), (1 << 30, 0, mp.MPFA_OK)):
         kv = (C.c_int32 * 1)(n)   # a plan that no call would take is none
         assert mp.lib().mpfa_kv4_decode_plan(1, C.addressof(kv), 32, 32, 1, 0, 0, flags, 256, *(C.byref(x) for x in out)) == status, n
+
+
+@pytest.mark.parametrize("tokens", [0, 1])
+@pytest.mark.parametrize("stride", [0, 1001, 1 << 33])
+def test_token_stride_of_a_single_token_does_not_matter(mp, tokens, stride):   # noqa: F811
+    x = torch.zeros(256, dtype=torch.bfloat16).as_strided((tokens, 2, 128), (stride, 128, 1))
+    assert mp._rows("x", x, 2, -1) == 256
