@@ -11,12 +11,14 @@
 // share the leading bytes (usually after two passes), each is compared with all of them.
 // Then two sweeps count and write the indices in order, each wave over a segment of its own.
 // The images stay in LDS, 32768 of them; what a longer sequence has more is read again each
-// sweep.  What bounds it: one compute unit, of whose 37000 cycles for 32768 tokens a third
+// sweep, a page at a time (65536 tokens 91 us, 131072 230).
+// What bounds it: one compute unit, of whose 37000 cycles for 32768 tokens a third
 // are the read of the weights (beside it the first histogram), a quarter the other sweep for
 // the threshold with the comparisons, a quarter the two sweeps for the indices; each spends
-// 10 to 20 instructions on 64 tokens.  32768 tokens to 4096, 8 heads: 17.7 us (76 with a
-// histogram per wave and the weights read each sweep; 32 with the images in registers; 23
-// with a sweep more for the first histogram and the places counted in vector registers).
+// 10 to 20 instructions on 64 tokens.  32768 tokens to 4096, 8 heads: 17.5 to 20 us over cards
+// (76 with a histogram per wave and the weights read each sweep; 32 with the images in
+// registers; 23 with a sweep more for the first histogram and the places counted in vector
+// registers).
 //
 // Move (kv4_move_kernel): destination place i takes source token kept[i] >= i.  With
 // separate pages the places are shared among workgroups; in place, a workgroup per half of
@@ -24,10 +26,11 @@
 // order, reading a chunk before it writes it: a later chunk's sources lie at or after its own
 // places, so no write reaches a token that is still to be read.  (The whole call in place,
 // by halves and by quarters: 32768 tokens to 4096, 8 heads, 117 and 51 us; 24 sequences to
-// 2048, 104 and 112, as the quarters read every line more than once.)
-// What bounds it: HBM lines.  A kept token brings the 256-byte V quad and the 128-byte line
-// of K codes that it lies in, about 450 bytes read for 148 where one token in six stays; 24
-// sequences to 2048 tokens, 8 heads: 47 us, about 5 TB/s of such lines.
+// 2048, 104 and 112, as the quarters read every line more than once.  Of it the move takes 27
+// by quarters and 84 by halves.)
+// What bounds it: memory lines.  A kept token's V codes are 4-byte words of two lines; where one
+// in four stays up to 330 bytes are read for its 148 (FETCH_SIZE).  24 sequences to 2048 tokens, 8
+// heads: 47 to 49 us for up to 124 MB read and 56 written.
 #include "kv4_device.h"
 
 namespace mpfa {
