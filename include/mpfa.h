@@ -563,6 +563,114 @@ typedef struct {
 mpfa_status mpfa_kv4_evict(const mpfa_kv4_evict_args* args, mpfa_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
+/* Linear attention with a decay, and the norm around attention               */
+/* ------------------------------------------------------------------------ */
+/*
+ * Attention without a softmax, for layers that keep a state instead of a cache.
+ * Per sequence and KV head, with g <= 0 the log decay of a token,
+ *   S_t = exp(g_t) S_{t-1} + k_t v_t^T       (FP32 [128][128], rows are channels of K)
+ *   o_t = scale * q_t^T S_t                  (BF16; query head h: KV head h / (H_q / H_kv))
+ *
+ *  - log_decay f32: token t, KV head h at t * decay_stride + h; with decay_stride
+ *    0 one per KV head.  A value below -200, -inf among them, counts as -200,
+ *    whose exponential times any FP32 number is 0: the token forgets what was
+ *    before it.  Values above 0 count as 0; they and NaN are a caller's mistake,
+ *    for which the debug library returns MPFA_ERR_DATA.
+ *  - states f32 [num_states][h_kv][128][128].  Sequence b starts from the state
+ *    in slot state_src[b] (negative: from zeros) and leaves its last state in
+ *    slot state_dst[b] (negative: nowhere).  Several sequences may start from one
+ *    slot (a shared prefix), and state_dst[b] may be state_src[b]; no two
+ *    sequences of a call may end in one slot, or one end in a slot from which
+ *    another starts.  A sequence without tokens leaves the state it starts from.
+ *  - q_stride, k_stride, v_stride: elements between tokens (at least heads * 128,
+ *    a multiple of 8; the heads of a token are contiguous).  q, k, v, states and
+ *    out are 16-byte aligned.  h_q and h_kv are 1 to 256, h_q % h_kv == 0.
+ * States, sums and decays are FP32.  Where the matrix cores take FP32 numbers as
+ * BF16 they are sums of such: of two for an output (a state, a score: at most
+ * 2^-16 of it is lost), of three for the state (2^-24).  q, k and v are finite, and
+ * so is what the formulas make of them.
+ *
+ * mpfa_linear_prefill: packed prompts; query, key and value i of sequence b are
+ * token cu_seqlens[b] + i.  total_tokens of q, k, v and out: cu_seqlens[batch],
+ * or more (padding, neither read nor written).  max_seqlen: at least the tokens
+ * of the longest sequence.  workspace: at least
+ * mpfa_linear_prefill_workspace_size bytes for the same arguments (0: none is
+ * read), 16-byte aligned; its contents on entry are ignored.  Calls (and captured
+ * graphs) that may overlap need workspaces and states of their own.  How long
+ * sequences are cut goes by batch, total_tokens, max_seqlen and the heads, and
+ * the order of FP32 sums with it; identical calls give identical bytes.
+ *
+ * mpfa_linear_decode: q_tokens rows per sequence (1, or a few drafted tokens);
+ * token b * q_tokens + i.  No workspace.  total_tokens, max_seqlen and cu_seqlens
+ * are not read.  To take drafted tokens back, leave the state in another slot, or
+ * nowhere, and call again with those that stay.
+ */
+typedef struct {
+    int32_t batch;               /* 1 .. 65535                                     */
+    int32_t total_tokens;        /* prefill                                        */
+    int32_t max_seqlen;          /* prefill                                        */
+    int32_t q_tokens;            /* decode: 1 .. 1024 rows per sequence            */
+    int32_t h_q, h_kv;
+    int32_t head_dim;            /* must be 128                                    */
+    uint32_t flags;              /* must be 0                                      */
+    float scale;
+    int32_t num_states;          /* slots of states                                */
+    int64_t q_stride, k_stride, v_stride;
+    int64_t decay_stride;        /* 0, or at least h_kv                            */
+    const int32_t* cu_seqlens;   /* prefill: [batch+1]                             */
+    const void* q;               /* bf16 [T][h_q][128]                             */
+    const void* k;               /* bf16 [T][h_kv][128]                            */
+    const void* v;               /* bf16 [T][h_kv][128]                            */
+    const float* log_decay;
+    const int32_t* state_src;    /* [batch]                                        */
+    const int32_t* state_dst;    /* [batch]                                        */
+    float* states;
+    void* out;                   /* bf16 [T][h_q][128]                             */
+} mpfa_linear_args;
+
+mpfa_status mpfa_linear_prefill_workspace_size(int32_t batch, int32_t total_tokens, int32_t max_seqlen,
+                                               int32_t h_q, int32_t h_kv, size_t* bytes);
+mpfa_status mpfa_linear_prefill(const mpfa_linear_args* args, void* workspace, size_t workspace_bytes,
+                                mpfa_stream_t stream);
+mpfa_status mpfa_linear_decode(const mpfa_linear_args* args, mpfa_stream_t stream);
+
+/*
+ * mpfa_rms_norm: root-mean-square norm of rows, as it stands before attention
+ * (with the residual's addition, and with codes for a product in 8 bits) and, per
+ * head, behind linear attention, whose sums nothing has divided.
+ *   r = BF16(x + residual) (x without a residual), stored in residual_out;
+ *   y = r * weight / sqrt(mean(r^2) + eps)   (weight 1 where it is NULL)
+ * Without scales out = BF16(y).  With scales out holds E4M3 codes and scales
+ * [rows][ceil(width / group)] the FP32 factor of each group of channels (the last
+ * may be short; group 0: one for the row): with m = max |r * weight| over the
+ * group, scale = m / (448 sqrt(mean(r^2) + eps)), and 1 where m is 0, and
+ *   code = E4M3_RNE(448 (r * weight) / m)
+ * of the exact quotient, so that codes do not depend on any order of sums.
+ * Sums are FP32: |r| and |r * weight| from about 2^63 on are outside the contract.
+ * Rows do not affect each other; one with a NaN or an infinity gets NaN outputs
+ * or scales somewhere.
+ * x_stride: elements between rows of x (a multiple of 8); residual, residual_out
+ * and out are contiguous, and residual_out may be residual (or x, where x is
+ * contiguous).  x, residual, residual_out, weight are 16-byte aligned, out too
+ * (codes: 8).
+ */
+typedef struct {
+    int32_t rows;                /* 0 or more                                      */
+    int32_t width;               /* 8 .. 32768, a multiple of 8                    */
+    int32_t group;               /* with scales: 0, 32, 64, 128, 256 or 512        */
+    float eps;                   /* above 0                                        */
+    int64_t x_stride;
+    const void* x;               /* bf16 [rows][width]                             */
+    const void* weight;          /* bf16 [width] or NULL                           */
+    const void* residual;        /* bf16 [rows][width] or NULL                     */
+    void* residual_out;          /* bf16 [rows][width], with a residual            */
+    void* out;                   /* bf16 or, with scales, E4M3 [rows][width]       */
+    float* scales;               /* or NULL                                        */
+} mpfa_rms_norm_args;
+
+mpfa_status mpfa_rms_norm(const mpfa_rms_norm_args* args, mpfa_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
 /* Utilities                                                                  */
 /* ------------------------------------------------------------------------ */
 /* Element-wise device conversions, exposed so that their rounding can be

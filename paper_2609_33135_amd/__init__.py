@@ -28,7 +28,8 @@ EXPORTED = ("mpfa_quantize_qk", "mpfa_prefill", "mpfa_decode_workspace_size",
             "mpfa_mixed_workspace_size",
             "mpfa_mixed_step", "mpfa_convert", "mpfa_status_string", "mpfa_version",
             "mpfa_kv4_write_workspace_size", "mpfa_kv4_write", "mpfa_kv4_prefill_plan", "mpfa_kv4_prefill",
-            "mpfa_kv4_decode_plan", "mpfa_kv4_decode", "mpfa_kv4_evict")
+            "mpfa_kv4_decode_plan", "mpfa_kv4_decode", "mpfa_kv4_evict",
+            "mpfa_linear_prefill_workspace_size", "mpfa_linear_prefill", "mpfa_linear_decode", "mpfa_rms_norm")
 
 
 class MpfaError(RuntimeError):
@@ -108,6 +109,21 @@ class Kv4EvictArgs(C.Structure):
                 ("kept", C.c_void_p), ("new_len", C.c_void_p)]
 
 
+class LinearArgs(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("total_tokens", C.c_int32), ("max_seqlen", C.c_int32), ("q_tokens", C.c_int32),
+                ("h_q", C.c_int32), ("h_kv", C.c_int32), ("head_dim", C.c_int32), ("flags", C.c_uint32), ("scale", C.c_float),
+                ("num_states", C.c_int32), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("decay_stride", C.c_int64), ("cu_seqlens", C.c_void_p), ("q", C.c_void_p), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("log_decay", C.c_void_p), ("state_src", C.c_void_p), ("state_dst", C.c_void_p),
+                ("states", C.c_void_p), ("out", C.c_void_p)]
+
+
+class RmsNormArgs(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("width", C.c_int32), ("group", C.c_int32), ("eps", C.c_float), ("x_stride", C.c_int64),
+                ("x", C.c_void_p), ("weight", C.c_void_p), ("residual", C.c_void_p), ("residual_out", C.c_void_p),
+                ("out", C.c_void_p), ("scales", C.c_void_p)]
+
+
 _libs: dict = {}
 
 
@@ -158,7 +174,11 @@ def _load(path):
                 ("mpfa_kv4_prefill", [C.POINTER(Kv4AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
                 ("mpfa_kv4_decode_plan", [i32, C.c_void_p, i32, i32, i32, i32, i32, C.c_uint32, i32, out, out, size]),
                 ("mpfa_kv4_decode", [C.POINTER(Kv4AttnArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
-                ("mpfa_kv4_evict", [C.POINTER(Kv4EvictArgs), C.c_void_p])):
+                ("mpfa_kv4_evict", [C.POINTER(Kv4EvictArgs), C.c_void_p]),
+                ("mpfa_linear_prefill_workspace_size", [i32, i32, i32, i32, i32, size]),
+                ("mpfa_linear_prefill", [C.POINTER(LinearArgs), C.c_void_p, C.c_size_t, C.c_void_p]),
+                ("mpfa_linear_decode", [C.POINTER(LinearArgs), C.c_void_p]),
+                ("mpfa_rms_norm", [C.POINTER(RmsNormArgs), C.c_void_p])):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = args
         L.mpfa_status_string.restype = C.c_char_p
@@ -622,3 +642,99 @@ def kv4_evict(cache: PagedCache4, kv_len, page_table, dst_page_table, budget: in
     a = Kv4EvictArgs(batch, h_kv, src[1], dst[1], budget, sinks, recent, KV4_IN_PLACE if in_place else 0, kv_len.data_ptr(),
                      page_table.data_ptr(), dst_page_table.data_ptr(), cache._c, kept.data_ptr(), new_len.data_ptr())
     _call("mpfa_kv4_evict", dev, stream, C.byref(a))
+
+
+# ---- linear attention with a decay, the norm around attention ---------------------------
+
+LINEAR_SCALE = HEAD_DIM ** -0.5
+
+
+def linear_prefill_workspace_size(batch: int, total_tokens: int, max_seqlen: int, h_q: int, h_kv: int) -> int:
+    n = C.c_size_t(0)
+    _check(lib().mpfa_linear_prefill_workspace_size(batch, total_tokens, max_seqlen, h_q, h_kv, C.byref(n)),
+           "mpfa_linear_prefill_workspace_size")
+    return n.value
+
+
+def _linear_args(what, q, k, v, log_decay, states, state_src, state_dst, out, batch, max_seqlen, q_tokens, cu, scale):
+    import torch
+    shape, slots, dev = q.shape, states.shape, states.get_device()
+    if len(shape) != 3 or len(slots) != 4 or slots[2] != HEAD_DIM or slots[3] != HEAD_DIM:
+        raise ValueError(f"{what}: q [T][Hq][{HEAD_DIM}] and states [slots][Hkv][{HEAD_DIM}][{HEAD_DIM}] are wanted")
+    T, h_q, h_kv = shape[0], shape[1], slots[1]
+    qs, ks, vs = _rows(what, q, h_q, dev), _rows(what, k, h_kv, dev), _rows(what, v, h_kv, dev)
+    _same(what, torch.float32, dev, states)
+    _same(what, torch.int32, dev, state_src, state_dst)
+    _same(what, torch.bfloat16, dev, out)
+    if k.shape[0] != T or v.shape[0] != T or out.numel() != q.numel() or state_src.numel() != batch or state_dst.numel() != batch:
+        raise ValueError(f"{what}: shapes")
+    gs, at = log_decay.shape, log_decay.stride()
+    if (log_decay.dtype is not torch.float32 or log_decay.get_device() != dev or len(gs) not in (1, 2) or gs[-1] != h_kv or
+            (h_kv > 1 and at[-1] != 1) or (len(gs) == 2 and gs[0] != T)):
+        raise ValueError(f"{what}: log_decay is float32 [Hkv] or [T][Hkv]")
+    decay_stride = 0 if len(gs) == 1 else at[0] if T > 1 else h_kv
+    return dev, LinearArgs(batch, T, max_seqlen, q_tokens, h_q, h_kv, HEAD_DIM, 0, LINEAR_SCALE if scale is None else scale,
+                           slots[0], qs, ks, vs, decay_stride, cu, q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(),
+                           state_src.data_ptr(), state_dst.data_ptr(), states.data_ptr(), out.data_ptr())
+
+
+def linear_prefill(q, k, v, log_decay, cu_seqlens, states, state_src, state_dst, out, max_seqlen: int, workspace=None,
+                   scale=None, stream=None):
+    """mpfa_linear_prefill: linear attention with a decay over packed prompts.  q bf16 [T][Hq][128], k, v bf16
+    [T][Hkv][128] (tokens may lie apart), log_decay f32 [Hkv] or [T][Hkv], states f32 [slots][Hkv][128][128] from
+    whose slots state_src (negative: zeros) the sequences start and in whose slots state_dst (negative: nowhere) they
+    end; workspace: linear_prefill_workspace_size bytes; scale: 1 / sqrt(128) by default."""
+    import torch
+    dev, a = _linear_args("linear_prefill", q, k, v, log_decay, states, state_src, state_dst, out, cu_seqlens.numel() - 1,
+                          max_seqlen, 0, cu_seqlens.data_ptr(), scale)
+    _same("linear_prefill", torch.int32, dev, cu_seqlens)
+    size = 0
+    if workspace is not None:
+        _same("linear_prefill: workspace", workspace.dtype, dev, workspace)
+        size = workspace.numel() * workspace.element_size()
+    _call("mpfa_linear_prefill", dev, stream, C.byref(a), _ptr(workspace), size)
+
+
+def linear_decode(q, k, v, log_decay, states, state_src, state_dst, out, q_tokens: int = 1, scale=None, stream=None):
+    """mpfa_linear_decode: q_tokens new tokens of each sequence (rows b * q_tokens + i) from the states in state_src,
+    which lead to those in state_dst; tensors as for linear_prefill."""
+    batch = state_src.numel()
+    if q.shape[0] != batch * q_tokens:
+        raise ValueError("linear_decode: q has q_tokens rows per sequence")
+    dev, a = _linear_args("linear_decode", q, k, v, log_decay, states, state_src, state_dst, out, batch, 0, q_tokens, None, scale)
+    _call("mpfa_linear_decode", dev, stream, C.byref(a))
+
+
+def rms_norm(x, weight, out, eps: float = 1e-6, residual=None, residual_out=None, scales=None, group: int = 0, stream=None):
+    """mpfa_rms_norm over the last dimension of x (bf16; contiguous, or rows of a matrix that lie apart): out bf16, or
+    with scales (f32 [rows][groups]) float8_e4m3fn codes, a scale per `group` channels (0: per row).  residual:
+    x + residual is normalised, and goes to residual_out (by default to residual).  weight: bf16 [width] or None."""
+    import torch
+    dev, shape = x.get_device(), x.shape
+    if x.dtype is not torch.bfloat16 or not shape or shape[-1] == 0:
+        raise ValueError("rms_norm: x is bf16 [..][width]")
+    width = shape[-1]
+    rows = x.numel() // width
+    if x.is_contiguous():
+        stride = width
+    elif len(shape) == 2 and x.stride(1) == 1:
+        stride = x.stride(0) if rows > 1 else width
+    else:
+        raise ValueError(f"rms_norm: x is contiguous or rows of a matrix, got strides {x.stride()}")
+    if residual is None:
+        _want(residual_out is None, "rms_norm: residual_out goes with a residual")
+    else:
+        residual_out = residual if residual_out is None else residual_out
+        _same("rms_norm", torch.bfloat16, dev, residual, residual_out)
+        _want(residual.numel() == residual_out.numel() == rows * width, "rms_norm: residual has the shape of x")
+    if weight is not None:
+        _same("rms_norm", torch.bfloat16, dev, weight)
+        _want(weight.numel() == width, "rms_norm: weight is [width]")
+    _same("rms_norm", torch.bfloat16 if scales is None else torch.float8_e4m3fn, dev, out)
+    _want(out.numel() == rows * width, "rms_norm: out has the shape of x")
+    if scales is not None:
+        _same("rms_norm", torch.float32, dev, scales)
+        _want(group >= 0 and scales.numel() == rows * -(-width // (group or width)), "rms_norm: scales are [rows][groups]")
+    a = RmsNormArgs(rows, width, group, eps, stride, x.data_ptr(), _ptr(weight), _ptr(residual), _ptr(residual_out),
+                    out.data_ptr(), _ptr(scales))
+    _call("mpfa_rms_norm", dev, stream, C.byref(a))

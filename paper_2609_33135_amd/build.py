@@ -15,9 +15,10 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmpfa.so")
 
-HOST_SOURCES = ["api.cpp", "kv4_api.cpp"]   # compiled again with data checks for the debug library
+HOST_SOURCES = ["api.cpp", "kv4_api.cpp", "linear_api.cpp"]   # compiled again with data checks for the debug library
 KERNEL_SOURCES = ["quantize.hip", "prefill.hip", "decode.hip", "mixed.hip", "debug_checks.hip",
-                  "kv4_write.hip", "kv4_prefill.hip", "kv4_decode.hip", "kv4_evict.hip"]
+                  "kv4_write.hip", "kv4_prefill.hip", "kv4_decode.hip", "kv4_evict.hip",
+                  "linear_prefill.hip", "linear_decode.hip", "rms_norm.hip"]
 SOURCES = HOST_SOURCES + KERNEL_SOURCES
 DEBUG_LIB = os.path.join(PKG, "libmpfa_debug.so")
 PROBE_LIB = os.path.join(PKG, "libmpfa_probe.so")

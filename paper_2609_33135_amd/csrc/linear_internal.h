@@ -1,0 +1,65 @@
+// linear_internal.h -- launch parameter blocks of linear attention (linear_*.hip) and of the norm
+// (rms_norm.hip), and how a prefill is cut.  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mpfa {
+
+constexpr int kLinChunk = 64;                  // tokens of a chunk
+constexpr int kLinState = 128 * 128;           // floats of a state
+constexpr float kLinLeastDecay = -200.0f;      // exp of it times any FP32 number is 0
+
+struct LinearParams {
+  int batch, total_tokens, h_q, h_kv;
+  int q_tokens;                  // decode: rows per sequence
+  int segment;                   // prefill: tokens per segment, a multiple of kLinChunk
+  int split;                     // prefill: some sequence may have several segments
+  float scale;
+  int64_t q_stride, k_stride, v_stride, decay_stride;
+  const int32_t* cu_seqlens;     // prefill
+  const uint16_t* q;
+  const uint16_t* k;
+  const uint16_t* v;
+  const float* log_decay;
+  const int32_t* state_src;
+  const int32_t* state_dst;
+  float* states;                 // [slot][h_kv][128][128]
+  uint16_t* out;
+  float* starts;                 // prefill: [segment id][h_kv][kLinState], see linear_prefill.hip
+  float* decays;                 // prefill: [segment id][h_kv]
+};
+
+// Segments are numbered over the batch, those of sequence b from cu_seqlens[b] / segment + b on:
+// ceil(n / segment) of them end at or before the next sequence's first.
+inline int64_t linear_segments(int64_t batch, int64_t total_tokens, int64_t segment) { return total_tokens / segment + batch; }
+
+struct NormParams {
+  int rows, width, group;        // group: channels per scale, width for one per row
+  float eps;
+  int64_t x_stride;
+  const uint16_t* x;
+  const uint16_t* weight;        // or null
+  const uint16_t* residual;      // or null
+  uint16_t* residual_out;
+  void* out;                     // bf16, or E4M3 where scales are given
+  float* scales;                 // or null
+};
+
+// Threads for a row: for more than 512 channels a workgroup, of norm_octets(width) octets a thread.
+constexpr int kNormWidth = 32768;
+inline int norm_octets(int width) { return width <= 16384 ? 2 : 4; }
+inline int norm_threads(int width) {
+  if (width <= 512) return width <= 64 ? 8 : width <= 128 ? 16 : width <= 256 ? 32 : 64;
+  const int wave = 64 * 8 * norm_octets(width);
+  return (width + wave - 1) / wave * 64;
+}
+
+hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream);
+hipError_t launch_linear_decode(const LinearParams& p, hipStream_t stream);
+hipError_t launch_rms_norm(const NormParams& p, hipStream_t stream);
+// whether any log decay [tokens][heads] is NaN or above 0 (debug library)
+hipError_t launch_scan_decay(const float* x, int64_t tokens, int heads, int64_t stride, int* flag, hipStream_t stream);
+
+}  // namespace mpfa
