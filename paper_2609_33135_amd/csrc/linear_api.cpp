@@ -166,10 +166,15 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   if (const mpfa_status st = linear_params(a, false, p)) return st;
   if (a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
   const PrefillSpace s = prefill_space(a->batch, a->total_tokens, a->max_seqlen, a->h_kv);
-  if (s.segments * a->h_kv > (int64_t)UINT32_MAX / 256) return MPFA_ERR_UNSUPPORTED;
+  const int64_t items = s.segments * a->h_kv;
+  if (items > (int64_t)UINT32_MAX / 256 - 8) return MPFA_ERR_UNSUPPORTED;
   if (s.split && (!workspace || workspace_bytes < s.bytes || !aligned16(workspace))) return MPFA_ERR_WORKSPACE;
   p.segment = s.segment;
   p.split = s.split;
+  // few items: a KV head's query heads apart, while that makes no more than fill the card
+  const int grp = a->h_q / a->h_kv;
+  p.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, items * grp / kItems));
+  p.parts = (grp + p.heads - 1) / p.heads;
   p.starts = s.split ? static_cast<float*>(workspace) : nullptr;
   p.decays = s.split ? p.starts + s.starts / sizeof(float) : nullptr;
 #ifdef MPFA_DEBUG_CHECKS

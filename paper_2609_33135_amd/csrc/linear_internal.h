@@ -16,6 +16,7 @@ struct LinearParams {
   int q_tokens;                  // decode: rows per sequence
   int segment;                   // prefill: tokens per segment, a multiple of kLinChunk
   int split;                     // prefill: some sequence may have several segments
+  int parts, heads;              // prefill: parts of a KV head's query heads, of so many each
   float scale;
   int64_t q_stride, k_stride, v_stride, decay_stride;
   const int32_t* cu_seqlens;     // prefill

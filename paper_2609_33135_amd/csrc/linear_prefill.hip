@@ -18,7 +18,6 @@ namespace mpfa {
 namespace {
 
 constexpr int kC = kLinChunk;
-constexpr int kRow = kD + 8;          // elements of a token's row in LDS
 constexpr double kLog2e = 1.4426950408889634;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -57,26 +56,41 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
   return g->s < g->count;
 }
 
+// Rows of 128 channels in LDS lie without padding, their 16-byte pieces exchanged by row so that neither 16
+// rows' same piece nor four rows' same 64 bytes (a transposing read) meet in a bank.
+typedef uint16_t LdsRows[kC][kD];
+__device__ __forceinline__ int piece(int row, int c) { return 8 * (c ^ ((row & 3) << 2 | (row >> 2 & 3))); }
+
 struct Lds {
-  uint16_t k[kC][kRow], v[kC][kRow], q[kC][kRow];
+  LdsRows k, v, q;                             // q: in each 16 channels those of a lane half side by side
   u32x4 p[3][2][2][64];                        // scores: block, step of 16 keys, high and low parts, lane
-  float hi[kC], lo[kC];                        // log2 of the decays from the chunk's start, in two parts
-  float from[kC], to[kC];                      // exp2 of them; exp2 from each token to the chunk's end
+  struct Decays {
+    float hi[kC], lo[kC];                      // log2 of the decays from the chunk's start, in two parts
+    float from[kC], to[kC];                    // exp2 of them; exp2 from each token to the chunk's end
+  } d[2];                                      // of this chunk and the next
 };
+
+// The lane, by a value of each use's own: what is worked out from it (LDS addresses above all) is not kept in
+// registers from one use to the next, of which there are not enough.
+__device__ __forceinline__ int lane_here() {
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
 
 // Four tokens (rows t .. t + 3) of the lane's column c0 + lane % 32, t = t0 + 4 * (lane / 32): each
 // group of 16 lanes reads a block of four rows and 16 columns, and gets it transposed.
-__device__ __forceinline__ s16x4 column4(const uint16_t (*rows)[kRow], int t0, int c0) {
+__device__ __forceinline__ s16x4 column4(const LdsRows& rows, int lane, int t0, int c0) {
   typedef __attribute__((address_space(3))) s16x4 lds4;
-  const int lane = threadIdx.x & 63, i = lane & 15;
-  const uint16_t* at = &rows[t0 + 4 * (lane >> 5) + (i >> 2)][c0 + (lane & 16) + 4 * (i & 3)];
+  const int i = lane & 15, row = t0 + 4 * (lane >> 5) + (i >> 2);
+  const uint16_t* at = &rows[row][piece(row, c0 / 8 + (lane >> 4 & 1) * 2 + (i >> 1 & 1)) + 4 * (i & 1)];
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)at);
 }
 // The tokens of one 16-token step in the order in which an accumulator holds its rows.
-__device__ __forceinline__ Frag columns(const uint16_t (*rows)[kRow], int t0, int c0) {
+__device__ __forceinline__ Frag columns(const LdsRows& rows, int lane, int t0, int c0) {
   Frag f;
-  f.s[0] = column4(rows, t0, c0);
-  f.s[1] = column4(rows, t0 + 8, c0);
+  f.s[0] = column4(rows, lane, t0, c0);
+  f.s[1] = column4(rows, lane, t0 + 8, c0);
   return f;
 }
 
@@ -115,10 +129,19 @@ __device__ __forceinline__ void load_rows(Rows& r, const uint16_t* x, int64_t st
     if (row + 16 * i < n) r.w[i] = *reinterpret_cast<const u32x4*>(x + (row + 16 * i) * stride + 8 * c);
   }
 }
-__device__ __forceinline__ void store_rows(const Rows& r, uint16_t (*to)[kRow]) {
+__device__ __forceinline__ void store_rows(const Rows& r, LdsRows& to) {
   const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(&to[row + 16 * i][8 * c]) = r.w[i];
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(&to[row + 16 * i][piece(row + 16 * i, c)]) = r.w[i];
+}
+// Queries: of 16 channels 0-3, 8-11 | 4-7, 12-15.
+__device__ __forceinline__ void store_queries(const Rows& r, LdsRows& to) {
+  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      *reinterpret_cast<u32x2*>(&to[row + 16 * i][piece(row + 16 * i, (c & ~1) + x) + 4 * (c & 1)]) = (u32x2){r.w[i][2 * x], r.w[i][2 * x + 1]};
 }
 
 // The state's part of a wave: 32 columns (channels of v), accumulator db the rows (channels of k) 32 db ..
@@ -169,33 +192,197 @@ __device__ __forceinline__ void raw_load(State& s, float* ws) {
     }
 }
 
-// log2 of the decay from the chunk's start to each token (lane = token).  Summed in 64 bits: after a token
-// that clears the state, sums are large and their differences small.
-__device__ __forceinline__ double decay_sums(const LinearParams& p, int64_t t, int n, int hk) {
+// Log decays of a chunk (lane = token; 0 behind its last).
+__device__ __forceinline__ float load_decays(const LinearParams& p, int64_t t, int n, int hk) {
   const int lane = threadIdx.x & 63;
-  double x = 0.0;
-  if (lane < n) x = (double)fminf(fmaxf(p.log_decay[(t + lane) * p.decay_stride + hk], kLinLeastDecay), 0.0f) * kLog2e;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const double y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
+  return lane < n ? p.log_decay[(t + lane) * p.decay_stride + hk] : 0.0f;
 }
 
-// One workgroup of four waves per (segment, KV head).  kOut: the outputs of its tokens from the state before
-// it, and of a sequence's last segment the state after it; else the segment's own state, for the next.
+template <int kControl, int kRows>
+__device__ __forceinline__ double moved(double x) {   // lanes without a source get 0
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, kControl, kRows, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), kControl, kRows, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// What a chunk needs of its decays g; returns log2 of the whole chunk's.  Summed in 64 bits: after a token that
+// clears the state sums are large and their differences small.
+__device__ __forceinline__ double put_decays(Lds::Decays& d, float g) {
+  const int lane = threadIdx.x & 63;
+  double x = (double)fminf(fmaxf(g, kLinLeastDecay), 0.0f) * kLog2e;
+  x += moved<0x111, 0xF>(x);   // from 1, 2, 4, 8 lanes before in a row of 16
+  x += moved<0x112, 0xF>(x);
+  x += moved<0x114, 0xF>(x);
+  x += moved<0x118, 0xF>(x);
+  x += moved<0x142, 0xA>(x);   // the last lane of a row to the next row, rows 1 and 3
+  x += moved<0x143, 0xC>(x);   // lane 31 to rows 2 and 3
+  const double end = __shfl(x, 63);
+  const float hi = (float)x;
+  d.hi[lane] = hi;
+  d.lo[lane] = (float)(x - (double)hi);
+  d.from[lane] = __builtin_amdgcn_exp2f(hi);
+  d.to[lane] = __builtin_amdgcn_exp2f((float)(end - x));
+  return end;
+}
+
+// S' = exp(b_last) S + K^T (exp(b_last - b_j) V): K is an operand as it is, V with its decay in three parts.
+__device__ __forceinline__ void update(State& st, const Lds& s, const Lds::Decays& d) {
+  const int wave = threadIdx.x >> 6, lane = lane_here(), half = lane >> 5;
+  const float whole = d.from[kC - 1];
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.a[db][r] *= whole;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const Frag v = columns(s.v, lane, 16 * j, 32 * wave);
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w = v.w[e >> 1];
+      y[e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * d.to[16 * j + 8 * (e >> 2) + 4 * half + (e & 3)];
+    }
+    Frag f[3];
+    split8<3>(y, f);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) {
+      const Frag k = columns(s.k, lane, 16 * j, 32 * db);
+#pragma unroll
+      for (int i = 2; i >= 0; --i) st.a[db] = mfma32_bf16(k.b, f[i].b, st.a[db]);
+    }
+  }
+}
+
+// Scores of one block (keys j0 .., queries i0 ..), transposed, with their decays, as operands.
+__device__ __forceinline__ void scores(Lds& s, const Lds::Decays& d, int block) {
+  const int lane = lane_here(), half = lane >> 5, l32 = lane & 31;
+  const int i0 = block == 0 ? 0 : 32, j0 = block == 2 ? 32 : 0, i = i0 + l32, jr = j0 + l32;
+  f32x16 x;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    Frag a, q;
+    a.d[0] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k) + 4 * half]);
+    a.d[1] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k + 1) + 4 * half]);
+    q.w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * k + half)]);
+    x = mfma32_bf16(a.b, q.b, x);
+  }
+  const float hi = d.hi[i], lo = d.lo[i];
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = j0 + 16 * y + 8 * (e >> 2) + 4 * half + (e & 3);
+      const float decay = __builtin_amdgcn_exp2f((hi - d.hi[j]) + (lo - d.lo[j]));
+      w[e] = j <= i ? x[8 * y + e] * decay : 0.0f;
+    }
+    Frag f[2];
+    split8<2>(w, f);
+    s.p[block][y][0][lane] = f[0].w;
+    s.p[block][y][1][lane] = f[1].w;
+  }
+}
+
+// o (transposed: rows are channels of v, 32 queries each) = exp(b_i) S^T q_i.
+__device__ __forceinline__ void from_state(f32x16 (&o)[2], State& st, const Lds& s, const Lds::Decays& d) {
+  const int lane = lane_here(), half = lane >> 5, l32 = lane & 31;
+#pragma unroll
+  for (int ib = 0; ib < 2; ++ib)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[ib][r] = 0.0f;
+#pragma unroll
+  for (int db = 0; db < 4; ++db) {
+    asm volatile("" : "+v"(st.a[db]));   // the parts are made for each query head anew: there is no room to keep them
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      float y[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = st.a[db][8 * x + e];
+      Frag f[2];
+      split8<2>(y, f);
+#pragma unroll
+      for (int ib = 0; ib < 2; ++ib) {
+        const int i = 32 * ib + l32;
+        Frag q;
+        q.w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 4 * db + 2 * x + half)]);
+        o[ib] = mfma32_bf16(f[1].b, q.b, o[ib]);
+        o[ib] = mfma32_bf16(f[0].b, q.b, o[ib]);
+      }
+    }
+  }
+#pragma unroll
+  for (int ib = 0; ib < 2; ++ib) {
+    const float from = d.from[32 * ib + l32];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[ib][r] *= from;
+  }
+}
+
+// o += V^T scores.
+__device__ __forceinline__ void from_chunk(f32x16 (&o)[2], const Lds& s) {
+  const int lane = lane_here(), wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int block = 0; block < 3; ++block)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const Frag v = columns(s.v, lane, (block == 2 ? 32 : 0) + 16 * y, 32 * wave);
+      f32x16& to = o[block == 0 ? 0 : 1];
+      Frag w;
+      w.w = s.p[block][y][1][lane];
+      to = mfma32_bf16(v.b, w.b, to);
+      w.w = s.p[block][y][0][lane];
+      to = mfma32_bf16(v.b, w.b, to);
+    }
+}
+
+// The halves of a wave exchange channels, so that each lane stores 16 bytes of its query's row.
+__device__ __forceinline__ void store_out(const f32x16& o, uint16_t* row, float scale) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int a = 0; a < 4; a += 2) {
+    u32x4 w;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t first = pack_bf16(o[4 * a + 2 * x] * scale, o[4 * a + 2 * x + 1] * scale);
+      const uint32_t second = pack_bf16(o[4 * a + 4 + 2 * x] * scale, o[4 * a + 5 + 2 * x] * scale);
+      const auto both = __builtin_amdgcn_permlane32_swap(first, second, false, false);
+      w[x] = both[0];
+      w[2 + x] = both[1];
+    }
+    if (row) *reinterpret_cast<u32x4*>(row + 8 * a + 8 * half) = w;
+  }
+}
+
+// One workgroup of four waves per (segment, KV head) and, for outputs, part of its query heads.  kOut: the
+// outputs of its tokens from the state before it, and of a sequence's last segment the state after it; else
+// the segment's own state, for the next.  What the next step reads is on its way to registers during this one.
 template <bool kOut>
-__global__ __launch_bounds__(256) void linear_chunks_kernel(LinearParams p) {
+__global__ __launch_bounds__(256, 2) void linear_chunks_kernel(LinearParams p, int items) {
   __shared__ Lds s;
-  const int hk = blockIdx.x % p.h_kv, id = blockIdx.x / p.h_kv;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
-  const int grp = p.h_q / p.h_kv;
+  // parts of an item follow each other on one XCD
+  const int parts = kOut ? p.parts : 1, item = blockIdx.x / (8 * parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % parts;
+  if (item >= items) return;
+  const int hk = item % p.h_kv, id = item / p.h_kv;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31;
+  const int grp = p.h_q / p.h_kv, h0 = hk * grp + part * p.heads, h1 = min(h0 + p.heads, hk * grp + grp);
   Segment g;
   if (!find_segment(p, id, &g)) return;
   const bool last = g.s == g.count - 1;
   if (!kOut && last) return;
   float* const slot = p.split ? p.starts + ((int64_t)id * p.h_kv + hk) * kLinState : nullptr;
+  const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
+  const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
+  const uint16_t* const q0 = p.q + g.t0 * p.q_stride;
+
+  Rows rk, rv, rq;
+  float decay = 0.0f;   // of the chunk after the next
+  double total = 0.0;
+  load_rows(rk, k0, p.k_stride, g.n);
+  load_rows(rv, v0, p.v_stride, g.n);
+  if (kOut) load_rows(rq, q0 + h0 * kD, p.q_stride, g.n);
 
   State st;
   state_zero(st);
@@ -206,146 +393,57 @@ __global__ __launch_bounds__(256) void linear_chunks_kernel(LinearParams p) {
   } else if (kOut) {
     raw_load(st, slot);
   }
+  if (wave == 3) {
+    total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk));
+    decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
+  }
+  store_rows(rk, s.k);
+  store_rows(rv, s.v);
+  if (kOut) store_queries(rq, s.q);
 
-  double total = 0.0;
-  for (int c = 0; c < g.n; c += kC) {
-    const int64_t t = g.t0 + c;
-    const int n = min(kC, g.n - c);
-    Rows rk, rv, rq;
-    load_rows(rk, p.k + t * p.k_stride + hk * kD, p.k_stride, n);
-    load_rows(rv, p.v + t * p.v_stride + hk * kD, p.v_stride, n);
-    const double b = decay_sums(p, t, n, hk), end = __shfl(b, 63);
-    total += end;
+  for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
+    const int rest = g.n - c - kC;   // tokens behind this chunk
+    const Lds::Decays& d = s.d[x];
     __syncthreads();
-    store_rows(rk, s.k);
-    store_rows(rv, s.v);
-    if (wave == 0) {
-      const float hi = (float)b;
-      s.hi[lane] = hi;
-      s.lo[lane] = (float)(b - (double)hi);
-      s.from[lane] = __builtin_amdgcn_exp2f(hi);
-      s.to[lane] = __builtin_amdgcn_exp2f((float)(end - b));
+    if (rest > 0) {
+      load_rows(rk, k0 + (c + kC) * p.k_stride, p.k_stride, rest);
+      load_rows(rv, v0 + (c + kC) * p.v_stride, p.v_stride, rest);
     }
-    const float whole = __builtin_amdgcn_exp2f((float)end);
-    __syncthreads();
-
-    Frag vf[4];   // V columns of this wave: steps of 16 tokens
-#pragma unroll
-    for (int j = 0; j < 4; ++j) vf[j] = columns(s.v, 16 * j, 32 * wave);
-
+    if (wave == 3 && rest > 0) {
+      total += put_decays(s.d[x ^ 1], decay);
+      decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
+    }
     if (kOut) {
-      Frag sf[4][2][2];
-#pragma unroll
-      for (int db = 0; db < 4; ++db)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float y[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = st.a[db][8 * x + e];
-          split8<2>(y, sf[db][x]);
-        }
-      for (int h = hk * grp; h < hk * grp + grp; ++h) {
-        load_rows(rq, p.q + t * p.q_stride + h * kD, p.q_stride, n);
+      for (int h = h0; h < h1; ++h) {
+        const bool more = h + 1 < h1;
+        if (more || rest > 0) load_rows(rq, q0 + (more ? c : c + kC) * p.q_stride + (more ? h + 1 : h0) * kD, p.q_stride, more ? rest + kC : rest);
+        if (h > h0) __syncthreads();
+        if (wave < 3) scores(s, d, wave);
+        f32x16 o[2];
+        from_state(o, st, s, d);
         __syncthreads();
-        store_rows(rq, s.q);
-        __syncthreads();
-        if (wave < 3) {   // scores: keys j0 .. against queries i0 .., transposed
-          const int i0 = wave == 0 ? 0 : 32, j0 = wave == 2 ? 32 : 0;
-          f32x16 x;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = 0.0f;
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            Frag a, q;
-            a.w = *reinterpret_cast<const u32x4*>(&s.k[j0 + l32][16 * k + 8 * half]);
-            q.w = *reinterpret_cast<const u32x4*>(&s.q[i0 + l32][16 * k + 8 * half]);
-            x = mfma32_bf16(a.b, q.b, x);
-          }
-          const float hi = s.hi[i0 + l32], lo = s.lo[i0 + l32];
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int j = j0 + 16 * y + 8 * (e >> 2) + 4 * half + (e & 3);
-              const float d = __builtin_amdgcn_exp2f((hi - s.hi[j]) + (lo - s.lo[j]));
-              w[e] = j <= i0 + l32 ? x[8 * y + e] * d : 0.0f;
-            }
-            Frag f[2];
-            split8<2>(w, f);
-            s.p[wave][y][0][lane] = f[0].w;
-            s.p[wave][y][1][lane] = f[1].w;
-          }
-        }
-        __syncthreads();
+        if (more) store_queries(rq, s.q);
+        from_chunk(o, s);
 #pragma unroll
         for (int ib = 0; ib < 2; ++ib) {
-          const int i = 32 * ib + l32;
-          f32x16 o;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[r] = 0.0f;
-#pragma unroll
-          for (int db = 0; db < 4; ++db)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              Frag q;
-              q.d[0] = *reinterpret_cast<const u32x2*>(&s.q[i][32 * db + 16 * x + 4 * half]);
-              q.d[1] = *reinterpret_cast<const u32x2*>(&s.q[i][32 * db + 16 * x + 8 + 4 * half]);
-              o = mfma32_bf16(sf[db][x][1].b, q.b, o);
-              o = mfma32_bf16(sf[db][x][0].b, q.b, o);
-            }
-          const float from = s.from[i];
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[r] *= from;
-#pragma unroll
-          for (int blk = ib; blk <= 2 * ib; ++blk)   // score blocks of these queries: 0, or 1 and 2
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              const Frag v = vf[(blk == 2 ? 2 : 0) + y];
-              Frag w;
-              w.w = s.p[blk][y][1][lane];
-              o = mfma32_bf16(v.b, w.b, o);
-              w.w = s.p[blk][y][0][lane];
-              o = mfma32_bf16(v.b, w.b, o);
-            }
-          if (i < n) {
-            uint16_t* to = p.out + ((t + i) * p.h_q + h) * kD + 32 * wave + 4 * half;
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-              *reinterpret_cast<u32x2*>(to + 8 * a) = (u32x2){pack_bf16(o[4 * a] * p.scale, o[4 * a + 1] * p.scale),
-                                                             pack_bf16(o[4 * a + 2] * p.scale, o[4 * a + 3] * p.scale)};
-          }
+          const int i = c + 32 * ib + l32;
+          store_out(o[ib], i < g.n ? p.out + ((g.t0 + i) * p.h_q + h) * kD + 32 * wave : nullptr, p.scale);
         }
       }
     }
-
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) st.a[db][r] *= whole;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t w = vf[j].w[e >> 1];
-        y[e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * s.to[16 * j + 8 * (e >> 2) + 4 * half + (e & 3)];
-      }
-      Frag f[3];
-      split8<3>(y, f);
-#pragma unroll
-      for (int db = 0; db < 4; ++db) {
-        const Frag k = columns(s.k, 16 * j, 32 * db);
-#pragma unroll
-        for (int i = 2; i >= 0; --i) st.a[db] = mfma32_bf16(k.b, f[i].b, st.a[db]);
-      }
+    if (!kOut || rest > 0 || (last && part == 0)) update(st, s, d);
+    if (rest > 0) {
+      __syncthreads();
+      store_rows(rk, s.k);
+      store_rows(rv, s.v);
+      if (kOut) store_queries(rq, s.q);
     }
   }
 
   if (!kOut) {
     raw_store(st, slot + (int64_t)p.h_kv * kLinState);
-    if (threadIdx.x == 0) p.decays[(int64_t)id * p.h_kv + hk] = __builtin_amdgcn_exp2f((float)total);
-  } else if (last) {
+    if (threadIdx.x == 255) p.decays[(int64_t)id * p.h_kv + hk] = __builtin_amdgcn_exp2f((float)total);
+  } else if (last && part == 0) {
     const int dst = p.state_dst[g.b];
     if (dst >= 0) state_store(st, p.states + ((int64_t)dst * p.h_kv + hk) * kLinState);
   }
@@ -362,12 +460,25 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p, int se
     if (!find_segment(p, id, &g) || g.s != 1 || g.count < 3) continue;
     f32x4* at = reinterpret_cast<f32x4*>(p.starts + ((int64_t)id * p.h_kv + hk) * kLinState) + part * 256 + threadIdx.x;
     const float* decay = p.decays + (int64_t)id * p.h_kv + hk;
+    const int64_t step = (int64_t)p.h_kv * (kLinState / 4);
     f32x4 x = *at;
-    for (int s = 2; s < g.count; ++s) {
-      at += p.h_kv * (kLinState / 4);
-      x = x * *decay + *at;
-      *at = x;
-      decay += p.h_kv;
+    for (int s = 2; s < g.count; s += 8) {   // eight loads in flight
+      f32x4 y[8];
+      float a[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int j = min(i, g.count - 1 - s);
+        y[i] = at[(j + 1) * step];
+        a[i] = decay[j * p.h_kv];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (s + i >= g.count) break;
+        x = x * a[i] + y[i];
+        at[(i + 1) * step] = x;
+      }
+      at += 8 * step;
+      decay += 8 * p.h_kv;
     }
   }
 }
@@ -376,12 +487,12 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p, int se
 
 hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream) {
   const int64_t segments = linear_segments(p.batch, p.total_tokens, p.segment);
-  const dim3 grid((unsigned)(segments * p.h_kv));
+  const int items = (int)(segments * p.h_kv), eighths = (items + 7) / 8 * 8;
   if (p.split) {
-    linear_chunks_kernel<false><<<grid, dim3(256), 0, stream>>>(p);
+    linear_chunks_kernel<false><<<dim3(eighths), dim3(256), 0, stream>>>(p, items);
     linear_join_kernel<<<dim3(kJoinBlocks * p.h_kv, (unsigned)std::min<int64_t>(segments, 2048)), dim3(256), 0, stream>>>(p, (int)segments);
   }
-  linear_chunks_kernel<true><<<grid, dim3(256), 0, stream>>>(p);
+  linear_chunks_kernel<true><<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(256), 0, stream>>>(p, items);
   return hipGetLastError();
 }
 
