@@ -70,6 +70,9 @@ struct Lds {
   } d[2];                                      // of this chunk and the next
 };
 
+// Reads above stay above what uses them: left alone, the compiler reads each operand right before its product.
+__device__ __forceinline__ void ahead() { __builtin_amdgcn_sched_barrier(0); }
+
 // The lane, by a value of each use's own: what is worked out from it (LDS addresses above all) is not kept in
 // registers from one use to the next, of which there are not enough.
 __device__ __forceinline__ int lane_here() {
@@ -110,24 +113,23 @@ __device__ __forceinline__ void split8(float* x, Frag* part) {
   for (int i = 0; i < kParts; ++i)
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      const uint32_t h = pack_bf16(x[e], x[e + 1]);
+      uint32_t h = pack_bf16(x[e], x[e + 1]);
+      asm("" : "+v"(h));   // else the compiler makes the low half once more by itself
       part[i].w[e >> 1] = h;
       x[e] -= bits_lo(h);
       x[e + 1] -= bits_hi(h);
     }
 }
 
-// Rows t .. of a chunk, 16 lanes a row: four rows of each thread; zeros from row n on.
+// Rows of a chunk, 16 lanes a row, four rows of each thread.  Rows from n (at least 1) on are row n - 1 again:
+// nothing of them reaches an output or the state, by the scores' mask and a decay of 0.
 struct Rows {
   u32x4 w[4];
 };
 __device__ __forceinline__ void load_rows(Rows& r, const uint16_t* x, int64_t stride, int n) {
   const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r.w[i] = (u32x4){0, 0, 0, 0};
-    if (row + 16 * i < n) r.w[i] = *reinterpret_cast<const u32x4*>(x + (row + 16 * i) * stride + 8 * c);
-  }
+  for (int i = 0; i < 4; ++i) r.w[i] = *reinterpret_cast<const u32x4*>(x + min(row + 16 * i, n - 1) * stride + 8 * c);
 }
 __device__ __forceinline__ void store_rows(const Rows& r, LdsRows& to) {
   const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
@@ -143,6 +145,9 @@ __device__ __forceinline__ void store_queries(const Rows& r, LdsRows& to) {
     for (int x = 0; x < 2; ++x)
       *reinterpret_cast<u32x2*>(&to[row + 16 * i][piece(row + 16 * i, (c & ~1) + x) + 4 * (c & 1)]) = (u32x2){r.w[i][2 * x], r.w[i][2 * x + 1]};
 }
+
+// The value is in its registers here: loads of it have arrived, and what is made of it is not made before.
+__device__ __forceinline__ void keep(f32x16& x) { asm volatile("" : "+v"(x)); }
 
 // The state's part of a wave: 32 columns (channels of v), accumulator db the rows (channels of k) 32 db ..
 struct State {
@@ -206,9 +211,9 @@ __device__ __forceinline__ double moved(double x) {   // lanes without a source 
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-// What a chunk needs of its decays g; returns log2 of the whole chunk's.  Summed in 64 bits: after a token that
+// What a chunk of n tokens needs of its decays g; returns log2 of the whole chunk's.  Summed in 64 bits: after a token that
 // clears the state sums are large and their differences small.
-__device__ __forceinline__ double put_decays(Lds::Decays& d, float g) {
+__device__ __forceinline__ double put_decays(Lds::Decays& d, float g, int n) {
   const int lane = threadIdx.x & 63;
   double x = (double)fminf(fmaxf(g, kLinLeastDecay), 0.0f) * kLog2e;
   x += moved<0x111, 0xF>(x);   // from 1, 2, 4, 8 lanes before in a row of 16
@@ -222,7 +227,7 @@ __device__ __forceinline__ double put_decays(Lds::Decays& d, float g) {
   d.hi[lane] = hi;
   d.lo[lane] = (float)(x - (double)hi);
   d.from[lane] = __builtin_amdgcn_exp2f(hi);
-  d.to[lane] = __builtin_amdgcn_exp2f((float)(end - x));
+  d.to[lane] = lane < n ? __builtin_amdgcn_exp2f((float)(end - x)) : 0.0f;
   return end;
 }
 
@@ -237,20 +242,25 @@ __device__ __forceinline__ void update(State& st, const Lds& s, const Lds::Decay
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const Frag v = columns(s.v, lane, 16 * j, 32 * wave);
+    f32x4 to[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) to[q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]);
+    Frag k[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db) k[db] = columns(s.k, lane, 16 * j, 32 * db);
+    ahead();
     float y[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t w = v.w[e >> 1];
-      y[e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * d.to[16 * j + 8 * (e >> 2) + 4 * half + (e & 3)];
+      y[e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * to[e >> 2][e & 3];
     }
     Frag f[3];
     split8<3>(y, f);
 #pragma unroll
-    for (int db = 0; db < 4; ++db) {
-      const Frag k = columns(s.k, lane, 16 * j, 32 * db);
+    for (int i = 2; i >= 0; --i)
 #pragma unroll
-      for (int i = 2; i >= 0; --i) st.a[db] = mfma32_bf16(k.b, f[i].b, st.a[db]);
-    }
+      for (int db = 0; db < 4; ++db) st.a[db] = mfma32_bf16(k[db].b, f[i].b, st.a[db]);
   }
 }
 
@@ -261,23 +271,30 @@ __device__ __forceinline__ void scores(Lds& s, const Lds::Decays& d, int block) 
   f32x16 x;
 #pragma unroll
   for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+  Frag a[8], q[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    Frag a, q;
-    a.d[0] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k) + 4 * half]);
-    a.d[1] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k + 1) + 4 * half]);
-    q.w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * k + half)]);
-    x = mfma32_bf16(a.b, q.b, x);
+    a[k].d[0] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k) + 4 * half]);
+    a[k].d[1] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k + 1) + 4 * half]);
+    q[k].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * k + half)]);
   }
+  ahead();
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x = mfma32_bf16(a[k].b, q[k].b, x);
   const float hi = d.hi[i], lo = d.lo[i];
+  const bool below = block == 1;   // every key before every query
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
     float w[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int j = j0 + 16 * y + 8 * (e >> 2) + 4 * half + (e & 3);
-      const float decay = __builtin_amdgcn_exp2f((hi - d.hi[j]) + (lo - d.lo[j]));
-      w[e] = j <= i ? x[8 * y + e] * decay : 0.0f;
+    for (int q = 0; q < 2; ++q) {
+      const int j = j0 + 16 * y + 8 * q + 4 * half;
+      const f32x4 jh = *reinterpret_cast<const f32x4*>(&d.hi[j]), jl = *reinterpret_cast<const f32x4*>(&d.lo[j]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float reach = (hi - jh[e]) + (lo - jl[e]);
+        w[4 * q + e] = x[8 * y + 4 * q + e] * __builtin_amdgcn_exp2f(below || j + e <= i ? reach : -INFINITY);
+      }
     }
     Frag f[2];
     split8<2>(w, f);
@@ -295,7 +312,16 @@ __device__ __forceinline__ void from_state(f32x16 (&o)[2], State& st, const Lds&
     for (int r = 0; r < 16; ++r) o[ib][r] = 0.0f;
 #pragma unroll
   for (int db = 0; db < 4; ++db) {
-    asm volatile("" : "+v"(st.a[db]));   // the parts are made for each query head anew: there is no room to keep them
+    Frag q[2][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int ib = 0; ib < 2; ++ib) {
+        const int i = 32 * ib + l32;
+        q[x][ib].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 4 * db + 2 * x + half)]);
+      }
+    ahead();
+    keep(st.a[db]);   // the parts are made for each query head anew: there is no room to keep them
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       float y[8];
@@ -304,13 +330,9 @@ __device__ __forceinline__ void from_state(f32x16 (&o)[2], State& st, const Lds&
       Frag f[2];
       split8<2>(y, f);
 #pragma unroll
-      for (int ib = 0; ib < 2; ++ib) {
-        const int i = 32 * ib + l32;
-        Frag q;
-        q.w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 4 * db + 2 * x + half)]);
-        o[ib] = mfma32_bf16(f[1].b, q.b, o[ib]);
-        o[ib] = mfma32_bf16(f[0].b, q.b, o[ib]);
-      }
+      for (int y = 1; y >= 0; --y)
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib) o[ib] = mfma32_bf16(f[y].b, q[x][ib].b, o[ib]);
     }
   }
 #pragma unroll
@@ -325,17 +347,22 @@ __device__ __forceinline__ void from_state(f32x16 (&o)[2], State& st, const Lds&
 __device__ __forceinline__ void from_chunk(f32x16 (&o)[2], const Lds& s) {
   const int lane = lane_here(), wave = threadIdx.x >> 6;
 #pragma unroll
-  for (int block = 0; block < 3; ++block)
+  for (int block = 0; block < 3; ++block) {
+    Frag v[2], w[2][2];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const Frag v = columns(s.v, lane, (block == 2 ? 32 : 0) + 16 * y, 32 * wave);
-      f32x16& to = o[block == 0 ? 0 : 1];
-      Frag w;
-      w.w = s.p[block][y][1][lane];
-      to = mfma32_bf16(v.b, w.b, to);
-      w.w = s.p[block][y][0][lane];
-      to = mfma32_bf16(v.b, w.b, to);
+      v[y] = columns(s.v, lane, (block == 2 ? 32 : 0) + 16 * y, 32 * wave);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[y][i].w = s.p[block][y][i][lane];
     }
+    ahead();
+    f32x16& to = o[block == 0 ? 0 : 1];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      to = mfma32_bf16(v[y].b, w[y][1].b, to);
+      to = mfma32_bf16(v[y].b, w[y][0].b, to);
+    }
+  }
 }
 
 // The halves of a wave exchange channels, so that each lane stores 16 bytes of its query's row.
@@ -380,9 +407,11 @@ __global__ __launch_bounds__(256, 2) void linear_chunks_kernel(LinearParams p, i
   Rows rk, rv, rq;
   float decay = 0.0f;   // of the chunk after the next
   double total = 0.0;
-  load_rows(rk, k0, p.k_stride, g.n);
-  load_rows(rv, v0, p.v_stride, g.n);
-  if (kOut) load_rows(rq, q0 + h0 * kD, p.q_stride, g.n);
+  if (g.n > 0) {
+    load_rows(rk, k0, p.k_stride, g.n);
+    load_rows(rv, v0, p.v_stride, g.n);
+    if (kOut) load_rows(rq, q0 + h0 * kD, p.q_stride, g.n);
+  }
 
   State st;
   state_zero(st);
@@ -393,13 +422,17 @@ __global__ __launch_bounds__(256, 2) void linear_chunks_kernel(LinearParams p, i
   } else if (kOut) {
     raw_load(st, slot);
   }
+#pragma unroll
+  for (int db = 0; db < 4; ++db) keep(st.a[db]);   // else the first use in the loop waits, in every chunk, for all loads before it
   if (wave == 3) {
-    total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk));
+    total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n);
     decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
   }
-  store_rows(rk, s.k);
-  store_rows(rv, s.v);
-  if (kOut) store_queries(rq, s.q);
+  if (g.n > 0) {
+    store_rows(rk, s.k);
+    store_rows(rv, s.v);
+    if (kOut) store_queries(rq, s.q);
+  }
 
   for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
     const int rest = g.n - c - kC;   // tokens behind this chunk
@@ -410,7 +443,7 @@ __global__ __launch_bounds__(256, 2) void linear_chunks_kernel(LinearParams p, i
       load_rows(rv, v0 + (c + kC) * p.v_stride, p.v_stride, rest);
     }
     if (wave == 3 && rest > 0) {
-      total += put_decays(s.d[x ^ 1], decay);
+      total += put_decays(s.d[x ^ 1], decay, rest);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
     }
     if (kOut) {
