@@ -70,8 +70,10 @@ struct Lds {
   } d[2];                                      // of this chunk and the next
 };
 
-// Reads above stay above what uses them: left alone, the compiler reads each operand right before its product.
-__device__ __forceinline__ void ahead() { __builtin_amdgcn_sched_barrier(0); }
+// What stands before in the source stays before.  Products and the vector work of the next ones are written in
+// turns: a wave's own matrix and vector instructions overlap only so, and with two waves a SIMD there is too
+// little else to run beside them.  The compiler by itself puts all products of a step behind all its vector work.
+__device__ __forceinline__ void turn() { __builtin_amdgcn_sched_barrier(0); }
 
 // The lane, by a value of each use's own: what is worked out from it (LDS addresses above all) is not kept in
 // registers from one use to the next, of which there are not enough.
@@ -107,18 +109,20 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 // Eight FP32 values as the sum of kParts BF16 operands.  Two lose at most 2^-16 of each value, little beside
 // the rounding of an output to BF16; three 2^-24, as FP32 itself, for sums that stay in the state.
+// The i-th part of values 2 w and 2 w + 1; x becomes what is left.
+__device__ __forceinline__ void split2(float* x, Frag* part, int i, int w) {
+  uint32_t h = pack_bf16(x[2 * w], x[2 * w + 1]);
+  asm("" : "+v"(h));   // else the compiler makes the low half once more by itself
+  part[i].w[w] = h;
+  x[2 * w] -= bits_lo(h);
+  x[2 * w + 1] -= bits_hi(h);
+}
 template <int kParts>
 __device__ __forceinline__ void split8(float* x, Frag* part) {
 #pragma unroll
   for (int i = 0; i < kParts; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      uint32_t h = pack_bf16(x[e], x[e + 1]);
-      asm("" : "+v"(h));   // else the compiler makes the low half once more by itself
-      part[i].w[e >> 1] = h;
-      x[e] -= bits_lo(h);
-      x[e + 1] -= bits_hi(h);
-    }
+    for (int w = 0; w < 4; ++w) split2(x, part, i, w);
 }
 
 // Rows of a chunk, 16 lanes a row, four rows of each thread.  Rows from n (at least 1) on are row n - 1 again:
@@ -235,67 +239,100 @@ __device__ __forceinline__ double put_decays(Lds::Decays& d, float g, int n) {
 __device__ __forceinline__ void update(State& st, const Lds& s, const Lds::Decays& d) {
   const int wave = threadIdx.x >> 6, lane = lane_here(), half = lane >> 5;
   const float whole = d.from[kC - 1];
+  Frag v[2], k[2][4], f[2][3];
+  f32x4 to[2][2];
+  float y[8];
+  auto read_v = [&](int j) { v[j & 1] = columns(s.v, lane, 16 * j, 32 * wave); };
+  auto read_to = [&](int j, int q) { to[j & 1][q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]); };
+  auto read_k = [&](int j, int db) { k[j & 1][db] = columns(s.k, lane, 16 * j, 32 * db); };
+  auto split = [&](int j, int i, int w) {   // part i of the w-th pair of step j
+    if (i == 0) {
+      const uint32_t x = v[j & 1].w[w];
+      y[2 * w] = bits_lo(x) * to[j & 1][w >> 1][2 * (w & 1)];
+      y[2 * w + 1] = bits_hi(x) * to[j & 1][w >> 1][2 * (w & 1) + 1];
+    }
+    split2(y, f[j & 1], i, w);
+  };
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    read_v(j);
+    read_to(j, 0);
+    read_to(j, 1);
+  }
+#pragma unroll
+  for (int db = 0; db < 4; ++db) read_k(0, db);
+  turn();
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) split(0, i, w);
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
     for (int r = 0; r < 16; ++r) st.a[db][r] *= whole;
+  turn();
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const Frag v = columns(s.v, lane, 16 * j, 32 * wave);
-    f32x4 to[2];
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int q = 0; q < 2; ++q) to[q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]);
-    Frag k[4];
-#pragma unroll
-    for (int db = 0; db < 4; ++db) k[db] = columns(s.k, lane, 16 * j, 32 * db);
-    ahead();
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t w = v.w[e >> 1];
-      y[e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * to[e >> 2][e & 3];
+    for (int n = 0; n < 12; ++n) {
+      const int i = 2 - n / 4, db = n % 4;
+      st.a[db] = mfma32_bf16(k[j & 1][db].b, f[j & 1][i].b, st.a[db]);
+      if (j < 3) {
+        split(j + 1, n / 4, n % 4);
+        if (n < 4) read_k(j + 1, n);
+      }
+      if (j < 2 && n >= 9) {   // the last reads of step j + 1's v and decays are behind
+        if (n == 9) read_v(j + 2);
+        else read_to(j + 2, n - 10);
+      }
+      turn();
     }
-    Frag f[3];
-    split8<3>(y, f);
-#pragma unroll
-    for (int i = 2; i >= 0; --i)
-#pragma unroll
-      for (int db = 0; db < 4; ++db) st.a[db] = mfma32_bf16(k[db].b, f[i].b, st.a[db]);
-  }
 }
 
 // Scores of one block (keys j0 .., queries i0 ..), transposed, with their decays, as operands.
 __device__ __forceinline__ void scores(Lds& s, const Lds::Decays& d, int block) {
   const int lane = lane_here(), half = lane >> 5, l32 = lane & 31;
   const int i0 = block == 0 ? 0 : 32, j0 = block == 2 ? 32 : 0, i = i0 + l32, jr = j0 + l32;
+  Frag a[4], q[4];
+  f32x4 jh[2], jl[2];
+  auto read = [&](int k) {
+    a[k & 3].d[0] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k) + 4 * half]);
+    a[k & 3].d[1] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k + 1) + 4 * half]);
+    q[k & 3].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * k + half)]);
+  };
+  auto read_decays = [&](int r4) {
+    const int j = j0 + 8 * r4 + 4 * half;
+    jh[r4 & 1] = *reinterpret_cast<const f32x4*>(&d.hi[j]);
+    jl[r4 & 1] = *reinterpret_cast<const f32x4*>(&d.lo[j]);
+  };
+  read_decays(0);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) read(k);
+  read_decays(1);
+  const float hi = d.hi[i], lo = d.lo[i];
+  const int last = block == 1 ? kC : i;   // of the keys that the query sees: in block 1 all
+  turn();
   f32x16 x;
 #pragma unroll
   for (int r = 0; r < 16; ++r) x[r] = 0.0f;
-  Frag a[8], q[8];
+  float decay[16];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    a[k].d[0] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k) + 4 * half]);
-    a[k].d[1] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k + 1) + 4 * half]);
-    q[k].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * k + half)]);
-  }
-  ahead();
+    x = mfma32_bf16(a[k & 3].b, q[k & 3].b, x);
+    if (k < 4) read(k + 4);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) x = mfma32_bf16(a[k].b, q[k].b, x);
-  const float hi = d.hi[i], lo = d.lo[i];
-  const bool below = block == 1;   // every key before every query
+    for (int r = 2 * k; r < 2 * k + 2; ++r) {
+      const float reach = (hi - jh[r >> 2 & 1][r & 3]) + (lo - jl[r >> 2 & 1][r & 3]);
+      decay[r] = __builtin_amdgcn_exp2f(j0 + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? reach : -INFINITY);
+    }
+    if (k == 1 || k == 3) read_decays(k / 2 + 2);
+    turn();
+  }
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
     float w[8];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int j = j0 + 16 * y + 8 * q + 4 * half;
-      const f32x4 jh = *reinterpret_cast<const f32x4*>(&d.hi[j]), jl = *reinterpret_cast<const f32x4*>(&d.lo[j]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float reach = (hi - jh[e]) + (lo - jl[e]);
-        w[4 * q + e] = x[8 * y + 4 * q + e] * __builtin_amdgcn_exp2f(below || j + e <= i ? reach : -INFINITY);
-      }
-    }
+    for (int e = 0; e < 8; ++e) w[e] = x[8 * y + e] * decay[8 * y + e];
     Frag f[2];
     split8<2>(w, f);
     s.p[block][y][0][lane] = f[0].w;
@@ -303,65 +340,78 @@ __device__ __forceinline__ void scores(Lds& s, const Lds::Decays& d, int block) 
   }
 }
 
-// o (transposed: rows are channels of v, 32 queries each) = exp(b_i) S^T q_i.
+// o (transposed: rows are channels of v, 32 queries each) = exp(b_i) S^T q_i.  The state's parts are made for each
+// query head anew: there is no room to keep them.
 __device__ __forceinline__ void from_state(f32x16 (&o)[2], State& st, const Lds& s, const Lds::Decays& d) {
   const int lane = lane_here(), half = lane >> 5, l32 = lane & 31;
+  Frag q[2][2], f[2][2];
+  float y[8];
+  auto read = [&](int g, int ib) {
+    const int i = 32 * ib + l32;
+    q[g & 1][ib].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * g + half)]);
+  };
+  auto split = [&](int g, int w) {
+    y[2 * w] = st.a[g >> 1][8 * (g & 1) + 2 * w];
+    y[2 * w + 1] = st.a[g >> 1][8 * (g & 1) + 2 * w + 1];
+    split2(y, f[g & 1], 0, w);
+    split2(y, f[g & 1], 1, w);
+  };
+#pragma unroll
+  for (int db = 0; db < 4; ++db) keep(st.a[db]);
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int ib = 0; ib < 2; ++ib) read(g, ib);
+  float from[2];
+#pragma unroll
+  for (int ib = 0; ib < 2; ++ib) from[ib] = d.from[32 * ib + l32];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) split(0, w);
 #pragma unroll
   for (int ib = 0; ib < 2; ++ib)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[ib][r] = 0.0f;
+  turn();
 #pragma unroll
-  for (int db = 0; db < 4; ++db) {
-    Frag q[2][2];
+  for (int g = 0; g < 8; ++g)
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int ib = 0; ib < 2; ++ib) {
-        const int i = 32 * ib + l32;
-        q[x][ib].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 4 * db + 2 * x + half)]);
-      }
-    ahead();
-    keep(st.a[db]);   // the parts are made for each query head anew: there is no room to keep them
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = st.a[db][8 * x + e];
-      Frag f[2];
-      split8<2>(y, f);
-#pragma unroll
-      for (int y = 1; y >= 0; --y)
-#pragma unroll
-        for (int ib = 0; ib < 2; ++ib) o[ib] = mfma32_bf16(f[y].b, q[x][ib].b, o[ib]);
+    for (int n = 0; n < 4; ++n) {
+      const int ib = n & 1;
+      o[ib] = mfma32_bf16(f[g & 1][1 - n / 2].b, q[g & 1][ib].b, o[ib]);
+      if (g < 7) split(g + 1, n);
+      if (g < 6 && n >= 2) read(g + 2, ib);
+      turn();
     }
-  }
 #pragma unroll
-  for (int ib = 0; ib < 2; ++ib) {
-    const float from = d.from[32 * ib + l32];
+  for (int ib = 0; ib < 2; ++ib)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[ib][r] *= from;
-  }
+    for (int r = 0; r < 16; ++r) o[ib][r] *= from[ib];
 }
 
 // o += V^T scores.
 __device__ __forceinline__ void from_chunk(f32x16 (&o)[2], const Lds& s) {
   const int lane = lane_here(), wave = threadIdx.x >> 6;
+  Frag v[2][2], w[2][2][2];
+  auto read = [&](int block) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      v[block & 1][y] = columns(s.v, lane, (block == 2 ? 32 : 0) + 16 * y, 32 * wave);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[block & 1][y][i].w = s.p[block][y][i][lane];
+    }
+  };
+  read(0);
+  read(1);
+  turn();
 #pragma unroll
   for (int block = 0; block < 3; ++block) {
-    Frag v[2], w[2][2];
-#pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      v[y] = columns(s.v, lane, (block == 2 ? 32 : 0) + 16 * y, 32 * wave);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) w[y][i].w = s.p[block][y][i][lane];
-    }
-    ahead();
     f32x16& to = o[block == 0 ? 0 : 1];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      to = mfma32_bf16(v[y].b, w[y][1].b, to);
-      to = mfma32_bf16(v[y].b, w[y][0].b, to);
-    }
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int i = 1; i >= 0; --i) to = mfma32_bf16(v[block & 1][y].b, w[block & 1][y][i].b, to);
+    if (block == 0) read(2);
+    turn();
   }
 }
 
