@@ -167,7 +167,7 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   if (a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
   const PrefillSpace s = prefill_space(a->batch, a->total_tokens, a->max_seqlen, a->h_kv);
   const int64_t items = s.segments * a->h_kv;
-  if (items > (int64_t)UINT32_MAX / 256 - 8) return MPFA_ERR_UNSUPPORTED;
+  if (items > (int64_t)UINT32_MAX / 512 - 8) return MPFA_ERR_UNSUPPORTED;
   if (s.split && (!workspace || workspace_bytes < s.bytes || !aligned16(workspace))) return MPFA_ERR_WORKSPACE;
   p.segment = s.segment;
   p.split = s.split;

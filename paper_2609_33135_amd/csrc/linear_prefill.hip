@@ -18,6 +18,7 @@ namespace mpfa {
 namespace {
 
 constexpr int kC = kLinChunk;
+constexpr int kThreads = 512;         // eight waves of 16 columns (channels of v) each
 constexpr double kLog2e = 1.4426950408889634;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -57,17 +58,23 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
 }
 
 // Rows of 128 channels in LDS lie without padding, their 16-byte pieces exchanged by row so that neither 16
-// rows' same piece nor four rows' same 64 bytes (a transposing read) meet in a bank.
+// rows' same piece nor eight rows' same two pieces (a transposing read) meet in a bank.
 typedef uint16_t LdsRows[kC][kD];
-__device__ __forceinline__ int piece(int row, int c) { return 8 * (c ^ ((row & 3) << 2 | (row >> 2 & 3))); }
+__device__ __forceinline__ int piece_row(int row) { return (row & 3) << 2 | (row >> 1 & 2) | (row >> 3 & 1); }
+__device__ __forceinline__ int piece(int row, int c) { return 8 * (c ^ piece_row(row)); }
 
-struct Lds {
-  LdsRows k, v, q;                             // q: in each 16 channels those of a lane half side by side
-  u32x4 p[3][2][2][64];                        // scores: block, step of 16 keys, high and low parts, lane
-  struct Decays {
-    float hi[kC], lo[kC];                      // log2 of the decays from the chunk's start, in two parts
-    float from[kC], to[kC];                    // exp2 of them; exp2 from each token to the chunk's end
-  } d[2];                                      // of this chunk and the next
+// What a chunk needs of its decays.
+struct Decays {
+  float hi[kC], lo[kC];                        // log2 of the decays from the chunk's start, in two parts
+  float from[kC], to[kC];                      // exp2 of them times the scale; exp2 from each token to the chunk's end
+};
+struct Keys {                                  // `sums` has these alone
+  LdsRows k, v;
+  Decays d[2];                                 // of this chunk and the next
+};
+struct Lds : Keys {
+  LdsRows q;                                   // queries, then outputs; see head_slot
+  u32x4 p[6][2][64];                           // scores: 16 queries by 32 keys (see unit_of), high and low parts, lane
 };
 
 // What stands before in the source stays before.  Products and the vector work of the next ones are written in
@@ -75,27 +82,43 @@ struct Lds {
 // little else to run beside them.  The compiler by itself puts all products of a step behind all its vector work.
 __device__ __forceinline__ void turn() { __builtin_amdgcn_sched_barrier(0); }
 
-// The lane, by a value of each use's own: what is worked out from it (LDS addresses above all) is not kept in
+// The thread, by a value of each use's own: what is worked out from it (LDS addresses above all) is not kept in
 // registers from one use to the next, of which there are not enough.
-__device__ __forceinline__ int lane_here() {
-  int lane = threadIdx.x & 63;
-  asm volatile("" : "+v"(lane));
-  return lane;
+__device__ __forceinline__ int thread_here() {
+  int thread = threadIdx.x;
+  asm volatile("" : "+v"(thread));
+  return thread;
+}
+__device__ __forceinline__ int lane_here() { return thread_here() & 63; }
+
+// LDS by byte offsets: rows are 256 bytes, so a piece's exchange is an exclusive or of a lane's offset, which
+// serves all rows that lie a constant apart.
+template <typename T>
+__device__ __forceinline__ T read_lds(const LdsRows& rows, int at) {
+  typedef __attribute__((address_space(3))) const char lds_char;
+  typedef __attribute__((address_space(3))) const T lds_T;
+  return *(lds_T*)((lds_char*)&rows + at);
 }
 
-// Four tokens (rows t .. t + 3) of the lane's column c0 + lane % 32, t = t0 + 4 * (lane / 32): each
-// group of 16 lanes reads a block of four rows and 16 columns, and gets it transposed.
-__device__ __forceinline__ s16x4 column4(const LdsRows& rows, int lane, int t0, int c0) {
-  typedef __attribute__((address_space(3))) s16x4 lds4;
-  const int i = lane & 15, row = t0 + 4 * (lane >> 5) + (i >> 2);
-  const uint16_t* at = &rows[row][piece(row, c0 / 8 + (lane >> 4 & 1) * 2 + (i >> 1 & 1)) + 4 * (i & 1)];
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)at);
+// Offset of the lane's own row of 16 rows, in it the piece 0.
+__device__ __forceinline__ int row_at(int lane) { return 256 * (lane & 15) + 16 * piece_row(lane & 15); }
+
+// Transposing reads: four tokens t .. t + 3, t = t0 + 4 * (lane / 16), of the lane's column c0 + lane % 16: each
+// group of 16 lanes reads a block of four rows and 16 columns.  columns_at: of t0 = c0 = 0.
+__device__ __forceinline__ int columns_at(int lane) {
+  const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2);
+  return 256 * row + 16 * ((i >> 1 & 1) ^ piece_row(row)) + 8 * (i & 1);
 }
-// The tokens of one 16-token step in the order in which an accumulator holds its rows.
-__device__ __forceinline__ Frag columns(const LdsRows& rows, int lane, int t0, int c0) {
+__device__ __forceinline__ s16x4 column4(const LdsRows& rows, int at) {
+  typedef __attribute__((address_space(3))) s16x4 lds4;
+  typedef __attribute__((address_space(3))) char lds_char;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)((lds_char*)const_cast<LdsRows*>(&rows) + at));
+}
+// The tokens t0 .. t0 + 31 in the order in which two accumulators of 16 rows hold theirs.
+__device__ __forceinline__ Frag columns(const LdsRows& rows, int at, int t0) {
   Frag f;
-  f.s[0] = column4(rows, lane, t0, c0);
-  f.s[1] = column4(rows, lane, t0 + 8, c0);
+  f.s[0] = column4(rows, at + 256 * t0);
+  f.s[1] = column4(rows, at + 256 * (t0 + 16));
   return f;
 }
 
@@ -125,80 +148,78 @@ __device__ __forceinline__ void split8(float* x, Frag* part) {
     for (int w = 0; w < 4; ++w) split2(x, part, i, w);
 }
 
-// Rows of a chunk, 16 lanes a row, four rows of each thread.  Rows from n (at least 1) on are row n - 1 again:
-// nothing of them reaches an output or the state, by the scores' mask and a decay of 0.
+// Rows of a chunk, 16 lanes a row.  Rows from n (at least 1) on are row n - 1 again: nothing of them reaches an
+// output or the state, by the scores' mask and a decay of 0.
 struct Rows {
-  u32x4 w[4];
-};
-__device__ __forceinline__ void load_rows(Rows& r, const uint16_t* x, int64_t stride, int n) {
-  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
+  static constexpr int kEach = kC * 16 / kThreads;
+  u32x4 w[kEach];
+  __device__ __forceinline__ void load(const uint16_t* x, int64_t stride, int n) {
+    const int thread = thread_here();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r.w[i] = *reinterpret_cast<const u32x4*>(x + min(row + 16 * i, n - 1) * stride + 8 * c);
-}
+    for (int i = 0; i < kEach; ++i)
+      w[i] = *reinterpret_cast<const u32x4*>(x + min(row(thread, i), n - 1) * stride + 8 * (thread & 15));
+  }
+  static __device__ __forceinline__ int row(int thread, int i) { return thread / 16 + kThreads / 16 * i; }
+};
 __device__ __forceinline__ void store_rows(const Rows& r, LdsRows& to) {
-  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
+  const int thread = thread_here();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(&to[row + 16 * i][piece(row + 16 * i, c)]) = r.w[i];
+  for (int i = 0; i < Rows::kEach; ++i) {
+    const int row = Rows::row(thread, i);
+    *reinterpret_cast<u32x4*>(&to[row][piece(row, thread & 15)]) = r.w[i];
+  }
 }
-// Queries: of 16 channels 0-3, 8-11 | 4-7, 12-15.
+// Queries of a head and later its outputs: of 32 channels those that a group of 16 lanes takes side by side, four
+// and the four that lie 16 further.  A thread's 16 bytes lie in two halves of pieces, for queries and outputs the
+// same, so a thread that has read its outputs may put queries in their place.
+__device__ __forceinline__ u32x2* head_slot(LdsRows& rows, int thread, int i, int x) {
+  const int row = Rows::row(thread, i), c = thread & 15;
+  return reinterpret_cast<u32x2*>(&rows[row][piece(row, (c & ~3) + 2 * (c & 1) + x) + 2 * (c & 2)]);
+}
 __device__ __forceinline__ void store_queries(const Rows& r, LdsRows& to) {
-  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
+  const int thread = thread_here();
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < Rows::kEach; ++i)
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-      *reinterpret_cast<u32x2*>(&to[row + 16 * i][piece(row + 16 * i, (c & ~1) + x) + 4 * (c & 1)]) = (u32x2){r.w[i][2 * x], r.w[i][2 * x + 1]};
+    for (int x = 0; x < 2; ++x) *head_slot(to, thread, i, x) = (u32x2){r.w[i][2 * x], r.w[i][2 * x + 1]};
 }
 
-// The value is in its registers here: loads of it have arrived, and what is made of it is not made before.
-__device__ __forceinline__ void keep(f32x16& x) { asm volatile("" : "+v"(x)); }
+// The value is in its registers here: loads of it have arrived.
+__device__ __forceinline__ void keep(f32x4& x) { asm volatile("" : "+v"(x)); }
 
-// The state's part of a wave: 32 columns (channels of v), accumulator db the rows (channels of k) 32 db ..
+// A wave's part of the state: its 16 columns (channels of v), blocks of 16 rows (channels of k).
 struct State {
-  f32x16 a[4];
+  f32x4 a[8];
 };
-__device__ __forceinline__ int state_row(int db, int r) { return 32 * db + 8 * (r >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (r & 3); }
-
+__device__ __forceinline__ int wave_here() { return threadIdx.x >> 6; }
+__device__ __forceinline__ int state_at(int m, int r) {   // in [128][128]
+  const int lane = threadIdx.x & 63;
+  return (16 * m + 4 * (lane >> 4) + r) * kD + 16 * wave_here() + (lane & 15);
+}
 __device__ __forceinline__ void state_zero(State& s) {
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s.a[db][r] = 0.0f;
+  for (int m = 0; m < 8; ++m) s.a[m] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
 }
 __device__ __forceinline__ void state_load(State& s, const float* from) {
-  const int col = 32 * (threadIdx.x >> 6) + (threadIdx.x & 31);
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+  for (int m = 0; m < 8; ++m)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s.a[db][r] = from[state_row(db, r) * kD + col];
+    for (int r = 0; r < 4; ++r) s.a[m][r] = from[state_at(m, r)];
 }
 __device__ __forceinline__ void state_store(const State& s, float* to) {
-  const int col = 32 * (threadIdx.x >> 6) + (threadIdx.x & 31);
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
+  for (int m = 0; m < 8; ++m)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) to[state_row(db, r) * kD + col] = s.a[db][r];
+    for (int r = 0; r < 4; ++r) to[state_at(m, r)] = s.a[m][r];
 }
 // In the workspace a state lies as the accumulators do.
-__device__ __forceinline__ f32x4* raw_at(float* ws, int db, int r4) {
-  return reinterpret_cast<f32x4*>(ws) + (((threadIdx.x >> 6) * 4 + db) * 4 + r4) * 64 + (threadIdx.x & 63);
-}
 __device__ __forceinline__ void raw_store(const State& s, float* ws) {
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4)
-      *raw_at(ws, db, r4) = (f32x4){s.a[db][4 * r4], s.a[db][4 * r4 + 1], s.a[db][4 * r4 + 2], s.a[db][4 * r4 + 3]};
+  for (int m = 0; m < 8; ++m) reinterpret_cast<f32x4*>(ws)[m * kThreads + threadIdx.x] = s.a[m];
 }
-__device__ __forceinline__ void raw_load(State& s, float* ws) {
+__device__ __forceinline__ void raw_load(State& s, const float* ws) {
 #pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      const f32x4 x = *raw_at(ws, db, r4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s.a[db][4 * r4 + e] = x[e];
-    }
+  for (int m = 0; m < 8; ++m) s.a[m] = reinterpret_cast<const f32x4*>(ws)[m * kThreads + threadIdx.x];
 }
 
 // Log decays of a chunk (lane = token; 0 behind its last).
@@ -217,7 +238,7 @@ __device__ __forceinline__ double moved(double x) {   // lanes without a source 
 
 // What a chunk of n tokens needs of its decays g; returns log2 of the whole chunk's.  Summed in 64 bits: after a token that
 // clears the state sums are large and their differences small.
-__device__ __forceinline__ double put_decays(Lds::Decays& d, float g, int n) {
+__device__ __forceinline__ double put_decays(Decays& d, float g, int n, float scale) {
   const int lane = threadIdx.x & 63;
   double x = (double)fminf(fmaxf(g, kLinLeastDecay), 0.0f) * kLog2e;
   x += moved<0x111, 0xF>(x);   // from 1, 2, 4, 8 lanes before in a row of 16
@@ -230,303 +251,300 @@ __device__ __forceinline__ double put_decays(Lds::Decays& d, float g, int n) {
   const float hi = (float)x;
   d.hi[lane] = hi;
   d.lo[lane] = (float)(x - (double)hi);
-  d.from[lane] = __builtin_amdgcn_exp2f(hi);
+  d.from[lane] = __builtin_amdgcn_exp2f(hi) * scale;
   d.to[lane] = lane < n ? __builtin_amdgcn_exp2f((float)(end - x)) : 0.0f;
   return end;
 }
 
 // S' = exp(b_last) S + K^T (exp(b_last - b_j) V): K is an operand as it is, V with its decay in three parts.
-__device__ __forceinline__ void update(State& st, const Lds& s, const Lds::Decays& d) {
-  const int wave = threadIdx.x >> 6, lane = lane_here(), half = lane >> 5;
-  const float whole = d.from[kC - 1];
-  Frag v[2], k[2][4], f[2][3];
-  f32x4 to[2][2];
-  float y[8];
-  auto read_v = [&](int j) { v[j & 1] = columns(s.v, lane, 16 * j, 32 * wave); };
-  auto read_to = [&](int j, int q) { to[j & 1][q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]); };
-  auto read_k = [&](int j, int db) { k[j & 1][db] = columns(s.k, lane, 16 * j, 32 * db); };
-  auto split = [&](int j, int i, int w) {   // part i of the w-th pair of step j
-    if (i == 0) {
-      const uint32_t x = v[j & 1].w[w];
-      y[2 * w] = bits_lo(x) * to[j & 1][w >> 1][2 * (w & 1)];
-      y[2 * w + 1] = bits_hi(x) * to[j & 1][w >> 1][2 * (w & 1) + 1];
-    }
-    split2(y, f[j & 1], i, w);
-  };
+__device__ __forceinline__ void update(State& st, const Keys& s, const Decays& d) {
+  const int lane = lane_here(), at = columns_at(lane), vat = at ^ 32 * wave_here();
+  const float whole = __builtin_amdgcn_exp2f(d.hi[kC - 1]);
+  Frag f[2][3], k[2];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    read_v(j);
-    read_to(j, 0);
-    read_to(j, 1);
+  for (int j = 0; j < 2; ++j) {   // 32 tokens each
+    const Frag v = columns(s.v, vat, 32 * j);
+    float y[8];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const f32x4 decay = *reinterpret_cast<const f32x4*>(&d.to[32 * j + 16 * q + 4 * (lane >> 4)]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t w = v.w[2 * q + (e >> 1)];
+        y[4 * q + e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * decay[e];
+      }
+    }
+    split8<3>(y, f[j]);
   }
+  auto read = [&](int n) { k[n & 1] = columns(s.k, at ^ 32 * (n >> 1), 32 * (n & 1)); };
+  read(0);
 #pragma unroll
-  for (int db = 0; db < 4; ++db) read_k(0, db);
-  turn();
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-#pragma unroll
-    for (int w = 0; w < 4; ++w) split(0, i, w);
-#pragma unroll
-  for (int db = 0; db < 4; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) st.a[db][r] *= whole;
-  turn();
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int n = 0; n < 12; ++n) {
-      const int i = 2 - n / 4, db = n % 4;
-      st.a[db] = mfma32_bf16(k[j & 1][db].b, f[j & 1][i].b, st.a[db]);
-      if (j < 3) {
-        split(j + 1, n / 4, n % 4);
-        if (n < 4) read_k(j + 1, n);
-      }
-      if (j < 2 && n >= 9) {   // the last reads of step j + 1's v and decays are behind
-        if (n == 9) read_v(j + 2);
-        else read_to(j + 2, n - 10);
-      }
-      turn();
-    }
-}
-
-// Scores of one block (keys j0 .., queries i0 ..), transposed, with their decays, as operands.
-__device__ __forceinline__ void scores(Lds& s, const Lds::Decays& d, int block) {
-  const int lane = lane_here(), half = lane >> 5, l32 = lane & 31;
-  const int i0 = block == 0 ? 0 : 32, j0 = block == 2 ? 32 : 0, i = i0 + l32, jr = j0 + l32;
-  Frag a[4], q[4];
-  f32x4 jh[2], jl[2];
-  auto read = [&](int k) {
-    a[k & 3].d[0] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k) + 4 * half]);
-    a[k & 3].d[1] = *reinterpret_cast<const u32x2*>(&s.k[jr][piece(jr, 2 * k + 1) + 4 * half]);
-    q[k & 3].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * k + half)]);
-  };
-  auto read_decays = [&](int r4) {
-    const int j = j0 + 8 * r4 + 4 * half;
-    jh[r4 & 1] = *reinterpret_cast<const f32x4*>(&d.hi[j]);
-    jl[r4 & 1] = *reinterpret_cast<const f32x4*>(&d.lo[j]);
-  };
-  read_decays(0);
-#pragma unroll
-  for (int k = 0; k < 4; ++k) read(k);
-  read_decays(1);
-  const float hi = d.hi[i], lo = d.lo[i];
-  const int last = block == 1 ? kC : i;   // of the keys that the query sees: in block 1 all
-  turn();
-  f32x16 x;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = 0.0f;
-  float decay[16];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    x = mfma32_bf16(a[k & 3].b, q[k & 3].b, x);
-    if (k < 4) read(k + 4);
-#pragma unroll
-    for (int r = 2 * k; r < 2 * k + 2; ++r) {
-      const float reach = (hi - jh[r >> 2 & 1][r & 3]) + (lo - jl[r >> 2 & 1][r & 3]);
-      decay[r] = __builtin_amdgcn_exp2f(j0 + 8 * (r >> 2) + 4 * half + (r & 3) <= last ? reach : -INFINITY);
-    }
-    if (k == 1 || k == 3) read_decays(k / 2 + 2);
+  for (int n = 0; n < 16; ++n) {
+    f32x4& a = st.a[n >> 1];
+    if (n < 15) read(n + 1);
     turn();
-  }
+    if (!(n & 1)) {
 #pragma unroll
-  for (int y = 0; y < 2; ++y) {
-    float w[8];
+      for (int r = 0; r < 4; ++r) a[r] *= whole;
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = x[8 * y + e] * decay[8 * y + e];
-    Frag f[2];
-    split8<2>(w, f);
-    s.p[block][y][0][lane] = f[0].w;
-    s.p[block][y][1][lane] = f[1].w;
+    for (int i = 2; i >= 0; --i) a = mfma_bf16(k[n & 1].b, f[n & 1][i].b, a);
   }
 }
 
-// o (transposed: rows are channels of v, 32 queries each) = exp(b_i) S^T q_i.  The state's parts are made for each
-// query head anew: there is no room to keep them.
-__device__ __forceinline__ void from_state(f32x16 (&o)[2], State& st, const Lds& s, const Lds::Decays& d) {
-  const int lane = lane_here(), half = lane >> 5, l32 = lane & 31;
-  Frag q[2][2], f[2][2];
-  float y[8];
-  auto read = [&](int g, int ib) {
-    const int i = 32 * ib + l32;
-    q[g & 1][ib].w = *reinterpret_cast<const u32x4*>(&s.q[i][piece(i, 2 * g + half)]);
-  };
-  auto split = [&](int g, int w) {
-    y[2 * w] = st.a[g >> 1][8 * (g & 1) + 2 * w];
-    y[2 * w + 1] = st.a[g >> 1][8 * (g & 1) + 2 * w + 1];
-    split2(y, f[g & 1], 0, w);
-    split2(y, f[g & 1], 1, w);
-  };
+// A unit of scores: queries 16 i .., keys 32 j .. .  Six of them hold all keys that queries see.
+struct Unit {
+  int i, j;
+};
+__device__ __forceinline__ Unit unit_of(int u) { return u < 2 ? Unit{u, 0} : Unit{2 + (u - 2) / 2, u & 1}; }
+
+// The decays of a unit's scores, as these lie in the accumulators, times the scale; 0 for keys behind the query.
+__device__ __forceinline__ void score_decays(const Decays& d, int u, float scale, float (&decay)[8]) {
+  const int lane = threadIdx.x & 63;
+  const Unit at = unit_of(u);
+  const int i = 16 * at.i + (lane & 15);
+  const float hi = d.hi[i], lo = d.lo[i];
 #pragma unroll
-  for (int db = 0; db < 4; ++db) keep(st.a[db]);
+  for (int q = 0; q < 2; ++q) {
+    const int j = 32 * at.j + 16 * q + 4 * (lane >> 4);
+    const f32x4 jh = *reinterpret_cast<const f32x4*>(&d.hi[j]), jl = *reinterpret_cast<const f32x4*>(&d.lo[j]);
 #pragma unroll
-  for (int g = 0; g < 2; ++g)
+    for (int e = 0; e < 4; ++e)
+      decay[4 * q + e] = __builtin_amdgcn_exp2f(j + e <= i ? (hi - jh[e]) + (lo - jl[e]) : -INFINITY) * scale;
+  }
+}
+
+// Scores of one unit, transposed, as operands.
+__device__ __forceinline__ void scores(Lds& s, int u, const float (&decay)[8]) {
+  const int lane = lane_here(), g = lane >> 4;
+  const Unit at = unit_of(u);
+  const int ka = (row_at(lane) ^ 16 * (g >> 1)) + 8 * (g & 1) + 256 * 32 * at.j, qa = (row_at(lane) ^ 16 * g) + 256 * 16 * at.i;
+  f32x4 x[2] = {};
 #pragma unroll
-    for (int ib = 0; ib < 2; ++ib) read(g, ib);
-  float from[2];
+  for (int k = 0; k < 4; ++k) {   // 32 channels each, in the order of the queries
+    Frag a[2], q;
 #pragma unroll
-  for (int ib = 0; ib < 2; ++ib) from[ib] = d.from[32 * ib + l32];
-#pragma unroll
-  for (int w = 0; w < 4; ++w) split(0, w);
-#pragma unroll
-  for (int ib = 0; ib < 2; ++ib)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[ib][r] = 0.0f;
-  turn();
-#pragma unroll
-  for (int g = 0; g < 8; ++g)
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int ib = n & 1;
-      o[ib] = mfma32_bf16(f[g & 1][1 - n / 2].b, q[g & 1][ib].b, o[ib]);
-      if (g < 7) split(g + 1, n);
-      if (g < 6 && n >= 2) read(g + 2, ib);
-      turn();
+    for (int y = 0; y < 2; ++y) {
+      a[y].d[0] = read_lds<u32x2>(s.k, (ka ^ 64 * k) + 256 * 16 * y);
+      a[y].d[1] = read_lds<u32x2>(s.k, (ka ^ (64 * k + 32)) + 256 * 16 * y);
     }
+    q.w = read_lds<u32x4>(s.q, qa ^ 64 * k);
 #pragma unroll
-  for (int ib = 0; ib < 2; ++ib)
+    for (int y = 0; y < 2; ++y) x[y] = mfma_bf16(a[y].b, q.b, x[y]);
+  }
+  float w[8];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) o[ib][r] *= from[ib];
+  for (int e = 0; e < 8; ++e) w[e] = x[e >> 2][e & 3] * decay[e];
+  Frag f[2];
+  split8<2>(w, f);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) s.p[u][i][lane] = f[i].w;
+}
+
+// Outputs of the chunk's queries, 16 a block: rows are the wave's channels of v.
+struct Outputs {
+  f32x4 o[4];
+};
+
+// o = scale exp(b_i) S^T q_i.
+__device__ __forceinline__ void from_state(Outputs& to, const State& st, const Lds& s, const Decays& d) {
+  const int lane = lane_here(), qa = row_at(lane) ^ 16 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to.o[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {   // 32 channels of k each
+    Frag q[4], f[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[i].w = read_lds<u32x4>(s.q, (qa ^ 64 * x) + 256 * 16 * i);
+    turn();
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = st.a[2 * x + (e >> 2)][e & 3];
+    split8<2>(y, f);
+#pragma unroll
+    for (int n = 1; n >= 0; --n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to.o[i] = mfma_bf16(f[n].b, q[i].b, to.o[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to.o[i] *= d.from[16 * i + (lane & 15)];
 }
 
 // o += V^T scores.
-__device__ __forceinline__ void from_chunk(f32x16 (&o)[2], const Lds& s) {
-  const int lane = lane_here(), wave = threadIdx.x >> 6;
-  Frag v[2][2], w[2][2][2];
-  auto read = [&](int block) {
+__device__ __forceinline__ void from_chunk(Outputs& to, const Lds& s) {
+  const int lane = lane_here(), vat = columns_at(lane) ^ 32 * wave_here();
+  Frag v[2];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      v[block & 1][y] = columns(s.v, lane, (block == 2 ? 32 : 0) + 16 * y, 32 * wave);
+  for (int j = 0; j < 2; ++j) v[j] = columns(s.v, vat, 32 * j);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) w[block & 1][y][i].w = s.p[block][y][i][lane];
+  for (int u = 0; u < 6; ++u) {
+    const Unit at = unit_of(u);
+#pragma unroll
+    for (int n = 1; n >= 0; --n) {
+      Frag w;
+      w.w = s.p[u][n][lane];
+      to.o[at.i] = mfma_bf16(v[at.j].b, w.b, to.o[at.i]);
     }
-  };
-  read(0);
-  read(1);
-  turn();
-#pragma unroll
-  for (int block = 0; block < 3; ++block) {
-    f32x16& to = o[block == 0 ? 0 : 1];
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int i = 1; i >= 0; --i) to = mfma32_bf16(v[block & 1][y].b, w[block & 1][y][i].b, to);
-    if (block == 0) read(2);
-    turn();
   }
 }
 
-// The halves of a wave exchange channels, so that each lane stores 16 bytes of its query's row.
-__device__ __forceinline__ void store_out(const f32x16& o, uint16_t* row, float scale) {
-  const int half = (threadIdx.x & 63) >> 5;
+// Outputs to the place of the queries, from there whole rows to memory.
+__device__ __forceinline__ void put_outputs(const Outputs& out, LdsRows& rows) {
+  const int lane = lane_here(), wave = wave_here(), at = (row_at(lane) ^ 16 * (4 * (wave >> 1) + (lane >> 4))) + 8 * (wave & 1);
 #pragma unroll
-  for (int a = 0; a < 4; a += 2) {
-    u32x4 w;
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<u32x2*>(reinterpret_cast<char*>(&rows) + at + 256 * 16 * i) =
+        (u32x2){pack_bf16(out.o[i][0], out.o[i][1]), pack_bf16(out.o[i][2], out.o[i][3])};
+}
+__device__ __forceinline__ void store_outputs(LdsRows& rows, uint16_t* to, int64_t stride, int n) {
+  const int thread = thread_here();
+  u32x4 w[Rows::kEach];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const uint32_t first = pack_bf16(o[4 * a + 2 * x] * scale, o[4 * a + 2 * x + 1] * scale);
-      const uint32_t second = pack_bf16(o[4 * a + 4 + 2 * x] * scale, o[4 * a + 5 + 2 * x] * scale);
-      const auto both = __builtin_amdgcn_permlane32_swap(first, second, false, false);
-      w[x] = both[0];
-      w[2 + x] = both[1];
-    }
-    if (row) *reinterpret_cast<u32x4*>(row + 8 * a + 8 * half) = w;
+  for (int i = 0; i < Rows::kEach; ++i) {
+    const u32x2 a = *head_slot(rows, thread, i, 0), b = *head_slot(rows, thread, i, 1);
+    w[i] = (u32x4){a[0], a[1], b[0], b[1]};
+  }
+#pragma unroll
+  for (int i = 0; i < Rows::kEach; ++i) {
+    const int row = Rows::row(thread, i);
+    if (row < n) *reinterpret_cast<u32x4*>(to + row * stride + 8 * (thread & 15)) = w[i];
   }
 }
 
-// One workgroup of four waves per (segment, KV head) and, for outputs, part of its query heads.  kOut: the
-// outputs of its tokens from the state before it, and of a sequence's last segment the state after it; else
-// the segment's own state, for the next.  What the next step reads is on its way to registers during this one.
-template <bool kOut>
-__global__ __launch_bounds__(256, 2) void linear_chunks_kernel(LinearParams p, int items) {
+// Item number to KV head and segment.  A KV head's rows are 256 bytes of each token: were the heads dealt to the
+// XCDs in order, an XCD would read from few of its L2's channels alone, so they rotate from segment to segment.
+struct Item {
+  int id, hk;
+};
+__device__ __forceinline__ Item item_of(const LinearParams& p, int item) {
+  const int id = item / p.h_kv;
+  return {id, (int)((uint32_t)(item + id + id / 8) % p.h_kv)};
+}
+
+// One workgroup per (segment, KV head): the segment's own state, for the next.
+__global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p) {
+  __shared__ Keys s;
+  const auto [id, hk] = item_of(p, blockIdx.x);
+  const int wave = threadIdx.x >> 6;
+  Segment g;
+  if (!find_segment(p, id, &g) || g.s == g.count - 1) return;
+  float* const slot = p.starts + ((int64_t)id * p.h_kv + hk) * kLinState;
+  const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
+  const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
+  Rows rk, rv;
+  float decay = 0.0f;   // of the chunk after the next
+  double total = 0.0;
+  rk.load(k0, p.k_stride, g.n);
+  rv.load(v0, p.v_stride, g.n);
+  State st;
+  state_zero(st);
+  if (g.s == 0) {
+    const int src = p.state_src[g.b];
+    if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
+    raw_store(st, slot);   // the slot that it comes from may be written by `outputs`
+  }
+  if (wave == 7) {
+    total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, 1.0f);
+    decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
+  }
+  store_rows(rk, s.k);
+  store_rows(rv, s.v);
+  for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
+    const int rest = g.n - c - kC, next = rest > 0 ? c + kC : c;   // behind the last chunk any rows will do
+    __syncthreads();
+    rk.load(k0 + next * p.k_stride, p.k_stride, g.n - next);
+    rv.load(v0 + next * p.v_stride, p.v_stride, g.n - next);
+    if (wave == 7 && rest > 0) {
+      total += put_decays(s.d[x ^ 1], decay, rest, 1.0f);
+      decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
+    }
+    update(st, s, s.d[x]);
+    __syncthreads();
+    store_rows(rk, s.k);
+    store_rows(rv, s.v);
+  }
+  raw_store(st, slot + (int64_t)p.h_kv * kLinState);
+  if (threadIdx.x == kThreads - 1) p.decays[(int64_t)id * p.h_kv + hk] = __builtin_amdgcn_exp2f((float)total);
+}
+
+// One workgroup per (segment, KV head, part of its query heads): the outputs of its tokens from the state before
+// it, and of a sequence's last segment the state after it.  What is read next is on its way to registers meanwhile.
+__global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParams p, int items) {
   __shared__ Lds s;
   // parts of an item follow each other on one XCD
-  const int parts = kOut ? p.parts : 1, item = blockIdx.x / (8 * parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % parts;
+  const int item = blockIdx.x / (8 * p.parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % p.parts;
   if (item >= items) return;
-  const int hk = item % p.h_kv, id = item / p.h_kv;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31;
+  const auto [id, hk] = item_of(p, item);
   const int grp = p.h_q / p.h_kv, h0 = hk * grp + part * p.heads, h1 = min(h0 + p.heads, hk * grp + grp);
+  const int wave = threadIdx.x >> 6;
   Segment g;
   if (!find_segment(p, id, &g)) return;
   const bool last = g.s == g.count - 1;
-  if (!kOut && last) return;
-  float* const slot = p.split ? p.starts + ((int64_t)id * p.h_kv + hk) * kLinState : nullptr;
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
   const uint16_t* const q0 = p.q + g.t0 * p.q_stride;
-
   Rows rk, rv, rq;
   float decay = 0.0f;   // of the chunk after the next
-  double total = 0.0;
   if (g.n > 0) {
-    load_rows(rk, k0, p.k_stride, g.n);
-    load_rows(rv, v0, p.v_stride, g.n);
-    if (kOut) load_rows(rq, q0 + h0 * kD, p.q_stride, g.n);
+    rk.load(k0, p.k_stride, g.n);
+    rv.load(v0, p.v_stride, g.n);
+    rq.load(q0 + h0 * kD, p.q_stride, g.n);
   }
-
   State st;
   state_zero(st);
-  if (g.s == 0 && (!kOut || g.count == 1)) {
+  if (g.count > 1) {
+    raw_load(st, p.starts + ((int64_t)id * p.h_kv + hk) * kLinState);
+  } else {
     const int src = p.state_src[g.b];
     if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
-    if (!kOut) raw_store(st, slot);   // the slot that it comes from may be written by `outputs`
-  } else if (kOut) {
-    raw_load(st, slot);
   }
 #pragma unroll
-  for (int db = 0; db < 4; ++db) keep(st.a[db]);   // else the first use in the loop waits, in every chunk, for all loads before it
-  if (wave == 3) {
-    total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n);
-    decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
-  }
+  for (int m = 0; m < 8; ++m) keep(st.a[m]);   // else the first use in the loop waits, in every chunk, for all loads before it
   if (g.n > 0) {
+    if (wave == 7) {
+      put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, p.scale);
+      decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
+    }
     store_rows(rk, s.k);
     store_rows(rv, s.v);
-    if (kOut) store_queries(rq, s.q);
+    store_queries(rq, s.q);
   }
 
   for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
-    const int rest = g.n - c - kC;   // tokens behind this chunk
-    const Lds::Decays& d = s.d[x];
+    const int rest = g.n - c - kC, next = rest > 0 ? c + kC : c;   // behind the last chunk any rows will do
+    const Decays& d = s.d[x];
     __syncthreads();
-    if (rest > 0) {
-      load_rows(rk, k0 + (c + kC) * p.k_stride, p.k_stride, rest);
-      load_rows(rv, v0 + (c + kC) * p.v_stride, p.v_stride, rest);
-    }
-    if (wave == 3 && rest > 0) {
-      total += put_decays(s.d[x ^ 1], decay, rest);
+    float decays[8];
+    if (wave < 6) score_decays(d, wave, p.scale, decays);
+    if (wave == 7 && rest > 0) {
+      put_decays(s.d[x ^ 1], decay, rest, p.scale);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
     }
-    if (kOut) {
-      for (int h = h0; h < h1; ++h) {
-        const bool more = h + 1 < h1;
-        if (more || rest > 0) load_rows(rq, q0 + (more ? c : c + kC) * p.q_stride + (more ? h + 1 : h0) * kD, p.q_stride, more ? rest + kC : rest);
-        if (h > h0) __syncthreads();
-        if (wave < 3) scores(s, d, wave);
-        f32x16 o[2];
-        from_state(o, st, s, d);
-        __syncthreads();
-        if (more) store_queries(rq, s.q);
-        from_chunk(o, s);
-#pragma unroll
-        for (int ib = 0; ib < 2; ++ib) {
-          const int i = c + 32 * ib + l32;
-          store_out(o[ib], i < g.n ? p.out + ((g.t0 + i) * p.h_q + h) * kD + 32 * wave : nullptr, p.scale);
-        }
-      }
+    for (int h = h0; h < h1; ++h) {
+      const bool more = h + 1 < h1;
+      const int from = more ? c : next;
+      rq.load(q0 + from * p.q_stride + (more ? h + 1 : h0) * kD, p.q_stride, g.n - from);
+      if (wave < 6) scores(s, wave, decays);
+      Outputs out;
+      from_state(out, st, s, d);
+      __syncthreads();   // the scores are there, the queries used
+      from_chunk(out, s);
+      put_outputs(out, s.q);
+      __syncthreads();
+      store_outputs(s.q, p.out + ((g.t0 + c) * p.h_q + h) * kD, (int64_t)p.h_q * kD, g.n - c);
+      store_queries(rq, s.q);
+      if (more) __syncthreads();
     }
-    if (!kOut || rest > 0 || (last && part == 0)) update(st, s, d);
+    rk.load(k0 + next * p.k_stride, p.k_stride, g.n - next);
+    rv.load(v0 + next * p.v_stride, p.v_stride, g.n - next);
+    if (rest > 0 || (last && part == 0)) update(st, s, d);
     if (rest > 0) {
       __syncthreads();
       store_rows(rk, s.k);
       store_rows(rv, s.v);
-      if (kOut) store_queries(rq, s.q);
     }
   }
-
-  if (!kOut) {
-    raw_store(st, slot + (int64_t)p.h_kv * kLinState);
-    if (threadIdx.x == 255) p.decays[(int64_t)id * p.h_kv + hk] = __builtin_amdgcn_exp2f((float)total);
-  } else if (last && part == 0) {
+  if (last && part == 0) {
     const int dst = p.state_dst[g.b];
     if (dst >= 0) state_store(st, p.states + ((int64_t)dst * p.h_kv + hk) * kLinState);
   }
@@ -572,10 +590,10 @@ hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream) {
   const int64_t segments = linear_segments(p.batch, p.total_tokens, p.segment);
   const int items = (int)(segments * p.h_kv), eighths = (items + 7) / 8 * 8;
   if (p.split) {
-    linear_chunks_kernel<false><<<dim3(eighths), dim3(256), 0, stream>>>(p, items);
+    linear_sums_kernel<<<dim3(items), dim3(kThreads), 0, stream>>>(p);
     linear_join_kernel<<<dim3(kJoinBlocks * p.h_kv, (unsigned)std::min<int64_t>(segments, 2048)), dim3(256), 0, stream>>>(p, (int)segments);
   }
-  linear_chunks_kernel<true><<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(256), 0, stream>>>(p, items);
+  linear_outputs_kernel<<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(kThreads), 0, stream>>>(p, items);
   return hipGetLastError();
 }
 
