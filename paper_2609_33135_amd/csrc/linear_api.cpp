@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kMostTokens = 1 << 28;              // of one call
 constexpr int kMostRows = 1024;                   // of one sequence in a decode call
-constexpr int64_t kMaxStride = (int64_t)1 << 31;  // elements between tokens
+constexpr int64_t kMaxStride = (int64_t)1 << 25;  // elements between tokens: 64 of them in 32 bits of bytes
 constexpr int64_t kItems = 512;                   // work items that fill the card, two a unit
 
 bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }

@@ -75,6 +75,7 @@ struct Keys {                                  // `sums` has these alone
 struct Lds : Keys {
   LdsRows q;                                   // queries, then outputs; see head_slot
   u32x4 p[6][2][64];                           // scores: 16 queries by 32 keys (see unit_of), high and low parts, lane
+  f32x4 w[6][2][64];                           // their decays
 };
 
 // What stands before in the source stays before.  Products and the vector work of the next ones are written in
@@ -153,11 +154,12 @@ __device__ __forceinline__ void split8(float* x, Frag* part) {
 struct Rows {
   static constexpr int kEach = kC * 16 / kThreads;
   u32x4 w[kEach];
-  __device__ __forceinline__ void load(const uint16_t* x, int64_t stride, int n) {
-    const int thread = thread_here();
+  // stride: bytes between rows, of which 64 stay below 2^32; at: of the thread's first row
+  __device__ __forceinline__ void load(const uint16_t* x, uint32_t stride, uint32_t at, int n) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      w[i] = *reinterpret_cast<const u32x4*>(x + min(row(thread, i), n - 1) * stride + 8 * (thread & 15));
+      w[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(x) +
+                                             (min(at + i * (kThreads / 16) * stride, (n - 1) * stride) + 16 * (threadIdx.x & 15)));
   }
   static __device__ __forceinline__ int row(int thread, int i) { return thread / 16 + kThreads / 16 * i; }
 };
@@ -299,8 +301,8 @@ struct Unit {
 __device__ __forceinline__ Unit unit_of(int u) { return u < 2 ? Unit{u, 0} : Unit{2 + (u - 2) / 2, u & 1}; }
 
 // The decays of a unit's scores, as these lie in the accumulators, times the scale; 0 for keys behind the query.
-__device__ __forceinline__ void score_decays(const Decays& d, int u, float scale, float (&decay)[8]) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ void put_score_decays(Lds& s, const Decays& d, int u, float scale) {
+  const int lane = lane_here();
   const Unit at = unit_of(u);
   const int i = 16 * at.i + (lane & 15);
   const float hi = d.hi[i], lo = d.lo[i];
@@ -308,33 +310,36 @@ __device__ __forceinline__ void score_decays(const Decays& d, int u, float scale
   for (int q = 0; q < 2; ++q) {
     const int j = 32 * at.j + 16 * q + 4 * (lane >> 4);
     const f32x4 jh = *reinterpret_cast<const f32x4*>(&d.hi[j]), jl = *reinterpret_cast<const f32x4*>(&d.lo[j]);
+    f32x4 w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      decay[4 * q + e] = __builtin_amdgcn_exp2f(j + e <= i ? (hi - jh[e]) + (lo - jl[e]) : -INFINITY) * scale;
+    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(j + e <= i ? (hi - jh[e]) + (lo - jl[e]) : -INFINITY) * scale;
+    s.w[u][q][lane] = w;
   }
 }
 
 // Scores of one unit, transposed, as operands.
-__device__ __forceinline__ void scores(Lds& s, int u, const float (&decay)[8]) {
+__device__ __forceinline__ void scores(Lds& s, int u) {
   const int lane = lane_here(), g = lane >> 4;
   const Unit at = unit_of(u);
-  const int ka = (row_at(lane) ^ 16 * (g >> 1)) + 8 * (g & 1) + 256 * 32 * at.j, qa = (row_at(lane) ^ 16 * g) + 256 * 16 * at.i;
+  const int ka = (row_at(lane) ^ 16 * g) + 256 * 32 * at.j, qa = (row_at(lane) ^ 32 * (g & 1)) + 8 * (g >> 1) + 256 * 16 * at.i;
   f32x4 x[2] = {};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {   // 32 channels each, in the order of the queries
+  for (int k = 0; k < 4; ++k) {   // 32 channels each
     Frag a[2], q;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      a[y].d[0] = read_lds<u32x2>(s.k, (ka ^ 64 * k) + 256 * 16 * y);
-      a[y].d[1] = read_lds<u32x2>(s.k, (ka ^ (64 * k + 32)) + 256 * 16 * y);
-    }
-    q.w = read_lds<u32x4>(s.q, qa ^ 64 * k);
+    for (int y = 0; y < 2; ++y) a[y].w = read_lds<u32x4>(s.k, (ka ^ 64 * k) + 256 * 16 * y);
+    q.d[0] = read_lds<u32x2>(s.q, qa ^ 64 * k);
+    q.d[1] = read_lds<u32x2>(s.q, qa ^ (64 * k + 16));
 #pragma unroll
     for (int y = 0; y < 2; ++y) x[y] = mfma_bf16(a[y].b, q.b, x[y]);
   }
   float w[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = x[e >> 2][e & 3] * decay[e];
+  for (int y = 0; y < 2; ++y) {
+    const f32x4 decay = s.w[u][y][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[4 * y + e] = x[y][e] * decay[e];
+  }
   Frag f[2];
   split8<2>(w, f);
 #pragma unroll
@@ -346,25 +351,34 @@ struct Outputs {
   f32x4 o[4];
 };
 
+// The state as operands: 32 channels of k each, high and low parts.
+struct Parts {
+  Frag f[4][2];
+};
+__device__ __forceinline__ void split_state(Parts& p, const State& st) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = st.a[2 * x + (e >> 2)][e & 3];
+    split8<2>(y, p.f[x]);
+  }
+}
+
 // o = scale exp(b_i) S^T q_i.
-__device__ __forceinline__ void from_state(Outputs& to, const State& st, const Lds& s, const Decays& d) {
+__device__ __forceinline__ void from_state(Outputs& to, const Parts& p, const Lds& s, const Decays& d) {
   const int lane = lane_here(), qa = row_at(lane) ^ 16 * (lane >> 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) to.o[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {   // 32 channels of k each
-    Frag q[4], f[2];
+  for (int x = 0; x < 4; ++x) {
+    Frag q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) q[i].w = read_lds<u32x4>(s.q, (qa ^ 64 * x) + 256 * 16 * i);
-    turn();
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = st.a[2 * x + (e >> 2)][e & 3];
-    split8<2>(y, f);
 #pragma unroll
     for (int n = 1; n >= 0; --n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) to.o[i] = mfma_bf16(f[n].b, q[i].b, to.o[i]);
+      for (int i = 0; i < 4; ++i) to.o[i] = mfma_bf16(p.f[x][n].b, q[i].b, to.o[i]);
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) to.o[i] *= d.from[16 * i + (lane & 15)];
@@ -396,18 +410,20 @@ __device__ __forceinline__ void put_outputs(const Outputs& out, LdsRows& rows) {
     *reinterpret_cast<u32x2*>(reinterpret_cast<char*>(&rows) + at + 256 * 16 * i) =
         (u32x2){pack_bf16(out.o[i][0], out.o[i][1]), pack_bf16(out.o[i][2], out.o[i][3])};
 }
-__device__ __forceinline__ void store_outputs(LdsRows& rows, uint16_t* to, int64_t stride, int n) {
+__device__ __forceinline__ void read_outputs(Rows& r, LdsRows& rows) {
   const int thread = thread_here();
-  u32x4 w[Rows::kEach];
 #pragma unroll
   for (int i = 0; i < Rows::kEach; ++i) {
     const u32x2 a = *head_slot(rows, thread, i, 0), b = *head_slot(rows, thread, i, 1);
-    w[i] = (u32x4){a[0], a[1], b[0], b[1]};
+    r.w[i] = (u32x4){a[0], a[1], b[0], b[1]};
   }
+}
+__device__ __forceinline__ void store_outputs(const Rows& r, uint16_t* to, int h_q, int n) {
+  const int thread = thread_here();
 #pragma unroll
   for (int i = 0; i < Rows::kEach; ++i) {
     const int row = Rows::row(thread, i);
-    if (row < n) *reinterpret_cast<u32x4*>(to + row * stride + 8 * (thread & 15)) = w[i];
+    if (row < n) *reinterpret_cast<u32x4*>(to + (row * h_q * kD + 8 * (thread & 15))) = r.w[i];
   }
 }
 
@@ -431,11 +447,12 @@ __global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p
   float* const slot = p.starts + ((int64_t)id * p.h_kv + hk) * kLinState;
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
+  const uint32_t row = threadIdx.x / 16, kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, kat = row * kb, vat = row * vb;
   Rows rk, rv;
   float decay = 0.0f;   // of the chunk after the next
   double total = 0.0;
-  rk.load(k0, p.k_stride, g.n);
-  rv.load(v0, p.v_stride, g.n);
+  rk.load(k0, kb, kat, g.n);
+  rv.load(v0, vb, vat, g.n);
   State st;
   state_zero(st);
   if (g.s == 0) {
@@ -452,8 +469,8 @@ __global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p
   for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
     const int rest = g.n - c - kC, next = rest > 0 ? c + kC : c;   // behind the last chunk any rows will do
     __syncthreads();
-    rk.load(k0 + next * p.k_stride, p.k_stride, g.n - next);
-    rv.load(v0 + next * p.v_stride, p.v_stride, g.n - next);
+    rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
+    rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);
     if (wave == 7 && rest > 0) {
       total += put_decays(s.d[x ^ 1], decay, rest, 1.0f);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
@@ -483,12 +500,14 @@ __global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParam
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
   const uint16_t* const q0 = p.q + g.t0 * p.q_stride;
+  const uint32_t row = threadIdx.x / 16, kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, kat = row * kb, vat = row * vb;
+  const uint32_t qb = 2 * (uint32_t)p.q_stride, qat = row * qb;
   Rows rk, rv, rq;
   float decay = 0.0f;   // of the chunk after the next
   if (g.n > 0) {
-    rk.load(k0, p.k_stride, g.n);
-    rv.load(v0, p.v_stride, g.n);
-    rq.load(q0 + h0 * kD, p.q_stride, g.n);
+    rk.load(k0, kb, kat, g.n);
+    rv.load(v0, vb, vat, g.n);
+    rq.load(q0 + h0 * kD, qb, qat, g.n);
   }
   State st;
   state_zero(st);
@@ -510,12 +529,13 @@ __global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParam
     store_queries(rq, s.q);
   }
 
-  for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
+  for (int c = 0, x = 0; g.n > 0; c += kC, x ^= 1) {
     const int rest = g.n - c - kC, next = rest > 0 ? c + kC : c;   // behind the last chunk any rows will do
     const Decays& d = s.d[x];
     __syncthreads();
-    float decays[8];
-    if (wave < 6) score_decays(d, wave, p.scale, decays);
+    Parts parts;
+    split_state(parts, st);
+    if (wave < 6) put_score_decays(s, d, wave, p.scale);
     if (wave == 7 && rest > 0) {
       put_decays(s.d[x ^ 1], decay, rest, p.scale);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
@@ -523,26 +543,28 @@ __global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParam
     for (int h = h0; h < h1; ++h) {
       const bool more = h + 1 < h1;
       const int from = more ? c : next;
-      rq.load(q0 + from * p.q_stride + (more ? h + 1 : h0) * kD, p.q_stride, g.n - from);
-      if (wave < 6) scores(s, wave, decays);
+      rq.load(q0 + from * p.q_stride + (more ? h + 1 : h0) * kD, qb, qat, g.n - from);
+      if (wave < 6) scores(s, wave);
       Outputs out;
-      from_state(out, st, s, d);
+      from_state(out, parts, s, d);
       __syncthreads();   // the scores are there, the queries used
       from_chunk(out, s);
       put_outputs(out, s.q);
       __syncthreads();
-      store_outputs(s.q, p.out + ((g.t0 + c) * p.h_q + h) * kD, (int64_t)p.h_q * kD, g.n - c);
+      Rows ro;
+      read_outputs(ro, s.q);
+      // before the outputs go to memory: a wait for loads behind stores that are not always made is one for these
       store_queries(rq, s.q);
+      store_outputs(ro, p.out + ((g.t0 + c) * p.h_q + h) * kD, p.h_q, g.n - c);
       if (more) __syncthreads();
     }
-    rk.load(k0 + next * p.k_stride, p.k_stride, g.n - next);
-    rv.load(v0 + next * p.v_stride, p.v_stride, g.n - next);
+    rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
+    rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);
     if (rest > 0 || (last && part == 0)) update(st, s, d);
-    if (rest > 0) {
-      __syncthreads();
-      store_rows(rk, s.k);
-      store_rows(rv, s.v);
-    }
+    if (rest <= 0) break;   // past it the compiler would take the loads for pending and wait in the next chunk
+    __syncthreads();
+    store_rows(rk, s.k);
+    store_rows(rv, s.v);
   }
   if (last && part == 0) {
     const int dst = p.state_dst[g.b];
