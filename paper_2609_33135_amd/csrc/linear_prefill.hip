@@ -9,6 +9,7 @@
 // A sequence is cut into segments so that there is work for every unit: `sums` adds up each segment's own
 // state, `join` makes the state before each segment out of those, `outputs` goes through the segments' chunks.
 #include <algorithm>
+#include <type_traits>
 
 #include "linear_internal.h"
 #include "mpfa_device.h"
@@ -18,7 +19,7 @@ namespace mpfa {
 namespace {
 
 constexpr int kC = kLinChunk;
-constexpr int kThreads = 512;         // eight waves of 16 columns (channels of v) each
+constexpr int kThreads = 256;         // four waves of 32 columns (channels of v) each
 constexpr double kLog2e = 1.4426950408889634;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -58,9 +59,9 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
 }
 
 // Rows of 128 channels in LDS lie without padding, their 16-byte pieces exchanged by row so that neither 16
-// rows' same piece nor eight rows' same two pieces (a transposing read) meet in a bank.
+// rows' same piece nor four rows' same four pieces (a transposing read) meet in a bank.
 typedef uint16_t LdsRows[kC][kD];
-__device__ __forceinline__ int piece_row(int row) { return (row & 3) << 2 | (row >> 1 & 2) | (row >> 3 & 1); }
+__device__ __forceinline__ int piece_row(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
 __device__ __forceinline__ int piece(int row, int c) { return 8 * (c ^ piece_row(row)); }
 
 // What a chunk needs of its decays.
@@ -74,8 +75,8 @@ struct Keys {                                  // `sums` has these alone
 };
 struct Lds : Keys {
   LdsRows q;                                   // queries, then outputs; see head_slot
-  u32x4 p[6][2][64];                           // scores: 16 queries by 32 keys (see unit_of), high and low parts, lane
-  f32x4 w[6][2][64];                           // their decays
+  u32x4 p[3][2][2][64];                        // scores: block, step of 16 keys, high and low parts, lane
+  f32x4 w[3][4][64];                           // their decays
 };
 
 // What stands before in the source stays before.  Products and the vector work of the next ones are written in
@@ -101,25 +102,25 @@ __device__ __forceinline__ T read_lds(const LdsRows& rows, int at) {
   return *(lds_T*)((lds_char*)&rows + at);
 }
 
-// Offset of the lane's own row of 16 rows, in it the piece 0.
-__device__ __forceinline__ int row_at(int lane) { return 256 * (lane & 15) + 16 * piece_row(lane & 15); }
+// Offset of the lane's own row of 32 rows, in it the piece 0.
+__device__ __forceinline__ int row_at(int lane) { return 256 * (lane & 31) + 16 * piece_row(lane); }
 
-// Transposing reads: four tokens t .. t + 3, t = t0 + 4 * (lane / 16), of the lane's column c0 + lane % 16: each
+// Transposing reads: four tokens t .. t + 3, t = t0 + 4 * (lane / 32), of the lane's column c0 + lane % 32: each
 // group of 16 lanes reads a block of four rows and 16 columns.  columns_at: of t0 = c0 = 0.
 __device__ __forceinline__ int columns_at(int lane) {
-  const int i = lane & 15, row = 4 * (lane >> 4) + (i >> 2);
-  return 256 * row + 16 * ((i >> 1 & 1) ^ piece_row(row)) + 8 * (i & 1);
+  const int i = lane & 15, row = 4 * (lane >> 5) + (i >> 2);
+  return 256 * row + 16 * (((lane >> 4 & 1) * 2 + (i >> 1 & 1)) ^ piece_row(row)) + 8 * (i & 1);
 }
 __device__ __forceinline__ s16x4 column4(const LdsRows& rows, int at) {
   typedef __attribute__((address_space(3))) s16x4 lds4;
   typedef __attribute__((address_space(3))) char lds_char;
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)((lds_char*)const_cast<LdsRows*>(&rows) + at));
 }
-// The tokens t0 .. t0 + 31 in the order in which two accumulators of 16 rows hold theirs.
+// The tokens t0 .. t0 + 15 in the order in which an accumulator holds its rows.
 __device__ __forceinline__ Frag columns(const LdsRows& rows, int at, int t0) {
   Frag f;
   f.s[0] = column4(rows, at + 256 * t0);
-  f.s[1] = column4(rows, at + 256 * (t0 + 16));
+  f.s[1] = column4(rows, (at ^ 32) + 256 * (t0 + 8));
   return f;
 }
 
@@ -171,12 +172,12 @@ __device__ __forceinline__ void store_rows(const Rows& r, LdsRows& to) {
     *reinterpret_cast<u32x4*>(&to[row][piece(row, thread & 15)]) = r.w[i];
   }
 }
-// Queries of a head and later its outputs: of 32 channels those that a group of 16 lanes takes side by side, four
-// and the four that lie 16 further.  A thread's 16 bytes lie in two halves of pieces, for queries and outputs the
-// same, so a thread that has read its outputs may put queries in their place.
+// Queries of a head and later its outputs: of 16 channels those that a lane half takes side by side, 0-3 and 8-11 |
+// 4-7 and 12-15.  A thread's 16 bytes lie in two halves of pieces, for queries and outputs the same, so a thread
+// that has read its outputs may put queries in their place.
 __device__ __forceinline__ u32x2* head_slot(LdsRows& rows, int thread, int i, int x) {
   const int row = Rows::row(thread, i), c = thread & 15;
-  return reinterpret_cast<u32x2*>(&rows[row][piece(row, (c & ~3) + 2 * (c & 1) + x) + 2 * (c & 2)]);
+  return reinterpret_cast<u32x2*>(&rows[row][piece(row, (c & ~1) + x) + 4 * (c & 1)]);
 }
 __device__ __forceinline__ void store_queries(const Rows& r, LdsRows& to) {
   const int thread = thread_here();
@@ -187,41 +188,51 @@ __device__ __forceinline__ void store_queries(const Rows& r, LdsRows& to) {
 }
 
 // The value is in its registers here: loads of it have arrived.
-__device__ __forceinline__ void keep(f32x4& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void keep(f32x16& x) { asm volatile("" : "+v"(x)); }
 
-// A wave's part of the state: its 16 columns (channels of v), blocks of 16 rows (channels of k).
+// A wave's part of the state: its 32 columns (channels of v), blocks of 32 rows (channels of k).
 struct State {
-  f32x4 a[8];
+  f32x16 a[4];
 };
 __device__ __forceinline__ int wave_here() { return threadIdx.x >> 6; }
 __device__ __forceinline__ int state_at(int m, int r) {   // in [128][128]
   const int lane = threadIdx.x & 63;
-  return (16 * m + 4 * (lane >> 4) + r) * kD + 16 * wave_here() + (lane & 15);
+  return (32 * m + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * kD + 32 * wave_here() + (lane & 31);
 }
 __device__ __forceinline__ void state_zero(State& s) {
 #pragma unroll
-  for (int m = 0; m < 8; ++m) s.a[m] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s.a[m][r] = 0.0f;
 }
 __device__ __forceinline__ void state_load(State& s, const float* from) {
 #pragma unroll
-  for (int m = 0; m < 8; ++m)
+  for (int m = 0; m < 4; ++m)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s.a[m][r] = from[state_at(m, r)];
+    for (int r = 0; r < 16; ++r) s.a[m][r] = from[state_at(m, r)];
 }
 __device__ __forceinline__ void state_store(const State& s, float* to) {
 #pragma unroll
-  for (int m = 0; m < 8; ++m)
+  for (int m = 0; m < 4; ++m)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) to[state_at(m, r)] = s.a[m][r];
+    for (int r = 0; r < 16; ++r) to[state_at(m, r)] = s.a[m][r];
 }
 // In the workspace a state lies as the accumulators do.
 __device__ __forceinline__ void raw_store(const State& s, float* ws) {
 #pragma unroll
-  for (int m = 0; m < 8; ++m) reinterpret_cast<f32x4*>(ws)[m * kThreads + threadIdx.x] = s.a[m];
+  for (int n = 0; n < 16; ++n) {
+    const f32x16& a = s.a[n >> 2];
+    const int r = 4 * (n & 3);
+    reinterpret_cast<f32x4*>(ws)[n * kThreads + threadIdx.x] = (f32x4){a[r], a[r + 1], a[r + 2], a[r + 3]};
+  }
 }
 __device__ __forceinline__ void raw_load(State& s, const float* ws) {
 #pragma unroll
-  for (int m = 0; m < 8; ++m) s.a[m] = reinterpret_cast<const f32x4*>(ws)[m * kThreads + threadIdx.x];
+  for (int n = 0; n < 16; ++n) {
+    const f32x4 x = reinterpret_cast<const f32x4*>(ws)[n * kThreads + threadIdx.x];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s.a[n >> 2][4 * (n & 3) + e] = x[e];
+  }
 }
 
 // Log decays of a chunk (lane = token; 0 behind its last).
@@ -260,155 +271,214 @@ __device__ __forceinline__ double put_decays(Decays& d, float g, int n, float sc
 
 // S' = exp(b_last) S + K^T (exp(b_last - b_j) V): K is an operand as it is, V with its decay in three parts.
 __device__ __forceinline__ void update(State& st, const Keys& s, const Decays& d) {
-  const int lane = lane_here(), at = columns_at(lane), vat = at ^ 32 * wave_here();
+  const int lane = lane_here(), half = lane >> 5, at = columns_at(lane), vat = at ^ 64 * wave_here();
   const float whole = __builtin_amdgcn_exp2f(d.hi[kC - 1]);
-  Frag f[2][3], k[2];
+  Frag v[2], k[2][4], f[2][3];
+  f32x4 to[2][2];
+  float y[8];
+  auto read_v = [&](int j) { v[j & 1] = columns(s.v, vat, 16 * j); };
+  auto read_to = [&](int j, int q) { to[j & 1][q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]); };
+  auto read_k = [&](int j, int m) { k[j & 1][m] = columns(s.k, at ^ 64 * m, 16 * j); };
+  auto split = [&](int j, int i, int w) {   // part i of the w-th pair of step j
+    if (i == 0) {
+      const uint32_t x = v[j & 1].w[w];
+      y[2 * w] = bits_lo(x) * to[j & 1][w >> 1][2 * (w & 1)];
+      y[2 * w + 1] = bits_hi(x) * to[j & 1][w >> 1][2 * (w & 1) + 1];
+    }
+    split2(y, f[j & 1], i, w);
+  };
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {   // 32 tokens each
-    const Frag v = columns(s.v, vat, 32 * j);
-    float y[8];
+  for (int j = 0; j < 2; ++j) {
+    read_v(j);
+    read_to(j, 0);
+    read_to(j, 1);
+  }
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const f32x4 decay = *reinterpret_cast<const f32x4*>(&d.to[32 * j + 16 * q + 4 * (lane >> 4)]);
+  for (int m = 0; m < 4; ++m) read_k(0, m);
+  turn();
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t w = v.w[2 * q + (e >> 1)];
-        y[4 * q + e] = (e & 1 ? bits_hi(w) : bits_lo(w)) * decay[e];
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) split(0, i, w);
+#pragma unroll
+  for (int m = 0; m < 4; ++m)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.a[m][r] *= whole;
+  turn();
+#pragma unroll
+  for (int j = 0; j < 4; ++j)   // 16 tokens each
+#pragma unroll
+    for (int n = 0; n < 12; ++n) {
+      const int i = 2 - n / 4, m = n % 4;
+      st.a[m] = mfma32_bf16(k[j & 1][m].b, f[j & 1][i].b, st.a[m]);
+      if (j < 3) {
+        split(j + 1, n / 4, n % 4);
+        if (n < 4) read_k(j + 1, n);
       }
+      if (j < 2 && n >= 9) {   // step j's v and decays are used up
+        if (n == 9) read_v(j + 2);
+        else read_to(j + 2, n - 10);
+      }
+      turn();
     }
-    split8<3>(y, f[j]);
-  }
-  auto read = [&](int n) { k[n & 1] = columns(s.k, at ^ 32 * (n >> 1), 32 * (n & 1)); };
-  read(0);
-#pragma unroll
-  for (int n = 0; n < 16; ++n) {
-    f32x4& a = st.a[n >> 1];
-    if (n < 15) read(n + 1);
-    turn();
-    if (!(n & 1)) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) a[r] *= whole;
-    }
-#pragma unroll
-    for (int i = 2; i >= 0; --i) a = mfma_bf16(k[n & 1].b, f[n & 1][i].b, a);
-  }
 }
 
-// A unit of scores: queries 16 i .., keys 32 j .. .  Six of them hold all keys that queries see.
-struct Unit {
+// A block of scores: queries i .., keys j .. (32 each).  Three of them hold all keys that queries see.
+struct Block {
   int i, j;
 };
-__device__ __forceinline__ Unit unit_of(int u) { return u < 2 ? Unit{u, 0} : Unit{2 + (u - 2) / 2, u & 1}; }
+__device__ __forceinline__ Block block_of(int b) { return {b == 0 ? 0 : 32, b == 2 ? 32 : 0}; }
 
-// The decays of a unit's scores, as these lie in the accumulators, times the scale; 0 for keys behind the query.
-__device__ __forceinline__ void put_score_decays(Lds& s, const Decays& d, int u, float scale) {
+// The decays of a block's scores, as these lie in the accumulators, times the scale; 0 for keys behind the query.
+__device__ __forceinline__ void put_score_decays(Lds& s, const Decays& d, int b, float scale) {
   const int lane = lane_here();
-  const Unit at = unit_of(u);
-  const int i = 16 * at.i + (lane & 15);
+  const Block at = block_of(b);
+  const int i = at.i + (lane & 31);
   const float hi = d.hi[i], lo = d.lo[i];
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    const int j = 32 * at.j + 16 * q + 4 * (lane >> 4);
+  for (int r4 = 0; r4 < 4; ++r4) {
+    const int j = at.j + 8 * r4 + 4 * (lane >> 5);
     const f32x4 jh = *reinterpret_cast<const f32x4*>(&d.hi[j]), jl = *reinterpret_cast<const f32x4*>(&d.lo[j]);
     f32x4 w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(j + e <= i ? (hi - jh[e]) + (lo - jl[e]) : -INFINITY) * scale;
-    s.w[u][q][lane] = w;
+    s.w[b][r4][lane] = w;
   }
 }
 
-// Scores of one unit, transposed, as operands.
-__device__ __forceinline__ void scores(Lds& s, int u) {
-  const int lane = lane_here(), g = lane >> 4;
-  const Unit at = unit_of(u);
-  const int ka = (row_at(lane) ^ 16 * g) + 256 * 32 * at.j, qa = (row_at(lane) ^ 32 * (g & 1)) + 8 * (g >> 1) + 256 * 16 * at.i;
-  f32x4 x[2] = {};
+// Scores of one block, transposed, as operands.
+__device__ __forceinline__ void scores(Lds& s, int b) {
+  const int lane = lane_here(), half = lane >> 5;
+  const Block at = block_of(b);
+  const int ka = (row_at(lane) ^ 16 * half) + 256 * at.j, qa = row_at(lane) + 8 * half + 256 * at.i;
+  f32x16 x;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {   // 32 channels each
-    Frag a[2], q;
+  for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+  Frag a[4], q[4];
+  auto read = [&](int k) {   // 16 channels each
+    a[k & 3].w = read_lds<u32x4>(s.k, ka ^ 32 * k);
+    q[k & 3].d[0] = read_lds<u32x2>(s.q, qa ^ 32 * k);
+    q[k & 3].d[1] = read_lds<u32x2>(s.q, qa ^ (32 * k + 16));
+  };
 #pragma unroll
-    for (int y = 0; y < 2; ++y) a[y].w = read_lds<u32x4>(s.k, (ka ^ 64 * k) + 256 * 16 * y);
-    q.d[0] = read_lds<u32x2>(s.q, qa ^ 64 * k);
-    q.d[1] = read_lds<u32x2>(s.q, qa ^ (64 * k + 16));
+  for (int k = 0; k < 4; ++k) read(k);
+  turn();
 #pragma unroll
-    for (int y = 0; y < 2; ++y) x[y] = mfma_bf16(a[y].b, q.b, x[y]);
+  for (int k = 0; k < 8; ++k) {
+    x = mfma32_bf16(a[k & 3].b, q[k & 3].b, x);
+    if (k < 4) read(k + 4);
+    turn();
   }
-  float w[8];
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
-    const f32x4 decay = s.w[u][y][lane];
+    float w[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[4 * y + e] = x[y][e] * decay[e];
+    for (int r4 = 0; r4 < 2; ++r4) {
+      const f32x4 decay = s.w[b][2 * y + r4][lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[4 * r4 + e] = x[8 * y + 4 * r4 + e] * decay[e];
+    }
+    Frag f[2];
+    split8<2>(w, f);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) s.p[b][y][i][lane] = f[i].w;
   }
-  Frag f[2];
-  split8<2>(w, f);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) s.p[u][i][lane] = f[i].w;
 }
 
-// Outputs of the chunk's queries, 16 a block: rows are the wave's channels of v.
+// Outputs of the chunk's queries, 32 a block: rows are the wave's channels of v.
 struct Outputs {
-  f32x4 o[4];
+  f32x16 o[2];
 };
 
-// The state as operands: 32 channels of k each, high and low parts.
+// The state as operands: 16 channels of k each, high and low parts.
 struct Parts {
-  Frag f[4][2];
+  Frag f[8][2];
 };
-__device__ __forceinline__ void split_state(Parts& p, const State& st) {
-#pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = st.a[2 * x + (e >> 2)][e & 3];
-    split8<2>(y, p.f[x]);
-  }
-}
 
-// o = scale exp(b_i) S^T q_i.
-__device__ __forceinline__ void from_state(Outputs& to, const Parts& p, const Lds& s, const Decays& d) {
-  const int lane = lane_here(), qa = row_at(lane) ^ 16 * (lane >> 4);
+// o = scale exp(b_i) S^T q_i.  kFirst: the chunk's first head makes the state's parts.
+template <bool kFirst>
+__device__ __forceinline__ void from_state(Outputs& to, const State& st, Parts& parts, const Lds& s, const Decays& d) {
+  const int lane = lane_here(), qa = row_at(lane) ^ 16 * (lane >> 5);
+  Frag q[2][2];
+  float y[8];
+  auto read = [&](int g, int i) { q[g & 1][i].w = read_lds<u32x4>(s.q, (qa ^ 32 * g) + 256 * 32 * i); };
+  auto split = [&](int g, int w) {
+    y[2 * w] = st.a[g >> 1][8 * (g & 1) + 2 * w];
+    y[2 * w + 1] = st.a[g >> 1][8 * (g & 1) + 2 * w + 1];
+    split2(y, parts.f[g], 0, w);
+    split2(y, parts.f[g], 1, w);
+  };
 #pragma unroll
-  for (int i = 0; i < 4; ++i) to.o[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+  for (int g = 0; g < 2; ++g)
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    Frag q[4];
+    for (int i = 0; i < 2; ++i) read(g, i);
+  float from[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q[i].w = read_lds<u32x4>(s.q, (qa ^ 64 * x) + 256 * 16 * i);
+  for (int i = 0; i < 2; ++i) from[i] = d.from[32 * i + (lane & 31)];
+  if (kFirst) {
 #pragma unroll
-    for (int n = 1; n >= 0; --n)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) to.o[i] = mfma_bf16(p.f[x][n].b, q[i].b, to.o[i]);
+    for (int w = 0; w < 4; ++w) split(0, w);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) to.o[i] *= d.from[16 * i + (lane & 15)];
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) to.o[i][r] = 0.0f;
+  turn();
+#pragma unroll
+  for (int g = 0; g < 8; ++g)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int i = n & 1;
+      to.o[i] = mfma32_bf16(parts.f[g][1 - n / 2].b, q[g & 1][i].b, to.o[i]);
+      if (kFirst && g < 7) split(g + 1, n);
+      if (g < 6 && n >= 2) read(g + 2, i);
+      turn();
+    }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) to.o[i][r] *= from[i];
 }
 
 // o += V^T scores.
 __device__ __forceinline__ void from_chunk(Outputs& to, const Lds& s) {
-  const int lane = lane_here(), vat = columns_at(lane) ^ 32 * wave_here();
-  Frag v[2];
+  const int lane = lane_here(), vat = columns_at(lane) ^ 64 * wave_here();
+  Frag v[2][2], w[2][2][2];
+  auto read = [&](int b) {
 #pragma unroll
-  for (int j = 0; j < 2; ++j) v[j] = columns(s.v, vat, 32 * j);
+    for (int y = 0; y < 2; ++y) {
+      v[b & 1][y] = columns(s.v, vat, block_of(b).j + 16 * y);
 #pragma unroll
-  for (int u = 0; u < 6; ++u) {
-    const Unit at = unit_of(u);
-#pragma unroll
-    for (int n = 1; n >= 0; --n) {
-      Frag w;
-      w.w = s.p[u][n][lane];
-      to.o[at.i] = mfma_bf16(v[at.j].b, w.b, to.o[at.i]);
+      for (int i = 0; i < 2; ++i) w[b & 1][y][i].w = s.p[b][y][i][lane];
     }
+  };
+  read(0);
+  read(1);
+  turn();
+#pragma unroll
+  for (int b = 0; b < 3; ++b) {
+    f32x16& o = to.o[b == 0 ? 0 : 1];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int i = 1; i >= 0; --i) o = mfma32_bf16(v[b & 1][y].b, w[b & 1][y][i].b, o);
+    if (b == 0) read(2);
+    turn();
   }
 }
 
 // Outputs to the place of the queries, from there whole rows to memory.
 __device__ __forceinline__ void put_outputs(const Outputs& out, LdsRows& rows) {
-  const int lane = lane_here(), wave = wave_here(), at = (row_at(lane) ^ 16 * (4 * (wave >> 1) + (lane >> 4))) + 8 * (wave & 1);
+  const int lane = lane_here(), at = row_at(lane) ^ (64 * wave_here() + 16 * (lane >> 5));
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<u32x2*>(reinterpret_cast<char*>(&rows) + at + 256 * 16 * i) =
-        (u32x2){pack_bf16(out.o[i][0], out.o[i][1]), pack_bf16(out.o[i][2], out.o[i][3])};
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = pack_bf16(out.o[i][8 * x + 2 * e], out.o[i][8 * x + 2 * e + 1]);
+      *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(&rows) + (at ^ 32 * x) + 256 * 32 * i) = w;
+    }
 }
 __device__ __forceinline__ void read_outputs(Rows& r, LdsRows& rows) {
   const int thread = thread_here();
@@ -438,7 +508,7 @@ __device__ __forceinline__ Item item_of(const LinearParams& p, int item) {
 }
 
 // One workgroup per (segment, KV head): the segment's own state, for the next.
-__global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p) {
+__global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p) {
   __shared__ Keys s;
   const auto [id, hk] = item_of(p, blockIdx.x);
   const int wave = threadIdx.x >> 6;
@@ -460,7 +530,7 @@ __global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p
     if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
     raw_store(st, slot);   // the slot that it comes from may be written by `outputs`
   }
-  if (wave == 7) {
+  if (wave == 3) {
     total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, 1.0f);
     decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
   }
@@ -471,7 +541,7 @@ __global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p
     __syncthreads();
     rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
     rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);
-    if (wave == 7 && rest > 0) {
+    if (wave == 3 && rest > 0) {
       total += put_decays(s.d[x ^ 1], decay, rest, 1.0f);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
     }
@@ -486,7 +556,7 @@ __global__ __launch_bounds__(kThreads, 4) void linear_sums_kernel(LinearParams p
 
 // One workgroup per (segment, KV head, part of its query heads): the outputs of its tokens from the state before
 // it, and of a sequence's last segment the state after it.  What is read next is on its way to registers meanwhile.
-__global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParams p, int items) {
+__global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParams p, int items) {
   __shared__ Lds s;
   // parts of an item follow each other on one XCD
   const int item = blockIdx.x / (8 * p.parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % p.parts;
@@ -518,9 +588,9 @@ __global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParam
     if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
   }
 #pragma unroll
-  for (int m = 0; m < 8; ++m) keep(st.a[m]);   // else the first use in the loop waits, in every chunk, for all loads before it
+  for (int m = 0; m < 4; ++m) keep(st.a[m]);   // else the first use in the loop waits, in every chunk, for all loads before it
   if (g.n > 0) {
-    if (wave == 7) {
+    if (wave == 3) {
       put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, p.scale);
       decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
     }
@@ -534,19 +604,18 @@ __global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParam
     const Decays& d = s.d[x];
     __syncthreads();
     Parts parts;
-    split_state(parts, st);
-    if (wave < 6) put_score_decays(s, d, wave, p.scale);
-    if (wave == 7 && rest > 0) {
+    if (wave < 3) put_score_decays(s, d, wave, p.scale);
+    if (wave == 3 && rest > 0) {
       put_decays(s.d[x ^ 1], decay, rest, p.scale);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
     }
-    for (int h = h0; h < h1; ++h) {
+    auto step = [&](auto first, int h) {
       const bool more = h + 1 < h1;
       const int from = more ? c : next;
       rq.load(q0 + from * p.q_stride + (more ? h + 1 : h0) * kD, qb, qat, g.n - from);
-      if (wave < 6) scores(s, wave);
+      if (wave < 3) scores(s, wave);
       Outputs out;
-      from_state(out, parts, s, d);
+      from_state<decltype(first)::value>(out, st, parts, s, d);
       __syncthreads();   // the scores are there, the queries used
       from_chunk(out, s);
       put_outputs(out, s.q);
@@ -557,7 +626,9 @@ __global__ __launch_bounds__(kThreads, 4) void linear_outputs_kernel(LinearParam
       store_queries(rq, s.q);
       store_outputs(ro, p.out + ((g.t0 + c) * p.h_q + h) * kD, p.h_q, g.n - c);
       if (more) __syncthreads();
-    }
+    };
+    step(std::true_type(), h0);
+    for (int h = h0 + 1; h < h1; ++h) step(std::false_type(), h);
     rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
     rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);
     if (rest > 0 || (last && part == 0)) update(st, s, d);
