@@ -76,7 +76,7 @@ struct Keys {                                  // `sums` has these alone
 struct Lds : Keys {
   LdsRows q;                                   // queries, then outputs; see head_slot
   u32x4 p[3][2][2][64];                        // scores: block, step of 16 keys, high and low parts, lane
-  f32x4 w[3][4][64];                           // their decays
+  f32x4 w[3][4][64];                           // their decays, for a chunk's second and later heads
 };
 
 // What stands before in the source stays before.  Products and the vector work of the next ones are written in
@@ -157,6 +157,7 @@ struct Rows {
   u32x4 w[kEach];
   // stride: bytes between rows, of which 64 stay below 2^32; at: of the thread's first row
   __device__ __forceinline__ void load(const uint16_t* x, uint32_t stride, uint32_t at, int n) {
+    asm volatile("" : "+v"(at));   // as for the thread below: offsets are not kept
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
       w[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(x) +
@@ -237,7 +238,7 @@ __device__ __forceinline__ void raw_load(State& s, const float* ws) {
 
 // Log decays of a chunk (lane = token; 0 behind its last).
 __device__ __forceinline__ float load_decays(const LinearParams& p, int64_t t, int n, int hk) {
-  const int lane = threadIdx.x & 63;
+  const int lane = lane_here();
   return lane < n ? p.log_decay[(t + lane) * p.decay_stride + hk] : 0.0f;
 }
 
@@ -252,7 +253,7 @@ __device__ __forceinline__ double moved(double x) {   // lanes without a source 
 // What a chunk of n tokens needs of its decays g; returns log2 of the whole chunk's.  Summed in 64 bits: after a token that
 // clears the state sums are large and their differences small.
 __device__ __forceinline__ double put_decays(Decays& d, float g, int n, float scale) {
-  const int lane = threadIdx.x & 63;
+  const int lane = lane_here();
   double x = (double)fminf(fmaxf(g, kLinLeastDecay), 0.0f) * kLog2e;
   x += moved<0x111, 0xF>(x);   // from 1, 2, 4, 8 lanes before in a row of 16
   x += moved<0x112, 0xF>(x);
@@ -270,58 +271,65 @@ __device__ __forceinline__ double put_decays(Decays& d, float g, int n, float sc
 }
 
 // S' = exp(b_last) S + K^T (exp(b_last - b_j) V): K is an operand as it is, V with its decay in three parts.
-__device__ __forceinline__ void update(State& st, const Keys& s, const Decays& d) {
-  const int lane = lane_here(), half = lane >> 5, at = columns_at(lane), vat = at ^ 64 * wave_here();
-  const float whole = __builtin_amdgcn_exp2f(d.hi[kC - 1]);
-  Frag v[2], k[2][4], f[2][3];
-  f32x4 to[2][2];
-  float y[8];
-  auto read_v = [&](int j) { v[j & 1] = columns(s.v, vat, 16 * j); };
-  auto read_to = [&](int j, int q) { to[j & 1][q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]); };
-  auto read_k = [&](int j, int m) { k[j & 1][m] = columns(s.k, at ^ 64 * m, 16 * j); };
-  auto split = [&](int j, int i, int w) {   // part i of the w-th pair of step j
+struct Update {
+  Frag v[4], f[2][3];                          // V of 16 tokens each; the parts of a step and of the next
+  f32x4 to[2][2];                              // the decays of a step's and the next one's tokens
+  float y[8], whole;
+
+  __device__ __forceinline__ void read(const Keys& s, int vat) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = columns(s.v, vat, 16 * j);
+  }
+  __device__ __forceinline__ void read_to(const Decays& d, int half, int j, int q) {
+    to[j & 1][q] = *reinterpret_cast<const f32x4*>(&d.to[16 * j + 8 * q + 4 * half]);
+  }
+  // part i of the w-th pair of step j
+  __device__ __forceinline__ void split(int j, int i, int w) {
     if (i == 0) {
-      const uint32_t x = v[j & 1].w[w];
+      const uint32_t x = v[j].w[w];
       y[2 * w] = bits_lo(x) * to[j & 1][w >> 1][2 * (w & 1)];
       y[2 * w + 1] = bits_hi(x) * to[j & 1][w >> 1][2 * (w & 1) + 1];
     }
     split2(y, f[j & 1], i, w);
-  };
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    read_v(j);
-    read_to(j, 0);
-    read_to(j, 1);
   }
+  // What comes before the products, as twelve turns' worth: a reading of decays, then a step's parts and the
+  // state's decay.
+  __device__ __forceinline__ void begin(const Decays& d, int half) {
+    whole = __builtin_amdgcn_exp2f(d.hi[kC - 1]);
 #pragma unroll
-  for (int m = 0; m < 4; ++m) read_k(0, m);
-  turn();
+    for (int q = 0; q < 2; ++q) read_to(d, half, 0, q);
+  }
+  __device__ __forceinline__ void prepare(State& st, int n) {
+    split(0, n / 4, n % 4);
 #pragma unroll
-  for (int i = 0; i < 3; ++i)
+    for (int e = 6 * n; e < 6 * n + 6; ++e)
+      if (e < 64) st.a[e >> 4][e & 15] *= whole;
+  }
+  // The products, a step's parts beside those of the step before.
+  __device__ __forceinline__ void add(State& st, const Keys& s, const Decays& d) {
+    const int lane = lane_here(), at = columns_at(lane);
+    Frag k[2][4];
+    auto read_k = [&](int j, int m) { k[j & 1][m] = columns(s.k, at ^ 64 * m, 16 * j); };
 #pragma unroll
-    for (int w = 0; w < 4; ++w) split(0, i, w);
+    for (int m = 0; m < 4; ++m) read_k(0, m);
 #pragma unroll
-  for (int m = 0; m < 4; ++m)
+    for (int q = 0; q < 2; ++q) read_to(d, lane >> 5, 1, q);
+    turn();
 #pragma unroll
-    for (int r = 0; r < 16; ++r) st.a[m][r] *= whole;
-  turn();
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-  for (int j = 0; j < 4; ++j)   // 16 tokens each
-#pragma unroll
-    for (int n = 0; n < 12; ++n) {
-      const int i = 2 - n / 4, m = n % 4;
-      st.a[m] = mfma32_bf16(k[j & 1][m].b, f[j & 1][i].b, st.a[m]);
-      if (j < 3) {
-        split(j + 1, n / 4, n % 4);
-        if (n < 4) read_k(j + 1, n);
+      for (int n = 0; n < 12; ++n) {
+        const int i = 2 - n / 4, m = n % 4;
+        st.a[m] = mfma32_bf16(k[j & 1][m].b, f[j & 1][i].b, st.a[m]);
+        if (j < 3) {
+          split(j + 1, n / 4, n % 4);
+          if (n < 4) read_k(j + 1, n);
+        }
+        if (j < 2 && n >= 10) read_to(d, lane >> 5, j + 2, n - 10);   // step j's decays are used up
+        turn();
       }
-      if (j < 2 && n >= 9) {   // step j's v and decays are used up
-        if (n == 9) read_v(j + 2);
-        else read_to(j + 2, n - 10);
-      }
-      turn();
-    }
-}
+  }
+};
 
 // A block of scores: queries i .., keys j .. (32 each).  Three of them hold all keys that queries see.
 struct Block {
@@ -329,55 +337,63 @@ struct Block {
 };
 __device__ __forceinline__ Block block_of(int b) { return {b == 0 ? 0 : 32, b == 2 ? 32 : 0}; }
 
-// The decays of a block's scores, as these lie in the accumulators, times the scale; 0 for keys behind the query.
-__device__ __forceinline__ void put_score_decays(Lds& s, const Decays& d, int b, float scale) {
-  const int lane = lane_here();
-  const Block at = block_of(b);
-  const int i = at.i + (lane & 31);
-  const float hi = d.hi[i], lo = d.lo[i];
-#pragma unroll
-  for (int r4 = 0; r4 < 4; ++r4) {
-    const int j = at.j + 8 * r4 + 4 * (lane >> 5);
-    const f32x4 jh = *reinterpret_cast<const f32x4*>(&d.hi[j]), jl = *reinterpret_cast<const f32x4*>(&d.lo[j]);
-    f32x4 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(j + e <= i ? (hi - jh[e]) + (lo - jl[e]) : -INFINITY) * scale;
-    s.w[b][r4][lane] = w;
-  }
-}
-
-// Scores of one block, transposed, as operands.
-__device__ __forceinline__ void scores(Lds& s, int b) {
+// Scores of one block, transposed, as operands, with their decays times the scale (0 for keys behind the query).
+// kFirst: the chunk's first head makes the decays, and with kMore keeps them for the others.
+template <bool kFirst, bool kMore>
+__device__ __forceinline__ void scores(Lds& s, const Decays& d, int b, float scale) {
   const int lane = lane_here(), half = lane >> 5;
-  const Block at = block_of(b);
+  const Block at = block_of(__builtin_amdgcn_readfirstlane(b));
   const int ka = (row_at(lane) ^ 16 * half) + 256 * at.j, qa = row_at(lane) + 8 * half + 256 * at.i;
-  f32x16 x;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+  const int i = at.i + (lane & 31), j0 = at.j + 4 * half;
   Frag a[4], q[4];
+  f32x4 jh[2], jl[2], decay[4];
+  float hi = 0.0f, lo = 0.0f;
   auto read = [&](int k) {   // 16 channels each
     a[k & 3].w = read_lds<u32x4>(s.k, ka ^ 32 * k);
     q[k & 3].d[0] = read_lds<u32x2>(s.q, qa ^ 32 * k);
     q[k & 3].d[1] = read_lds<u32x2>(s.q, qa ^ (32 * k + 16));
   };
+  auto read_decays = [&](int r4) {
+    if (kFirst) {
+      jh[r4 & 1] = *reinterpret_cast<const f32x4*>(&d.hi[j0 + 8 * r4]);
+      jl[r4 & 1] = *reinterpret_cast<const f32x4*>(&d.lo[j0 + 8 * r4]);
+    } else {
+      decay[r4] = s.w[b][r4][lane];
+    }
+  };
+  if (kFirst) {
+    hi = d.hi[i];
+    lo = d.lo[i];
+  }
+  read(0);
+  read_decays(0);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) read(k);
+  for (int k = 1; k < 4; ++k) read(k);
+  read_decays(1);
   turn();
+  f32x16 x;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = 0.0f;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     x = mfma32_bf16(a[k & 3].b, q[k & 3].b, x);
     if (k < 4) read(k + 4);
+    if (kFirst) {
+#pragma unroll
+      for (int r = 2 * k; r < 2 * k + 2; ++r) {
+        const float reach = (hi - jh[r >> 2 & 1][r & 3]) + (lo - jl[r >> 2 & 1][r & 3]);
+        decay[r >> 2][r & 3] = __builtin_amdgcn_exp2f(j0 + 8 * (r >> 2) + (r & 3) <= i ? reach : -INFINITY) * scale;
+      }
+      if (kMore && (k & 1)) s.w[b][k >> 1][lane] = decay[k >> 1];
+    }
+    if (k == 1 || k == 3) read_decays(k / 2 + 2);
     turn();
   }
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
     float w[8];
 #pragma unroll
-    for (int r4 = 0; r4 < 2; ++r4) {
-      const f32x4 decay = s.w[b][2 * y + r4][lane];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[4 * r4 + e] = x[8 * y + 4 * r4 + e] * decay[e];
-    }
+    for (int e = 0; e < 8; ++e) w[e] = x[8 * y + e] * decay[2 * y + (e >> 2)][e & 3];
     Frag f[2];
     split8<2>(w, f);
 #pragma unroll
@@ -440,29 +456,30 @@ __device__ __forceinline__ void from_state(Outputs& to, const State& st, Parts& 
     for (int r = 0; r < 16; ++r) to.o[i][r] *= from[i];
 }
 
-// o += V^T scores.
-__device__ __forceinline__ void from_chunk(Outputs& to, const Lds& s) {
+// o += V^T scores.  kFinal: beside the products the state's update is prepared.
+template <bool kFinal>
+__device__ __forceinline__ void from_chunk(Outputs& to, Update& u, State& st, const Lds& s, const Decays& d) {
   const int lane = lane_here(), vat = columns_at(lane) ^ 64 * wave_here();
-  Frag v[2][2], w[2][2][2];
-  auto read = [&](int b) {
+  Frag w[2][2][2];
+  auto read = [&](int b, int y) {
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      v[b & 1][y] = columns(s.v, vat, block_of(b).j + 16 * y);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) w[b & 1][y][i].w = s.p[b][y][i][lane];
-    }
+    for (int i = 0; i < 2; ++i) w[b & 1][y][i].w = s.p[b][y][i][lane];
   };
-  read(0);
-  read(1);
+  if (kFinal) u.begin(d, lane >> 5);
+  u.read(s, vat);
+#pragma unroll
+  for (int y = 0; y < 2; ++y)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) read(b, y);
   turn();
+  // blocks 0 and 1, of one 16 keys and of different queries, in turns, then block 2
 #pragma unroll
-  for (int b = 0; b < 3; ++b) {
+  for (int n = 0; n < 12; ++n) {
+    const int b = n < 8 ? n & 1 : 2, y = n < 8 ? n >> 2 : n >> 1 & 1, i = n < 8 ? 1 - (n >> 1 & 1) : 1 - (n & 1);
     f32x16& o = to.o[b == 0 ? 0 : 1];
-#pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int i = 1; i >= 0; --i) o = mfma32_bf16(v[b & 1][y].b, w[b & 1][y][i].b, o);
-    if (b == 0) read(2);
+    o = mfma32_bf16(u.v[(b == 2 ? 2 : 0) + y].b, w[b & 1][y][i].b, o);
+    if (n == 3 || n == 7) read(2, n >> 2);   // block 0's of the same keys are used up
+    if (kFinal) u.prepare(st, n);
     turn();
   }
 }
@@ -488,13 +505,14 @@ __device__ __forceinline__ void read_outputs(Rows& r, LdsRows& rows) {
     r.w[i] = (u32x4){a[0], a[1], b[0], b[1]};
   }
 }
+// Of n rows, a multiple of 256 bytes apart; buffer stores, which drop what lies behind the last row without a
+// branch: a wait for loads behind stores that are not always made would be one for these too.
 __device__ __forceinline__ void store_outputs(const Rows& r, uint16_t* to, int h_q, int n) {
   const int thread = thread_here();
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(to, 0, (min(n, kC) - 1) * h_q * 256 + 256, 0x00027000);
 #pragma unroll
-  for (int i = 0; i < Rows::kEach; ++i) {
-    const int row = Rows::row(thread, i);
-    if (row < n) *reinterpret_cast<u32x4*>(to + (row * h_q * kD + 8 * (thread & 15))) = r.w[i];
-  }
+  for (int i = 0; i < Rows::kEach; ++i)
+    __builtin_amdgcn_raw_buffer_store_b128(r.w[i], rsrc, Rows::row(thread, i) * h_q * 256 + 16 * (thread & 15), 0, 0);
 }
 
 // Item number to KV head and segment.  A KV head's rows are 256 bytes of each token: were the heads dealt to the
@@ -510,19 +528,27 @@ __device__ __forceinline__ Item item_of(const LinearParams& p, int item) {
 // One workgroup per (segment, KV head): the segment's own state, for the next.
 __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p) {
   __shared__ Keys s;
-  const auto [id, hk] = item_of(p, blockIdx.x);
-  const int wave = threadIdx.x >> 6;
+  const Item item = item_of(p, blockIdx.x);
+  const int id = item.id, hk = item.hk;
+  const int wave = wave_here();
   Segment g;
   if (!find_segment(p, id, &g) || g.s == g.count - 1) return;
   float* const slot = p.starts + ((int64_t)id * p.h_kv + hk) * kLinState;
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
   const uint32_t row = threadIdx.x / 16, kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, kat = row * kb, vat = row * vb;
-  Rows rk, rv;
+  struct {
+    Rows k, v;
+  } r[2];   // of the next chunk and the one after it
+  auto load = [&](int x, int c) {   // behind the last chunk any rows will do
+    const int at = c < g.n ? c : 0;
+    r[x].k.load(k0 + at * p.k_stride, kb, kat, g.n - at);
+    r[x].v.load(v0 + at * p.v_stride, vb, vat, g.n - at);
+  };
+  load(0, 0);
+  load(1, kC);
   float decay = 0.0f;   // of the chunk after the next
   double total = 0.0;
-  rk.load(k0, kb, kat, g.n);
-  rv.load(v0, vb, vat, g.n);
   State st;
   state_zero(st);
   if (g.s == 0) {
@@ -534,21 +560,32 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
     total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, 1.0f);
     decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
   }
-  store_rows(rk, s.k);
-  store_rows(rv, s.v);
-  for (int c = 0, x = 0; c < g.n; c += kC, x ^= 1) {
-    const int rest = g.n - c - kC, next = rest > 0 ? c + kC : c;   // behind the last chunk any rows will do
+  auto chunk = [&](int x, int c) {
+    const int rest = g.n - c - kC;
+    store_rows(r[x].k, s.k);
+    store_rows(r[x].v, s.v);
     __syncthreads();
-    rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
-    rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);
+    load(x, c + 2 * kC);
     if (wave == 3 && rest > 0) {
       total += put_decays(s.d[x ^ 1], decay, rest, 1.0f);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
     }
-    update(st, s, s.d[x]);
+    Update u;
+    const int lane = lane_here();
+    u.begin(s.d[x], lane >> 5);
+    u.read(s, columns_at(lane) ^ 64 * wave_here());
+    turn();
+#pragma unroll
+    for (int n = 0; n < 12; ++n) u.prepare(st, n);
+    turn();
+    u.add(st, s, s.d[x]);
     __syncthreads();
-    store_rows(rk, s.k);
-    store_rows(rv, s.v);
+  };
+  for (int c = 0;; c += 2 * kC) {
+    chunk(0, c);
+    if (c + kC >= g.n) break;
+    chunk(1, c + kC);
+    if (c + 2 * kC >= g.n) break;
   }
   raw_store(st, slot + (int64_t)p.h_kv * kLinState);
   if (threadIdx.x == kThreads - 1) p.decays[(int64_t)id * p.h_kv + hk] = __builtin_amdgcn_exp2f((float)total);
@@ -559,11 +596,12 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
 __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParams p, int items) {
   __shared__ Lds s;
   // parts of an item follow each other on one XCD
-  const int item = blockIdx.x / (8 * p.parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % p.parts;
-  if (item >= items) return;
-  const auto [id, hk] = item_of(p, item);
+  const int number = blockIdx.x / (8 * p.parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % p.parts;
+  if (number >= items) return;
+  const Item item = item_of(p, number);
+  const int id = item.id, hk = item.hk;
   const int grp = p.h_q / p.h_kv, h0 = hk * grp + part * p.heads, h1 = min(h0 + p.heads, hk * grp + grp);
-  const int wave = threadIdx.x >> 6;
+  const int wave = wave_here();
   Segment g;
   if (!find_segment(p, id, &g)) return;
   const bool last = g.s == g.count - 1;
@@ -604,38 +642,46 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
     const Decays& d = s.d[x];
     __syncthreads();
     Parts parts;
-    if (wave < 3) put_score_decays(s, d, wave, p.scale);
     if (wave == 3 && rest > 0) {
       put_decays(s.d[x ^ 1], decay, rest, p.scale);
       decay = load_decays(p, g.t0 + c + 2 * kC, rest - kC, hk);
     }
-    auto step = [&](auto first, int h) {
-      const bool more = h + 1 < h1;
-      const int from = more ? c : next;
-      rq.load(q0 + from * p.q_stride + (more ? h + 1 : h0) * kD, qb, qat, g.n - from);
-      if (wave < 3) scores(s, wave);
+    auto step = [&](auto first, auto final, int h) {
+      const int from = decltype(final)::value ? next : c;
+      rq.load(q0 + from * p.q_stride + (decltype(final)::value ? h0 : h + 1) * kD, qb, qat, g.n - from);
+      if (wave < 3) scores<decltype(first)::value, !decltype(final)::value>(s, d, wave, p.scale);
       Outputs out;
       from_state<decltype(first)::value>(out, st, parts, s, d);
+      if (decltype(final)::value) {   // not before: the state's parts were in these registers
+        rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
+      }
       __syncthreads();   // the scores are there, the queries used
-      from_chunk(out, s);
+      Update u;
+      from_chunk<decltype(final)::value>(out, u, st, s, d);
+      if (decltype(final)::value) rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);   // nor this: the scores were
       put_outputs(out, s.q);
+      if (decltype(final)::value && (rest > 0 || (last && part == 0))) u.add(st, s, d);
       __syncthreads();
       Rows ro;
       read_outputs(ro, s.q);
-      // before the outputs go to memory: a wait for loads behind stores that are not always made is one for these
       store_queries(rq, s.q);
+      if (decltype(final)::value) {
+        store_rows(rk, s.k);
+        store_rows(rv, s.v);
+      }
       store_outputs(ro, p.out + ((g.t0 + c) * p.h_q + h) * kD, p.h_q, g.n - c);
-      if (more) __syncthreads();
+      if (!decltype(final)::value) __syncthreads();
     };
-    step(std::true_type(), h0);
-    for (int h = h0 + 1; h < h1; ++h) step(std::false_type(), h);
-    rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
-    rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);
-    if (rest > 0 || (last && part == 0)) update(st, s, d);
-    if (rest <= 0) break;   // past it the compiler would take the loads for pending and wait in the next chunk
-    __syncthreads();
-    store_rows(rk, s.k);
-    store_rows(rv, s.v);
+    const std::true_type yes;
+    const std::false_type no;
+    if (h0 + 1 == h1) {
+      step(yes, yes, h0);
+    } else {
+      step(yes, no, h0);
+      for (int h = h0 + 1; h < h1 - 1; ++h) step(no, no, h);
+      step(no, yes, h1 - 1);
+    }
+    if (rest <= 0) break;
   }
   if (last && part == 0) {
     const int dst = p.state_dst[g.b];
@@ -644,35 +690,54 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
 }
 
 // The states before the segments of a sequence: `sums` left, in the place of segment s + 1, the state that
-// segment s alone leaves (segment 0 with the sequence's first state).  A thread takes four values through
-// all segments.
-constexpr int kJoinBlocks = kLinState / 4 / 256;
-__global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p, int segments) {
-  const int part = blockIdx.x % kJoinBlocks, hk = blockIdx.x / kJoinBlocks;
-  for (int id = blockIdx.y; id < segments; id += gridDim.y) {
-    Segment g;
-    if (!find_segment(p, id, &g) || g.s != 1 || g.count < 3) continue;
-    f32x4* at = reinterpret_cast<f32x4*>(p.starts + ((int64_t)id * p.h_kv + hk) * kLinState) + part * 256 + threadIdx.x;
-    const float* decay = p.decays + (int64_t)id * p.h_kv + hk;
-    const int64_t step = (int64_t)p.h_kv * (kLinState / 4);
-    f32x4 x = *at;
-    for (int s = 2; s < g.count; s += 8) {   // eight loads in flight
-      f32x4 y[8];
-      float a[8];
+// segment s alone leaves (segment 0 with the sequence's first state).  A workgroup has 256 values of it; each of
+// its four waves reads up to eight segments at once, and adds to their sums what the segments before them left.
+constexpr int kJoinEach = 8;
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
+  constexpr int kBlocks = kLinState / 256;
+  __shared__ f32x4 s_end[4][64];
+  __shared__ float s_decay[4];
+  const int part = blockIdx.x % kBlocks, hk = blockIdx.x / kBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t step = (int64_t)p.h_kv * (kLinState / 4);
+  for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
+    const int begin = p.cu_seqlens[b], id = begin / p.segment + b + 1;   // of segment 1
+    const int last = (p.cu_seqlens[b + 1] - begin + p.segment - 1) / p.segment - 2;   // places 1 .. last behind its own
+    if (last < 1) continue;
+    f32x4* const at = reinterpret_cast<f32x4*>(p.starts + ((int64_t)id * p.h_kv + hk) * kLinState) + part * 64 + lane;
+    const float* const decay = p.decays + (int64_t)id * p.h_kv + hk;
+    f32x4 carry = *at;
+    for (int base = 1; base <= last; base += 4 * kJoinEach) {
+      const int first = base + wave * kJoinEach;
+      f32x4 x[kJoinEach];
+      float a[kJoinEach];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int j = min(i, g.count - 1 - s);
-        y[i] = at[(j + 1) * step];
-        a[i] = decay[j * p.h_kv];
+      for (int i = 0; i < kJoinEach; ++i) {
+        x[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
+        a[i] = 1.0f;
+        if (first + i <= last) {
+          x[i] = at[(first + i) * step];
+          a[i] = decay[(int64_t)(first + i - 1) * p.h_kv];
+        }
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (s + i >= g.count) break;
-        x = x * a[i] + y[i];
-        at[(i + 1) * step] = x;
+      for (int i = 1; i < kJoinEach; ++i) {
+        x[i] += x[i - 1] * a[i];
+        a[i] *= a[i - 1];
       }
-      at += 8 * step;
-      decay += 8 * p.h_kv;
+      __syncthreads();
+      // behind the last place the decays are 1 and the sums 0: the wave's end is its last place's
+      s_end[wave][lane] = x[kJoinEach - 1];
+      if (lane == 0) s_decay[wave] = a[kJoinEach - 1];
+      __syncthreads();
+      f32x4 before = carry;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        if (w == wave) before = carry;
+        carry = carry * s_decay[w] + s_end[w][lane];
+      }
+#pragma unroll
+      for (int i = 0; i < kJoinEach; ++i)
+        if (first + i <= last) at[(first + i) * step] = x[i] + before * a[i];
     }
   }
 }
@@ -684,7 +749,7 @@ hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream) {
   const int items = (int)(segments * p.h_kv), eighths = (items + 7) / 8 * 8;
   if (p.split) {
     linear_sums_kernel<<<dim3(items), dim3(kThreads), 0, stream>>>(p);
-    linear_join_kernel<<<dim3(kJoinBlocks * p.h_kv, (unsigned)std::min<int64_t>(segments, 2048)), dim3(256), 0, stream>>>(p, (int)segments);
+    linear_join_kernel<<<dim3(kLinState / 256 * p.h_kv, std::min(p.batch, 64)), dim3(256), 0, stream>>>(p);
   }
   linear_outputs_kernel<<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(kThreads), 0, stream>>>(p, items);
   return hipGetLastError();
