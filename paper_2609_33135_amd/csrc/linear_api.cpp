@@ -9,12 +9,11 @@
 #include <cstdint>
 
 #include "linear_internal.h"
+#include "mpfa_internal.h"
 
 #ifdef MPFA_DEBUG_CHECKS
 #include <new>
 #include <vector>
-
-#include "mpfa_internal.h"
 #endif
 
 namespace {
@@ -22,7 +21,7 @@ namespace {
 constexpr int kMostTokens = 1 << 28;              // of one call
 constexpr int kMostRows = 1024;                   // of one sequence in a decode call
 constexpr int64_t kMaxStride = (int64_t)1 << 25;  // elements between tokens: 64 of them in 32 bits of bytes
-constexpr int64_t kItems = 512;                   // work items that fill the card, two a unit
+constexpr int64_t kUnits = mpfa::kComputeUnits;
 
 bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
 
@@ -36,10 +35,14 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 mpfa_status done(hipError_t e) { return e == hipSuccess ? MPFA_OK : MPFA_ERR_HIP; }
 
-// Tokens per segment: as many items as fill the card, in whole chunks.
+// Tokens per segment, in whole chunks: as many items as there are units, from segments of 1024 tokens on two a
+// unit.  Two at once on a unit take 1.1 to 1.3 times less than one after the other, but every segment's states
+// are written and read twice, 256 KB, which is what the rows of some hundred tokens are.  us: 4096 tokens of 8:8
+// heads 36 by 256 items, 45 by 512; 8192 of 32:32 130 and 131; 65536 of 32:8 482 and 440.
 int segment_tokens(int64_t total_tokens, int h_kv) {
-  const int64_t n = (total_tokens * h_kv + kItems - 1) / kItems;
-  return (int)std::max<int64_t>(mpfa::kLinChunk, (n + mpfa::kLinChunk - 1) / mpfa::kLinChunk * mpfa::kLinChunk);
+  auto chunks = [&](int64_t items) { return (total_tokens * h_kv + items * mpfa::kLinChunk - 1) / (items * mpfa::kLinChunk); };
+  const int64_t n = chunks(kUnits) > 16 ? chunks(2 * kUnits) : chunks(kUnits);
+  return (int)std::max<int64_t>(1, n) * mpfa::kLinChunk;
 }
 
 // What both calls check; fills what does not depend on the kind.
@@ -171,9 +174,10 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   if (s.split && (!workspace || workspace_bytes < s.bytes || !aligned16(workspace))) return MPFA_ERR_WORKSPACE;
   p.segment = s.segment;
   p.split = s.split;
-  // few items: a KV head's query heads apart, while that makes no more than fill the card
+  // few items: a KV head's query heads apart, as long as two items a unit hold them (16384 tokens of 16:1 heads 70 us
+  // with all 16 together, 63 by eight)
   const int grp = a->h_q / a->h_kv;
-  p.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, items * grp / kItems));
+  p.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, (items * grp + 2 * kUnits - 1) / (2 * kUnits)));
   p.parts = (grp + p.heads - 1) / p.heads;
   p.starts = s.split ? static_cast<float*>(workspace) : nullptr;
   p.decays = s.split ? p.starts + s.starts / sizeof(float) : nullptr;
