@@ -9,67 +9,109 @@ namespace mpfa {
 
 namespace {
 
-constexpr int kHeads = 8;   // query heads whose sums are joined together
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-// One workgroup of 256 threads per (sequence, KV head, kCols columns of the state): kCols / 4 lanes side by
-// side on a row, 1024 / kCols rows at a time.
-template <int kCols>
+constexpr int kCols = 32;              // columns of the state per workgroup: four workgroups a state
+constexpr int kLanes = kCols / 4;      // lanes side by side on a row of it
+constexpr int kRows = 256 / kLanes;    // rows at a time
+constexpr int kEach = kD / kRows;      // a thread's, one after the other
+static_assert(kEach == 4, "one vector of k, of q");
+constexpr int kPairs = 16;             // rows of queries (token and head) between two barriers
+
+// Eight BF16 as FP32.
+__device__ __forceinline__ void widen(const u32x4& w, float* to) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<f32x4*>(to)[i] = (f32x4){__uint_as_float(w[2 * i] << 16), __uint_as_float(w[2 * i] & 0xFFFF0000u),
+                                              __uint_as_float(w[2 * i + 1] << 16), __uint_as_float(w[2 * i + 1] & 0xFFFF0000u)};
+}
+
+// Sums over the eight lanes of a wave that hold the same four columns: column 2 (lane / 16 % 2) + lane / 32 of the
+// four.  A swap of two registers' halves (or rows of 16 lanes) leaves in each half one column's values of both, so
+// every step also halves the values that are left.
+static_assert(kLanes == 8, "rows of a wave");
+__device__ __forceinline__ float rows_sum(const f32x4& x) {
+  float y[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[2 * i]), __float_as_uint(x[2 * i + 1]), false, false);
+    y[i] = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  }
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y[0]), __float_as_uint(y[1]), false, false);
+  const float z = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+  return z + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(z), 0x128, 0xF, 0xF, false));   // 8 lanes on in 16
+}
+
+// One workgroup per (sequence, KV head, kCols columns of the state).
 __global__ __launch_bounds__(256) void linear_decode_kernel(LinearParams p) {
-  constexpr int kLanes = kCols / 4, kRows = 256 / kLanes, kEach = kD / kRows, kParts = kD / kCols;
-  __shared__ float s_k[kD], s_q[kHeads][kD];
-  __shared__ f32x4 s_sum[4][kHeads][kLanes];
+  __shared__ float s_k[kPairs][kD], s_q[kPairs][kD], s_v[kPairs][kCols], s_a[kPairs];
+  __shared__ float s_sum[4][kPairs][kCols];
+  constexpr int kParts = kD / kCols;
   const int part = blockIdx.x % kParts, hk = blockIdx.x / kParts % p.h_kv, b = blockIdx.x / kParts / p.h_kv;
   const int tid = threadIdx.x, c = tid % kLanes, row = tid / kLanes, lane = tid & 63, wave = tid >> 6;
-  const int grp = p.h_q / p.h_kv, col = part * kCols + 4 * c;
+  const int grp = p.h_q / p.h_kv, heads = min(grp, kPairs), tokens = kPairs / heads;
+  const int64_t t0 = (int64_t)b * p.q_tokens;
   const int src = p.state_src[b], dst = p.state_dst[b];
   f32x4 st[kEach];
   if (src >= 0) {
-    const float* from = p.states + ((int64_t)src * p.h_kv + hk) * kLinState + col;
+    const float* from = p.states + ((int64_t)src * p.h_kv + hk) * kLinState + part * kCols + 4 * c;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) st[i] = *reinterpret_cast<const f32x4*>(from + (row + kRows * i) * kD);
+    for (int i = 0; i < kEach; ++i) st[i] = *reinterpret_cast<const f32x4*>(from + (kEach * row + i) * kD);
   } else {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) st[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
   }
-  for (int r = 0; r < p.q_tokens; ++r) {
-    const int64_t t = (int64_t)b * p.q_tokens + r;
-    const float g = fminf(fmaxf(p.log_decay[t * p.decay_stride + hk], kLinLeastDecay), 0.0f), a = expf(g);
-    const uint32_t* vw = reinterpret_cast<const uint32_t*>(p.v + t * p.v_stride + hk * kD + col);
-    const f32x4 v = {__uint_as_float(vw[0] << 16), __uint_as_float(vw[0] & 0xFFFF0000u), __uint_as_float(vw[1] << 16),
-                     __uint_as_float(vw[1] & 0xFFFF0000u)};
-    for (int h0 = 0; h0 < grp; h0 += kHeads) {
-      const int heads = min(kHeads, grp - h0);
+  for (int r0 = 0; r0 < p.q_tokens; r0 += tokens) {
+    const int nr = min(tokens, p.q_tokens - r0);
+    for (int h0 = 0; h0 < grp; h0 += heads) {   // more than one turn: a token at a time
+      const int nh = min(heads, grp - h0);
       __syncthreads();
-      if (h0 == 0 && tid < kD) s_k[tid] = bf16_to_f32(p.k[t * p.k_stride + hk * kD + tid]);
-      for (int i = tid; i < heads * kD; i += 256) s_q[i / kD][i % kD] = bf16_to_f32(p.q[t * p.q_stride + (hk * grp + h0) * kD + i]);
-      __syncthreads();
-      if (h0 == 0)
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) st[i] = st[i] * a + v * s_k[row + kRows * i];
-      for (int h = 0; h < heads; ++h) {
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) o += st[i] * s_q[h][row + kRows * i];
-#pragma unroll
-        for (int off = kLanes; off < 64; off <<= 1)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off);
-        if (lane < kLanes) s_sum[wave][h][lane] = o;
+      {   // 16 threads a row
+        const int i = tid >> 4, at = 8 * (tid & 15);
+        if (i < nr * nh) {
+          const uint16_t* q = p.q + (t0 + r0 + i / nh) * p.q_stride + (hk * grp + h0 + i % nh) * kD;
+          widen(*reinterpret_cast<const u32x4*>(q + at), &s_q[i][at]);
+        }
+        if (h0 == 0 && i < nr) {
+          const int64_t t = t0 + r0 + i;
+          widen(*reinterpret_cast<const u32x4*>(p.k + t * p.k_stride + hk * kD + at), &s_k[i][at]);
+          if (at < kCols) widen(*reinterpret_cast<const u32x4*>(p.v + t * p.v_stride + hk * kD + part * kCols + at), &s_v[i][at]);
+          if (at == kCols) s_a[i] = expf(fminf(fmaxf(p.log_decay[t * p.decay_stride + hk], kLinLeastDecay), 0.0f));
+        }
       }
       __syncthreads();
-      for (int i = tid; i < heads * kLanes; i += 256) {
-        const int h = i / kLanes, x = i % kLanes;
-        const f32x4 o = ((s_sum[0][h][x] + s_sum[1][h][x]) + (s_sum[2][h][x] + s_sum[3][h][x])) * p.scale;
-        uint16_t* to = p.out + (t * p.h_q + hk * grp + h0 + h) * kD + part * kCols + 4 * x;
+      for (int r = 0; r < nr; ++r) {
+        if (h0 == 0) {
+          const float a = s_a[r];
+          const f32x4 v = *reinterpret_cast<const f32x4*>(&s_v[r][4 * c]), k = *reinterpret_cast<const f32x4*>(&s_k[r][kEach * row]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[e] = bf16_rne(o[e]);
+          for (int i = 0; i < kEach; ++i) st[i] = st[i] * a + v * k[i];
+        }
+        for (int h = 0; h < nh; ++h) {
+          const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[r * nh + h][kEach * row]);
+          f32x4 o = st[0] * q[0];
+#pragma unroll
+          for (int i = 1; i < kEach; ++i) o += st[i] * q[i];
+          const float sum = rows_sum(o);
+          if (!(lane & 8)) s_sum[wave][r * nh + h][4 * c + 2 * (lane >> 4 & 1) + (lane >> 5)] = sum;
+        }
+      }
+      __syncthreads();
+      if (tid < nr * nh * kLanes) {
+        const int i = tid / kLanes, x = tid % kLanes;
+        f32x4 w[4];
+#pragma unroll
+        for (int n = 0; n < 4; ++n) w[n] = *reinterpret_cast<const f32x4*>(&s_sum[n][i][4 * x]);
+        const f32x4 o = ((w[0] + w[1]) + (w[2] + w[3])) * p.scale;
+        uint16_t* to = p.out + ((t0 + r0 + i / nh) * p.h_q + hk * grp + h0 + i % nh) * kD + part * kCols + 4 * x;
+        *reinterpret_cast<u32x2*>(to) = (u32x2){bf16_rne(o[0]) | (uint32_t)bf16_rne(o[1]) << 16, bf16_rne(o[2]) | (uint32_t)bf16_rne(o[3]) << 16};
       }
     }
   }
   if (dst >= 0) {
-    float* to = p.states + ((int64_t)dst * p.h_kv + hk) * kLinState + col;
+    float* to = p.states + ((int64_t)dst * p.h_kv + hk) * kLinState + part * kCols + 4 * c;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) *reinterpret_cast<f32x4*>(to + (row + kRows * i) * kD) = st[i];
+    for (int i = 0; i < kEach; ++i) *reinterpret_cast<f32x4*>(to + (kEach * row + i) * kD) = st[i];
   }
 }
 
@@ -77,7 +119,7 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearParams p) {
 
 hipError_t launch_linear_decode(const LinearParams& p, hipStream_t stream) {
   const int64_t heads = (int64_t)p.batch * p.h_kv;
-  linear_decode_kernel<32><<<dim3((unsigned)(heads * 4)), dim3(256), 0, stream>>>(p);
+  linear_decode_kernel<<<dim3((unsigned)(heads * (kD / kCols))), dim3(256), 0, stream>>>(p);
   return hipGetLastError();
 }
 
