@@ -583,8 +583,8 @@ mpfa_status mpfa_kv4_evict(const mpfa_kv4_evict_args* args, mpfa_stream_t stream
  *    sequences of a call may end in one slot, or one end in a slot from which
  *    another starts.  A sequence without tokens leaves the state it starts from.
  *  - q_stride, k_stride, v_stride: elements between tokens (at least heads * 128,
- *    a multiple of 8; the heads of a token are contiguous).  q, k, v, states and
- *    out are 16-byte aligned.  h_q and h_kv are 1 to 256, h_q % h_kv == 0.
+ *    a multiple of 8; the heads of a token are contiguous), like decay_stride
+ *    below 2^25.  q, k, v, states and out are 16-byte aligned.  h_q and h_kv are 1 to 256, h_q % h_kv == 0.
  * States, sums and decays are FP32.  Where the matrix cores take FP32 numbers as
  * BF16 they are sums of such: of two for an output (a state, a score: at most
  * 2^-16 of it is lost), of three for the state (2^-24).  q, k and v are finite, and
@@ -649,7 +649,7 @@ mpfa_status mpfa_linear_decode(const mpfa_linear_args* args, mpfa_stream_t strea
  * Sums are FP32: |r| and |r * weight| from about 2^63 on are outside the contract.
  * Rows do not affect each other; one with a NaN or an infinity gets NaN outputs
  * or scales somewhere.
- * x_stride: elements between rows of x (a multiple of 8); residual, residual_out
+ * x_stride: elements between rows of x (a multiple of 8, below 2^31); residual, residual_out
  * and out are contiguous, and residual_out may be residual (or x, where x is
  * contiguous).  x, residual, residual_out, weight are 16-byte aligned, out too
  * (codes: 8).

@@ -21,6 +21,7 @@ namespace {
 constexpr int kMostTokens = 1 << 28;              // of one call
 constexpr int kMostRows = 1024;                   // of one sequence in a decode call
 constexpr int64_t kMaxStride = (int64_t)1 << 25;  // elements between tokens: 64 of them in 32 bits of bytes
+constexpr int64_t kMaxRow = (int64_t)1 << 31;     // elements between rows of the norm
 constexpr int64_t kUnits = mpfa::kComputeUnits;
 
 bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
@@ -83,20 +84,26 @@ mpfa_status linear_params(const mpfa_linear_args* a, bool decode, mpfa::LinearPa
   return MPFA_OK;
 }
 
-// A prefill's segments and its two tables in the workspace: states before segments, then decays.
+// A prefill's segments, the parts of a KV head's query heads that go apart, and the two tables in the workspace:
+// states before segments, then decays.
 struct PrefillSpace {
-  int segment;
+  int segment, parts, heads;
   bool split;
-  int64_t segments;
+  int64_t items;
   size_t starts, bytes;
 };
-PrefillSpace prefill_space(int batch, int total_tokens, int max_seqlen, int h_kv) {
+PrefillSpace prefill_space(int batch, int total_tokens, int max_seqlen, int h_q, int h_kv) {
   PrefillSpace s;
   s.segment = segment_tokens(total_tokens, h_kv);
   s.split = std::min(max_seqlen, total_tokens) > s.segment;
-  s.segments = mpfa::linear_segments(batch, total_tokens, s.segment);
-  s.starts = align256((size_t)s.segments * h_kv * mpfa::kLinState * sizeof(float));
-  s.bytes = s.split ? s.starts + (size_t)s.segments * h_kv * sizeof(float) : 0;
+  s.items = mpfa::linear_segments(batch, total_tokens, s.segment) * h_kv;
+  // few items: a KV head's query heads apart, as long as two items a unit hold them (16384 tokens of 16:1 heads 70 us
+  // with all 16 together, 63 by eight)
+  const int grp = h_q / h_kv;
+  s.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, (s.items * grp + 2 * kUnits - 1) / (2 * kUnits)));
+  s.parts = (grp + s.heads - 1) / s.heads;
+  s.starts = align256((size_t)s.items * mpfa::kLinState * sizeof(float));
+  s.bytes = s.split || s.parts > 1 ? s.starts + (size_t)s.items * sizeof(float) : 0;
   return s;
 }
 
@@ -160,7 +167,7 @@ mpfa_status mpfa_linear_prefill_workspace_size(int32_t batch, int32_t total_toke
                                                size_t* bytes) {
   if (!bytes || batch < 1 || batch > 65535 || total_tokens < 0 || max_seqlen < 0 || !heads_ok(h_q, h_kv)) return MPFA_ERR_INVALID;
   if (total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
-  *bytes = prefill_space(batch, total_tokens, max_seqlen, h_kv).bytes;
+  *bytes = prefill_space(batch, total_tokens, max_seqlen, h_q, h_kv).bytes;
   return MPFA_OK;
 }
 
@@ -168,19 +175,15 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   mpfa::LinearParams p;
   if (const mpfa_status st = linear_params(a, false, p)) return st;
   if (a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
-  const PrefillSpace s = prefill_space(a->batch, a->total_tokens, a->max_seqlen, a->h_kv);
-  const int64_t items = s.segments * a->h_kv;
-  if (items > (int64_t)UINT32_MAX / 512 - 8) return MPFA_ERR_UNSUPPORTED;
-  if (s.split && (!workspace || workspace_bytes < s.bytes || !aligned16(workspace))) return MPFA_ERR_WORKSPACE;
+  const PrefillSpace s = prefill_space(a->batch, a->total_tokens, a->max_seqlen, a->h_q, a->h_kv);
+  if (s.items > (int64_t)UINT32_MAX / 512 - 8) return MPFA_ERR_UNSUPPORTED;
+  if (s.bytes && (!workspace || workspace_bytes < s.bytes || !aligned16(workspace))) return MPFA_ERR_WORKSPACE;
   p.segment = s.segment;
   p.split = s.split;
-  // few items: a KV head's query heads apart, as long as two items a unit hold them (16384 tokens of 16:1 heads 70 us
-  // with all 16 together, 63 by eight)
-  const int grp = a->h_q / a->h_kv;
-  p.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, (items * grp + 2 * kUnits - 1) / (2 * kUnits)));
-  p.parts = (grp + p.heads - 1) / p.heads;
-  p.starts = s.split ? static_cast<float*>(workspace) : nullptr;
-  p.decays = s.split ? p.starts + s.starts / sizeof(float) : nullptr;
+  p.parts = s.parts;
+  p.heads = s.heads;
+  p.starts = s.bytes ? static_cast<float*>(workspace) : nullptr;
+  p.decays = s.bytes ? p.starts + s.starts / sizeof(float) : nullptr;
 #ifdef MPFA_DEBUG_CHECKS
   if (const mpfa_status st = check_linear(a, false, reinterpret_cast<hipStream_t>(stream))) return st;
 #endif
@@ -202,7 +205,7 @@ mpfa_status mpfa_rms_norm(const mpfa_rms_norm_args* a, mpfa_stream_t stream) {
   if (!(a->eps > 0.0f) || !std::isfinite(a->eps)) return MPFA_ERR_INVALID;
   if (a->scales ? a->group != 0 && (a->group < 32 || a->group > 512 || (a->group & (a->group - 1))) : a->group != 0) return MPFA_ERR_INVALID;
   if (a->rows == 0) return MPFA_OK;
-  if (a->x_stride < (a->rows > 1 ? a->width : 0) || a->x_stride % 8 || a->x_stride >= kMaxStride) return MPFA_ERR_INVALID;
+  if (a->x_stride < (a->rows > 1 ? a->width : 0) || a->x_stride % 8 || a->x_stride >= kMaxRow) return MPFA_ERR_INVALID;
   if (!a->x || !a->out || (a->residual != nullptr) != (a->residual_out != nullptr)) return MPFA_ERR_INVALID;
   if (!aligned16(a->x) || !aligned16(a->weight) || !aligned16(a->residual) || !aligned16(a->residual_out)) return MPFA_ERR_INVALID;
   if ((reinterpret_cast<uintptr_t>(a->out) & (a->scales ? 7 : 15)) || (reinterpret_cast<uintptr_t>(a->scales) & 3)) return MPFA_ERR_INVALID;

@@ -52,7 +52,7 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
   const int begin = p.cu_seqlens[lo], len = p.cu_seqlens[lo + 1] - begin;
   g->b = lo;
   g->s = id - (begin / p.segment + lo);
-  g->count = max(1, (len + p.segment - 1) / p.segment);
+  g->count = p.split ? max(1, (len + p.segment - 1) / p.segment) : 1;
   g->t0 = (int64_t)begin + (int64_t)g->s * p.segment;
   g->n = min(p.segment, len - g->s * p.segment);
   return g->s < g->count;
@@ -157,11 +157,12 @@ struct Rows {
   u32x4 w[kEach];
   // stride: bytes between rows, of which 64 stay below 2^32; at: of the thread's first row
   __device__ __forceinline__ void load(const uint16_t* x, uint32_t stride, uint32_t at, int n) {
-    asm volatile("" : "+v"(at));   // as for the thread below: offsets are not kept
+    asm volatile("" : "+v"(at));   // as for the thread above: offsets are not kept
+    const uint32_t last = (min(n, kC) - 1) * stride;
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
       w[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(x) +
-                                             (min(at + i * (kThreads / 16) * stride, (n - 1) * stride) + 16 * (threadIdx.x & 15)));
+                                             (min(at + i * (kThreads / 16) * stride, last) + 16 * (threadIdx.x & 15)));
   }
   static __device__ __forceinline__ int row(int thread, int i) { return thread / 16 + kThreads / 16 * i; }
 };
@@ -525,15 +526,26 @@ __device__ __forceinline__ Item item_of(const LinearParams& p, int item) {
   return {id, (int)((uint32_t)(item + id + id / 8) % p.h_kv)};
 }
 
-// One workgroup per (segment, KV head): the segment's own state, for the next.
+// One workgroup per (segment, KV head): the segment's own state, for the next.  A sequence's first state goes to the
+// place of its first segment, where several workgroups read it: its slot is written by whichever is done first.
 __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p) {
   __shared__ Keys s;
   const Item item = item_of(p, blockIdx.x);
   const int id = item.id, hk = item.hk;
   const int wave = wave_here();
   Segment g;
-  if (!find_segment(p, id, &g) || g.s == g.count - 1) return;
+  if (!find_segment(p, id, &g)) return;
+  const bool last = g.s == g.count - 1;
+  if (last && (g.s > 0 || p.parts == 1)) return;
   float* const slot = p.starts + ((int64_t)id * p.h_kv + hk) * kLinState;
+  State st;
+  state_zero(st);
+  if (g.s == 0) {
+    const int src = p.state_src[g.b];
+    if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
+    raw_store(st, slot);
+    if (last) return;
+  }
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
   const uint32_t row = threadIdx.x / 16, kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, kat = row * kb, vat = row * vb;
@@ -549,13 +561,6 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
   load(1, kC);
   float decay = 0.0f;   // of the chunk after the next
   double total = 0.0;
-  State st;
-  state_zero(st);
-  if (g.s == 0) {
-    const int src = p.state_src[g.b];
-    if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
-    raw_store(st, slot);   // the slot that it comes from may be written by `outputs`
-  }
   if (wave == 3) {
     total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, 1.0f);
     decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
@@ -619,7 +624,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
   }
   State st;
   state_zero(st);
-  if (g.count > 1) {
+  if (g.count > 1 || p.parts > 1) {
     raw_load(st, p.starts + ((int64_t)id * p.h_kv + hk) * kLinState);
   } else {
     const int src = p.state_src[g.b];
@@ -747,8 +752,8 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
 hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream) {
   const int64_t segments = linear_segments(p.batch, p.total_tokens, p.segment);
   const int items = (int)(segments * p.h_kv), eighths = (items + 7) / 8 * 8;
+  if (p.split || p.parts > 1) linear_sums_kernel<<<dim3(items), dim3(kThreads), 0, stream>>>(p);
   if (p.split) {
-    linear_sums_kernel<<<dim3(items), dim3(kThreads), 0, stream>>>(p);
     linear_join_kernel<<<dim3(kLinState / 256 * p.h_kv, std::min(p.batch, 64)), dim3(256), 0, stream>>>(p);
   }
   linear_outputs_kernel<<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(kThreads), 0, stream>>>(p, items);

@@ -155,6 +155,31 @@ def test_in_place_many_segments(mp):
     c.check(lambda: c.prefill(mp))
 
 
+@pytest.mark.parametrize("h_q,h_kv", [(16, 1), (40, 8)])
+def test_in_place_heads_apart(mp, h_q, h_kv):
+    """Workgroups that share a state start from what it was, though one of them replaces it, and whenever each of them
+    gets to run: beside large products on another stream, against the same call out of place."""
+    lens = [40, 0, 1, 64, 130]
+    a = Case(lens, h_q, h_kv, src=[3, 1, 4, 0, 2], dst=[3, 1, 4, 0, 2], slots=5, seed=20)
+    b = Case(lens, h_q, h_kv, src=[3, 1, 4, 0, 2], dst=[8, 6, 9, 5, 7], slots=10, seed=20)
+    b.states[:5] = a.states
+    b.prefill(mp)
+    start, x, side = a.states.clone(), torch.zeros(4096, 4096, dtype=torch.bfloat16, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        a.states.copy_(start)
+        a.out.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                x @ x
+        a.prefill(mp)
+        torch.cuda.synchronize()
+        assert torch.equal(a.states, b.states[5:]) and torch.equal(a.out, b.out)
+    a.states.copy_(start)
+    a.check(lambda: a.prefill(mp))
+
+
 @pytest.mark.parametrize("kind", ["prefill", "decode"])
 def test_strides_and_padding(mp, kind):
     """Tokens that are slices of wider rows, decays of a wider matrix; rows behind the last sequence hold NaN and stay."""
@@ -255,6 +280,21 @@ def test_far_offsets(mp):
     mp.linear_decode(q, k, v, c.g, states, _i32(far[:2]), _i32(far[2:]), a, q_tokens=70, scale=c.scale)
     mp.linear_decode(c.q, c.k, c.v, c.g, ref_states, _i32([0, 1]), _i32([2, 3]), b, q_tokens=70, scale=c.scale)
     assert torch.equal(a, b) and torch.equal(states[far[3]], ref_states[3])
+
+
+def test_widest_strides(mp):
+    """Tokens as far apart as a call may have them: more than 64 of them lie more than 2^32 bytes apart."""
+    if torch.cuda.get_device_properties(0).total_memory < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    h, lens = 128, [100, 50]
+    c = Case(lens, h, h, seed=21)
+    out, states = torch.empty_like(c.out), c.states.clone()
+    c.prefill(mp)
+    wide = torch.empty(sum(lens), (1 << 25) - 8, dtype=torch.bfloat16, device="cuda")
+    lay = lambda x, n: wide[:, n * h * D:(n + 1) * h * D].unflatten(1, (h, D)).copy_(x)   # noqa: E731
+    mp.linear_prefill(lay(c.q, 0), lay(c.k, 1), lay(c.v, 2), c.g, _i32(c.cu), states, _i32(c.src), _i32(c.dst), out, 100,
+                      workspace=c.workspace(mp), scale=c.scale)
+    assert torch.equal(out, c.out) and torch.equal(states, c.states)
 
 
 def test_graph(mp):

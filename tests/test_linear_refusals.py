@@ -34,6 +34,7 @@ BAD = [(dict(batch=0), INVALID), (dict(batch=65536), INVALID), (dict(h_q=7), INV
        (dict(flags=1), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
        (dict(num_states=-1), INVALID), (dict(q_stride=1016), INVALID), (dict(q_stride=1028), INVALID),
        (dict(k_stride=128), INVALID), (dict(v_stride=257), INVALID), (dict(k_stride=1 << 31), INVALID),
+       (dict(q_stride=1 << 25), INVALID), (dict(k_stride=1 << 25), INVALID), (dict(v_stride=1 << 25), INVALID), (dict(decay_stride=1 << 25), INVALID),
        (dict(decay_stride=1), INVALID), (dict(decay_stride=-1), INVALID), (dict(decay_stride=1 << 31), INVALID)] + \
     [({n: None}, INVALID) for n in POINTERS[1:]] + [({n: 0x1008}, INVALID) for n in ("q", "k", "v", "states", "out")]
 
@@ -55,7 +56,7 @@ def test_decode(mp, kw, status):   # noqa: F811
 def test_workspace(mp):   # noqa: F811
     a = _linear(mp, total_tokens=1000, max_seqlen=900)
     need = mp.linear_prefill_workspace_size(2, 1000, 900, 8, 2)
-    assert need > 0 and mp.linear_prefill_workspace_size(2, 10, 7, 8, 2) == 0
+    assert need > 0 and mp.linear_prefill_workspace_size(2, 10, 7, 2, 2) == 0
     for ws, size in ((None, need), (0x1000, need - 1), (0x1008, need)):
         assert mp.lib().mpfa_linear_prefill(C.byref(a), ws, size, None) == WORKSPACE
     out = C.c_size_t(0)
@@ -71,12 +72,21 @@ def test_workspace(mp):   # noqa: F811
     (1, 1, 1, 1, 1), (1, 64, 64, 256, 256), (1, 65, 65, 1, 1), (3, 1000, 700, 8, 2), (1, 65536, 65536, 32, 8), (512, 40000, 9000, 8, 8),
     (65535, 1 << 20, 1 << 20, 1, 1), (1, 1 << 28, 1 << 28, 8, 1)])
 def test_workspace_holds_every_segment(mp, batch, total, longest, h_q, h_kv):   # noqa: F811
-    """A state and a decay per segment and KV head, at least one segment per sequence; none for prompts of one segment."""
+    """A state and a decay per segment and KV head, at least one segment per sequence; none for prompts of one segment
+    whose heads one workgroup takes."""
     size = mp.linear_prefill_workspace_size(batch, total, longest, h_q, h_kv)
-    if longest <= 64:
+    if longest <= 64 and h_q == h_kv:
         assert size == 0
     if size:
-        assert size >= (batch + 1) * h_kv * (65536 + 4)
+        assert size >= batch * h_kv * (65536 + 4)
+
+
+@pytest.mark.parametrize("h_q,h_kv", [(2, 1), (40, 8), (256, 1)])
+def test_workspace_where_workgroups_share_a_state(mp, h_q, h_kv):   # noqa: F811
+    """Query heads that several workgroups take start from one state, which one of them replaces: it is read from a copy."""
+    assert mp.linear_prefill_workspace_size(1, 10, 10, h_q, h_kv) >= h_kv * (65536 + 4)
+    a = _linear(mp, batch=1, h_q=h_q, h_kv=h_kv, max_seqlen=10, q_stride=h_q * 128, k_stride=h_kv * 128, v_stride=h_kv * 128, decay_stride=0)
+    assert mp.lib().mpfa_linear_prefill(C.byref(a), None, 0, None) == WORKSPACE
 
 
 @pytest.mark.parametrize("kw,status", [
