@@ -697,7 +697,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
 // The states before the segments of a sequence: `sums` left, in the place of segment s + 1, the state that
 // segment s alone leaves (segment 0 with the sequence's first state).  A workgroup has 256 values of it; each of
 // its four waves reads up to eight segments at once, and adds to their sums what the segments before them left.
-constexpr int kJoinEach = 8;
+constexpr int kJoinEach = 4;
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
   constexpr int kBlocks = kLinState / 256;
   __shared__ f32x4 s_end[4][64];
