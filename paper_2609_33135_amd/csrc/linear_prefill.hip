@@ -62,7 +62,6 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
 // rows' same piece nor four rows' same four pieces (a transposing read) meet in a bank.
 typedef uint16_t LdsRows[kC][kD];
 __device__ __forceinline__ int piece_row(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
-__device__ __forceinline__ int piece(int row, int c) { return 8 * (c ^ piece_row(row)); }
 
 // What a chunk needs of its decays.
 struct Decays {
@@ -86,8 +85,8 @@ __device__ __forceinline__ void turn() { __builtin_amdgcn_sched_barrier(0); }
 
 // The thread, by a value of each use's own: what is worked out from it (LDS addresses above all) is not kept in
 // registers from one use to the next, of which there are not enough.
-__device__ __forceinline__ int thread_here() {
-  int thread = threadIdx.x;
+__device__ __forceinline__ uint32_t thread_here() {
+  uint32_t thread = threadIdx.x;
   asm volatile("" : "+v"(thread));
   return thread;
 }
@@ -150,43 +149,49 @@ __device__ __forceinline__ void split8(float* x, Frag* part) {
     for (int w = 0; w < 4; ++w) split2(x, part, i, w);
 }
 
-// Rows of a chunk, 16 lanes a row.  Rows from n (at least 1) on are row n - 1 again: nothing of them reaches an
-// output or the state, by the scores' mask and a decay of 0.
+// Rows of a chunk, 16 lanes a row; 0 from row n on.
 struct Rows {
-  static constexpr int kEach = kC * 16 / kThreads;
+  static constexpr int kEach = kC * 16 / kThreads, kStep = kThreads / 16;
   u32x4 w[kEach];
-  // stride: bytes between rows, of which 64 stay below 2^32; at: of the thread's first row
-  __device__ __forceinline__ void load(const uint16_t* x, uint32_t stride, uint32_t at, int n) {
-    asm volatile("" : "+v"(at));   // as for the thread above: offsets are not kept
-    const uint32_t last = (min(n, kC) - 1) * stride;
+  // stride: bytes between rows, of which 64 stay below 2^32; buffer loads check each row's offset by themselves
+  __device__ __forceinline__ void load(const uint16_t* x, uint32_t stride, int n) {
+    const uint32_t thread = thread_here();
+    uint32_t at = (thread / 16) * stride + 16 * (thread & 15);
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(x), 0, (min(n, kC) - 1) * stride + 256, 0x00027000);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-      w[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(x) +
-                                             (min(at + i * (kThreads / 16) * stride, last) + 16 * (threadIdx.x & 15)));
+    for (int i = 0; i < kEach; ++i, at += kStep * stride) w[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0);
   }
-  static __device__ __forceinline__ int row(int thread, int i) { return thread / 16 + kThreads / 16 * i; }
 };
+// A thread's piece of its first row in LDS; kStep rows on it lies in the same place.
+static_assert(Rows::kStep % 16 == 0, "see piece_row");
+__device__ __forceinline__ char* row_piece(LdsRows& rows, uint32_t thread, uint32_t c) {
+  const uint32_t row = thread / 16;
+  return reinterpret_cast<char*>(&rows) + 256 * row + 16 * (c ^ piece_row(row));
+}
 __device__ __forceinline__ void store_rows(const Rows& r, LdsRows& to) {
-  const int thread = thread_here();
+  const uint32_t thread = thread_here();
+  char* const at = row_piece(to, thread, thread & 15);
 #pragma unroll
-  for (int i = 0; i < Rows::kEach; ++i) {
-    const int row = Rows::row(thread, i);
-    *reinterpret_cast<u32x4*>(&to[row][piece(row, thread & 15)]) = r.w[i];
-  }
+  for (int i = 0; i < Rows::kEach; ++i) *reinterpret_cast<u32x4*>(at + 256 * Rows::kStep * i) = r.w[i];
 }
 // Queries of a head and later its outputs: of 16 channels those that a lane half takes side by side, 0-3 and 8-11 |
 // 4-7 and 12-15.  A thread's 16 bytes lie in two halves of pieces, for queries and outputs the same, so a thread
 // that has read its outputs may put queries in their place.
-__device__ __forceinline__ u32x2* head_slot(LdsRows& rows, int thread, int i, int x) {
-  const int row = Rows::row(thread, i), c = thread & 15;
-  return reinterpret_cast<u32x2*>(&rows[row][piece(row, (c & ~1) + x) + 4 * (c & 1)]);
-}
+struct HeadSlot {
+  char* at[2];
+  __device__ __forceinline__ HeadSlot(LdsRows& rows) {
+    const uint32_t thread = thread_here(), c = thread & 15;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) at[x] = row_piece(rows, thread, (c & ~1u) + x) + 8 * (c & 1);
+  }
+  __device__ __forceinline__ u32x2* operator()(int i, int x) const { return reinterpret_cast<u32x2*>(at[x] + 256 * Rows::kStep * i); }
+};
 __device__ __forceinline__ void store_queries(const Rows& r, LdsRows& to) {
-  const int thread = thread_here();
+  const HeadSlot slot(to);
 #pragma unroll
   for (int i = 0; i < Rows::kEach; ++i)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) *head_slot(to, thread, i, x) = (u32x2){r.w[i][2 * x], r.w[i][2 * x + 1]};
+    for (int x = 0; x < 2; ++x) *slot(i, x) = (u32x2){r.w[i][2 * x], r.w[i][2 * x + 1]};
 }
 
 // The value is in its registers here: loads of it have arrived.
@@ -499,21 +504,21 @@ __device__ __forceinline__ void put_outputs(const Outputs& out, LdsRows& rows) {
     }
 }
 __device__ __forceinline__ void read_outputs(Rows& r, LdsRows& rows) {
-  const int thread = thread_here();
+  const HeadSlot slot(rows);
 #pragma unroll
   for (int i = 0; i < Rows::kEach; ++i) {
-    const u32x2 a = *head_slot(rows, thread, i, 0), b = *head_slot(rows, thread, i, 1);
+    const u32x2 a = *slot(i, 0), b = *slot(i, 1);
     r.w[i] = (u32x4){a[0], a[1], b[0], b[1]};
   }
 }
 // Of n rows, a multiple of 256 bytes apart; buffer stores, which drop what lies behind the last row without a
 // branch: a wait for loads behind stores that are not always made would be one for these too.
 __device__ __forceinline__ void store_outputs(const Rows& r, uint16_t* to, int h_q, int n) {
-  const int thread = thread_here();
-  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(to, 0, (min(n, kC) - 1) * h_q * 256 + 256, 0x00027000);
+  const uint32_t thread = thread_here(), stride = 256 * h_q;
+  uint32_t at = (thread / 16) * stride + 16 * (thread & 15);
+  const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(to, 0, (min(n, kC) - 1) * stride + 256, 0x00027000);
 #pragma unroll
-  for (int i = 0; i < Rows::kEach; ++i)
-    __builtin_amdgcn_raw_buffer_store_b128(r.w[i], rsrc, Rows::row(thread, i) * h_q * 256 + 16 * (thread & 15), 0, 0);
+  for (int i = 0; i < Rows::kEach; ++i, at += Rows::kStep * stride) __builtin_amdgcn_raw_buffer_store_b128(r.w[i], rsrc, at, 0, 0);
 }
 
 // Item number to KV head and segment.  A KV head's rows are 256 bytes of each token: were the heads dealt to the
@@ -548,14 +553,14 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
   }
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
-  const uint32_t row = threadIdx.x / 16, kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, kat = row * kb, vat = row * vb;
+  const uint32_t kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride;
   struct {
     Rows k, v;
   } r[2];   // of the next chunk and the one after it
   auto load = [&](int x, int c) {   // behind the last chunk any rows will do
     const int at = c < g.n ? c : 0;
-    r[x].k.load(k0 + at * p.k_stride, kb, kat, g.n - at);
-    r[x].v.load(v0 + at * p.v_stride, vb, vat, g.n - at);
+    r[x].k.load(k0 + at * p.k_stride, kb, g.n - at);
+    r[x].v.load(v0 + at * p.v_stride, vb, g.n - at);
   };
   load(0, 0);
   load(1, kC);
@@ -613,14 +618,13 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
   const uint16_t* const q0 = p.q + g.t0 * p.q_stride;
-  const uint32_t row = threadIdx.x / 16, kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, kat = row * kb, vat = row * vb;
-  const uint32_t qb = 2 * (uint32_t)p.q_stride, qat = row * qb;
+  const uint32_t kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, qb = 2 * (uint32_t)p.q_stride;
   Rows rk, rv, rq;
   float decay = 0.0f;   // of the chunk after the next
   if (g.n > 0) {
-    rk.load(k0, kb, kat, g.n);
-    rv.load(v0, vb, vat, g.n);
-    rq.load(q0 + h0 * kD, qb, qat, g.n);
+    rk.load(k0, kb, g.n);
+    rv.load(v0, vb, g.n);
+    rq.load(q0 + h0 * kD, qb, g.n);
   }
   State st;
   state_zero(st);
@@ -653,17 +657,17 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
     }
     auto step = [&](auto first, auto final, int h) {
       const int from = decltype(final)::value ? next : c;
-      rq.load(q0 + from * p.q_stride + (decltype(final)::value ? h0 : h + 1) * kD, qb, qat, g.n - from);
+      rq.load(q0 + from * p.q_stride + (decltype(final)::value ? h0 : h + 1) * kD, qb, g.n - from);
       if (wave < 3) scores<decltype(first)::value, !decltype(final)::value>(s, d, wave, p.scale);
       Outputs out;
       from_state<decltype(first)::value>(out, st, parts, s, d);
       if (decltype(final)::value) {   // not before: the state's parts were in these registers
-        rk.load(k0 + next * p.k_stride, kb, kat, g.n - next);
+        rk.load(k0 + next * p.k_stride, kb, g.n - next);
       }
       __syncthreads();   // the scores are there, the queries used
       Update u;
       from_chunk<decltype(final)::value>(out, u, st, s, d);
-      if (decltype(final)::value) rv.load(v0 + next * p.v_stride, vb, vat, g.n - next);   // nor this: the scores were
+      if (decltype(final)::value) rv.load(v0 + next * p.v_stride, vb, g.n - next);   // nor this: the scores were
       put_outputs(out, s.q);
       if (decltype(final)::value && (rest > 0 || (last && part == 0))) u.add(st, s, d);
       __syncthreads();
