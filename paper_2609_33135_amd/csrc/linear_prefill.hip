@@ -314,8 +314,8 @@ struct Update {
   // The products, a step's parts beside those of the step before.
   __device__ __forceinline__ void add(State& st, const Keys& s, const Decays& d) {
     const int lane = lane_here(), at = columns_at(lane);
-    Frag k[2][4];
-    auto read_k = [&](int j, int m) { k[j & 1][m] = columns(s.k, at ^ 64 * m, 16 * j); };
+    Frag k[4];
+    auto read_k = [&](int j, int m) { k[m] = columns(s.k, at ^ 64 * m, 16 * j); };
 #pragma unroll
     for (int m = 0; m < 4; ++m) read_k(0, m);
 #pragma unroll
@@ -326,10 +326,10 @@ struct Update {
 #pragma unroll
       for (int n = 0; n < 12; ++n) {
         const int i = 2 - n / 4, m = n % 4;
-        st.a[m] = mfma32_bf16(k[j & 1][m].b, f[j & 1][i].b, st.a[m]);
+        st.a[m] = mfma32_bf16(k[m].b, f[j & 1][i].b, st.a[m]);
         if (j < 3) {
           split(j + 1, n / 4, n % 4);
-          if (n < 4) read_k(j + 1, n);
+          if (n >= 8) read_k(j + 1, m);   // the last product with it
         }
         if (j < 2 && n >= 10) read_to(d, lane >> 5, j + 2, n - 10);   // step j's decays are used up
         turn();
@@ -667,8 +667,11 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
       __syncthreads();   // the scores are there, the queries used
       Update u;
       from_chunk<decltype(final)::value>(out, u, st, s, d);
-      if (decltype(final)::value) rv.load(v0 + next * p.v_stride, vb, g.n - next);   // nor this: the scores were
       put_outputs(out, s.q);
+      if (decltype(final)::value) {
+        turn();
+        rv.load(v0 + next * p.v_stride, vb, g.n - next);   // nor this: the scores and outputs were
+      }
       if (decltype(final)::value && (rest > 0 || (last && part == 0))) u.add(st, s, d);
       __syncthreads();
       Rows ro;
