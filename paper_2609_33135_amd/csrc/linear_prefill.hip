@@ -62,6 +62,8 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
 // rows' same piece nor four rows' same four pieces (a transposing read) meet in a bank.
 typedef uint16_t LdsRows[kC][kD];
 __device__ __forceinline__ int piece_row(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
+// Of queries and outputs, whose half pieces of two rows that follow each other are written and read at once.
+__device__ __forceinline__ int query_row(int row) { return row & 15; }
 
 // What a chunk needs of its decays.
 struct Decays {
@@ -103,6 +105,7 @@ __device__ __forceinline__ T read_lds(const LdsRows& rows, int at) {
 
 // Offset of the lane's own row of 32 rows, in it the piece 0.
 __device__ __forceinline__ int row_at(int lane) { return 256 * (lane & 31) + 16 * piece_row(lane); }
+__device__ __forceinline__ int query_at(int lane) { return 256 * (lane & 31) + 16 * query_row(lane); }
 
 // Transposing reads: four tokens t .. t + 3, t = t0 + 4 * (lane / 32), of the lane's column c0 + lane % 32: each
 // group of 16 lanes reads a block of four rows and 16 columns.  columns_at: of t0 = c0 = 0.
@@ -162,15 +165,11 @@ struct Rows {
     for (int i = 0; i < kEach; ++i, at += kStep * stride) w[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0);
   }
 };
-// A thread's piece of its first row in LDS; kStep rows on it lies in the same place.
+// Pieces lie in the same place kStep rows on.
 static_assert(Rows::kStep % 16 == 0, "see piece_row");
-__device__ __forceinline__ char* row_piece(LdsRows& rows, uint32_t thread, uint32_t c) {
-  const uint32_t row = thread / 16;
-  return reinterpret_cast<char*>(&rows) + 256 * row + 16 * (c ^ piece_row(row));
-}
 __device__ __forceinline__ void store_rows(const Rows& r, LdsRows& to) {
   const uint32_t thread = thread_here();
-  char* const at = row_piece(to, thread, thread & 15);
+  char* const at = reinterpret_cast<char*>(&to) + 256 * (thread / 16) + 16 * ((thread & 15) ^ piece_row(thread / 16));
 #pragma unroll
   for (int i = 0; i < Rows::kEach; ++i) *reinterpret_cast<u32x4*>(at + 256 * Rows::kStep * i) = r.w[i];
 }
@@ -182,7 +181,7 @@ struct HeadSlot {
   __device__ __forceinline__ HeadSlot(LdsRows& rows) {
     const uint32_t thread = thread_here(), c = thread & 15;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) at[x] = row_piece(rows, thread, (c & ~1u) + x) + 8 * (c & 1);
+    for (int x = 0; x < 2; ++x) at[x] = reinterpret_cast<char*>(&rows) + 256 * (thread / 16) + 16 * (((c & ~1u) + x) ^ query_row(thread / 16)) + 8 * (c & 1);
   }
   __device__ __forceinline__ u32x2* operator()(int i, int x) const { return reinterpret_cast<u32x2*>(at[x] + 256 * Rows::kStep * i); }
 };
@@ -349,7 +348,7 @@ template <bool kFirst, bool kMore>
 __device__ __forceinline__ void scores(Lds& s, const Decays& d, int b, float scale) {
   const int lane = lane_here(), half = lane >> 5;
   const Block at = block_of(__builtin_amdgcn_readfirstlane(b));
-  const int ka = (row_at(lane) ^ 16 * half) + 256 * at.j, qa = row_at(lane) + 8 * half + 256 * at.i;
+  const int ka = (row_at(lane) ^ 16 * half) + 256 * at.j, qa = query_at(lane) + 8 * half + 256 * at.i;
   const int i = at.i + (lane & 31), j0 = at.j + 4 * half;
   Frag a[4], q[4];
   f32x4 jh[2], jl[2], decay[4];
@@ -420,7 +419,7 @@ struct Parts {
 // o = scale exp(b_i) S^T q_i.  kFirst: the chunk's first head makes the state's parts.
 template <bool kFirst>
 __device__ __forceinline__ void from_state(Outputs& to, const State& st, Parts& parts, const Lds& s, const Decays& d) {
-  const int lane = lane_here(), qa = row_at(lane) ^ 16 * (lane >> 5);
+  const int lane = lane_here(), qa = query_at(lane) ^ 16 * (lane >> 5);
   Frag q[2][2];
   float y[8];
   auto read = [&](int g, int i) { q[g & 1][i].w = read_lds<u32x4>(s.q, (qa ^ 32 * g) + 256 * 32 * i); };
@@ -492,7 +491,7 @@ __device__ __forceinline__ void from_chunk(Outputs& to, Update& u, State& st, co
 
 // Outputs to the place of the queries, from there whole rows to memory.
 __device__ __forceinline__ void put_outputs(const Outputs& out, LdsRows& rows) {
-  const int lane = lane_here(), at = row_at(lane) ^ (64 * wave_here() + 16 * (lane >> 5));
+  const int lane = lane_here(), at = query_at(lane) ^ (64 * wave_here() + 16 * (lane >> 5));
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
