@@ -17,6 +17,8 @@ constexpr int kRows = 256 / kLanes;    // rows at a time
 constexpr int kEach = kD / kRows;      // a thread's, one after the other
 static_assert(kEach == 4, "one vector of k, of q");
 constexpr int kPairs = 16;             // rows of queries (token and head) between two barriers
+constexpr int kStaged = 20;            // and with their keys: what leaves LDS for eight workgroups a unit
+constexpr int kTokens = kStaged / 2;   // at most
 
 // Eight BF16 as FP32.
 __device__ __forceinline__ void widen(const u32x4& w, float* to) {
@@ -44,12 +46,13 @@ __device__ __forceinline__ float rows_sum(const f32x4& x) {
 
 // One workgroup per (sequence, KV head, kCols columns of the state).
 __global__ __launch_bounds__(256) void linear_decode_kernel(LinearParams p) {
-  __shared__ float s_k[kPairs][kD], s_q[kPairs][kD], s_v[kPairs][kCols], s_a[kPairs];
+  __shared__ float s_row[kStaged][kD], s_v[kTokens][kCols], s_a[kTokens];   // queries, then keys
   __shared__ float s_sum[4][kPairs][kCols];
   constexpr int kParts = kD / kCols;
   const int part = blockIdx.x % kParts, hk = blockIdx.x / kParts % p.h_kv, b = blockIdx.x / kParts / p.h_kv;
   const int tid = threadIdx.x, c = tid % kLanes, row = tid / kLanes, lane = tid & 63, wave = tid >> 6;
-  const int grp = p.h_q / p.h_kv, heads = min(grp, kPairs), tokens = kPairs / heads;
+  const int grp = p.h_q / p.h_kv, heads = min(grp, kPairs), tokens = min(kPairs / heads, kStaged / (heads + 1));
+  float (*const s_k)[kD] = &s_row[tokens * heads];
   const int64_t t0 = (int64_t)b * p.q_tokens;
   const int src = p.state_src[b], dst = p.state_dst[b];
   f32x4 st[kEach];
@@ -70,7 +73,7 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearParams p) {
         const int i = tid >> 4, at = 8 * (tid & 15);
         if (i < nr * nh) {
           const uint16_t* q = p.q + (t0 + r0 + i / nh) * p.q_stride + (hk * grp + h0 + i % nh) * kD;
-          widen(*reinterpret_cast<const u32x4*>(q + at), &s_q[i][at]);
+          widen(*reinterpret_cast<const u32x4*>(q + at), &s_row[i][at]);
         }
         if (h0 == 0 && i < nr) {
           const int64_t t = t0 + r0 + i;
@@ -88,7 +91,7 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearParams p) {
           for (int i = 0; i < kEach; ++i) st[i] = st[i] * a + v * k[i];
         }
         for (int h = 0; h < nh; ++h) {
-          const f32x4 q = *reinterpret_cast<const f32x4*>(&s_q[r * nh + h][kEach * row]);
+          const f32x4 q = *reinterpret_cast<const f32x4*>(&s_row[r * nh + h][kEach * row]);
           f32x4 o = st[0] * q[0];
 #pragma unroll
           for (int i = 1; i < kEach; ++i) o += st[i] * q[i];
@@ -108,10 +111,10 @@ __global__ __launch_bounds__(256) void linear_decode_kernel(LinearParams p) {
       }
     }
   }
-  if (dst >= 0) {
+  if (dst >= 0) {   // read again a step of the whole model later: streamed past the cache
     float* to = p.states + ((int64_t)dst * p.h_kv + hk) * kLinState + part * kCols + 4 * c;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) *reinterpret_cast<f32x4*>(to + (kEach * row + i) * kD) = st[i];
+    for (int i = 0; i < kEach; ++i) __builtin_nontemporal_store(st[i], reinterpret_cast<f32x4*>(to + (kEach * row + i) * kD));
   }
 }
 
