@@ -36,13 +36,20 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 mpfa_status done(hipError_t e) { return e == hipSuccess ? MPFA_OK : MPFA_ERR_HIP; }
 
-// Tokens per segment, in whole chunks: as many items as there are units, from segments of 1024 tokens on two a
-// unit.  Two at once on a unit take 1.1 to 1.3 times less than one after the other, but every segment's states
-// are written and read twice, 256 KB, which is what the rows of some hundred tokens are.  us: 4096 tokens of 8:8
-// heads 36 by 256 items, 45 by 512; 8192 of 32:32 130 and 131; 65536 of 32:8 482 and 440.
-int segment_tokens(int64_t total_tokens, int h_kv) {
+// Tokens per segment, in whole chunks: as many items as there are units, or, with longer segments, two a unit.  Two
+// at once on a unit take less than one after the other, but every segment's states are written and read twice, 256
+// KB, which is what the rows of some hundred tokens are.  Where three or more query heads share a KV head, one item
+// a unit has its heads in two parts (below), each of which takes the state through the whole segment.  By chunks of
+// the longer segments, us with one and with two items a unit:
+//   one head per KV head   8: 75, 82 (16384 tokens of 8:8)   16: 117, 120 (8192 of 32:32)   32: 228, 221
+//   two                    8: 89, 96                          16: 158, 157
+//   three and four         2: 50, 53 (4096 of 32:8)  4: 81, 77  8: 142, 124  32: 520, 415 (65536)
+//   eight                  2: 66, 71 (16384 of 16:2) 4: 111, 108  8: 205, 188
+//   sixteen                2: 99, 119 (32768 of 16:1) 4: 176, 195  8: 335, 331
+int segment_tokens(int64_t total_tokens, int h_q, int h_kv) {
+  const int grp = h_q / h_kv, least = grp < 3 ? 17 : std::max(4, grp / 2);
   auto chunks = [&](int64_t items) { return (total_tokens * h_kv + items * mpfa::kLinChunk - 1) / (items * mpfa::kLinChunk); };
-  const int64_t n = chunks(kUnits) > 16 ? chunks(2 * kUnits) : chunks(kUnits);
+  const int64_t n = chunks(kUnits) >= least ? chunks(2 * kUnits) : chunks(kUnits);
   return (int)std::max<int64_t>(1, n) * mpfa::kLinChunk;
 }
 
@@ -94,11 +101,11 @@ struct PrefillSpace {
 };
 PrefillSpace prefill_space(int batch, int total_tokens, int max_seqlen, int h_q, int h_kv) {
   PrefillSpace s;
-  s.segment = segment_tokens(total_tokens, h_kv);
+  s.segment = segment_tokens(total_tokens, h_q, h_kv);
   s.split = std::min(max_seqlen, total_tokens) > s.segment;
   s.items = mpfa::linear_segments(batch, total_tokens, s.segment) * h_kv;
   // few items: a KV head's query heads apart, as long as two items a unit hold them (16384 tokens of 16:1 heads 70 us
-  // with all 16 together, 63 by eight)
+  // with all 16 together, 66 by eight; 777 of 32:8 26.3 with four together, 22.9 one by one)
   const int grp = h_q / h_kv;
   s.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, (s.items * grp + 2 * kUnits - 1) / (2 * kUnits)));
   s.parts = (grp + s.heads - 1) / s.heads;
@@ -182,6 +189,11 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   p.split = s.split;
   p.parts = s.parts;
   p.heads = s.heads;
+  // what the longest sequence has to join, in one turn if four waves can; with one or two KV heads there are few
+  // workgroups and long sequences (32768 tokens of 16:1 heads 102 us by four waves, 99 by sixteen; 4096 of 32:8 49.3
+  // by four, 49.9 by eight)
+  const int64_t places = std::min(a->max_seqlen, a->total_tokens) / s.segment;
+  p.join_waves = (int)std::max<int64_t>(1, std::min<int64_t>((places + mpfa::kLinJoin - 1) / mpfa::kLinJoin, std::max(4, mpfa::kLinJoinWaves / a->h_kv)));
   p.starts = s.bytes ? static_cast<float*>(workspace) : nullptr;
   p.decays = s.bytes ? p.starts + s.starts / sizeof(float) : nullptr;
 #ifdef MPFA_DEBUG_CHECKS

@@ -9,6 +9,8 @@ namespace mpfa {
 
 constexpr int kLinChunk = 64;                  // tokens of a chunk
 constexpr int kLinState = 128 * 128;           // floats of a state
+constexpr int kLinJoin = 4;                    // places that a wave of `join` has at once
+constexpr int kLinJoinWaves = 16;              // at most
 constexpr float kLinLeastDecay = -200.0f;      // exp of it times any FP32 number is 0
 
 struct LinearParams {
@@ -17,6 +19,7 @@ struct LinearParams {
   int segment;                   // prefill: tokens per segment, a multiple of kLinChunk
   int split;                     // prefill: some sequence may have several segments
   int parts, heads;              // prefill: parts of a KV head's query heads, of so many each
+  int join_waves;                // prefill: waves of a workgroup that joins states
   float scale;
   int64_t q_stride, k_stride, v_stride, decay_stride;
   const int32_t* cu_seqlens;     // prefill

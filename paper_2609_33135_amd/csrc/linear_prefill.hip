@@ -545,14 +545,6 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
   const bool last = g.s == g.count - 1;
   if (last && (g.s > 0 || p.parts == 1)) return;
   float* const slot = p.starts + ((int64_t)id * p.h_kv + hk) * kLinState;
-  State st;
-  state_zero(st);
-  if (g.s == 0) {
-    const int src = p.state_src[g.b];
-    if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
-    raw_store(st, slot);
-    if (last) return;
-  }
   const uint16_t* const k0 = p.k + g.t0 * p.k_stride + hk * kD;
   const uint16_t* const v0 = p.v + g.t0 * p.v_stride + hk * kD;
   const uint32_t kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride;
@@ -564,14 +556,25 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
     r[x].k.load(k0 + at * p.k_stride, kb, g.n - at);
     r[x].v.load(v0 + at * p.v_stride, vb, g.n - at);
   };
-  load(0, 0);
-  load(1, kC);
-  float decay = 0.0f;   // of the chunk after the next
+  float now = 0.0f, decay = 0.0f;   // of this chunk and the next
   double total = 0.0;
-  if (wave == 3) {
-    total = put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, 1.0f);
-    decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
+  if (!last) {
+    load(0, 0);
+    load(1, kC);
+    if (wave == 3) {
+      now = load_decays(p, g.t0, g.n, hk);
+      decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
+    }
   }
+  State st;
+  state_zero(st);
+  if (g.s == 0) {
+    const int src = p.state_src[g.b];
+    if (src >= 0) state_load(st, p.states + ((int64_t)src * p.h_kv + hk) * kLinState);
+    raw_store(st, slot);
+    if (last) return;
+  }
+  if (wave == 3) total = put_decays(s.d[0], now, g.n, 1.0f);
   auto chunk = [&](int x, int c) {
     const int rest = g.n - c - kC;
     store_rows(r[x].k, s.k);
@@ -622,8 +625,12 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
   const uint16_t* const q0 = p.q + g.t0 * p.q_stride;
   const uint32_t kb = 2 * (uint32_t)p.k_stride, vb = 2 * (uint32_t)p.v_stride, qb = 2 * (uint32_t)p.q_stride;
   Rows rk, rv, rq;
-  float decay = 0.0f;   // of the chunk after the next
+  float now = 0.0f, decay = 0.0f;   // log decays of this chunk and the next
   if (g.n > 0) {
+    if (wave == 3) {
+      now = load_decays(p, g.t0, g.n, hk);
+      decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
+    }
     rk.load(k0, kb, g.n);
     rv.load(v0, vb, g.n);
     rq.load(q0 + h0 * kD, qb, g.n);
@@ -639,10 +646,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
 #pragma unroll
   for (int m = 0; m < 4; ++m) keep(st.a[m]);   // else the first use in the loop waits, in every chunk, for all loads before it
   if (g.n > 0) {
-    if (wave == 3) {
-      put_decays(s.d[0], load_decays(p, g.t0, g.n, hk), g.n, p.scale);
-      decay = load_decays(p, g.t0 + kC, g.n - kC, hk);
-    }
+    if (wave == 3) put_decays(s.d[0], now, g.n, p.scale);
     store_rows(rk, s.k);
     store_rows(rv, s.v);
     store_queries(rq, s.q);
@@ -705,13 +709,12 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
 
 // The states before the segments of a sequence: `sums` left, in the place of segment s + 1, the state that
 // segment s alone leaves (segment 0 with the sequence's first state).  A workgroup has 256 values of it; each of
-// its four waves reads up to eight segments at once, and adds to their sums what the segments before them left.
-constexpr int kJoinEach = 4;
-__global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
+// its waves reads up to kLinJoin places at once, and adds to their sums what the segments before them left.
+__global__ __launch_bounds__(64 * kLinJoinWaves) void linear_join_kernel(LinearParams p) {
   constexpr int kBlocks = kLinState / 256;
-  __shared__ f32x4 s_end[4][64];
-  __shared__ float s_decay[4];
-  const int part = blockIdx.x % kBlocks, hk = blockIdx.x / kBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ f32x4 s_end[kLinJoinWaves][64];
+  __shared__ float s_decay[kLinJoinWaves];
+  const int part = blockIdx.x % kBlocks, hk = blockIdx.x / kBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int64_t step = (int64_t)p.h_kv * (kLinState / 4);
   for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
     const int begin = p.cu_seqlens[b], id = begin / p.segment + b + 1;   // of segment 1
@@ -720,12 +723,12 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
     f32x4* const at = reinterpret_cast<f32x4*>(p.starts + ((int64_t)id * p.h_kv + hk) * kLinState) + part * 64 + lane;
     const float* const decay = p.decays + (int64_t)id * p.h_kv + hk;
     f32x4 carry = *at;
-    for (int base = 1; base <= last; base += 4 * kJoinEach) {
-      const int first = base + wave * kJoinEach;
-      f32x4 x[kJoinEach];
-      float a[kJoinEach];
+    for (int base = 1; base <= last; base += waves * kLinJoin) {
+      const int first = base + wave * kLinJoin;
+      f32x4 x[kLinJoin];
+      float a[kLinJoin];
 #pragma unroll
-      for (int i = 0; i < kJoinEach; ++i) {
+      for (int i = 0; i < kLinJoin; ++i) {
         x[i] = (f32x4){0.0f, 0.0f, 0.0f, 0.0f};
         a[i] = 1.0f;
         if (first + i <= last) {
@@ -734,23 +737,22 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
         }
       }
 #pragma unroll
-      for (int i = 1; i < kJoinEach; ++i) {
+      for (int i = 1; i < kLinJoin; ++i) {
         x[i] += x[i - 1] * a[i];
         a[i] *= a[i - 1];
       }
       __syncthreads();
       // behind the last place the decays are 1 and the sums 0: the wave's end is its last place's
-      s_end[wave][lane] = x[kJoinEach - 1];
-      if (lane == 0) s_decay[wave] = a[kJoinEach - 1];
+      s_end[wave][lane] = x[kLinJoin - 1];
+      if (lane == 0) s_decay[wave] = a[kLinJoin - 1];
       __syncthreads();
       f32x4 before = carry;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
+      for (int w = 0; w < waves; ++w) {
         if (w == wave) before = carry;
         carry = carry * s_decay[w] + s_end[w][lane];
       }
 #pragma unroll
-      for (int i = 0; i < kJoinEach; ++i)
+      for (int i = 0; i < kLinJoin; ++i)
         if (first + i <= last) at[(first + i) * step] = x[i] + before * a[i];
     }
   }
@@ -763,7 +765,7 @@ hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream) {
   const int items = (int)(segments * p.h_kv), eighths = (items + 7) / 8 * 8;
   if (p.split || p.parts > 1) linear_sums_kernel<<<dim3(items), dim3(kThreads), 0, stream>>>(p);
   if (p.split) {
-    linear_join_kernel<<<dim3(kLinState / 256 * p.h_kv, std::min(p.batch, 64)), dim3(256), 0, stream>>>(p);
+    linear_join_kernel<<<dim3(kLinState / 256 * p.h_kv, std::min(p.batch, 64)), dim3(64 * p.join_waves), 0, stream>>>(p);
   }
   linear_outputs_kernel<<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(kThreads), 0, stream>>>(p, items);
   return hipGetLastError();
