@@ -646,7 +646,8 @@ mpfa_status mpfa_linear_decode(const mpfa_linear_args* args, mpfa_stream_t strea
  * group, scale = m / (448 sqrt(mean(r^2) + eps)), and 1 where m is 0, and
  *   code = E4M3_RNE(448 (r * weight) / m)
  * of the exact quotient, so that codes do not depend on any order of sums.
- * Sums are FP32: |r| and |r * weight| from about 2^63 on are outside the contract.
+ * Sums are FP32: |r| and |r * weight| from about 2^63 on are outside the contract,
+ * and so are codes of a group whose m is below 2^-100 but not 0.
  * Rows do not affect each other; one with a NaN or an infinity gets NaN outputs
  * or scales somewhere.
  * x_stride: elements between rows of x (a multiple of 8, below 2^31); residual, residual_out
