@@ -36,21 +36,67 @@ size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 mpfa_status done(hipError_t e) { return e == hipSuccess ? MPFA_OK : MPFA_ERR_HIP; }
 
-// Tokens per segment, in whole chunks: as many items as there are units, or, with longer segments, two a unit.  Two
-// at once on a unit take less than one after the other, but every segment's states are written and read twice, 256
-// KB, which is what the rows of some hundred tokens are.  Where three or more query heads share a KV head, one item
-// a unit has its heads in two parts (below), each of which takes the state through the whole segment.  By chunks of
-// the longer segments, us with one and with two items a unit:
-//   one head per KV head   8: 75, 82 (16384 tokens of 8:8)   16: 117, 120 (8192 of 32:32)   32: 228, 221
-//   two                    8: 89, 96                          16: 158, 157
-//   three and four         2: 50, 53 (4096 of 32:8)  4: 81, 77  8: 142, 124  32: 520, 415 (65536)
-//   eight                  2: 66, 71 (16384 of 16:2) 4: 111, 108  8: 205, 188
-//   sixteen                2: 99, 119 (32768 of 16:1) 4: 176, 195  8: 335, 331
-int segment_tokens(int64_t total_tokens, int h_q, int h_kv) {
-  const int grp = h_q / h_kv, least = grp < 3 ? 17 : std::max(4, grp / 2);
-  auto chunks = [&](int64_t items) { return (total_tokens * h_kv + items * mpfa::kLinChunk - 1) / (items * mpfa::kLinChunk); };
-  const int64_t n = chunks(kUnits) >= least ? chunks(2 * kUnits) : chunks(kUnits);
-  return (int)std::max<int64_t>(1, n) * mpfa::kLinChunk;
+// How prompts are cut.  Into as many segments (times KV heads: items) as there are units, or, where these get long,
+// two a unit: two at once on a unit take less than one after the other, but every segment's states are written and
+// read twice, 256 KB, which is what the rows of some hundred tokens are.  us with one and with two items a unit, by
+// the chunks of the longer segments:
+//   one head per KV head   8: 75, 82 (16384 tokens of 8:8)   16: 125, 124   24: 174, 174   32: 228, 221 (16384 of 32:32)
+//   two                    8: 89, 100                         16: 167, 159
+//   four                   2: 46, 52 (4096 of 32:8)   4: 71, 76   8: 130, 126   16: 238, 227   32: 474, 424
+//   eight                  4: 106, 110 (32768 of 16:2)   8: 201, 196
+//   sixteen                4: 178, 192 (65536 of 16:1)   8: 327, 335
+// Then the query heads of a KV head go in parts to workgroups of their own, where that fills the card better; each
+// part takes the state through the segment for itself.
+struct Cut {
+  int chunks, parts, heads;   // of a segment; of a KV head's query heads; of a part
+  int64_t items;              // at most
+};
+// What a chunk takes, in heads' times: its keys and the state's update once, every head; and more beside another
+// workgroup of the unit.  us measured: 777 tokens of 32:8 heads, 104 items, 27.4 with four heads together, 24.8 with
+// two, 25.6 one by one; 8192 (256) 71, 73, 88; 16384 of 16:1 in 128 items 87, 59 by eight, 56 by four, 64 by two; 5000
+// of 10:2 (158) 33.9, 33.9 by three, 31.8 by two.
+double time_of(int heads, int64_t workgroups) {
+  const double busy = (double)(workgroups - kUnits) / kUnits;
+  return (1.33 + heads) * (busy <= 0.0 ? 1.0 : 1.25 + 0.37 * busy);
+}
+Cut cut_of(int batch, int64_t total_tokens, int max_seqlen, int h_q, int h_kv) {
+  const int grp = h_q / h_kv;
+  const int64_t longest = std::min<int64_t>(max_seqlen, total_tokens);
+  // segments of n chunks: at most, and as many as sequences of any lengths are cut into on average
+  auto ends = [&](int64_t n) { return batch * std::max<int64_t>(1, (longest + n * mpfa::kLinChunk - 1) / (n * mpfa::kLinChunk)); };
+  auto some = [&](int64_t n) {
+    const int64_t spread = (total_tokens + n * mpfa::kLinChunk - 1) / (n * mpfa::kLinChunk) + (batch - 1) / 2;
+    return std::max<int64_t>(batch, std::min(spread, ends(n)));
+  };
+  auto chunks = [&](int64_t items) {
+    const int64_t least = std::max<int64_t>(1, (total_tokens * h_kv + items * mpfa::kLinChunk - 1) / (items * mpfa::kLinChunk));
+    if ((int64_t)batch * h_kv <= items)
+      for (int64_t n = least; n <= 2 * least; ++n)
+        if (some(n) * h_kv <= items) return n;
+    return least;   // sequences fill the card by themselves
+  };
+  Cut c;
+  int64_t n = chunks(kUnits);
+  if (n >= std::max(8, 24 / grp)) n = chunks(2 * kUnits);
+  const int64_t items = some(n) * h_kv;
+  c.chunks = (int)n;
+  c.heads = grp;
+  c.parts = 1;
+  const double copy = longest > n * mpfa::kLinChunk ? 0.0 : 2.0 / n;   // a launch that only parts need
+  double best = time_of(grp, items);
+  for (int64_t parts = 2; parts <= grp && parts * items <= 2 * kUnits; ++parts) {
+    const int heads = (grp + (int)parts - 1) / (int)parts;
+    const double time = time_of(heads, (grp + heads - 1) / heads * items) + copy;
+    if (time < best) {
+      best = time;
+      c.heads = heads;
+      c.parts = (grp + heads - 1) / heads;
+    }
+  }
+  // without gaps in the numbers the longest sequence bounds them too
+  const int64_t numbers = mpfa::linear_segments(batch, total_tokens, n * mpfa::kLinChunk);
+  c.items = (batch <= mpfa::kLinDense ? std::min(numbers, ends(n)) : numbers) * h_kv;
+  return c;
 }
 
 // What both calls check; fills what does not depend on the kind.
@@ -91,8 +137,7 @@ mpfa_status linear_params(const mpfa_linear_args* a, bool decode, mpfa::LinearPa
   return MPFA_OK;
 }
 
-// A prefill's segments, the parts of a KV head's query heads that go apart, and the two tables in the workspace:
-// states before segments, then decays.
+// A prefill's cut and the two tables in its workspace: states before segments, then decays.
 struct PrefillSpace {
   int segment, parts, heads;
   bool split;
@@ -100,17 +145,16 @@ struct PrefillSpace {
   size_t starts, bytes;
 };
 PrefillSpace prefill_space(int batch, int total_tokens, int max_seqlen, int h_q, int h_kv) {
+  const Cut cut = cut_of(batch, total_tokens, max_seqlen, h_q, h_kv);
   PrefillSpace s;
-  s.segment = segment_tokens(total_tokens, h_q, h_kv);
+  s.segment = cut.chunks * mpfa::kLinChunk;
+  s.parts = cut.parts;
+  s.heads = cut.heads;
+  s.items = cut.items;
   s.split = std::min(max_seqlen, total_tokens) > s.segment;
-  s.items = mpfa::linear_segments(batch, total_tokens, s.segment) * h_kv;
-  // few items: a KV head's query heads apart, as long as two items a unit hold them (16384 tokens of 16:1 heads 70 us
-  // with all 16 together, 66 by eight; 777 of 32:8 26.3 with four together, 22.9 one by one)
-  const int grp = h_q / h_kv;
-  s.heads = (int)std::max<int64_t>(1, std::min<int64_t>(grp, (s.items * grp + 2 * kUnits - 1) / (2 * kUnits)));
-  s.parts = (grp + s.heads - 1) / s.heads;
-  s.starts = align256((size_t)s.items * mpfa::kLinState * sizeof(float));
-  s.bytes = s.split || s.parts > 1 ? s.starts + (size_t)s.items * sizeof(float) : 0;
+  const int64_t places = mpfa::linear_segments(batch, total_tokens, s.segment) * h_kv;
+  s.starts = align256((size_t)places * mpfa::kLinState * sizeof(float));
+  s.bytes = s.split || s.parts > 1 ? s.starts + (size_t)places * sizeof(float) : 0;
   return s;
 }
 
@@ -189,6 +233,7 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   p.split = s.split;
   p.parts = s.parts;
   p.heads = s.heads;
+  p.items = (int)s.items;
   // what the longest sequence has to join, in one turn if four waves can; with one or two KV heads there are few
   // workgroups and long sequences (32768 tokens of 16:1 heads 102 us by four waves, 99 by sixteen; 4096 of 32:8 49.3
   // by four, 49.9 by eight)

@@ -19,6 +19,7 @@ struct LinearParams {
   int segment;                   // prefill: tokens per segment, a multiple of kLinChunk
   int split;                     // prefill: some sequence may have several segments
   int parts, heads;              // prefill: parts of a KV head's query heads, of so many each
+  int items;                     // prefill: workgroups, a segment and KV head each
   int join_waves;                // prefill: waves of a workgroup that joins states
   float scale;
   int64_t q_stride, k_stride, v_stride, decay_stride;
@@ -35,8 +36,8 @@ struct LinearParams {
   float* decays;                 // prefill: [segment id][h_kv]
 };
 
-// Segments are numbered over the batch, those of sequence b from cu_seqlens[b] / segment + b on:
-// ceil(n / segment) of them end at or before the next sequence's first.
+// Numbers of segments that a batch may have, see linear_prefill.hip.
+constexpr int kLinDense = 64;                  // sequences whose segments are numbered without gaps
 inline int64_t linear_segments(int64_t batch, int64_t total_tokens, int64_t segment) { return total_tokens / segment + batch; }
 
 struct NormParams {

@@ -46,21 +46,71 @@ struct Segment {
   int n;                  // tokens
 };
 
-// Segment number id: the last sequence whose first number is at most id, by 64-ary search.
+__device__ __forceinline__ int count_of(const LinearParams& p, int len) { return p.split ? max(1, (len + p.segment - 1) / p.segment) : 1; }
+
+// Sums over the lanes up to each: from 1, 2, 4, 8 lanes before in a row of 16, then the last lane of a row to the next
+// row (rows 1 and 3), then lane 31 to rows 2 and 3.
+template <int kControl, int kRows>
+__device__ __forceinline__ int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, kControl, kRows, 0xF, false); }
+template <int kControl, int kRows>
+__device__ __forceinline__ double moved(double x) {   // lanes without a source get 0
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)moved<kControl, kRows>((int)(u >> 32)) << 32 | (uint32_t)moved<kControl, kRows>((int)u));
+}
+template <typename T>
+__device__ __forceinline__ T sums_to(T x) {
+  x += moved<0x111, 0xF>(x);
+  x += moved<0x112, 0xF>(x);
+  x += moved<0x114, 0xF>(x);
+  x += moved<0x118, 0xF>(x);
+  x += moved<0x142, 0xA>(x);
+  x += moved<0x143, 0xC>(x);
+  return x;
+}
+
+// Segments are numbered over the batch.  Up to 64 sequences: without a gap, so that the workgroups that have work are
+// the first ones and lie evenly over the units (eight prompts of 1000 tokens 92 -> 70 us); lane b has the first number
+// of sequence b.
+__device__ __forceinline__ int first_dense(const LinearParams& p, int* begin, int* count) {
+  const int lane = threadIdx.x & 63;
+  *begin = *count = 0;
+  if (lane < p.batch) {
+    *begin = p.cu_seqlens[lane];
+    *count = count_of(p, p.cu_seqlens[lane + 1] - *begin);
+  }
+  return sums_to(*count) - *count;
+}
+// More: those of sequence b from cu_seqlens[b] / segment + b on, of which ceil(len / segment) lie before the next one's.
+__device__ __forceinline__ int first_spread(const LinearParams& p, int begin, int b) { return begin / p.segment + b; }
+
+// Segment number id.
 __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segment* g) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, n = p.batch;
-  while (n > 1) {
-    const int step = (n + 63) >> 6, at = lane * step;
-    const bool before = at < n && p.cu_seqlens[lo + min(at, n - 1)] / p.segment + lo + at <= id;
-    const int last = __popcll(__builtin_amdgcn_ballot_w64(before)) - 1;
-    lo += last * step;
-    n = min(step, n - last * step);
+  int first;
+  if (p.batch == 1) {
+    g->b = first = 0;
+  } else if (p.batch <= kLinDense) {
+    int begin, count;
+    const int mine = first_dense(p, &begin, &count);
+    const uint64_t at = __builtin_amdgcn_ballot_w64(mine <= id && id < mine + count);
+    if (at == 0) return false;
+    g->b = __builtin_ctzll(at);
+    first = __builtin_amdgcn_readlane(mine, g->b);
+  } else {   // the last sequence whose first number is at most id, by 64-ary search
+    int lo = 0, n = p.batch;
+    while (n > 1) {
+      const int step = (n + 63) >> 6, at = lane * step;
+      const bool before = at < n && first_spread(p, p.cu_seqlens[lo + min(at, n - 1)], lo + at) <= id;
+      const int last = __popcll(__builtin_amdgcn_ballot_w64(before)) - 1;
+      lo += last * step;
+      n = min(step, n - last * step);
+    }
+    g->b = lo;
+    first = first_spread(p, p.cu_seqlens[lo], lo);
   }
-  const int begin = p.cu_seqlens[lo], len = p.cu_seqlens[lo + 1] - begin;
-  g->b = lo;
-  g->s = id - (begin / p.segment + lo);
-  g->count = p.split ? max(1, (len + p.segment - 1) / p.segment) : 1;
+  const int begin = p.cu_seqlens[g->b], len = p.cu_seqlens[g->b + 1] - begin;
+  g->s = id - first;
+  g->count = count_of(p, len);
   g->t0 = (int64_t)begin + (int64_t)g->s * p.segment;
   g->n = min(p.segment, len - g->s * p.segment);
   return g->s < g->count;
@@ -255,25 +305,11 @@ __device__ __forceinline__ float load_decays(const LinearParams& p, int64_t t, i
   return lane < n ? p.log_decay[(t + lane) * p.decay_stride + hk] : 0.0f;
 }
 
-template <int kControl, int kRows>
-__device__ __forceinline__ double moved(double x) {   // lanes without a source get 0
-  const uint64_t u = __builtin_bit_cast(uint64_t, x);
-  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, kControl, kRows, 0xF, false);
-  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), kControl, kRows, 0xF, false);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
 // What a chunk of n tokens needs of its decays g; returns log2 of the whole chunk's.  Summed in 64 bits: after a token that
 // clears the state sums are large and their differences small.
 __device__ __forceinline__ double put_decays(Decays& d, float g, int n, float scale) {
   const int lane = lane_here();
-  double x = (double)fminf(fmaxf(g, kLinLeastDecay), 0.0f) * kLog2e;
-  x += moved<0x111, 0xF>(x);   // from 1, 2, 4, 8 lanes before in a row of 16
-  x += moved<0x112, 0xF>(x);
-  x += moved<0x114, 0xF>(x);
-  x += moved<0x118, 0xF>(x);
-  x += moved<0x142, 0xA>(x);   // the last lane of a row to the next row, rows 1 and 3
-  x += moved<0x143, 0xC>(x);   // lane 31 to rows 2 and 3
+  const double x = sums_to((double)fminf(fmaxf(g, kLinLeastDecay), 0.0f) * kLog2e);
   const double end = __shfl(x, 63);
   const float hi = (float)x;
   d.hi[lane] = hi;
@@ -622,11 +658,11 @@ __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p
 // chunk's heads; scores are made by three waves, one block each, and go to all four through LDS.  (Eight waves of 16
 // columns, four a SIMD, read queries, keys and scores twice as often and were no faster: four prompts 73 us by them
 // and 71 by these, 65536 tokens 430 and 433, where both were built alike.)
-__global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParams p, int items) {
+__global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParams p) {
   __shared__ Lds s;
   // parts of an item follow each other on one XCD
   const int number = blockIdx.x / (8 * p.parts) * 8 + blockIdx.x % 8, part = blockIdx.x / 8 % p.parts;
-  if (number >= items) return;
+  if (number >= p.items) return;
   const Item item = item_of(p, number);
   const int id = item.id, hk = item.hk;
   const int grp = p.h_q / p.h_kv, h0 = hk * grp + part * p.heads, h1 = min(h0 + p.heads, hk * grp + grp);
@@ -732,8 +768,13 @@ __global__ __launch_bounds__(64 * kLinJoinWaves) void linear_join_kernel(LinearP
   __shared__ float s_decay[kLinJoinWaves];
   const int part = blockIdx.x % kBlocks, hk = blockIdx.x / kBlocks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int64_t step = (int64_t)p.h_kv * (kLinState / 4);
+  int dense = 0;
+  if (p.batch > 1 && p.batch <= kLinDense) {
+    int begin, count;
+    dense = first_dense(p, &begin, &count);
+  }
   for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
-    const int begin = p.cu_seqlens[b], id = begin / p.segment + b + 1;   // of segment 1
+    const int begin = p.cu_seqlens[b], id = 1 + (p.batch <= kLinDense ? __shfl(dense, b) : first_spread(p, begin, b));   // of segment 1
     const int last = (p.cu_seqlens[b + 1] - begin + p.segment - 1) / p.segment - 2;   // places 1 .. last behind its own
     if (last < 1) continue;
     f32x4* const at = reinterpret_cast<f32x4*>(p.starts + ((int64_t)id * p.h_kv + hk) * kLinState) + part * 64 + lane;
@@ -777,13 +818,12 @@ __global__ __launch_bounds__(64 * kLinJoinWaves) void linear_join_kernel(LinearP
 }  // namespace
 
 hipError_t launch_linear_prefill(const LinearParams& p, hipStream_t stream) {
-  const int64_t segments = linear_segments(p.batch, p.total_tokens, p.segment);
-  const int items = (int)(segments * p.h_kv), eighths = (items + 7) / 8 * 8;
-  if (p.split || p.parts > 1) linear_sums_kernel<<<dim3(items), dim3(kThreads), 0, stream>>>(p);
+  const int eighths = (p.items + 7) / 8 * 8;
+  if (p.split || p.parts > 1) linear_sums_kernel<<<dim3(p.items), dim3(kThreads), 0, stream>>>(p);
   if (p.split) {
     linear_join_kernel<<<dim3(kLinState / 256 * p.h_kv, std::min(p.batch, 64)), dim3(64 * p.join_waves), 0, stream>>>(p);
   }
-  linear_outputs_kernel<<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(kThreads), 0, stream>>>(p, items);
+  linear_outputs_kernel<<<dim3((unsigned)(eighths * (int64_t)p.parts)), dim3(kThreads), 0, stream>>>(p);
   return hipGetLastError();
 }
 

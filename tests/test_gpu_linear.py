@@ -99,9 +99,11 @@ def test_prefill(mp, lens, h_q, h_kv, decay):
 
 
 @pytest.mark.parametrize("lens,h_q,h_kv", [([2500, 300], 16, 16), ([1700], 32, 32), ([129] * 40, 16, 16), ([33] * 300, 2, 2), ([700, 1] * 3, 40, 8),
-                                           ([5000, 70, 1], 1, 1), ([2600], 2, 2), ([1100], 4, 4), ([4200], 12, 4)], ids=lambda x: str(x)[:24])
+                                           ([5000, 70, 1], 1, 1), ([2600], 2, 2), ([1100], 4, 4), ([4200], 12, 4), ([70, 1, 200] * 30, 2, 2), ([66] * 65, 4, 1), ([66] * 64, 4, 1), ([0, 500, 0] * 3, 10, 2),
+                                           ([90, 7], 256, 1)], ids=lambda x: str(x)[:24])
 def test_prefill_longer_segments(mp, lens, h_q, h_kv):
-    """Segments of several chunks, sequences that lie in one, and such whose segments are joined in several turns."""
+    """Segments of several chunks, sequences that lie in one, and such whose segments are joined in several turns; few
+    sequences, whose segments are numbered without gaps, and many."""
     c = Case(lens, h_q, h_kv, seed=3)
     c.check(lambda: c.prefill(mp))
 

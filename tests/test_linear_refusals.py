@@ -81,7 +81,7 @@ def test_workspace_holds_every_segment(mp, batch, total, longest, h_q, h_kv):   
         assert size >= batch * h_kv * (65536 + 4)
 
 
-@pytest.mark.parametrize("h_q,h_kv", [(2, 1), (40, 8), (256, 1)])
+@pytest.mark.parametrize("h_q,h_kv", [(8, 1), (40, 8), (256, 1)])
 def test_workspace_where_workgroups_share_a_state(mp, h_q, h_kv):   # noqa: F811
     """Query heads that several workgroups take start from one state, which one of them replaces: it is read from a copy."""
     assert mp.linear_prefill_workspace_size(1, 10, 10, h_q, h_kv) >= h_kv * (65536 + 4)
