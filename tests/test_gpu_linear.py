@@ -109,7 +109,7 @@ def test_prefill_longer_segments(mp, lens, h_q, h_kv):
 
 
 @pytest.mark.parametrize("h_q,h_kv,batch,rows", [(1, 1, 1, 1), (4, 4, 3, 1), (8, 2, 5, 2), (24, 1, 2, 3), (16, 1, 7, 8), (40, 8, 33, 1), (256, 256, 2, 1),
-                                                 (256, 1, 1, 2), (32, 32, 130, 1), (9, 3, 2, 70)])
+                                                 (256, 1, 1, 2), (32, 32, 130, 1), (9, 3, 2, 70), (2, 2, 3, 23), (34, 2, 2, 5)])
 @pytest.mark.parametrize("decay", ["head", "token"])
 def test_decode(mp, h_q, h_kv, batch, rows, decay):
     c = Case([rows] * batch, h_q, h_kv, decay, seed=rows)
@@ -167,6 +167,7 @@ def test_in_place_heads_apart(mp, h_q, h_kv):
     b = Case(lens, h_q, h_kv, src=[3, 1, 4, 0, 2], dst=[8, 6, 9, 5, 7], slots=10, seed=20)
     b.states[:5] = a.states
     b.prefill(mp)
+    ws = a.workspace(mp).fill_(255)
     start, x, side = a.states.clone(), torch.zeros(4096, 4096, dtype=torch.bfloat16, device="cuda"), torch.cuda.Stream()
     torch.cuda.synchronize()
     for _ in range(5):
@@ -176,7 +177,8 @@ def test_in_place_heads_apart(mp, h_q, h_kv):
         with torch.cuda.stream(side):
             for _ in range(4):
                 x @ x
-        a.prefill(mp)
+        a.prefill(mp, workspace=ws)
+        ws.fill_(255)
         torch.cuda.synchronize()
         assert torch.equal(a.states, b.states[5:]) and torch.equal(a.out, b.out)
     a.states.copy_(start)
