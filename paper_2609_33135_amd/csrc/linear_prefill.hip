@@ -714,13 +714,18 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
     auto step = [&](auto first, auto final, int h) {
       const int from = decltype(final)::value ? next : c;
       rq.load(q0 + from * p.q_stride + (decltype(final)::value ? h0 : h + 1) * kD, qb, g.n - from);
+      // what all waves wait for goes before the other workgroup's work: the scores, then all between the barriers (four
+      // prompts 59.4 -> 58.3 us, 65536 tokens 407 -> 400)
+      __builtin_amdgcn_s_setprio(2);
       if (wave < 3) scores<decltype(first)::value, !decltype(final)::value>(s, d, wave, p.scale);
+      __builtin_amdgcn_s_setprio(0);
       Outputs out;
       from_state<decltype(first)::value>(out, st, parts, s, d);
       if (decltype(final)::value) {   // not before: the state's parts were in these registers
         rk.load(k0 + next * p.k_stride, kb, g.n - next);
       }
       __syncthreads();   // the scores are there, the queries used
+      __builtin_amdgcn_s_setprio(1);
       Update u;
       from_chunk<decltype(final)::value>(out, u, st, s, d);
       put_outputs(out, s.q);
@@ -737,6 +742,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
         store_rows(rk, s.k);
         store_rows(rv, s.v);
       }
+      __builtin_amdgcn_s_setprio(0);
       store_outputs(ro, p.out + ((g.t0 + c) * p.h_q + h) * kD, p.h_q, g.n - c);
       if (!decltype(final)::value) __syncthreads();
     };
