@@ -578,7 +578,7 @@ __device__ __forceinline__ Item item_of(const LinearParams& p, int item) {
 
 // One workgroup per (segment, KV head): the segment's own state, for the next.  Three BF16 parts of V with its decay
 // make 48 products a wave and chunk, beside 450 vector instructions, most of which make the parts; the loads of two
-// chunks are on their way meanwhile.  2.7 us a chunk and unit (84 us for 65536 tokens of eight KV heads, 44 for 8192
+// chunks are on their way meanwhile.  2.7 us a chunk and unit (81 us for 65536 tokens of eight KV heads, 45 for 8192
 // of 32); without its loads 10 % less, with a third of the products 13 %, with a third of the parts 2 %.  A sequence's first state goes to the
 // place of its first segment, where several workgroups read it: its slot is written by whichever is done first.
 __global__ __launch_bounds__(kThreads, 2) void linear_sums_kernel(LinearParams p) {
@@ -766,8 +766,9 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
 // The states before the segments of a sequence: `sums` left, in the place of segment s + 1, the state that
 // segment s alone leaves (segment 0 with the sequence's first state).  A workgroup has 256 values of it; each of
 // its waves reads up to kLinJoin places at once, and adds to their sums what the segments before them left.  Memory
-// and latency bound it: 33 MB read and 33 written in 14 us for 65536 tokens of 32:8 heads, 8 us for four prompts of
-// 40:8; eight places a wave, which leave room for half the waves, took 13 there.
+// and latency bound it: 33 MB read and 33 written in 14 us for 65536 tokens of 32:8 heads, 6 us for four prompts of
+// 40:8 cut into 25 segments; eight places a wave, which leave room for half the waves, took 13 for 34 segments of
+// theirs, four 8.
 __global__ __launch_bounds__(64 * kLinJoinWaves) void linear_join_kernel(LinearParams p) {
   constexpr int kBlocks = kLinState / 256;
   __shared__ f32x4 s_end[kLinJoinWaves][64];
