@@ -647,10 +647,17 @@ def kv4_evict(cache: PagedCache4, kv_len, page_table, dst_page_table, budget: in
 # ---- linear attention with a decay, the norm around attention ---------------------------
 
 LINEAR_SCALE = HEAD_DIM ** -0.5
+_INT32 = 1 << 31   # ctypes drops the bits of a larger number without a word
+
+
+def _fits(what, *numbers):
+    for n in numbers:
+        _want(-_INT32 <= n < _INT32, f"{what}: {n} is not a 32-bit number")
 
 
 def linear_prefill_workspace_size(batch: int, total_tokens: int, max_seqlen: int, h_q: int, h_kv: int) -> int:
     n = C.c_size_t(0)
+    _fits("linear_prefill_workspace_size", batch, total_tokens, max_seqlen, h_q, h_kv)
     _check(lib().mpfa_linear_prefill_workspace_size(batch, total_tokens, max_seqlen, h_q, h_kv, C.byref(n)),
            "mpfa_linear_prefill_workspace_size")
     return n.value
@@ -668,6 +675,8 @@ def _linear_args(what, q, k, v, log_decay, states, state_src, state_dst, out, ba
     _same(what, torch.bfloat16, dev, out)
     if k.shape[0] != T or v.shape[0] != T or out.numel() != q.numel() or state_src.numel() != batch or state_dst.numel() != batch:
         raise ValueError(f"{what}: shapes")
+    if T >= _INT32 or batch >= _INT32 or not -_INT32 <= max_seqlen < _INT32:
+        _fits(what, T, batch, max_seqlen)
     gs, at = log_decay.shape, log_decay.stride()
     if (log_decay.dtype is not torch.float32 or log_decay.get_device() != dev or len(gs) not in (1, 2) or gs[-1] != h_kv or
             (h_kv > 1 and at[-1] != 1) or (len(gs) == 2 and gs[0] != T)):
@@ -715,6 +724,8 @@ def rms_norm(x, weight, out, eps: float = 1e-6, residual=None, residual_out=None
         raise ValueError("rms_norm: x is bf16 [..][width]")
     width = shape[-1]
     rows = x.numel() // width
+    if rows >= _INT32 or width >= _INT32 or not -_INT32 <= group < _INT32:
+        _fits("rms_norm", rows, width, group)
     if x.is_contiguous():
         stride = width
     elif len(shape) == 2 and x.stride(1) == 1:
