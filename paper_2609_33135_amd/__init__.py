@@ -656,6 +656,8 @@ def _fits(what, *numbers):
 
 
 def linear_prefill_workspace_size(batch: int, total_tokens: int, max_seqlen: int, h_q: int, h_kv: int) -> int:
+    """Bytes that linear_prefill needs for these sizes and for every smaller batch, total_tokens and max_seqlen of the
+    same heads."""
     n = C.c_size_t(0)
     _fits("linear_prefill_workspace_size", batch, total_tokens, max_seqlen, h_q, h_kv)
     _check(lib().mpfa_linear_prefill_workspace_size(batch, total_tokens, max_seqlen, h_q, h_kv, C.byref(n)),

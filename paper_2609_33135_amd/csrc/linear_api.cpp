@@ -158,6 +158,14 @@ PrefillSpace prefill_space(int batch, int total_tokens, int max_seqlen, int h_q,
   return s;
 }
 
+// A workspace that serves every call of up to these sizes.  Longer prompts may be cut into fewer segments than shorter
+// ones, but no prompts into more than a chunk each or, beside one for each sequence, than two items a unit.
+size_t most_space(int batch, int total_tokens, int max_seqlen, int h_q, int h_kv) {
+  if (h_q == h_kv && std::min(max_seqlen, total_tokens) <= mpfa::kLinChunk) return 0;   // one segment, one workgroup a state
+  const int64_t places = std::min<int64_t>((int64_t)(total_tokens / mpfa::kLinChunk) * h_kv, 2 * kUnits) + (int64_t)batch * h_kv;
+  return (size_t)places * (mpfa::kLinState + 1) * sizeof(float);
+}
+
 #ifdef MPFA_DEBUG_CHECKS
 template <typename T>
 bool to_host(const T* dev, size_t n, std::vector<T>& out) {
@@ -218,7 +226,7 @@ mpfa_status mpfa_linear_prefill_workspace_size(int32_t batch, int32_t total_toke
                                                size_t* bytes) {
   if (!bytes || batch < 1 || batch > 65535 || total_tokens < 0 || max_seqlen < 0 || !heads_ok(h_q, h_kv)) return MPFA_ERR_INVALID;
   if (total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
-  *bytes = prefill_space(batch, total_tokens, max_seqlen, h_q, h_kv).bytes;
+  *bytes = most_space(batch, total_tokens, max_seqlen, h_q, h_kv);
   return MPFA_OK;
 }
 
