@@ -1,5 +1,5 @@
 // linear_api.cpp -- the C ABI of linear attention and of the norm (include/mpfa.h): host-side
-// validation (no HIP call before an argument set is accepted), how prompts are cut, workspace sizes.
+// validation (no HIP call before an argument set is accepted).
 #include "mpfa.h"
 
 #include <hip/hip_runtime.h>
@@ -22,7 +22,7 @@ constexpr int kMostTokens = 1 << 28;              // of one call
 constexpr int kMostRows = 1024;                   // of one sequence in a decode call
 constexpr int64_t kMaxStride = (int64_t)1 << 25;  // elements between tokens: 64 of them in 32 bits of bytes
 constexpr int64_t kMaxRow = (int64_t)1 << 31;     // elements between rows of the norm
-constexpr int64_t kUnits = mpfa::kComputeUnits;
+static_assert(mpfa::kLinUnits == mpfa::kComputeUnits, "by which prompts are cut");
 
 bool aligned16(const void* x) { return (reinterpret_cast<uintptr_t>(x) & 15) == 0; }
 
@@ -32,72 +32,7 @@ bool stride_ok(int64_t stride, int heads) {
 
 bool heads_ok(int h_q, int h_kv) { return h_kv >= 1 && h_q >= 1 && h_q <= MPFA_MAX_HEADS && h_q % h_kv == 0; }
 
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
 mpfa_status done(hipError_t e) { return e == hipSuccess ? MPFA_OK : MPFA_ERR_HIP; }
-
-// How prompts are cut.  Into as many segments (times KV heads: items) as there are units, or, where these get long,
-// two a unit: two at once on a unit take less than one after the other, but every segment's states are written and
-// read twice, 256 KB, which is what the rows of some hundred tokens are.  us with one and with two items a unit, by
-// the chunks of the longer segments:
-//   one head per KV head   8: 75, 82 (16384 tokens of 8:8)   16: 125, 124   24: 174, 174   32: 228, 221 (16384 of 32:32)
-//   two                    8: 89, 100                         16: 167, 159
-//   four                   2: 46, 52 (4096 of 32:8)   4: 71, 76   8: 130, 126   16: 238, 227   32: 474, 424
-//   eight                  4: 106, 110 (32768 of 16:2)   8: 201, 196
-//   sixteen                4: 178, 192 (65536 of 16:1)   8: 327, 335
-// Then the query heads of a KV head go in parts to workgroups of their own, where that fills the card better; each
-// part takes the state through the segment for itself.
-struct Cut {
-  int chunks, parts, heads;   // of a segment; of a KV head's query heads; of a part
-  int64_t items;              // at most
-};
-// What a chunk takes, in heads' times: its keys and the state's update once, every head; and more beside another
-// workgroup of the unit.  us measured: 777 tokens of 32:8 heads, 104 items, 27.4 with four heads together, 24.8 with
-// two, 25.6 one by one; 8192 (256) 71, 73, 88; 16384 of 16:1 in 128 items 87, 59 by eight, 56 by four, 64 by two; 5000
-// of 10:2 (158) 33.9, 33.9 by three, 31.8 by two.
-double time_of(int heads, int64_t workgroups) {
-  const double busy = (double)(workgroups - kUnits) / kUnits;
-  return (1.33 + heads) * (busy <= 0.0 ? 1.0 : 1.25 + 0.37 * busy);
-}
-Cut cut_of(int batch, int64_t total_tokens, int max_seqlen, int h_q, int h_kv) {
-  const int grp = h_q / h_kv;
-  const int64_t longest = std::min<int64_t>(max_seqlen, total_tokens);
-  // segments of n chunks: at most, and as many as sequences of any lengths are cut into on average
-  auto ends = [&](int64_t n) { return batch * std::max<int64_t>(1, (longest + n * mpfa::kLinChunk - 1) / (n * mpfa::kLinChunk)); };
-  auto some = [&](int64_t n) {
-    const int64_t spread = (total_tokens + n * mpfa::kLinChunk - 1) / (n * mpfa::kLinChunk) + (batch - 1) / 2;
-    return std::max<int64_t>(batch, std::min(spread, ends(n)));
-  };
-  auto chunks = [&](int64_t items) {
-    const int64_t least = std::max<int64_t>(1, (total_tokens * h_kv + items * mpfa::kLinChunk - 1) / (items * mpfa::kLinChunk));
-    if ((int64_t)batch * h_kv <= items)
-      for (int64_t n = least; n <= 2 * least; ++n)
-        if (some(n) * h_kv <= items) return n;
-    return least;   // sequences fill the card by themselves
-  };
-  Cut c;
-  int64_t n = chunks(kUnits);
-  if (n >= std::max(8, 24 / grp)) n = chunks(2 * kUnits);
-  const int64_t items = some(n) * h_kv;
-  c.chunks = (int)n;
-  c.heads = grp;
-  c.parts = 1;
-  const double copy = longest > n * mpfa::kLinChunk ? 0.0 : 2.0 / n;   // a launch that only parts need
-  double best = time_of(grp, items);
-  for (int64_t parts = 2; parts <= grp && parts * items <= 2 * kUnits; ++parts) {
-    const int heads = (grp + (int)parts - 1) / (int)parts;
-    const double time = time_of(heads, (grp + heads - 1) / heads * items) + copy;
-    if (time < best) {
-      best = time;
-      c.heads = heads;
-      c.parts = (grp + heads - 1) / heads;
-    }
-  }
-  // without gaps in the numbers the longest sequence bounds them too
-  const int64_t numbers = mpfa::linear_segments(batch, total_tokens, n * mpfa::kLinChunk);
-  c.items = (batch <= mpfa::kLinDense ? std::min(numbers, ends(n)) : numbers) * h_kv;
-  return c;
-}
 
 // What both calls check; fills what does not depend on the kind.
 mpfa_status linear_params(const mpfa_linear_args* a, bool decode, mpfa::LinearParams& p) {
@@ -135,35 +70,6 @@ mpfa_status linear_params(const mpfa_linear_args* a, bool decode, mpfa::LinearPa
   p.states = a->states;
   p.out = static_cast<uint16_t*>(a->out);
   return MPFA_OK;
-}
-
-// A prefill's cut and the two tables in its workspace: states before segments, then decays.
-struct PrefillSpace {
-  int segment, parts, heads;
-  bool split;
-  int64_t items;
-  size_t starts, bytes;
-};
-PrefillSpace prefill_space(int batch, int total_tokens, int max_seqlen, int h_q, int h_kv) {
-  const Cut cut = cut_of(batch, total_tokens, max_seqlen, h_q, h_kv);
-  PrefillSpace s;
-  s.segment = cut.chunks * mpfa::kLinChunk;
-  s.parts = cut.parts;
-  s.heads = cut.heads;
-  s.items = cut.items;
-  s.split = std::min(max_seqlen, total_tokens) > s.segment;
-  const int64_t places = mpfa::linear_segments(batch, total_tokens, s.segment) * h_kv;
-  s.starts = align256((size_t)places * mpfa::kLinState * sizeof(float));
-  s.bytes = s.split || s.parts > 1 ? s.starts + (size_t)places * sizeof(float) : 0;
-  return s;
-}
-
-// A workspace that serves every call of up to these sizes.  Longer prompts may be cut into fewer segments than shorter
-// ones, but no prompts into more than a chunk each or, beside one for each sequence, than two items a unit.
-size_t most_space(int batch, int total_tokens, int max_seqlen, int h_q, int h_kv) {
-  if (h_q == h_kv && std::min(max_seqlen, total_tokens) <= mpfa::kLinChunk) return 0;   // one segment, one workgroup a state
-  const int64_t places = std::min<int64_t>((int64_t)(total_tokens / mpfa::kLinChunk) * h_kv, 2 * kUnits) + (int64_t)batch * h_kv;
-  return (size_t)places * (mpfa::kLinState + 1) * sizeof(float);
 }
 
 #ifdef MPFA_DEBUG_CHECKS
@@ -226,7 +132,7 @@ mpfa_status mpfa_linear_prefill_workspace_size(int32_t batch, int32_t total_toke
                                                size_t* bytes) {
   if (!bytes || batch < 1 || batch > 65535 || total_tokens < 0 || max_seqlen < 0 || !heads_ok(h_q, h_kv)) return MPFA_ERR_INVALID;
   if (total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
-  *bytes = most_space(batch, total_tokens, max_seqlen, h_q, h_kv);
+  *bytes = mpfa::linear_most_space(batch, total_tokens, max_seqlen, h_q, h_kv);
   return MPFA_OK;
 }
 
@@ -234,7 +140,7 @@ mpfa_status mpfa_linear_prefill(const mpfa_linear_args* a, void* workspace, size
   mpfa::LinearParams p;
   if (const mpfa_status st = linear_params(a, false, p)) return st;
   if (a->total_tokens > kMostTokens) return MPFA_ERR_UNSUPPORTED;
-  const PrefillSpace s = prefill_space(a->batch, a->total_tokens, a->max_seqlen, a->h_q, a->h_kv);
+  const mpfa::LinearSpace s = mpfa::linear_space(a->batch, a->total_tokens, a->max_seqlen, a->h_q, a->h_kv);
   if (s.items > (int64_t)UINT32_MAX / 512 - 8) return MPFA_ERR_UNSUPPORTED;
   if (s.bytes && (!workspace || workspace_bytes < s.bytes || !aligned16(workspace))) return MPFA_ERR_WORKSPACE;
   p.segment = s.segment;

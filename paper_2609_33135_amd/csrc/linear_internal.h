@@ -1,14 +1,14 @@
 // linear_internal.h -- launch parameter blocks of linear attention (linear_*.hip) and of the norm
-// (rms_norm.hip), and how a prefill is cut.  Not part of the public ABI.
+// (rms_norm.hip).  Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "linear_cut.h"
+
 namespace mpfa {
 
-constexpr int kLinChunk = 64;                  // tokens of a chunk
-constexpr int kLinState = 128 * 128;           // floats of a state
 constexpr int kLinJoin = 4;                    // places that a wave of `join` has at once
 constexpr int kLinJoinWaves = 16;              // at most
 constexpr float kLinLeastDecay = -200.0f;      // exp of it times any FP32 number is 0
@@ -35,10 +35,6 @@ struct LinearParams {
   float* starts;                 // prefill: [segment id][h_kv][kLinState], see linear_prefill.hip
   float* decays;                 // prefill: [segment id][h_kv]
 };
-
-// Numbers of segments that a batch may have, see linear_prefill.hip.
-constexpr int kLinDense = 64;                  // sequences whose segments are numbered without gaps
-inline int64_t linear_segments(int64_t batch, int64_t total_tokens, int64_t segment) { return total_tokens / segment + batch; }
 
 struct NormParams {
   int rows, width, group;        // group: channels per scale, width for one per row

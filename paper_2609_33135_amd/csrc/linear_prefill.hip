@@ -46,7 +46,7 @@ struct Segment {
   int n;                  // tokens
 };
 
-__device__ __forceinline__ int count_of(const LinearParams& p, int len) { return p.split ? max(1, (len + p.segment - 1) / p.segment) : 1; }
+__device__ __forceinline__ int count_of(const LinearParams& p, int len) { return linear_count(len, p.segment, p.split); }
 
 // Sums over the lanes up to each: from 1, 2, 4, 8 lanes before in a row of 16, then the last lane of a row to the next
 // row (rows 1 and 3), then lane 31 to rows 2 and 3.
@@ -80,8 +80,8 @@ __device__ __forceinline__ int first_dense(const LinearParams& p, int* begin, in
   }
   return sums_to(*count) - *count;
 }
-// More: those of sequence b from cu_seqlens[b] / segment + b on, of which ceil(len / segment) lie before the next one's.
-__device__ __forceinline__ int first_spread(const LinearParams& p, int begin, int b) { return begin / p.segment + b; }
+// More: with gaps.
+__device__ __forceinline__ int first_spread(const LinearParams& p, int begin, int b) { return linear_first(begin, p.segment, b); }
 
 // Segment number id.
 __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segment* g) {
