@@ -51,7 +51,6 @@ mpfa_status linear_params(const mpfa_linear_args* a, bool decode, mpfa::LinearPa
   if (!aligned16(a->q) || !aligned16(a->k) || !aligned16(a->v) || !aligned16(a->out)) return MPFA_ERR_INVALID;
   p = mpfa::LinearParams{};
   p.batch = a->batch;
-  p.total_tokens = a->total_tokens;
   p.h_q = a->h_q;
   p.h_kv = a->h_kv;
   p.q_tokens = a->q_tokens;

@@ -14,7 +14,7 @@ constexpr int kLinJoinWaves = 16;              // at most
 constexpr float kLinLeastDecay = -200.0f;      // exp of it times any FP32 number is 0
 
 struct LinearParams {
-  int batch, total_tokens, h_q, h_kv;
+  int batch, h_q, h_kv;
   int q_tokens;                  // decode: rows per sequence
   int segment;                   // prefill: tokens per segment, a multiple of kLinChunk
   int split;                     // prefill: some sequence may have several segments

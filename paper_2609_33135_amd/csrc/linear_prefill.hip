@@ -767,7 +767,7 @@ __global__ __launch_bounds__(kThreads, 2) void linear_outputs_kernel(LinearParam
 // segment s alone leaves (segment 0 with the sequence's first state).  A workgroup has 256 values of it; each of
 // its waves reads up to kLinJoin places at once, and adds to their sums what the segments before them left.  Memory
 // and latency bound it: 33 MB read and 33 written in 14 us for 65536 tokens of 32:8 heads, 6 us for four prompts of
-// 40:8 cut into 25 segments; eight places a wave, which leave room for half the waves, took 13 for 34 segments of
+// 40:8 cut into 23 segments; eight places a wave, which leave room for half the waves, took 13 for 34 segments of
 // theirs, four 8.
 __global__ __launch_bounds__(64 * kLinJoinWaves) void linear_join_kernel(LinearParams p) {
   constexpr int kBlocks = kLinState / 256;
