@@ -584,7 +584,11 @@ mpfa_status mpfa_kv4_evict(const mpfa_kv4_evict_args* args, mpfa_stream_t stream
  *    another starts.  A sequence without tokens leaves the state it starts from.
  *  - q_stride, k_stride, v_stride: elements between tokens (at least heads * 128,
  *    a multiple of 8; the heads of a token are contiguous), like decay_stride
- *    below 2^25.  q, k, v, states and out are 16-byte aligned.  h_q and h_kv are 1 to 256, h_q % h_kv == 0.
+ *    below 2^25.  q, k, v, states and out are 16-byte aligned.  h_q and h_kv are
+ *    1 to 256, h_q % h_kv == 0.  out overlaps no input.
+ *  - MPFA_ERR_UNSUPPORTED above 2^28 total_tokens, and where a grid would be too
+ *    large: from batch * h_kv = 2^22 on in a decode, 2^23 in a prefill (where
+ *    prompts are cut, from up to 1024 below that on).
  * States, sums and decays are FP32.  Where the matrix cores take FP32 numbers as
  * BF16 they are sums of such: of two for an output (a state, a score: at most
  * 2^-16 of it is lost), of three for the state (2^-24).  q, k and v are finite, and
@@ -651,10 +655,14 @@ mpfa_status mpfa_linear_decode(const mpfa_linear_args* args, mpfa_stream_t strea
  * and so are codes of a group whose m is below 2^-100 but not 0.
  * Rows do not affect each other; one with a NaN or an infinity gets NaN outputs
  * or scales somewhere.
- * x_stride: elements between rows of x (a multiple of 8, below 2^31); residual, residual_out
- * and out are contiguous, and residual_out may be residual (or x, where x is
- * contiguous).  x, residual, residual_out, weight are 16-byte aligned, out too
- * (codes: 8).
+ * x_stride: elements between rows of x (a multiple of 8, below 2^31), the only
+ * stride there is: heads that lie in wider tokens are copied first.  residual,
+ * residual_out and out are contiguous.  Where x is contiguous, residual_out or a
+ * BF16 out may be x, and residual_out may be residual; nothing else overlaps.
+ * x, residual, residual_out, weight are 16-byte aligned, out too (codes: 8).
+ * MPFA_ERR_UNSUPPORTED where rows times the threads of one (8 up to 64 channels,
+ * 16 up to 128, 32 up to 256, 64 up to 512, then 64 for every 1024 begun, above
+ * 16384 for every 2048) come to 2^32 - 256 or more.
  */
 typedef struct {
     int32_t rows;                /* 0 or more                                      */

@@ -719,7 +719,8 @@ def linear_decode(q, k, v, log_decay, states, state_src, state_dst, out, q_token
 def rms_norm(x, weight, out, eps: float = 1e-6, residual=None, residual_out=None, scales=None, group: int = 0, stream=None):
     """mpfa_rms_norm over the last dimension of x (bf16; contiguous, or rows of a matrix that lie apart): out bf16, or
     with scales (f32 [rows][groups]) float8_e4m3fn codes, a scale per `group` channels (0: per row).  residual:
-    x + residual is normalised, and goes to residual_out (by default to residual).  weight: bf16 [width] or None."""
+    x + residual is normalised, and goes to residual_out (by default to residual).  weight: bf16 [width] or None.
+    A bf16 out may be x, where that is contiguous."""
     import torch
     dev, shape = x.get_device(), x.shape
     if x.dtype is not torch.bfloat16 or not shape or shape[-1] == 0:

@@ -55,6 +55,8 @@ def _check(cut, mp, lens, total, longest, h_q, h_kv):   # noqa: F811
     what = (lens, total, longest, h_q, h_kv)
     s = Space(cut, len(lens), total, longest, h_q, h_kv)
     assert s.segment > 0 and s.segment % CHUNK == 0 and s.items % h_kv == 0, what
+    if len(lens) * h_kv < 2 ** 23 - 1024:   # such a call is taken
+        assert s.items <= (2 ** 32 - 1) // 512 - 8, what
     grp = h_q // h_kv
     assert 1 <= s.parts <= grp and (s.parts - 1) * s.heads < grp <= s.parts * s.heads, what
     behind = 0   # numbers of the sequences so far end here
