@@ -595,15 +595,16 @@ mpfa_status mpfa_kv4_evict(const mpfa_kv4_evict_args* args, mpfa_stream_t stream
  * so is what the formulas make of them.
  *
  * mpfa_linear_prefill: packed prompts; query, key and value i of sequence b are
- * token cu_seqlens[b] + i.  total_tokens of q, k, v and out: cu_seqlens[batch],
- * or more (padding, neither read nor written).  max_seqlen: at least the tokens
- * of the longest sequence.  workspace: mpfa_linear_prefill_workspace_size bytes
- * for the same arguments, or for more sequences, tokens or a longer longest one
- * of the same heads (that of a server's largest call serves all its calls; 0:
- * none is read), 16-byte aligned; its contents on entry are ignored.  Calls (and captured
- * graphs) that may overlap need workspaces and states of their own.  How long
- * sequences are cut goes by batch, total_tokens, max_seqlen and the heads, and
- * the order of FP32 sums with it; identical calls give identical bytes.
+ * token cu_seqlens[b] + i, and cu_seqlens[0] is 0.  total_tokens of q, k, v and
+ * out: cu_seqlens[batch], or more (padding, neither read nor written).
+ * max_seqlen: at least the tokens of the longest sequence.  workspace:
+ * mpfa_linear_prefill_workspace_size bytes for the same arguments, or for more
+ * sequences, tokens or a longer longest one of the same heads (that of a server's
+ * largest call serves all its calls; 0: none is read), 16-byte aligned; its
+ * contents on entry are ignored.  Calls (and captured graphs) that may overlap
+ * need workspaces and states of their own.  How long sequences are cut goes by
+ * batch, total_tokens, max_seqlen and the heads, and the order of FP32 sums with
+ * it; identical calls give identical bytes.
  *
  * mpfa_linear_decode: q_tokens rows per sequence (1, or a few drafted tokens);
  * token b * q_tokens + i.  No workspace.  total_tokens, max_seqlen and cu_seqlens

@@ -17,6 +17,22 @@ constexpr int64_t kLinUnits = 256;
 constexpr int linear_count(int len, int segment, int split) { return split ? std::max(1, (len + segment - 1) / segment) : 1; }
 // With gaps, sequence b has the numbers from here on, of which ceil(len / segment) lie before the next one's.
 constexpr int linear_first(int begin, int segment, int b) { return begin / segment + b; }
+// The last of its sequences whose first number is at most id (the first one, if there is none), by 64-ary search; `lanes`
+// counts the lanes of 64 for which it is told to.
+template <typename Offsets, typename Lanes>
+constexpr int linear_search(const Offsets& cu_seqlens, int batch, int segment, int id, const Lanes& lanes) {
+  int lo = 0, n = batch;
+  while (n > 1) {
+    const int step = (n + 63) >> 6;
+    const int last = std::max(1, lanes([&](int lane) {
+      const int at = lane * step;
+      return at < n && linear_first(cu_seqlens[lo + std::min(at, n - 1)], segment, lo + at) <= id;
+    })) - 1;
+    lo += last * step;
+    n = std::min(step, n - last * step);
+  }
+  return lo;
+}
 // Numbers of segments that a batch may have.
 constexpr int64_t linear_segments(int64_t batch, int64_t total_tokens, int64_t segment) { return total_tokens / segment + batch; }
 

@@ -96,24 +96,18 @@ __device__ __forceinline__ bool find_segment(const LinearParams& p, int id, Segm
     if (at == 0) return false;
     g->b = __builtin_ctzll(at);
     first = __builtin_amdgcn_readlane(mine, g->b);
-  } else {   // the last sequence whose first number is at most id, by 64-ary search
-    int lo = 0, n = p.batch;
-    while (n > 1) {
-      const int step = (n + 63) >> 6, at = lane * step;
-      const bool before = at < n && first_spread(p, p.cu_seqlens[lo + min(at, n - 1)], lo + at) <= id;
-      const int last = __popcll(__builtin_amdgcn_ballot_w64(before)) - 1;
-      lo += last * step;
-      n = min(step, n - last * step);
-    }
-    g->b = lo;
-    first = first_spread(p, p.cu_seqlens[lo], lo);
+  } else {
+    g->b = linear_search(p.cu_seqlens, p.batch, p.segment, id, [lane](auto before) {
+      return (int)__popcll(__builtin_amdgcn_ballot_w64(before(lane)));
+    });
+    first = first_spread(p, p.cu_seqlens[g->b], g->b);
   }
   const int begin = p.cu_seqlens[g->b], len = p.cu_seqlens[g->b + 1] - begin;
   g->s = id - first;
   g->count = count_of(p, len);
   g->t0 = (int64_t)begin + (int64_t)g->s * p.segment;
   g->n = min(p.segment, len - g->s * p.segment);
-  return g->s < g->count;
+  return g->s >= 0 && g->s < g->count;
 }
 
 // Rows of 128 channels in LDS lie without padding, their 16-byte pieces exchanged by row so that neither 16

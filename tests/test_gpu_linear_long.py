@@ -97,3 +97,25 @@ def test_norm_of_the_states_error(mp, n):   # noqa: F811
     error = np.linalg.norm(R.np64(c.states[0]) - ref) / np.linalg.norm(ref)
     print(f"{error / R.U:.2f} half steps")
     assert error < L.FROBENIUS
+
+
+@pytest.mark.parametrize("batch", [3, 65, 130])
+def test_a_first_sequence_behind_other_tokens(mp, batch):   # noqa: F811
+    """cu_seqlens of a batch's second half: a mistake by the header, which the debug library names, but nothing is read or
+    written out of range for it, and the tokens before are left alone."""
+    lens = [70, 0, 1, 130, 64] * (batch // 5) + [5] * (batch % 5)
+    c = Case([500] + lens, 4, 2, src=[-1] * (batch + 1), dst=list(range(batch + 1)), seed=35)
+    keep = c.states[0].clone()
+    cu, src, dst = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (c.cu[1:], c.src[1:], c.dst[1:]))
+    size = mp.linear_prefill_workspace_size(batch, c.T, 130, 4, 2)
+    mp.linear_prefill(c.q, c.k, c.v, c.g, cu, c.states, src, dst, c.out, 130, workspace=torch.empty(size, dtype=torch.uint8, device="cuda"), scale=c.scale)
+    torch.cuda.synchronize()
+    assert (c.out[:500] == 7.0).all() and torch.equal(c.states[0], keep)
+    before = np.zeros((2, 128, 128))
+    for b, n in enumerate(lens):
+        at = slice(c.cu[b + 1], c.cu[b + 1] + n)
+        g = R.np64(c.g[at])
+        o, s, oa, sa = R.linear(*(R.np64(x[at]) for x in (c.q, c.k, c.v)), g, before, c.scale)
+        if n:
+            R.check_out(R.np64(c.out[at]), o, oa, n, g, b)
+        R.check_state(R.np64(c.states[b + 1]), s, sa, n, g, b)

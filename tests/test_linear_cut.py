@@ -21,6 +21,25 @@ void space(int batch, int total, int longest, int h_q, int h_kv, int64_t* out) {
 }
 int count(int len, int segment, int split) { return linear_count(len, segment, split); }
 int first(int begin, int segment, int b) { return linear_first(begin, segment, b); }
+// the sequence that number id is looked up in, -1 if offsets out of range are read
+int search(const int* cu, int batch, int segment, int id) {
+  struct Offsets {
+    const int* cu;
+    int n;
+    bool* bad;
+    int operator[](int i) const {
+      if (i < 0 || i >= n) *bad = true;
+      return i < 0 || i >= n ? 0 : cu[i];
+    }
+  };
+  bool bad = false;
+  const int b = linear_search(Offsets{cu, batch, &bad}, batch, segment, id, [](auto before) {
+    int n = 0;
+    for (int lane = 0; lane < 64; ++lane) n += before(lane);
+    return n;
+  });
+  return bad ? -1 : b;
+}
 }
 """
 STATE, UNITS, DENSE, CHUNK = 128 * 128 * 4, 256, 64, 64
@@ -104,6 +123,28 @@ def test_long_calls_have_two_items_a_unit(cut, mp, lens, h_q, h_kv, chunks):   #
     items = sum(count for _, count in _numbers(cut, lens, s)) * h_kv
     assert s.split and s.segment == chunks * CHUNK and UNITS < items <= 2 * UNITS + len(lens) * h_kv
     _check(cut, mp, lens, sum(lens), max(lens), h_q, h_kv)
+
+
+@pytest.mark.parametrize("begin", [0, 1, 64, 5000, 100000])
+@pytest.mark.parametrize("batch", [65, 66, 130, 4096, 5000])
+def test_numbers_are_found(cut, batch, begin):
+    """Every number by its sequence, and those before a first sequence that does not begin at token 0 (a mistake of the caller)
+    within the offsets."""
+    rng, segment = random.Random(batch), 64
+    lens = [0 if rng.random() < 0.2 else rng.randint(1, 300) for _ in range(batch)]
+    cu = [begin]
+    for n in lens:
+        cu.append(cu[-1] + n)
+    of, behind = {}, 0
+    for b, n in enumerate(lens):
+        behind = cut.first(cu[b], segment, b)
+        for i in range(cut.count(n, segment, 1)):
+            assert behind + i not in of
+            of[behind + i] = b
+    at = (C.c_int * (batch + 1))(*cu)
+    for number in range(max(of) + 3):
+        got = cut.search(at, batch, segment, number)
+        assert 0 <= got < batch and got == of.get(number, got), (number, got)
 
 
 def test_the_check_notices(cut, mp, monkeypatch):   # noqa: F811
