@@ -652,7 +652,8 @@ _INT32 = 1 << 31   # ctypes drops the bits of a larger number without a word
 
 def _fits(what, *numbers):
     for n in numbers:
-        _want(-_INT32 <= n < _INT32, f"{what}: {n} is not a 32-bit number")
+        if not -_INT32 <= n < _INT32:
+            raise ValueError(f"{what}: {n} is not a 32-bit number")
 
 
 def linear_prefill_workspace_size(batch: int, total_tokens: int, max_seqlen: int, h_q: int, h_kv: int) -> int:
@@ -677,8 +678,6 @@ def _linear_args(what, q, k, v, log_decay, states, state_src, state_dst, out, ba
     _same(what, torch.bfloat16, dev, out)
     if k.shape[0] != T or v.shape[0] != T or out.numel() != q.numel() or state_src.numel() != batch or state_dst.numel() != batch:
         raise ValueError(f"{what}: shapes")
-    if T >= _INT32 or batch >= _INT32 or not -_INT32 <= max_seqlen < _INT32:
-        _fits(what, T, batch, max_seqlen)
     gs, at = log_decay.shape, log_decay.stride()
     if (log_decay.dtype is not torch.float32 or log_decay.get_device() != dev or len(gs) not in (1, 2) or gs[-1] != h_kv or
             (h_kv > 1 and at[-1] != 1) or (len(gs) == 2 and gs[0] != T)):
@@ -696,8 +695,10 @@ def linear_prefill(q, k, v, log_decay, cu_seqlens, states, state_src, state_dst,
     whose slots state_src (negative: zeros) the sequences start and in whose slots state_dst (negative: nowhere) they
     end; workspace: linear_prefill_workspace_size bytes; scale: 1 / sqrt(128) by default."""
     import torch
-    dev, a = _linear_args("linear_prefill", q, k, v, log_decay, states, state_src, state_dst, out, cu_seqlens.numel() - 1,
-                          max_seqlen, 0, cu_seqlens.data_ptr(), scale)
+    batch = cu_seqlens.numel() - 1
+    if batch >= _INT32 or not -_INT32 <= max_seqlen < _INT32:
+        _fits("linear_prefill", batch, max_seqlen)
+    dev, a = _linear_args("linear_prefill", q, k, v, log_decay, states, state_src, state_dst, out, batch, max_seqlen, 0, cu_seqlens.data_ptr(), scale)
     _same("linear_prefill", torch.int32, dev, cu_seqlens)
     size = 0
     if workspace is not None:
@@ -726,8 +727,9 @@ def rms_norm(x, weight, out, eps: float = 1e-6, residual=None, residual_out=None
     if x.dtype is not torch.bfloat16 or not shape or shape[-1] == 0:
         raise ValueError("rms_norm: x is bf16 [..][width]")
     width = shape[-1]
-    rows = x.numel() // width
-    if rows >= _INT32 or width >= _INT32 or not -_INT32 <= group < _INT32:
+    values = x.numel()
+    rows = values // width
+    if values >= _INT32 or group >> 31:
         _fits("rms_norm", rows, width, group)
     if x.is_contiguous():
         stride = width
