@@ -3,9 +3,10 @@
 // S_t = a_t S_{t-1} + k_t v_t^T, o_t = scale q_t^T S_t in FP32.  Bound by the state's 64 KB per KV head, read
 // and written once: the rows of a call are taken one after the other with the state in registers.  128 sequences of
 // 32:32 heads, a row each, take 105 us (537 MB, 5.1 TB/s, a large copy's rate), 64 of 40:8 heads 13.6 (67 MB, 4.9)
-// and with four rows each 19.4, since 20 dot products a column and the staging of rows are vector and LDS work that
-// the state's loads and stores do not hide in full.  32 columns a workgroup: 256 threads hold them in 16 registers
-// each, and one sequence of eight KV heads has 32 workgroups.
+// and with four rows each 19.4 to 20.2, since 20 dot products a column and the staging of rows are vector and LDS work
+// that the state's loads and stores do not hide in full (22.2 over twelve sets of inputs, none of which stays in the
+// cache; within it a copy of as many bytes reaches 8 TB/s).  32 columns a workgroup: 256 threads hold them in 16
+// registers each, and one sequence of eight KV heads has 32 workgroups.
 #include "linear_internal.h"
 #include "mpfa_device.h"
 

@@ -11,10 +11,11 @@
 // Chunks of 64: the products with the state cost a token 2 * 128 * 128 each whatever the chunk, those within it
 // 64 * 128, and the decays' vector work grows with it too.
 //
-// What bounds it is what a workgroup's waves can issue, not memory (65536 tokens of 32:8 heads, 1.3 GB in 401 us):
-// products and vector instructions fill 70 % of a SIMD's cycles between them with the two waves that the state's
-// registers leave it, at 1.9 GHz, to which this work brings the clock (the first calls, at 2.3, take 278 us of
-// `outputs` instead of 352).
+// What bounds it for long prompts is what a workgroup's waves can issue, not memory (65536 tokens of 32:8 heads, 1.3 GB
+// in 403 us): products and vector instructions fill 70 % of a SIMD's cycles between them in `outputs`, 53 % in `sums`,
+// with the two waves that the state's registers leave it, at 2.0 GHz and below, to which this work brings the clock
+// (the first calls, at 2.3, take 278 us of `outputs`, later ones 320 to 355).  Where a unit has one workgroup waves wait
+// for each other: 52 % and 36 % for 8192 tokens of 32:32 heads, 33 % and 12 % for four prompts of 40:8.
 #include <algorithm>
 #include <type_traits>
 

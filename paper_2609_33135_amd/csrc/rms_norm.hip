@@ -6,8 +6,9 @@
 // border of E4M3 that the true one does not lie on (16 + 5 bits), so codes are exact.
 //
 // Bound by memory: a row is read once, into registers, and every output written once.  16384 rows of 5120 channels
-// with a residual and a scale per 128 channels 115 us (590 MB, 5.1 TB/s, a large copy's rate); 161920 rows of 128
-// channels to BF16 15.2 us (83 MB, 5.5 TB/s); 32 rows of 4096 4.6 us, a launch and two trips to memory.
+// with a residual and a scale per 128 channels 116 us (590 MB, 5.1 TB/s, a large copy's rate); 161920 rows of 128
+// channels to BF16 18.7 us where no input is left in the cache from calls before (83 MB, 4.4 TB/s) and 15.3 over three
+// sets of inputs, most of which are; 32 rows of 4096 4.6 us, a launch and two trips to memory.
 #include "linear_internal.h"
 #include "mpfa_device.h"
 
