@@ -592,7 +592,8 @@ mpfa_status mpfa_kv4_evict(const mpfa_kv4_evict_args* args, mpfa_stream_t stream
  * States, sums and decays are FP32.  Where the matrix cores take FP32 numbers as
  * BF16 they are sums of such: of two for an output (a state, a score: at most
  * 2^-16 of it is lost), of three for the state (2^-24).  q, k and v are finite, and
- * so is what the formulas make of them.
+ * so is what the formulas make of them; in a prefill so are the products q_t . k_s
+ * of all tokens of a sequence, by which its chunks are computed.
  *
  * mpfa_linear_prefill: packed prompts; query, key and value i of sequence b are
  * token cu_seqlens[b] + i, and cu_seqlens[0] is 0.  total_tokens of q, k, v and
